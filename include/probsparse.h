@@ -277,6 +277,130 @@ int dense_attn_fwd(const void* Q, const void* K, const void* V, const int32_t* l
                    void* out, const psa_shape_t* shape,
                    void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * What stands around the attention of a layer: layer norm, rotary positions, and dense
+ * attention over sequences that are packed without padding, each with its gradient.
+ *
+ * Heads of 64 elements lie in memory by head ([.., H, L, 64], as probsparse_qkv_project writes
+ * them), by frame ([.., L, H, 64], as a fused projection does) or as a part of a larger array:
+ * element e of row l of head h of batch item b is data[b * batch_stride + h * head_stride +
+ * l * row_stride + e].  Strides are in elements, not negative, and multiples of 16 bytes, and
+ * data is 16-byte aligned (else PSA_ERR_ALIGN); 0 repeats an input's rows or heads.  The rows
+ * of an output must not overlap (PSA_ERR_ARG for strides under 64 where there is more than one).
+ * Outputs must not alias inputs unless an entry point says that they may. */
+typedef struct psa_heads {
+    void*   data;                                    /* DEVICE */
+    int64_t batch_stride, head_stride, row_stride;
+} psa_heads_t;
+
+/* Layer norm over the last dimension of X [rows, cols]:
+ *   Y = (X - mean) * rstd * gamma + beta,   rstd = 1 / sqrt(mean((X - mean)^2) + eps)
+ *   gamma, beta [cols]    the tensors' dtype; NULL: 1 and 0
+ *   mean, rstd  [rows]    float32, what the backward reads; both or neither may be NULL
+ *   rows 1 .. 2^31 - 1, cols 1 .. 2^24 (PSA_ERR_SHAPE); eps finite and >= 0 (PSA_ERR_ARG)
+ * Y may be X.  Sums are formed in float32, those of the squares over deviations from the row's
+ * own mean.  X and Y 16-byte aligned, gamma and beta too. */
+int probsparse_layer_norm_fwd(const void* X, const void* gamma, const void* beta, double eps, void* Y,
+                              float* mean, float* rstd, int64_t rows, int32_t cols, int32_t dtype, void* stream);
+
+/* Its gradients.  With g = dY * gamma and xhat = (X - mean) * rstd, means over a row's columns:
+ *   dX = rstd * (g - mean(g) - xhat * mean(g * xhat))
+ *   dgamma = sum over rows of dY * xhat,   dbeta = sum over rows of dY
+ * dgamma and dbeta [cols] are float32 for either dtype: they are sums over all rows, formed in
+ * float32 in a fixed order, and left in it.  Both or neither may be NULL. */
+size_t probsparse_layer_norm_bwd_workspace_bytes(int64_t rows, int32_t cols, int32_t dtype);
+int probsparse_layer_norm_bwd(const void* dY, const void* X, const void* gamma, const float* mean, const float* rstd,
+                              void* dX, float* dgamma, float* dbeta, int64_t rows, int32_t cols, int32_t dtype,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rotary positions.  The first `dim` elements of a head are dim / 2 pairs; pair i of the row at
+ * position p is turned by the angle p * f_i and multiplied by `magnitude`:
+ *   (a, b) -> magnitude * (a cos - b sin, a sin + b cos)
+ * The elements behind them are copied.  f_i = base^(-2 i / dim), for long contexts scaled:
+ *   PSA_ROTARY_LINEAR  f_i / factor
+ *   PSA_ROTARY_BASE    base * factor^(dim / (dim - 2)) in the place of base (dim > 2): the
+ *                      slowest pair turns `factor` times slower, the fastest as before
+ *   PSA_ROTARY_PARTS   with r = original_length * f_i / (2 pi), the turns of pair i over the
+ *                      length that the model was trained on, and s = clamp((r - slow_turns) /
+ *                      (fast_turns - slow_turns), 0, 1):  f_i * s + f_i / factor * (1 - s)
+ * Angles are formed and reduced in float64, so far positions lose nothing. */
+typedef enum psa_rotary_layout {
+    PSA_ROTARY_HALF        = 0,   /* pair i is elements i and i + dim / 2 */
+    PSA_ROTARY_INTERLEAVED = 1    /* pair i is elements 2 i and 2 i + 1   */
+} psa_rotary_layout_t;
+typedef enum psa_rotary_scaling {
+    PSA_ROTARY_PLAIN = 0, PSA_ROTARY_LINEAR = 1, PSA_ROTARY_BASE = 2, PSA_ROTARY_PARTS = 3
+} psa_rotary_scaling_t;
+typedef struct psa_rotary {
+    int32_t dim;                  /* even, 2 .. 64 */
+    int32_t layout, scaling;      /* psa_rotary_layout_t, psa_rotary_scaling_t */
+    double  base, factor;         /* finite, > 0; base >= 1 */
+    double  original_length;      /* PSA_ROTARY_PARTS alone: finite, > 0 */
+    double  fast_turns, slow_turns;   /* PSA_ROTARY_PARTS alone: finite, fast_turns > slow_turns */
+    double  magnitude;            /* finite, > 0 */
+} psa_rotary_t;
+
+/* The frequencies f_i in radians per position into freq[dim / 2] (HOST); no GPU needed. */
+int probsparse_rotary_frequencies(const psa_rotary_t* rotary, double* freq);
+
+/* Q [B, H, L, 64] and K [B, H_kv, L, 64] turned in one launch, into Q_out and K_out; K and
+ * K_out may be NULL.  An output may be its own input (same data, same strides).
+ *   positions  DEVICE int32, 4-byte aligned: row l of item b stands at
+ *              positions[b * positions_stride + l]; positions_stride 0: the same for every
+ *              item, else >= L.  NULL: row l stands at first + l (first + L <= 2^31 - 1)
+ *   shape      L_Q = L_K = L; U is ignored
+ * The backward turns the gradients of Q_out and K_out the other way (and multiplies by the same
+ * magnitude), which makes them those of Q and K. */
+int probsparse_rotary_fwd(const psa_heads_t* Q, const psa_heads_t* K, int32_t H_kv, const psa_rotary_t* rotary,
+                          const int32_t* positions, int64_t positions_stride, int32_t first,
+                          const psa_heads_t* Q_out, const psa_heads_t* K_out, const psa_shape_t* shape, void* stream);
+int probsparse_rotary_bwd(const psa_heads_t* dQ_out, const psa_heads_t* dK_out, int32_t H_kv, const psa_rotary_t* rotary,
+                          const int32_t* positions, int64_t positions_stride, int32_t first,
+                          const psa_heads_t* dQ, const psa_heads_t* dK, const psa_shape_t* shape, void* stream);
+
+/* Dense attention over packed sequences.  Sequence s owns the query rows q_offsets[s] ..
+ * q_offsets[s + 1] - 1 and the key rows k_offsets[s] .. k_offsets[s + 1] - 1 of every head, n_q
+ * and n_k of them; query head h reads key head h / (H / H_kv).  Query t of a sequence sees all
+ * of its n_k keys or, `causal`, its keys j <= t + n_k - n_q: the last query sees the last key,
+ * so queries may be the newest rows of sequences whose earlier rows are keys alone.
+ *   out[h, t] = sum_j p_tj V[j],   p_tj = exp(scale * Q[h, t].K[j] - lse[h, t])
+ *   lse[h, t] = ln sum_j exp(scale * Q[h, t].K[j])   over the keys that t sees
+ * A query that sees no key, and a row of Q in no sequence, get zeros in out and -infinity in
+ * lse.  What a query does not see has no part in its output, infinities and NaN included.
+ *   q_offsets, k_offsets  DEVICE int32 [B + 1], not decreasing (values are clamped to [0, T],
+ *             and a sequence that would end before it begins is empty); both NULL: one
+ *             sequence of all rows (B = 1)
+ *   Q, out    H heads of T_q rows;  K, V: H_kv heads of T_k rows; batch_stride is ignored
+ *   lse       [H, T_q] float32 DEVICE, or NULL
+ * Arithmetic: bfloat16 operands are multiplied exactly and summed in float32; the weights p are
+ * rounded to bfloat16 before they are multiplied with V.  float32 operands are multiplied and
+ * summed in float32.  Softmax statistics are float32. */
+typedef struct psa_packed_shape {
+    int32_t B, H, H_kv;           /* sequences; heads, H a multiple of H_kv */
+    int32_t T_q, T_k;             /* rows of Q and of K and V; T_q * (H / H_kv) <= 2^31 - 2^16 */
+    int32_t D;                    /* 64 */
+    int32_t dtype;                /* psa_dtype_t */
+    int32_t causal;               /* 0 or 1 */
+    double  scale;                /* finite, > 0; 1 / sqrt(64) as a rule */
+} psa_packed_shape_t;
+size_t dense_attn_packed_workspace_bytes(const psa_packed_shape_t* shape);
+int dense_attn_packed_fwd(const psa_heads_t* Q, const psa_heads_t* K, const psa_heads_t* V,
+                          const int32_t* q_offsets, const int32_t* k_offsets, const psa_heads_t* out, float* lse,
+                          const psa_packed_shape_t* shape, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Its gradients, from the forward's inputs, out and lse.  With G = dOut,
+ * d_t = sum_e G[t, e] out[t, e] and ds_tj = p_tj (G[t].V[j] - d_t):
+ *   dQ[t] = scale * sum_j ds_tj K[j],  dK[j] = scale * sum_t ds_tj Q[t],  dV[j] = sum_t p_tj G[t]
+ * the sums over t also over the query heads that share the key head.  Every element of dQ, dK
+ * and dV is written; rows in no sequence get zeros.  p and ds are rounded to bfloat16 before
+ * they are multiplied where the tensors are bfloat16.  The order of all sums is fixed.
+ * Infinities and NaN stay within the gradients of their own sequence. */
+size_t dense_attn_packed_bwd_workspace_bytes(const psa_packed_shape_t* shape);
+int dense_attn_packed_bwd(const psa_heads_t* Q, const psa_heads_t* K, const psa_heads_t* V,
+                          const int32_t* q_offsets, const int32_t* k_offsets, const psa_heads_t* out, const float* lse,
+                          const psa_heads_t* dOut, const psa_heads_t* dQ, const psa_heads_t* dK, const psa_heads_t* dV,
+                          const psa_packed_shape_t* shape, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Host only, no GPU needed: which kernels a call with this shape would launch, as
  * one line of `key=value` words in `buf` (NUL-terminated), e.g. which measure kernel
  * (`measure=lds|lds_half|stream|none`; `measure_parts` > 0: the keys of streamed heads go

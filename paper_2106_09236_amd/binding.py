@@ -26,6 +26,8 @@ PSA_F32, PSA_BF16 = 0, 1
 STAGE_MEASURE, STAGE_SELECT, STAGE_ATTEND, STAGE_ALL = 1, 2, 4, 7
 U_LOG, U_RATIO = 0, 1
 FILL_MEAN, FILL_VALUE = 0, 1
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
 
 EXPORTS = [
     "probsparse_attn_workspace_bytes", "probsparse_attn_fwd", "probsparse_attn_fwd_debug",
@@ -37,6 +39,10 @@ EXPORTS = [
     "probsparse_describe_plan", "probsparse_init", "probsparse_strerror", "probsparse_version",
     "probsparse_static_workspace_bytes", "probsparse_attn_fwd_static",
     "probsparse_attn_bwd_workspace_bytes", "probsparse_attn_bwd",
+    "probsparse_layer_norm_fwd", "probsparse_layer_norm_bwd_workspace_bytes", "probsparse_layer_norm_bwd",
+    "probsparse_rotary_frequencies", "probsparse_rotary_fwd", "probsparse_rotary_bwd",
+    "dense_attn_packed_workspace_bytes", "dense_attn_packed_fwd",
+    "dense_attn_packed_bwd_workspace_bytes", "dense_attn_packed_bwd",
 ]
 
 
@@ -51,6 +57,23 @@ class PsaOptions(ctypes.Structure):
 
 class PsaMhsaWeights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("Wq", "Wk", "Wv", "Wo", "bq", "bk", "bv", "bo")]
+
+
+class PsaHeads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64)]
+
+
+class PsaRotary(ctypes.Structure):
+    _fields_ = [("dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("original_length", ctypes.c_double), ("fast_turns", ctypes.c_double),
+                ("slow_turns", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class PsaPackedShape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("T_q", ctypes.c_int32),
+                ("T_k", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("scale", ctypes.c_double)]
 
 
 class ProbSparseError(RuntimeError):
@@ -150,6 +173,26 @@ def load() -> ctypes.CDLL:
     lib.probsparse_version.argtypes = []
     lib.probsparse_init.restype = ctypes.c_int
     lib.probsparse_init.argtypes = []
+    hp, rp, kp = ctypes.POINTER(PsaHeads), ctypes.POINTER(PsaRotary), ctypes.POINTER(PsaPackedShape)
+    i32, i64 = ctypes.c_int32, ctypes.c_int64
+    lib.probsparse_layer_norm_fwd.restype = ctypes.c_int
+    lib.probsparse_layer_norm_fwd.argtypes = [vp, vp, vp, ctypes.c_double, vp, f32p, f32p, i64, i32, i32, vp]
+    lib.probsparse_layer_norm_bwd_workspace_bytes.restype = ctypes.c_size_t
+    lib.probsparse_layer_norm_bwd_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.probsparse_layer_norm_bwd.restype = ctypes.c_int
+    lib.probsparse_layer_norm_bwd.argtypes = [vp, vp, vp, f32p, f32p, vp, f32p, f32p, i64, i32, i32, vp, ctypes.c_size_t, vp]
+    lib.probsparse_rotary_frequencies.restype = ctypes.c_int
+    lib.probsparse_rotary_frequencies.argtypes = [rp, ctypes.POINTER(ctypes.c_double)]
+    for f in (lib.probsparse_rotary_fwd, lib.probsparse_rotary_bwd):
+        f.restype = ctypes.c_int
+        f.argtypes = [hp, hp, i32, rp, i32p, i64, i32, hp, hp, shp, vp]
+    for f in (lib.dense_attn_packed_workspace_bytes, lib.dense_attn_packed_bwd_workspace_bytes):
+        f.restype = ctypes.c_size_t
+        f.argtypes = [kp]
+    lib.dense_attn_packed_fwd.restype = ctypes.c_int
+    lib.dense_attn_packed_fwd.argtypes = [hp, hp, hp, i32p, i32p, hp, f32p, kp, vp, ctypes.c_size_t, vp]
+    lib.dense_attn_packed_bwd.restype = ctypes.c_int
+    lib.dense_attn_packed_bwd.argtypes = [hp, hp, hp, i32p, i32p, hp, f32p, hp, hp, hp, hp, kp, vp, ctypes.c_size_t, vp]
     lib.probsparse_describe_plan.restype = ctypes.c_int
     lib.probsparse_describe_plan.argtypes = [shp, optp, ctypes.c_int32, ctypes.c_char_p, ctypes.c_size_t]
     _lib, _native = lib, _load_native()
@@ -429,6 +472,205 @@ def dense_attn_fwd(Q, K, V, lengths, out=None, workspace=None):
     _check(load().dense_attn_fwd(_ptr(Q), _ptr(K), _ptr(V), _ptr(lengths), _ptr(out), ctypes.byref(shape),
                                  _ptr(workspace), workspace.numel(), _stream_ptr()))
     return out
+
+
+# ---- what stands around the attention: layer norm, rotary positions, dense attention over packed sequences.
+# Tensors of heads may have any strides the library takes (see psa_heads_t): [B, H, L, 64] or [H, T, 64] views of tensors
+# that lie by head, by frame or inside a larger one.  Calls run on the tensors' own device, on its current stream.
+
+def _device_of(*ts) -> torch.device:
+    device = ts[0].device
+    for t in ts:
+        if t is not None and (not t.is_cuda or t.device != device):
+            raise ValueError("tensors must be on one GPU")
+    return device
+
+
+def _require(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _require_like(t: Optional[torch.Tensor], shape, dtype, what: str, contiguous: bool = True):
+    """`t` is None or has this shape and type (and, unless it is a tensor of heads, no strides)."""
+    if t is not None:
+        _require(tuple(t.shape) == tuple(shape), f"{what} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+        if t.dtype != dtype:
+            raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
+        _require(t.is_contiguous() if contiguous else t.stride(-1) == 1,
+                 f"{what} must be contiguous" + ("" if contiguous else " in its last dimension"))
+
+
+def _launch(device: torch.device, function, *args):
+    """One call of the library on the current stream of `device`."""
+    if device.index == torch.cuda.current_device():
+        _check(function(*args, torch.cuda.current_stream(device).cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            _check(function(*args, torch.cuda.current_stream(device).cuda_stream))
+
+
+def _room(n: int, device: torch.device, given: Optional[torch.Tensor]) -> torch.Tensor:
+    """The caller's workspace, or one of n bytes."""
+    if n == 0:
+        raise ProbSparseError(-2, "invalid shape or options for workspace sizing")
+    if given is None:
+        return torch.empty(n, dtype=torch.uint8, device=device)
+    _require(given.is_contiguous() and given.device == device, "the workspace must be contiguous and on the tensors' device")
+    return given
+
+
+def _heads(t: torch.Tensor) -> PsaHeads:
+    return PsaHeads(t.data_ptr(), t.stride(0) if t.dim() == 4 else 0, t.stride(-3), t.stride(-2))
+
+
+def probsparse_layer_norm_fwd(X, gamma=None, beta=None, eps: float = 1e-5, Y=None, stats: bool = True):
+    """Layer norm over the last dimension of X.  Returns (Y, mean, rstd) with stats (what the backward reads: float32, one
+    for each row), else Y.  Y may be X."""
+    device = _device_of(X, gamma, beta, Y)
+    _require(X.dim() >= 1 and X.numel() > 0 and X.is_contiguous(), "X must be contiguous and not empty")
+    dtype, cols = _dtype_code(X), X.shape[-1]
+    for t, what in ((gamma, "gamma"), (beta, "beta")):
+        _require_like(t, (cols,), X.dtype, what)
+    _require_like(Y, X.shape, X.dtype, "Y")
+    if Y is None:
+        Y = torch.empty_like(X)
+    mean = rstd = None
+    if stats:
+        mean, rstd = (torch.empty(X.shape[:-1], dtype=torch.float32, device=device) for _ in range(2))
+    _launch(device, load().probsparse_layer_norm_fwd, _ptr(X), _ptr(gamma), _ptr(beta), eps, _ptr(Y), _ptr(mean), _ptr(rstd),
+            X.numel() // cols, cols, dtype)
+    return (Y, mean, rstd) if stats else Y
+
+
+def probsparse_layer_norm_bwd(dY, X, gamma, mean, rstd, workspace=None):
+    """Gradients (dX, dgamma, dbeta) of probsparse_layer_norm_fwd; dgamma and dbeta are float32."""
+    device = _device_of(X, dY, gamma, mean, rstd, workspace)
+    _require(X.dim() >= 1 and X.numel() > 0 and X.is_contiguous(), "X must be contiguous and not empty")
+    dtype, cols = _dtype_code(X), X.shape[-1]
+    rows = X.numel() // cols
+    _require_like(dY, X.shape, X.dtype, "dY")
+    _require_like(gamma, (cols,), X.dtype, "gamma")
+    for t, what in ((mean, "mean"), (rstd, "rstd")):
+        _require_like(t, X.shape[:-1], torch.float32, what)
+    lib = load()
+    workspace = _room(lib.probsparse_layer_norm_bwd_workspace_bytes(rows, cols, dtype), device, workspace)
+    dX = torch.empty_like(X)
+    dgamma, dbeta = (torch.empty(cols, dtype=torch.float32, device=device) for _ in range(2))
+    _launch(device, lib.probsparse_layer_norm_bwd, _ptr(dY), _ptr(X), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dX), _ptr(dgamma),
+            _ptr(dbeta), rows, cols, dtype, _ptr(workspace), workspace.numel() * workspace.element_size())
+    return dX, dgamma, dbeta
+
+
+def make_rotary(dim: int, layout: int = ROTARY_HALF, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0,
+                original_length: float = 0.0, fast_turns: float = 32.0, slow_turns: float = 1.0, magnitude: float = 1.0) -> PsaRotary:
+    """How positions turn the first `dim` elements of a head (see psa_rotary_t); checked here."""
+    rotary = PsaRotary(dim, layout, scaling, base, factor, original_length, fast_turns, slow_turns, magnitude)
+    _check(load().probsparse_rotary_frequencies(ctypes.byref(rotary), (ctypes.c_double * 32)()))
+    return rotary
+
+
+def rotary_frequencies(rotary: PsaRotary) -> list:
+    """Radians per position of each of the dim / 2 pairs."""
+    freq = (ctypes.c_double * 32)()
+    _check(load().probsparse_rotary_frequencies(ctypes.byref(rotary), freq))
+    return list(freq)[:rotary.dim // 2]
+
+
+def _rotary(function, Q, K, rotary, positions, first, Q_out, K_out):
+    device = _device_of(Q, K, positions, Q_out, K_out)
+    _require(Q.dim() in (3, 4) and Q.shape[-1] == 64, "Q must be [B, H, L, 64] or [H, T, 64]")
+    dtype = _dtype_code(Q)
+    B, (H, L) = Q.shape[0] if Q.dim() == 4 else 1, Q.shape[-3:-1]
+    _require_like(Q, Q.shape, Q.dtype, "Q", contiguous=False)
+    stride = 0
+    if positions is not None:
+        _require(positions.shape in ((L,), (B, L)), f"positions must be [{L}] or [{B}, {L}]")
+        _require_like(positions, positions.shape, torch.int32, "positions")
+        stride = L if positions.dim() == 2 else 0
+    if K is not None:
+        _require(K.dim() == Q.dim() and K.shape[:-3] == Q.shape[:-3] and K.shape[-2:] == Q.shape[-2:], "K must be Q but for its number of heads")
+        _require_like(K, K.shape, Q.dtype, "K", contiguous=False)
+        _require_like(K_out, K.shape, Q.dtype, "K_out", contiguous=False)
+        if K_out is None:
+            K_out = torch.empty_like(K)
+    _require_like(Q_out, Q.shape, Q.dtype, "Q_out", contiguous=False)
+    if Q_out is None:
+        Q_out = torch.empty_like(Q)
+    shape = make_shape(B, H, L, 1, dtype)
+    q, qo = _heads(Q), _heads(Q_out)
+    k, ko = (None, None) if K is None else (_heads(K), _heads(K_out))
+    _launch(device, function, ctypes.byref(q), None if k is None else ctypes.byref(k), 0 if K is None else K.shape[-3], ctypes.byref(rotary),
+            _ptr(positions), stride, first, ctypes.byref(qo), None if ko is None else ctypes.byref(ko), ctypes.byref(shape))
+    return Q_out if K is None else (Q_out, K_out)
+
+
+def probsparse_rotary_fwd(Q, K, rotary: PsaRotary, positions=None, first: int = 0, Q_out=None, K_out=None):
+    """Q [B, H, L, 64] and K [B, H_kv, L, 64] (or [H, T, 64] and [H_kv, T, 64]) turned by their positions: `positions` int32 [L] or
+    [B, L], or row l stands at first + l.  K may be None.  Returns (Q_out, K_out), or Q_out alone; an output may be its input."""
+    return _rotary(load().probsparse_rotary_fwd, Q, K, rotary, positions, first, Q_out, K_out)
+
+
+def probsparse_rotary_bwd(dQ_out, dK_out, rotary: PsaRotary, positions=None, first: int = 0, dQ=None, dK=None):
+    """The gradients of probsparse_rotary_fwd's inputs from those of its outputs."""
+    return _rotary(load().probsparse_rotary_bwd, dQ_out, dK_out, rotary, positions, first, dQ, dK)
+
+
+def _packed(Q, K, V, q_offsets, k_offsets, causal, scale):
+    _require(Q.dim() == 3 and Q.shape[-1] == 64, "Q must be [H, T_q, 64]")
+    _require(K.dim() == 3 and K.shape[-1] == 64, "K must be [H_kv, T_k, 64]")
+    _require(K.shape[0] > 0 and Q.shape[0] % K.shape[0] == 0, "the heads of Q must be a multiple of those of K")
+    _require_like(Q, Q.shape, Q.dtype, "Q", contiguous=False)
+    _require_like(K, K.shape, Q.dtype, "K", contiguous=False)
+    _require_like(V, K.shape, Q.dtype, "V", contiguous=False)
+    if k_offsets is None and q_offsets is not None:
+        _require(Q.shape[1] == K.shape[1], "without k_offsets Q and K must have the same rows")
+        k_offsets = q_offsets
+    _require((q_offsets is None) == (k_offsets is None), "k_offsets need q_offsets")
+    B = 1
+    if q_offsets is not None:
+        _require(q_offsets.dim() == 1 and q_offsets.numel() >= 2, "q_offsets must be [B + 1]")
+        B = q_offsets.numel() - 1
+        _require_like(q_offsets, (B + 1,), torch.int32, "q_offsets")
+        _require_like(k_offsets, (B + 1,), torch.int32, "k_offsets")
+    return k_offsets, PsaPackedShape(B, Q.shape[0], K.shape[0], Q.shape[1], K.shape[1], 64, _dtype_code(Q), int(bool(causal)),
+                                     0.125 if scale is None else scale)
+
+
+def dense_attn_packed_fwd(Q, K, V, q_offsets=None, k_offsets=None, causal: bool = False, scale: Optional[float] = None,
+                          out=None, lse: bool = False, workspace=None):
+    """Dense attention over packed sequences: Q [H, T_q, 64], K and V [H_kv, T_k, 64]; sequence s has the query rows
+    q_offsets[s] .. q_offsets[s + 1] - 1 (int32 [B + 1]; None: one sequence) and the key rows of k_offsets (None: the same).
+    `scale` is 1 / 8 unless given.  Returns out, or (out, lse) with lse [H, T_q] float32."""
+    device = _device_of(Q, K, V, q_offsets, k_offsets, out, workspace)
+    k_offsets, shape = _packed(Q, K, V, q_offsets, k_offsets, causal, scale)
+    _require_like(out, Q.shape, Q.dtype, "out", contiguous=False)
+    lib = load()
+    workspace = _room(lib.dense_attn_packed_workspace_bytes(ctypes.byref(shape)), device, workspace)
+    if out is None:
+        out = torch.empty_like(Q)
+    norm = torch.empty(Q.shape[:2], dtype=torch.float32, device=device) if lse else None
+    q, k, v, o = _heads(Q), _heads(K), _heads(V), _heads(out)
+    _launch(device, lib.dense_attn_packed_fwd, ctypes.byref(q), ctypes.byref(k), ctypes.byref(v), _ptr(q_offsets), _ptr(k_offsets),
+            ctypes.byref(o), _ptr(norm), ctypes.byref(shape), _ptr(workspace), workspace.numel() * workspace.element_size())
+    return (out, norm) if lse else out
+
+
+def dense_attn_packed_bwd(Q, K, V, out, lse, dOut, q_offsets=None, k_offsets=None, causal: bool = False,
+                          scale: Optional[float] = None, dQ=None, dK=None, dV=None, workspace=None):
+    """Gradients (dQ, dK, dV) of dense_attn_packed_fwd, from its out and lse."""
+    device = _device_of(Q, K, V, out, lse, dOut, q_offsets, k_offsets, dQ, dK, dV, workspace)
+    k_offsets, shape = _packed(Q, K, V, q_offsets, k_offsets, causal, scale)
+    for t, like, what in ((out, Q, "out"), (dOut, Q, "dOut"), (dQ, Q, "dQ"), (dK, K, "dK"), (dV, V, "dV")):
+        _require_like(t, like.shape, Q.dtype, what, contiguous=False)
+    _require_like(lse, Q.shape[:2], torch.float32, "lse")
+    lib = load()
+    workspace = _room(lib.dense_attn_packed_bwd_workspace_bytes(ctypes.byref(shape)), device, workspace)
+    dQ, dK, dV = (torch.empty_like(t) if g is None else g for t, g in ((Q, dQ), (K, dK), (V, dV)))
+    heads = [ctypes.byref(_heads(t)) for t in (Q, K, V, out, dOut, dQ, dK, dV)]
+    _launch(device, lib.dense_attn_packed_bwd, *heads[:3], _ptr(q_offsets), _ptr(k_offsets), heads[3], _ptr(lse), *heads[4:],
+            ctypes.byref(shape), _ptr(workspace), workspace.numel() * workspace.element_size())
+    return dQ, dK, dV
 
 
 def version() -> int:

@@ -787,6 +787,6 @@ int probsparse_init(void)
     return PSA_OK;
 }
 
-int probsparse_version(void) { return 100; }
+int probsparse_version(void) { return 200; }
 
 }  // extern "C"

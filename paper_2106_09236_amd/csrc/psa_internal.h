@@ -164,4 +164,35 @@ hipError_t launch_qkv_project(const psa_shape_t& s, const void* X, const psa_mhs
 hipError_t launch_out_project(const psa_shape_t& s, const void* A, const psa_mhsa_weights_t& w, void* Y, hipStream_t stream);
 const char* project_route_name(const psa_shape_t& s, int n_mat);         // the kernel for n_mat = 3 (Q, K, V) or 1 (output) matrices
 
+// Layer norm (psa_norm.hip): tpr threads with nv vectors of 16 bytes for a row, nv = 0 for rows too long to keep;
+// n_part partial rows of the weights' gradients.
+struct NormPlan { int tpr, nv, n_part; size_t off_part, total; };
+NormPlan make_norm_plan(int64_t rows, int cols, int dtype);
+hipError_t launch_norm_fwd(const NormPlan& p, const void* X, const void* gamma, const void* beta, float eps, void* Y, float* mean,
+                           float* rstd, int64_t rows, int cols, int dtype, hipStream_t stream);
+hipError_t launch_norm_bwd(const NormPlan& p, const void* dY, const void* X, const void* gamma, const float* mean, const float* rstd,
+                           void* dX, float* dgamma, float* dbeta, int64_t rows, int cols, int dtype, void* workspace, hipStream_t stream);
+
+// Rotary positions (psa_rotary.hip); freq: radians per position of each pair; back: the other way.
+hipError_t launch_rotary(const psa_heads_t* Q, const psa_heads_t* K, int H_kv, const psa_rotary_t& o, const double* freq, bool back,
+                         const int* positions, int64_t positions_stride, int first, const psa_heads_t* Qo, const psa_heads_t* Ko,
+                         const psa_shape_t& s, hipStream_t stream);
+
+// Dense attention over packed sequences (psa_packed.hip, psa_packed_backward.hip).
+//   few      1: the waves of a work-group share 32 rows and divide its keys; 0: each wave has rows of its own
+//   n_tile   work-groups along the rows of a key head (rows of one token for each head of its group), an upper bound
+//   n_split  parts of the keys, joined by a second kernel where there are several
+struct PackedPlan {
+    int few, rows, n_tile, n_split;
+    size_t off_part, total;
+};
+PackedPlan make_packed_plan(const psa_packed_shape_t& s);
+hipError_t launch_packed(const PackedPlan& p, const psa_packed_shape_t& s, const psa_heads_t& Q, const psa_heads_t& K, const psa_heads_t& V,
+                         const int* q_offsets, const int* k_offsets, const psa_heads_t& out, float* lse, void* workspace, hipStream_t stream);
+struct PackedBwdPlan { int n_qtile, n_ktile; size_t total; };
+PackedBwdPlan make_packed_bwd_plan(const psa_packed_shape_t& s);
+hipError_t launch_packed_bwd(const PackedBwdPlan& p, const psa_packed_shape_t& s, const psa_heads_t& Q, const psa_heads_t& K, const psa_heads_t& V,
+                             const int* q_offsets, const int* k_offsets, const psa_heads_t& out, const float* lse, const psa_heads_t& dOut,
+                             const psa_heads_t& dQ, const psa_heads_t& dK, const psa_heads_t& dV, void* workspace, hipStream_t stream);
+
 }  // namespace psa

@@ -1,0 +1,275 @@
+// Dense attention over packed sequences: what the forward and backward kernels share.
+//
+// A key head's rows.  The query heads of a group read the same keys, so the rows of a tile are (query, head of the group)
+// pairs: row r of a sequence is query r / G of head r % G of the group (G = H / H_kv), and a tile of keys that is in LDS
+// serves the whole group.  With one head to a group rows are queries.
+//
+// Products are taken with the queries (or keys) that a wave owns on the column axis of the matrix instruction
+// (D[i][j], i = 8 (r / 4) + 4 h + r % 4 for accumulator register r, j = c; lane (c, h) = (lane % 32, lane / 32)): a lane
+// owns one column, so everything softmax keeps per row is a scalar of the lane, and the accumulator registers of the first
+// product are the second operand of the next as they are (their row order taken as its order of summation).
+#pragma once
+
+#include "psa_tile.h"
+#include "psa_vec.h"
+
+namespace psa {
+
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kMaxInit = -3.0e38f;       // below every finite score; finite, so that exp2(-inf - it) is 0 and not NaN
+
+// One tensor's heads as a kernel takes them (strides in elements).
+template <typename T>
+struct Heads {
+    T* data; int64_t head, row;
+    __device__ __forceinline__ T* at(int h, int64_t l) const { return data + h * head + l * row; }
+};
+template <typename T>
+inline Heads<T> heads_of(const psa_heads_t& t) { return Heads<T>{static_cast<T*>(t.data), t.head_stride, t.row_stride}; }
+
+// The sequences of a call: offsets and what they are clamped to.
+struct Packing { const int* qo; const int* ko; int B, Tq, Tk, G; };
+
+// The tile a work-group takes: rows (or keys) tile * PER .. of the sequence; tile < 0: there is none.
+struct SeqTile { int q0, nq, k0, nk, tile; };
+
+// Tile x of the call, counted from the last tile of the last sequence (with a causal mask the last tiles of a sequence have
+// the most keys, and the longest work should start first).  64 sequences at a time: a prefix sum over the lanes of how many
+// tiles each has.  Every wave finds it for itself.
+template <int PER, bool KEYS>
+__device__ __forceinline__ SeqTile find_tile(const Packing& p, int x)
+{
+    SeqTile f{0, 0, 0, 0, -1};
+    if (!p.qo) {
+        f.nq = p.Tq; f.nk = p.Tk;
+        const int n = ((KEYS ? p.Tk : p.Tq * p.G) + PER - 1) / PER;
+        f.tile = n - 1 - x;
+        return f;
+    }
+    const int lane = threadIdx.x & 63;
+    for (int base = 0; base < p.B; base += 64) {
+        const int s = p.B - 1 - base - lane;
+        int q0 = 0, q1 = 0, k0 = 0, k1 = 0;
+        if (s >= 0) {
+            q0 = min(max(p.qo[s], 0), p.Tq); q1 = min(max(p.qo[s + 1], q0), p.Tq);
+            k0 = min(max(p.ko[s], 0), p.Tk); k1 = min(max(p.ko[s + 1], k0), p.Tk);
+        }
+        const int n = ((KEYS ? k1 - k0 : (q1 - q0) * p.G) + PER - 1) / PER;
+        int sum = n;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int y = __shfl_up(sum, d, 64);
+            if (lane >= d) sum += y;
+        }
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(sum > x);
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            f.q0 = __builtin_amdgcn_readlane(q0, l); f.nq = __builtin_amdgcn_readlane(q1, l) - f.q0;
+            f.k0 = __builtin_amdgcn_readlane(k0, l); f.nk = __builtin_amdgcn_readlane(k1, l) - f.k0;
+            f.tile = __builtin_amdgcn_readlane(sum, l) - 1 - x;
+            return f;
+        }
+        x -= __builtin_amdgcn_readlane(sum, 63);
+    }
+    return f;
+}
+
+// Zeros in the rows of `t` that belong to no sequence (before the first offset, from the last one on), the share `x` of
+// `n` work-groups; `each(head, row)` is called by one thread of the work-group for each head.
+template <typename T, typename F>
+__device__ __forceinline__ void zero_outside(const Heads<T>& t, const int* offsets, int B, int rows, int head0, int heads, int x, int n, F each)
+{
+    if (!offsets) return;
+    const int first = min(max(offsets[0], 0), rows), last = min(max(offsets[B], first), rows);
+    const int per = (rows + n - 1) / n;
+    const int64_t r0 = (int64_t)x * per;
+    const int r1 = (int)min((int64_t)rows, r0 + per);
+    if (r0 >= first && r1 <= last) return;
+    constexpr int CH = 64 * sizeof(T) / 16;
+    const int per_row = heads * CH;
+    for (int64_t i = threadIdx.x; i < (int64_t)(r1 - r0) * per_row; i += blockDim.x) {
+        const int row = (int)(r0 + i / per_row), k = (int)(i % per_row), h = head0 + k / CH;
+        if (row >= first && row < last) continue;
+        reinterpret_cast<uint4*>(t.at(h, row))[k % CH] = make_uint4(0u, 0u, 0u, 0u);
+        if (k % CH == 0) each(h, row);
+    }
+}
+
+// Rows base .. base + n - 1 (n may be <= 0) of a head as a buffer: reads of rows behind them give zeros.  The base moves with the tile, so
+// that offsets into a long tensor stay small.
+template <typename T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rows(const T* base, int64_t row_stride, int n)
+{
+    const int bytes = n > 0 ? (int)((n - 1) * row_stride * (int64_t)sizeof(T)) + 64 * (int)sizeof(T) : 0;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, bytes, 0x00020000);
+}
+
+// Any infinity or NaN among the elements of 16 bytes?
+__device__ __forceinline__ bool nonfinite(const uint4& x, float)
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    bool b = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b |= (w[i] & 0x7F800000u) == 0x7F800000u;
+    return b;
+}
+__device__ __forceinline__ bool nonfinite(const uint4& x, bf16_t)
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    bool b = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b |= (w[i] & 0x7F80u) == 0x7F80u || (w[i] & 0x7F800000u) == 0x7F800000u;
+    return b;
+}
+__device__ __forceinline__ uint4 finite_only(const uint4& x, float)
+{
+    uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if ((w[i] & 0x7F800000u) == 0x7F800000u) w[i] = 0u;
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint4 finite_only(const uint4& x, bf16_t)
+{
+    uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if ((w[i] & 0x7F80u) == 0x7F80u) w[i] &= 0xFFFF0000u;
+        if ((w[i] & 0x7F800000u) == 0x7F800000u) w[i] &= 0x0000FFFFu;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Key (or row) of a tile of 32 that accumulator register r of half h holds.
+__device__ __forceinline__ constexpr int acc_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
+
+__device__ __forceinline__ void clear(floatx16& a)
+{
+#pragma unroll
+    for (int r = 0; r < 16; ++r) a[r] = 0.f;
+}
+
+// ---- a tile of rows in LDS, row-major with its 16-byte chunks permuted inside a row by the row's low bits, so that reads
+// of one chunk of many rows and of many chunks of one row both spread over the banks.
+template <typename T> struct LdsTile;
+template <> struct LdsTile<bf16_t> {
+    static constexpr int kRowBytes = 128;
+    static __device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ row) & 7) * 16; }
+};
+template <> struct LdsTile<float> {
+    static constexpr int kRowBytes = 256;
+    // rows 4 apart, which the two halves of a wave read at once in the second product, land in different halves of the banks
+    static __device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 256 + ((chunk ^ (row & 7) ^ ((row & 4) << 1)) & 15) * 16; }
+};
+
+// ---- operands.  Q (or the columns' tensor of any product over the head's elements): this lane's column as B operand,
+// the elements a lane holds in the order that the rows' operand has them.
+template <typename T> struct ColOperand;
+template <> struct ColOperand<bf16_t> {
+    uint4 v[4];                            // elements 32 h + 8 k .. + 7
+    __device__ __forceinline__ void load(const bf16_t* row, int h) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = reinterpret_cast<const uint4*>(row)[4 * h + k];
+    }
+};
+template <> struct ColOperand<float> {
+    float4 v[8];                           // elements 8 k + 4 h .. + 3
+    __device__ __forceinline__ void load(const float* row, int h) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = reinterpret_cast<const float4*>(row)[2 * k + h];
+    }
+};
+// Rows of an LDS tile (32 from `row0`) as A operand, the same elements: lane (c, h) holds row row0 + c.
+template <typename T> using RowOperand = ColOperand<T>;
+__device__ __forceinline__ void lds_rows(RowOperand<bf16_t>& a, const unsigned char* s, int row0, int c, int h)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) a.v[k] = *reinterpret_cast<const uint4*>(s + LdsTile<bf16_t>::chunk_at(row0 + c, 4 * h + k));
+}
+__device__ __forceinline__ void lds_rows(RowOperand<float>& a, const unsigned char* s, int row0, int c, int h)
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k) a.v[k] = *reinterpret_cast<const float4*>(s + LdsTile<float>::chunk_at(row0 + c, 2 * k + h));
+}
+// D[row][col] += sum over the head's 64 elements
+__device__ __forceinline__ floatx16 product(const RowOperand<bf16_t>& a, const ColOperand<bf16_t>& b, floatx16 d)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.v[k]), __builtin_bit_cast(bf16x8, b.v[k]), d, 0, 0, 0);
+    return d;
+}
+__device__ __forceinline__ floatx16 product(const RowOperand<float>& a, const ColOperand<float>& b, floatx16 d)
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        d = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[k].x, b.v[k].x, d, 0, 0, 0);
+        d = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[k].y, b.v[k].y, d, 0, 0, 0);
+        d = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[k].z, b.v[k].z, d, 0, 0, 0);
+        d = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[k].w, b.v[k].w, d, 0, 0, 0);
+    }
+    return d;
+}
+
+// D^T[e][col] += sum over 32 rows of the LDS tile from row0 of X[row][e] * w[row], w in accumulator order (row acc_row(r, h) in
+// w[r]); D in two accumulators of 32 elements e.
+// bfloat16: w is rounded to bfloat16; the tile is read through the transposing LDS read: of each group of 16 lanes, lane s
+// points at row s / 4 of four rows, columns 4 (s % 4) .., and lane i receives column i of the four rows.
+__device__ __forceinline__ void accumulate(floatx16 (&d)[2], const unsigned char* s, int row0, const floatx16& w, int c, int h, bf16_t)
+{
+    const int s16 = c & 15, row = row0 + 4 * h + (s16 >> 2), col = (c & 16) + 4 * (s16 & 3);
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+        uint4 b;
+        b.x = cvt_pk_bf16(w[8 * st], w[8 * st + 1]);
+        b.y = cvt_pk_bf16(w[8 * st + 2], w[8 * st + 3]);
+        b.z = cvt_pk_bf16(w[8 * st + 4], w[8 * st + 5]);
+        b.w = cvt_pk_bf16(w[8 * st + 6], w[8 * st + 7]);
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt) {
+            uint2 part[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = row + 16 * st + 8 * e, byte = (col + 32 * dt) * 2;
+                const unsigned char* p = s + LdsTile<bf16_t>::chunk_at(r, byte >> 4) + (byte & 15);
+                part[e] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((shortx4 __attribute__((address_space(3)))*)(p)));
+            }
+            const uint4 a = make_uint4(part[0].x, part[0].y, part[1].x, part[1].y);
+            d[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), d[dt], 0, 0, 0);
+        }
+    }
+}
+__device__ __forceinline__ void accumulate(floatx16 (&d)[2], const unsigned char* s, int row0, const floatx16& w, int c, int h, float)
+{
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt) {
+            const float a = *reinterpret_cast<const float*>(s + LdsTile<float>::chunk_at(row0 + acc_row(r, h), (32 * dt + c) >> 2) + (c & 3) * 4);
+            d[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], d[dt], 0, 0, 0);
+        }
+}
+
+// Column c's 64 elements of D^T (elements 32 dt + acc_row(r, h) in d[dt][r]) times f, to its row of a tensor.
+__device__ __forceinline__ void store_row(bf16_t* row, const floatx16 (&d)[2], float f, int h)
+{
+#pragma unroll
+    for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<uint2*>(row + 32 * dt + 8 * k + 4 * h) =
+                make_uint2(cvt_pk_bf16(d[dt][4 * k] * f, d[dt][4 * k + 1] * f), cvt_pk_bf16(d[dt][4 * k + 2] * f, d[dt][4 * k + 3] * f));
+}
+__device__ __forceinline__ void store_row(float* row, const floatx16 (&d)[2], float f, int h)
+{
+#pragma unroll
+    for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<float4*>(row + 32 * dt + 8 * k + 4 * h) =
+                make_float4(d[dt][4 * k] * f, d[dt][4 * k + 1] * f, d[dt][4 * k + 2] * f, d[dt][4 * k + 3] * f);
+}
+
+}  // namespace psa

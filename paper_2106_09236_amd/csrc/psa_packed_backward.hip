@@ -1,0 +1,250 @@
+// Dense attention over packed sequences, backward.  With p the weights, recomputed from Q, K and the forward's lse, G = dOut
+// and d_t = G[t].out[t]:
+//   ds_tj = p_tj (G[t].V[j] - d_t),  dQ[t] = scale sum_j ds_tj K[j],  dK[j] = scale sum_t ds_tj Q[t],  dV[j] = sum_t p_tj G[t]
+// Three launches: d_t and lse row by row (bound by memory); dK and dV with a work-group's keys held and the rows passing by;
+// dQ with the rows held and the keys passing by.  The scores and G.V are computed in both of the latter, seven products
+// where five would do if dQ were added up in memory by atomics, whose order would change the result.
+#include "psa_packed.h"
+
+namespace psa {
+
+// lse (base 2; +infinity for a row that sees no key, whose weights then are 0) and d of every row, [H_kv][T_q * G] each.
+template <typename T>
+__global__ __launch_bounds__(256)
+void packed_stats_kernel(Heads<const T> out, Heads<const T> dOut, const float* __restrict__ lse, Heads<T> dQ, Packing p, int H,
+                         float* __restrict__ stat_l, float* __restrict__ stat_d)
+{
+    constexpr int VEC = kVec<T>, CH = 64 / VEC;        // lanes of a row
+    const int n_wg = gridDim.x;
+    zero_outside(dQ, p.qo, p.B, p.Tq, 0, H, blockIdx.x, n_wg, [](int, int) {});
+    const int64_t id = (int64_t)blockIdx.x * (256 / CH) + threadIdx.x / CH;
+    if (id >= (int64_t)p.Tq * H) return;
+    const int head = (int)(id / p.Tq), t = (int)(id % p.Tq), ch = threadIdx.x % CH;
+    float a[VEC], b[VEC], sum = 0.f;
+    load_vec(a, out.at(head, t) + ch * VEC, VEC);
+    load_vec(b, dOut.at(head, t) + ch * VEC, VEC);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) sum = fmaf(a[i], b[i], sum);
+#pragma unroll
+    for (int k = 1; k < CH; k *= 2) sum += __shfl_xor(sum, k, 64);
+    if (ch == 0) {
+        const float l = lse[(int64_t)head * p.Tq + t];
+        const int64_t o = (int64_t)(head / p.G) * p.Tq * p.G + (int64_t)t * p.G + head % p.G;
+        stat_l[o] = l == -INFINITY ? INFINITY : l * kLog2e;
+        stat_d[o] = sum;
+    }
+}
+
+// dK and dV of 128 keys: 4 waves of 32, tiles of 32 rows of Q and dOut through LDS.
+template <typename T>
+__global__ __launch_bounds__(256)
+void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, const float* __restrict__ stat_l,
+                       const float* __restrict__ stat_d, Packing p, Heads<T> dK, Heads<T> dV, int H_kv, int causal, float scale,
+                       float scale_log2, int n_tile)
+{
+    constexpr int QT = 32;
+    constexpr int CH = 64 * sizeof(T) / 16, NL = QT * CH / 256;
+    constexpr int kTileBytes = QT * LdsTile<T>::kRowBytes;
+    __shared__ __attribute__((aligned(16))) unsigned char sQ[2][kTileBytes], sG[2][kTileBytes];
+    __shared__ __attribute__((aligned(16))) float sL[2][QT], sD[2][QT];
+    const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
+    zero_outside(dK, p.ko, p.B, p.Tk, hk, 1, x, n_tile, [](int, int) {});
+    zero_outside(dV, p.ko, p.B, p.Tk, hk, 1, x, n_tile, [](int, int) {});
+    const SeqTile f = find_tile<128, true>(p, x);
+    if (f.tile < 0) return;
+    const int n_rows = f.nq * p.G;
+    const int shift = f.nk - f.nq + 1;
+    // the first row that sees key j (rows are in the order of their queries)
+    auto first_row = [&](int j) { return causal ? max(j - shift + 1, 0) * p.G : 0; };
+    const int key = f.tile * 128 + wave * 32 + c, kc = min(key, f.nk - 1);
+    const int first = first_row(kc);
+    const int first_all = __builtin_amdgcn_readfirstlane(first_row(f.tile * 128));
+    const int wave_key = min(f.tile * 128 + wave * 32, f.nk - 1);
+    const int first_wave = __builtin_amdgcn_readfirstlane(first_row(wave_key));
+    const int first_every = __builtin_amdgcn_readfirstlane(first_row(min(wave_key + 31, f.nk - 1)));
+
+    ColOperand<T> k, v;
+    k.load(K.at(hk, f.k0 + kc), h);
+    v.load(V.at(hk, f.k0 + kc), h);
+    floatx16 dk[2], dv[2];
+    clear(dk[0]); clear(dk[1]); clear(dv[0]); clear(dv[1]);
+
+    const int64_t stat0 = ((int64_t)hk * p.Tq + f.q0) * p.G;
+    uint4 qr[NL], gr[NL];
+    float lr = INFINITY, dr = 0.f;
+    auto fetch = [&](int r0) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int id = i * 256 + tid, r = r0 + id / CH, ch = id % CH;
+            qr[i] = gr[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (r < n_rows) {
+                const int t = r / p.G, head = hk * p.G + (r - t * p.G);
+                qr[i] = reinterpret_cast<const uint4*>(Q.at(head, f.q0 + t))[ch];
+                gr[i] = reinterpret_cast<const uint4*>(dOut.at(head, f.q0 + t))[ch];
+            }
+        }
+        if (tid < QT) {
+            const bool in = r0 + tid < n_rows;
+            lr = in ? stat_l[stat0 + r0 + tid] : INFINITY;
+            dr = in ? stat_d[stat0 + r0 + tid] : 0.f;
+        }
+    };
+    int r0 = first_all / QT * QT;
+    if (r0 < n_rows) fetch(r0);
+    for (int buf = 0; r0 < n_rows; r0 += QT, buf ^= 1) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int id = i * 256 + tid, ofs = LdsTile<T>::chunk_at(id / CH, id % CH);
+            *reinterpret_cast<uint4*>(sQ[buf] + ofs) = qr[i];
+            *reinterpret_cast<uint4*>(sG[buf] + ofs) = gr[i];
+        }
+        if (tid < QT) { sL[buf][tid] = lr; sD[buf][tid] = dr; }
+        if (r0 + QT < n_rows) fetch(r0 + QT);
+        lds_barrier();
+        if (r0 + QT <= first_wave) continue;
+        RowOperand<T> a;
+        floatx16 s, w;
+        clear(s); clear(w);
+        lds_rows(a, sQ[buf], 0, c, h);
+        s = product(a, k, s);
+        lds_rows(a, sG[buf], 0, c, h);
+        w = product(a, v, w);
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+            const float4 l4 = *reinterpret_cast<const float4*>(&sL[buf][8 * r4 + 4 * h]), d4 = *reinterpret_cast<const float4*>(&sD[buf][8 * r4 + 4 * h]);
+            const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[4 * r4 + e] = fast_exp2(fmaf(s[4 * r4 + e], scale_log2, -l[e]));
+                w[4 * r4 + e] = s[4 * r4 + e] * (w[4 * r4 + e] - d[e]);
+            }
+        }
+        if (r0 < first_every) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (r0 + acc_row(r, h) < first) { s[r] = 0.f; w[r] = 0.f; }
+        }
+        accumulate(dv, sG[buf], 0, s, c, h, T{});
+        accumulate(dk, sQ[buf], 0, w, c, h, T{});
+    }
+    if (key >= f.nk) return;
+    store_row(dK.at(hk, f.k0 + key), dk, scale, h);
+    store_row(dV.at(hk, f.k0 + key), dv, 1.f, h);
+}
+
+// dQ of 128 rows: 4 waves of 32, tiles of 32 keys and values through LDS.
+template <typename T>
+__global__ __launch_bounds__(256)
+void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, const float* __restrict__ stat_l,
+                      const float* __restrict__ stat_d, Packing p, Heads<T> dQ, int H_kv, int causal, float scale, float scale_log2)
+{
+    constexpr int KT = 32;
+    constexpr int CH = 64 * sizeof(T) / 16, NL = KT * CH / 256;
+    constexpr int kTileBytes = KT * LdsTile<T>::kRowBytes;
+    __shared__ __attribute__((aligned(16))) unsigned char sK[2][kTileBytes], sV[2][kTileBytes];
+    const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
+    const SeqTile f = find_tile<128, false>(p, x);
+    if (f.tile < 0) return;
+    const int n_rows = f.nq * p.G;
+    const int shift = f.nk - f.nq + 1;
+    auto visible = [&](int r) { const int t = r / p.G; return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
+    const int row0 = f.tile * 128 + wave * 32;
+    const int row = row0 + c, rc = min(row, n_rows - 1);
+    const int t = rc / p.G, head = hk * p.G + (rc - t * p.G);
+    const int n_vis = visible(rc);
+    const int n_all = __builtin_amdgcn_readfirstlane(visible(min(f.tile * 128 + 127, n_rows - 1)));
+    const int n_wave = __builtin_amdgcn_readfirstlane(row0 < n_rows ? visible(min(row0 + 31, n_rows - 1)) : 0);
+    const int n_every = __builtin_amdgcn_readfirstlane(visible(min(row0, n_rows - 1)));
+    ColOperand<T> q, g;
+    q.load(Q.at(head, f.q0 + t), h);
+    g.load(dOut.at(head, f.q0 + t), h);
+    const int64_t so = ((int64_t)hk * p.Tq + f.q0) * p.G + rc;
+    const float l = stat_l[so], d = stat_d[so];
+    floatx16 dq[2];
+    clear(dq[0]); clear(dq[1]);
+    const T* Kh = K.at(hk, f.k0);
+    const T* Vh = V.at(hk, f.k0);
+    uint4 kr[NL], vr[NL];
+    auto fetch = [&](int j0) {
+        const int n = min(KT, f.nk - j0);
+        const auto kb = tile_rows(Kh + j0 * K.row, K.row, n), vb = tile_rows(Vh + j0 * V.row, V.row, n);
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int id = i * 256 + tid, r = id / CH, ch = id % CH;
+            kr[i] = buffer_load16<uint4>(kb, (int)(r * K.row * (int64_t)sizeof(T)) + ch * 16);
+            vr[i] = buffer_load16<uint4>(vb, (int)(r * V.row * (int64_t)sizeof(T)) + ch * 16);
+        }
+    };
+    if (n_all > 0) fetch(0);
+    int buf = 0;
+    for (int j0 = 0; j0 < n_all; j0 += KT, buf ^= 1) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int id = i * 256 + tid, ofs = LdsTile<T>::chunk_at(id / CH, id % CH);
+            *reinterpret_cast<uint4*>(sK[buf] + ofs) = kr[i];
+            *reinterpret_cast<uint4*>(sV[buf] + ofs) = vr[i];
+        }
+        if (j0 + KT < n_all) fetch(j0 + KT);
+        lds_barrier();
+        if (j0 >= n_wave) continue;
+        RowOperand<T> a;
+        floatx16 s, w;
+        clear(s); clear(w);
+        lds_rows(a, sK[buf], 0, c, h);
+        s = product(a, q, s);
+        lds_rows(a, sV[buf], 0, c, h);
+        w = product(a, g, w);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w[r] = fast_exp2(fmaf(s[r], scale_log2, -l)) * (w[r] - d);
+        if (j0 + KT > n_every) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (j0 + acc_row(r, h) >= n_vis) w[r] = 0.f;
+        }
+        accumulate(dq, sK[buf], 0, w, c, h, T{});
+    }
+    if (row >= n_rows) return;
+    store_row(dQ.at(head, f.q0 + t), dq, scale, h);
+}
+
+PackedBwdPlan make_packed_bwd_plan(const psa_packed_shape_t& s)
+{
+    PackedBwdPlan p{};
+    p.n_qtile = (int)((int64_t)s.T_q * (s.H / s.H_kv) / 128) + s.B;
+    p.n_ktile = s.T_k / 128 + s.B;
+    p.total = 2 * (((size_t)s.T_q * s.H * sizeof(float) + 255) & ~(size_t)255);
+    return p;
+}
+
+template <typename T>
+static void packed_bwd_go(const PackedBwdPlan& p, const psa_packed_shape_t& s, const psa_heads_t& Q, const psa_heads_t& K, const psa_heads_t& V,
+                          const Packing& pk, const psa_heads_t& out, const float* lse, const psa_heads_t& dOut, const psa_heads_t& dQ,
+                          const psa_heads_t& dK, const psa_heads_t& dV, void* workspace, hipStream_t stream)
+{
+    float* stat_l = static_cast<float*>(workspace);
+    float* stat_d = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.total / 2);
+    const float scale = (float)s.scale, scale_log2 = (float)(s.scale * 1.4426950408889634);
+    constexpr int rows = 256 / (64 / kVec<T>);
+    packed_stats_kernel<T><<<(unsigned)(((int64_t)s.T_q * s.H + rows - 1) / rows), 256, 0, stream>>>(
+        heads_of<const T>(out), heads_of<const T>(dOut), lse, heads_of<T>(dQ), pk, s.H, stat_l, stat_d);
+    packed_dkv_kernel<T><<<(unsigned)(p.n_ktile * s.H_kv), 256, 0, stream>>>(
+        heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), heads_of<const T>(dOut), stat_l, stat_d, pk,
+        heads_of<T>(dK), heads_of<T>(dV), s.H_kv, s.causal, scale, scale_log2, p.n_ktile);
+    packed_dq_kernel<T><<<(unsigned)(p.n_qtile * s.H_kv), 256, 0, stream>>>(
+        heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), heads_of<const T>(dOut), stat_l, stat_d, pk,
+        heads_of<T>(dQ), s.H_kv, s.causal, scale, scale_log2);
+}
+hipError_t launch_packed_bwd(const PackedBwdPlan& p, const psa_packed_shape_t& s, const psa_heads_t& Q, const psa_heads_t& K, const psa_heads_t& V,
+                             const int* q_offsets, const int* k_offsets, const psa_heads_t& out, const float* lse, const psa_heads_t& dOut,
+                             const psa_heads_t& dQ, const psa_heads_t& dK, const psa_heads_t& dV, void* workspace, hipStream_t stream)
+{
+    (void)hipGetLastError();
+    const Packing pk{q_offsets, k_offsets, s.B, s.T_q, s.T_k, s.H / s.H_kv};
+    if (s.dtype == PSA_F32) packed_bwd_go<float>(p, s, Q, K, V, pk, out, lse, dOut, dQ, dK, dV, workspace, stream);
+    else packed_bwd_go<bf16_t>(p, s, Q, K, V, pk, out, lse, dOut, dQ, dK, dV, workspace, stream);
+    return hipGetLastError();
+}
+
+}  // namespace psa
