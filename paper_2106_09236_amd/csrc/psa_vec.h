@@ -47,6 +47,19 @@ __device__ __forceinline__ void load_vec(float (&v)[kVec<T>], const T* p, int n)
         for (int i = 0; i < kVec<T>; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
     }
 }
+// the same without the conversion: to be asked for ahead of its use
+template <typename T>
+__device__ __forceinline__ Chunk<T> load_chunk(const T* p, int n) {
+    Chunk<T> c;
+    if (n >= kVec<T>) {
+        c = *reinterpret_cast<const Chunk<T>*>(p);
+    } else {
+        float v[kVec<T>];
+        load_vec(v, p, n);
+        pack(c.w, v, T{});
+    }
+    return c;
+}
 template <typename T>
 __device__ __forceinline__ void store_vec(T* p, const float (&v)[kVec<T>], int n) {
     if (n >= kVec<T>) {
