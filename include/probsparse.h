@@ -367,9 +367,9 @@ int probsparse_rotary_bwd(const psa_heads_t* dQ_out, const psa_heads_t* dK_out, 
  *   lse[h, t] = ln sum_j exp(scale * Q[h, t].K[j])   over the keys that t sees
  * A query that sees no key, and a row of Q in no sequence, get zeros in out and -infinity in
  * lse.  What a query does not see has no part in its output, infinities and NaN included.
- *   q_offsets, k_offsets  DEVICE int32 [B + 1], not decreasing (values are clamped to [0, T],
- *             and a sequence that would end before it begins is empty); both NULL: one
- *             sequence of all rows (B = 1)
+ *   q_offsets, k_offsets  DEVICE int32 [B + 1], not decreasing (values are clamped to [0, T];
+ *             where they decrease the results are unspecified, but nothing outside the tensors
+ *             is touched); both NULL: one sequence of all rows (B = 1)
  *   Q, out    H heads of T_q rows;  K, V: H_kv heads of T_k rows; batch_stride is ignored
  *   lse       [H, T_q] float32 DEVICE, or NULL
  * Arithmetic: bfloat16 operands are multiplied exactly and summed in float32; the weights p are

@@ -88,6 +88,7 @@ class _CtypesOnly:
     def attn_fwd(*args):
         return None
     attn_fwd_opt = attn_fwd_with_indices = attn_bwd = mhsa_fwd = attn_fwd
+    layer_norm_fwd = layer_norm_bwd = rotary = packed_fwd = packed_bwd = attn_fwd
 
 
 _lib = None
@@ -527,6 +528,9 @@ def _heads(t: torch.Tensor) -> PsaHeads:
 def probsparse_layer_norm_fwd(X, gamma=None, beta=None, eps: float = 1e-5, Y=None, stats: bool = True):
     """Layer norm over the last dimension of X.  Returns (Y, mean, rstd) with stats (what the backward reads: float32, one
     for each row), else Y.  Y may be X."""
+    done = (_native or _fast()).layer_norm_fwd(X, gamma, beta, eps, Y, stats)
+    if done is not None:
+        return done
     device = _device_of(X, gamma, beta, Y)
     _require(X.dim() >= 1 and X.numel() > 0 and X.is_contiguous(), "X must be contiguous and not empty")
     dtype, cols = _dtype_code(X), X.shape[-1]
@@ -545,6 +549,9 @@ def probsparse_layer_norm_fwd(X, gamma=None, beta=None, eps: float = 1e-5, Y=Non
 
 def probsparse_layer_norm_bwd(dY, X, gamma, mean, rstd, workspace=None):
     """Gradients (dX, dgamma, dbeta) of probsparse_layer_norm_fwd; dgamma and dbeta are float32."""
+    done = (_native or _fast()).layer_norm_bwd(dY, X, gamma, mean, rstd, workspace)
+    if done is not None:
+        return done
     device = _device_of(X, dY, gamma, mean, rstd, workspace)
     _require(X.dim() >= 1 and X.numel() > 0 and X.is_contiguous(), "X must be contiguous and not empty")
     dtype, cols = _dtype_code(X), X.shape[-1]
@@ -577,7 +584,12 @@ def rotary_frequencies(rotary: PsaRotary) -> list:
     return list(freq)[:rotary.dim // 2]
 
 
-def _rotary(function, Q, K, rotary, positions, first, Q_out, K_out):
+def _rotary(back, Q, K, rotary, positions, first, Q_out, K_out):
+    done = (_native or _fast()).rotary(back, Q, K, rotary, positions, first, Q_out, K_out)
+    if done is not None:
+        return done
+    lib = load()
+    function = lib.probsparse_rotary_bwd if back else lib.probsparse_rotary_fwd
     device = _device_of(Q, K, positions, Q_out, K_out)
     _require(Q.dim() in (3, 4) and Q.shape[-1] == 64, "Q must be [B, H, L, 64] or [H, T, 64]")
     dtype = _dtype_code(Q)
@@ -588,6 +600,7 @@ def _rotary(function, Q, K, rotary, positions, first, Q_out, K_out):
         _require(positions.shape in ((L,), (B, L)), f"positions must be [{L}] or [{B}, {L}]")
         _require_like(positions, positions.shape, torch.int32, "positions")
         stride = L if positions.dim() == 2 else 0
+    _require(K is not None or K_out is None, "K_out needs K")
     if K is not None:
         _require(K.dim() == Q.dim() and K.shape[:-3] == Q.shape[:-3] and K.shape[-2:] == Q.shape[-2:], "K must be Q but for its number of heads")
         _require_like(K, K.shape, Q.dtype, "K", contiguous=False)
@@ -608,12 +621,12 @@ def _rotary(function, Q, K, rotary, positions, first, Q_out, K_out):
 def probsparse_rotary_fwd(Q, K, rotary: PsaRotary, positions=None, first: int = 0, Q_out=None, K_out=None):
     """Q [B, H, L, 64] and K [B, H_kv, L, 64] (or [H, T, 64] and [H_kv, T, 64]) turned by their positions: `positions` int32 [L] or
     [B, L], or row l stands at first + l.  K may be None.  Returns (Q_out, K_out), or Q_out alone; an output may be its input."""
-    return _rotary(load().probsparse_rotary_fwd, Q, K, rotary, positions, first, Q_out, K_out)
+    return _rotary(False, Q, K, rotary, positions, first, Q_out, K_out)
 
 
 def probsparse_rotary_bwd(dQ_out, dK_out, rotary: PsaRotary, positions=None, first: int = 0, dQ=None, dK=None):
     """The gradients of probsparse_rotary_fwd's inputs from those of its outputs."""
-    return _rotary(load().probsparse_rotary_bwd, dQ_out, dK_out, rotary, positions, first, dQ, dK)
+    return _rotary(True, dQ_out, dK_out, rotary, positions, first, dQ, dK)
 
 
 def _packed(Q, K, V, q_offsets, k_offsets, causal, scale):
@@ -642,6 +655,9 @@ def dense_attn_packed_fwd(Q, K, V, q_offsets=None, k_offsets=None, causal: bool 
     """Dense attention over packed sequences: Q [H, T_q, 64], K and V [H_kv, T_k, 64]; sequence s has the query rows
     q_offsets[s] .. q_offsets[s + 1] - 1 (int32 [B + 1]; None: one sequence) and the key rows of k_offsets (None: the same).
     `scale` is 1 / 8 unless given.  Returns out, or (out, lse) with lse [H, T_q] float32."""
+    done = (_native or _fast()).packed_fwd(Q, K, V, q_offsets, k_offsets, causal, scale, out, lse, workspace)
+    if done is not None:
+        return done
     device = _device_of(Q, K, V, q_offsets, k_offsets, out, workspace)
     k_offsets, shape = _packed(Q, K, V, q_offsets, k_offsets, causal, scale)
     _require_like(out, Q.shape, Q.dtype, "out", contiguous=False)
@@ -659,6 +675,9 @@ def dense_attn_packed_fwd(Q, K, V, q_offsets=None, k_offsets=None, causal: bool 
 def dense_attn_packed_bwd(Q, K, V, out, lse, dOut, q_offsets=None, k_offsets=None, causal: bool = False,
                           scale: Optional[float] = None, dQ=None, dK=None, dV=None, workspace=None):
     """Gradients (dQ, dK, dV) of dense_attn_packed_fwd, from its out and lse."""
+    done = (_native or _fast()).packed_bwd(Q, K, V, out, lse, dOut, q_offsets, k_offsets, causal, scale, dQ, dK, dV, workspace)
+    if done is not None:
+        return done
     device = _device_of(Q, K, V, out, lse, dOut, q_offsets, k_offsets, dQ, dK, dV, workspace)
     k_offsets, shape = _packed(Q, K, V, q_offsets, k_offsets, causal, scale)
     for t, like, what in ((out, Q, "out"), (dOut, Q, "dOut"), (dQ, Q, "dQ"), (dK, K, "dK"), (dV, V, "dV")):

@@ -193,6 +193,17 @@ __device__ __forceinline__ void lds_rows(RowOperand<float>& a, const unsigned ch
 #pragma unroll
     for (int k = 0; k < 8; ++k) a.v[k] = *reinterpret_cast<const float4*>(s + LdsTile<float>::chunk_at(row0 + c, 2 * k + h));
 }
+// Row c of a tile in memory as A operand; `ofs` is the row's offset in the buffer.
+__device__ __forceinline__ void buffer_rows(RowOperand<bf16_t>& a, __amdgpu_buffer_rsrc_t b, int ofs, int h)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) a.v[k] = buffer_load16<uint4>(b, ofs + 64 * h + 16 * k);
+}
+__device__ __forceinline__ void buffer_rows(RowOperand<float>& a, __amdgpu_buffer_rsrc_t b, int ofs, int h)
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k) a.v[k] = buffer_load16<float4>(b, ofs + 16 * h + 32 * k);
+}
 // D[row][col] += sum over the head's 64 elements
 __device__ __forceinline__ floatx16 product(const RowOperand<bf16_t>& a, const ColOperand<bf16_t>& b, floatx16 d)
 {
@@ -270,6 +281,25 @@ __device__ __forceinline__ void store_row(float* row, const floatx16 (&d)[2], fl
         for (int k = 0; k < 4; ++k)
             *reinterpret_cast<float4*>(row + 32 * dt + 8 * k + 4 * h) =
                 make_float4(d[dt][4 * k] * f, d[dt][4 * k + 1] * f, d[dt][4 * k + 2] * f, d[dt][4 * k + 3] * f);
+}
+
+__device__ __forceinline__ void store4(float* dst, float4 v) { *reinterpret_cast<float4*>(dst) = v; }
+__device__ __forceinline__ void store4(bf16_t* dst, float4 v) { *reinterpret_cast<uint2*>(dst) = make_uint2(cvt_pk_bf16(v.x, v.y), cvt_pk_bf16(v.z, v.w)); }
+// 8 elements of a row's sums over its weights' sum, 0 where that is 0 (no key)
+template <typename T>
+__device__ __forceinline__ void store_joined(T* dst, const float (&o)[8], float sum)
+{
+    const float f = sum != 0.f ? 1.f / sum : 0.f;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = sum != 0.f ? o[i] * f : 0.f;
+#pragma unroll
+    for (int k = 0; k < 8 / kVec<T>; ++k) {
+        float part[kVec<T>];
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) part[i] = v[k * kVec<T> + i];
+        store_vec(dst + k * kVec<T>, part, kVec<T>);
+    }
 }
 
 }  // namespace psa

@@ -155,32 +155,240 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
     if (lse && h == 0) lse[(int64_t)head * p.Tq + f.q0 + t] = n_vis > 0 ? acc.m * kLn2 + logf(l) : -INFINITY;
 }
 
+// ---- few rows: 32 to a work-group, whose 4 waves divide the keys (of its split) among themselves, 32 at a time, and join their
+// sums at the end.  Keys come straight from memory as the first product's operand, values through LDS of the wave's own;
+// there is no barrier before the join.
+template <typename T>
+__global__ __launch_bounds__(256)
+void packed_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Packing p, Heads<T> out, float* __restrict__ lse,
+                       int H_kv, int causal, float scale, int n_tile, int n_split, float* __restrict__ part_o, float2* __restrict__ part_ml)
+{
+    constexpr int CH = 64 * sizeof(T) / 16;
+    constexpr int NL = 32 * CH / 64;                   // chunks of a tile of 32 rows, to a lane
+    constexpr int kTileBytes = 32 * LdsTile<T>::kRowBytes;
+    constexpr int kRow = 68;                           // floats of a row of the join: 64, and 16 bytes against bank conflicts
+    constexpr int kJoinBytes = 4 * 32 * kRow * 4;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kTileBytes > kJoinBytes ? 4 * kTileBytes : kJoinBytes];
+    __shared__ float s_m[4][32], s_l[4][32];
+    const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv, split = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
+    if (split == 0)
+        zero_outside(out, p.qo, p.B, p.Tq, hk * p.G, p.G, x, n_tile, [&](int head, int row) { if (lse) lse[(int64_t)head * p.Tq + row] = -INFINITY; });
+    const SeqTile f = find_tile<32, false>(p, x);
+    if (f.tile < 0) return;
+    const int n_rows = f.nq * p.G;
+    const int shift = f.nk - f.nq + 1;
+    auto visible = [&](int r) { const int t = r / p.G; return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
+    const int row0 = f.tile * 32, row = row0 + c, rc = min(row, n_rows - 1);
+    const int t = rc / p.G, head = hk * p.G + (rc - t * p.G);
+    const int n_vis = visible(rc);
+    const int n_all = __builtin_amdgcn_readfirstlane(visible(min(row0 + 31, n_rows - 1)));
+    const int n_every = __builtin_amdgcn_readfirstlane(visible(row0));
+    // this split's tiles of 32 keys, every fourth of them this wave's
+    const int tiles = (n_all + 31) / 32, per = (tiles + n_split - 1) / n_split;
+    const int end = min(n_all, (split + 1) * per * 32);
+
+    ColOperand<T> q;
+    q.load(Q.at(head, f.q0 + t), h);
+    const T* Kh = K.at(hk, f.k0);
+    const T* Vh = V.at(hk, f.k0);
+    unsigned char* sV = lds + wave * kTileBytes;
+    RowOperand<T> kn;
+    uint4 vn[NL];
+    auto fetch = [&](int j0) {
+        const int n = min(32, f.nk - j0);
+        const auto kb = tile_rows(Kh + j0 * K.row, K.row, n), vb = tile_rows(Vh + j0 * V.row, V.row, n);
+        buffer_rows(kn, kb, (int)(c * K.row * (int64_t)sizeof(T)), h);
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int id = i * 64 + lane;
+            vn[i] = buffer_load16<uint4>(vb, (int)((id / CH) * V.row * (int64_t)sizeof(T)) + (id % CH) * 16);
+        }
+    };
+    Rows32 acc;
+    acc.init();
+    int j0 = (split * per + wave) * 32;
+    if (j0 < end) fetch(j0);
+    for (; j0 < end; j0 += 128) {
+        const bool part = j0 + 32 > n_every;
+        bool any = false;
+        if (part) {
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < NL; ++i) bad |= nonfinite(vn[i], T{});
+            any = __builtin_amdgcn_ballot_w64(bad) != 0;
+            if (any)
+#pragma unroll
+                for (int i = 0; i < NL; ++i) vn[i] = finite_only(vn[i], T{});
+        }
+        wave_lds_sync();
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int id = i * 64 + lane;
+            *reinterpret_cast<uint4*>(sV + LdsTile<T>::chunk_at(id / CH, id % CH)) = vn[i];
+        }
+        floatx16 s[1];
+        clear(s[0]);
+        s[0] = product(kn, q, s[0]);
+        wave_lds_sync();
+        if (j0 + 128 < end) fetch(j0 + 128);
+        if (part) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[0][r] = j0 + acc_row(r, h) < n_vis ? s[0][r] : -INFINITY;
+        }
+        acc.weights(s, scale);
+        accumulate(acc.o, sV, 0, s[0], c, h, T{});
+        if (any) acc.add_nonfinite(Vh + j0 * V.row, V.row, min(32, f.nk - j0), n_vis - j0, h);
+    }
+    // join: wave w's sums of row r at join[w][r]; a wave that saw no key has m = kMaxInit and sums of 0
+    __syncthreads();
+    float* join = reinterpret_cast<float*>(lds);
+    const float l = acc.l + swap_half(acc.l);
+    if (h == 0) { s_m[wave][c] = acc.m; s_l[wave][c] = l; }
+    store_row(join + (wave * 32 + c) * kRow, acc.o, 1.f, h);
+    __syncthreads();
+    // 8 threads of 8 elements to a row
+    const int r = tid >> 3, e = (tid & 7) * 8;
+    if (row0 + r >= n_rows) return;
+    float m = s_m[0][r];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) m = fmaxf(m, s_m[w][r]);
+    float sum = 0.f, o[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (s_m[w][r] == kMaxInit && s_l[w][r] == 0.f) continue;       // (saw no key: its accumulators may hold 0 * NaN)
+        const float a = fast_exp2(s_m[w][r] - m);
+        sum = fmaf(s_l[w][r], a, sum);
+        const float* src = join + (w * 32 + r) * kRow + e;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = fmaf(src[i], a, o[i]);
+    }
+    const int rt = (row0 + r) / p.G, rh = hk * p.G + (row0 + r - rt * p.G);
+    if (n_split > 1) {
+        const int64_t rec = ((int64_t)split * H_kv + hk) * p.Tq * p.G + (int64_t)f.q0 * p.G + row0 + r;
+        float4* dst = reinterpret_cast<float4*>(part_o + rec * 64 + e);
+        dst[0] = make_float4(o[0], o[1], o[2], o[3]);
+        dst[1] = make_float4(o[4], o[5], o[6], o[7]);
+        if (e == 0) part_ml[rec] = make_float2(m, sum);
+    } else {
+        store_joined(out.at(rh, f.q0 + rt) + e, o, sum);
+        if (lse && e == 0) lse[(int64_t)rh * p.Tq + f.q0 + rt] = sum == 0.f ? -INFINITY : m * kLn2 + logf(sum);
+    }
+}
+
+// Joins the splits of each row that is in a sequence: a wave to a row, 16 lanes of 4 elements for every fourth split.  The loads of
+// several splits are in flight at once (8 threads to a row and one split after the other: 10.2 us for 15 splits of 256 rows).
+template <typename T>
+__global__ __launch_bounds__(256)
+void packed_merge_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, int n_split, Packing p, int H_kv, Heads<T> out,
+                         float* __restrict__ lse)
+{
+    const int64_t rows = (int64_t)p.Tq * p.G;
+    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (id >= rows * H_kv) return;
+    const int lane = threadIdx.x & 63, e = (lane & 15) * 4, s0 = lane >> 4;
+    const int hk = (int)(id / rows);
+    const int r = (int)(id - hk * rows), t = r / p.G, head = hk * p.G + (r - t * p.G);
+    if (p.qo && (t < p.qo[0] || t >= p.qo[p.B])) return;
+    float m = kMaxInit, sum = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int base = s0; base < n_split; base += 16) {
+        float2 ml[4];
+        float4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t rec = (int64_t)min(base + 4 * k, n_split - 1) * rows * H_kv + id;
+            ml[k] = part_ml[rec];
+            v[k] = *reinterpret_cast<const float4*>(part_o + rec * 64 + e);
+            if (base + 4 * k >= n_split) { ml[k] = make_float2(kMaxInit, 0.f); v[k] = make_float4(0.f, 0.f, 0.f, 0.f); }
+        }
+        const float top = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m);
+        const float a0 = fast_exp2(m - top);
+        sum *= a0; o.x *= a0; o.y *= a0; o.z *= a0; o.w *= a0;
+        m = top;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float a = fast_exp2(ml[k].x - m);
+            sum = fmaf(ml[k].y, a, sum);
+            o.x = fmaf(v[k].x, a, o.x); o.y = fmaf(v[k].y, a, o.y); o.z = fmaf(v[k].z, a, o.z); o.w = fmaf(v[k].w, a, o.w);
+        }
+    }
+#pragma unroll
+    for (int k = 16; k < 64; k *= 2) {
+        const float m2 = __shfl_xor(m, k, 64), top = fmaxf(m, m2);
+        const float a = fast_exp2(m - top), b = fast_exp2(m2 - top);
+        sum = sum * a + __shfl_xor(sum, k, 64) * b;
+        o.x = o.x * a + __shfl_xor(o.x, k, 64) * b;
+        o.y = o.y * a + __shfl_xor(o.y, k, 64) * b;
+        o.z = o.z * a + __shfl_xor(o.z, k, 64) * b;
+        o.w = o.w * a + __shfl_xor(o.w, k, 64) * b;
+        m = top;
+    }
+    if (s0 != 0) return;
+    const float f = sum != 0.f ? 1.f / sum : 0.f;
+    store4(out.at(head, t) + e, sum != 0.f ? make_float4(o.x * f, o.y * f, o.z * f, o.w * f) : make_float4(0.f, 0.f, 0.f, 0.f));
+    if (lse && e == 0) lse[(int64_t)head * p.Tq + t] = sum == 0.f ? -INFINITY : m * kLn2 + logf(sum);
+}
+
+// Few rows or many?  A wave owns 32 rows either way.  Work-groups of 128 rows read K and V a quarter as often but leave waves idle
+// in sequences of fewer rows, and there must be enough of them.
 PackedPlan make_packed_plan(const psa_packed_shape_t& s)
 {
     PackedPlan p{};
     const int64_t rows = (int64_t)s.T_q * (s.H / s.H_kv);
-    p.rows = 128;
+    const int64_t wide = (rows / 128 + s.B) * s.H_kv;
+    p.few = rows / s.B <= 64 || wide < 256;
+    p.rows = p.few ? 32 : 128;
     p.n_tile = (int)(rows / p.rows) + s.B;
     p.n_split = 1;
-    p.total = 256;
+    if (p.few) {
+        // splits: until there are 4 work-groups to a compute unit, each with a round of its 4 waves at the least (by the mean length)
+        const int64_t wgs = (int64_t)p.n_tile * s.H_kv;
+        int64_t split = (1024 + wgs - 1) / wgs;
+        const int64_t most = ((int64_t)s.T_k / s.B + 127) / 128;
+        if (split > most) split = most;
+        if (split > 64) split = 64;
+        p.n_split = (int)(split < 1 ? 1 : split);
+    }
+    p.off_part = 0;
+    if (p.n_split > 1) {
+        p.off_part = ((size_t)p.n_split * (size_t)rows * s.H_kv * sizeof(float2) + 255) & ~(size_t)255;
+        p.total = p.off_part + (size_t)p.n_split * (size_t)rows * s.H_kv * 64 * sizeof(float);
+    } else {
+        p.total = 256;
+    }
     return p;
 }
 
 template <typename T, int KT>
 static void packed_go(const PackedPlan& p, const psa_packed_shape_t& s, const psa_heads_t& Q, const psa_heads_t& K, const psa_heads_t& V,
-                      const Packing& pk, const psa_heads_t& out, float* lse, hipStream_t stream)
+                      const Packing& pk, const psa_heads_t& out, float* lse, void* workspace, hipStream_t stream)
 {
-    packed_rows_kernel<T, KT><<<(unsigned)(p.n_tile * s.H_kv), 256, 0, stream>>>(
-        heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), pk, heads_of<T>(out), lse, s.H_kv, s.causal,
-        (float)(s.scale * 1.4426950408889634), p.n_tile);
+    const float scale = (float)(s.scale * 1.4426950408889634);
+    const dim3 grid((unsigned)(p.n_tile * s.H_kv), (unsigned)p.n_split);
+    if (!p.few) {
+        packed_rows_kernel<T, KT><<<grid, 256, 0, stream>>>(heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), pk, heads_of<T>(out),
+                                                            lse, s.H_kv, s.causal, scale, p.n_tile);
+        return;
+    }
+    float2* part_ml = static_cast<float2*>(workspace);
+    float* part_o = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.off_part);
+    packed_few_kernel<T><<<grid, 256, 0, stream>>>(heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), pk, heads_of<T>(out), lse,
+                                                   s.H_kv, s.causal, scale, p.n_tile, p.n_split, part_o, part_ml);
+    if (p.n_split > 1) {
+        const int64_t rows = (int64_t)s.T_q * s.H;
+        packed_merge_kernel<T><<<(unsigned)((rows + 3) / 4), 256, 0, stream>>>(part_o, part_ml, p.n_split, pk, s.H_kv, heads_of<T>(out), lse);
+    }
 }
 hipError_t launch_packed(const PackedPlan& p, const psa_packed_shape_t& s, const psa_heads_t& Q, const psa_heads_t& K, const psa_heads_t& V,
                          const int* q_offsets, const int* k_offsets, const psa_heads_t& out, float* lse, void* workspace, hipStream_t stream)
 {
     (void)hipGetLastError();
     const Packing pk{q_offsets, k_offsets, s.B, s.T_q, s.T_k, s.H / s.H_kv};
-    if (s.dtype == PSA_F32) packed_go<float, 32>(p, s, Q, K, V, pk, out, lse, stream);
-    else packed_go<bf16_t, 64>(p, s, Q, K, V, pk, out, lse, stream);
+    if (s.dtype == PSA_F32) packed_go<float, 32>(p, s, Q, K, V, pk, out, lse, workspace, stream);
+    else packed_go<bf16_t, 64>(p, s, Q, K, V, pk, out, lse, workspace, stream);
     return hipGetLastError();
 }
 

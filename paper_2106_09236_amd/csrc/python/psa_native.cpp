@@ -13,6 +13,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -227,6 +228,245 @@ PyObject* mhsa_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
     return rc == PSA_OK ? result(a[7], std::move(made)) : failed(rc);
 }
 
+// ---- layer norm, rotary positions, dense attention over packed sequences.  Everything has to be on the current device here; the
+// caller's path switches to the tensors' own.
+bool here(const at::Tensor& t) { return t.is_cuda() && t.device().index() == c10::hip::current_device(); }
+
+bool take_like(PyObject* o, Arg& a, at::IntArrayRef sizes, at::ScalarType type, bool optional)
+{
+    if (!take(o, a, optional)) return false;
+    return !a.t || (here(*a.t) && a.t->scalar_type() == type && a.t->sizes() == sizes);
+}
+// A tensor of heads [B, H, L, 64] or [H, T, 64] with any strides
+struct HeadsArg {
+    const at::Tensor* t = nullptr;
+    psa_heads_t h{};
+    const psa_heads_t* ptr() const { return t ? &h : nullptr; }
+    void set(const at::Tensor& x) {
+        const int64_t n = x.dim();
+        h = psa_heads_t{x.data_ptr(), n == 4 ? x.stride(0) : 0, x.stride(n - 3), x.stride(n - 2)};
+    }
+};
+bool take_heads(PyObject* o, HeadsArg& a, bool optional)
+{
+    if (o == Py_None) return optional;
+    if (!THPVariable_Check(o)) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if ((t.dim() != 3 && t.dim() != 4) || t.size(-1) != 64 || t.stride(-1) != 1 || t.numel() == 0 || !here(t)) return false;
+    a.t = &t;
+    a.set(t);
+    return true;
+}
+bool take_heads_like(PyObject* o, HeadsArg& a, const at::Tensor& like, bool optional)
+{
+    return take_heads(o, a, optional) && (!a.t || (a.t->sizes() == like.sizes() && a.t->scalar_type() == like.scalar_type()));
+}
+void make_heads(HeadsArg& a, at::Tensor& made, const at::Tensor& like)
+{
+    if (a.t) return;
+    made = at::empty_like(like);
+    a.set(made);
+}
+PyObject* tuple(PyObject* const* objects, int n)
+{
+    PyObject* t = PyTuple_New(n);
+    for (int i = 0; i < n; ++i) {
+        if (t && objects[i]) PyTuple_SET_ITEM(t, i, objects[i]);
+        else Py_XDECREF(objects[i]);
+    }
+    return t;
+}
+
+// layer_norm_fwd(X, gamma, beta, eps, Y, stats) -> Y or (Y, mean, rstd)
+PyObject* layer_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Arg x, g, b, y;
+    if (n != 6 || !take(a[0], x, false) || !here(*x.t) || x.t->dim() < 1 || x.t->numel() == 0) return none();
+    const int64_t cols = x.t->size(-1), rows = x.t->numel() / cols;
+    const auto type = x.t->scalar_type();
+    int32_t dtype;
+    const double eps = PyFloat_AsDouble(a[3]);
+    const int stats = PyObject_IsTrue(a[5]);
+    if (PyErr_Occurred()) { PyErr_Clear(); return none(); }
+    if (cols > INT32_MAX || !dtype_of(*x.t, &dtype) || !take_like(a[1], g, {cols}, type, true) || !take_like(a[2], b, {cols}, type, true) ||
+        !take_like(a[4], y, x.t->sizes(), type, true)) return none();
+    at::Tensor made, mean, rstd;
+    int rc;
+    {
+        const Unlocked unlocked;
+        if (!y.t) { made = at::empty_like(*x.t); y.ptr = made.data_ptr(); }
+        if (stats) {
+            const auto lead = x.t->sizes().slice(0, x.t->dim() - 1);
+            mean = at::empty(lead, x.t->options().dtype(at::kFloat));
+            rstd = at::empty(lead, x.t->options().dtype(at::kFloat));
+        }
+        rc = probsparse_layer_norm_fwd(x.ptr, g.ptr, b.ptr, eps, y.ptr, stats ? mean.data_ptr<float>() : nullptr,
+                                       stats ? rstd.data_ptr<float>() : nullptr, rows, (int32_t)cols, dtype, stream());
+    }
+    if (rc != PSA_OK) return failed(rc);
+    PyObject* r = result(a[4], std::move(made));
+    if (!stats) return r;
+    PyObject* const all[] = {r, THPVariable_Wrap(std::move(mean)), THPVariable_Wrap(std::move(rstd))};
+    return tuple(all, 3);
+}
+
+// layer_norm_bwd(dY, X, gamma, mean, rstd, workspace) -> (dX, dgamma, dbeta)
+PyObject* layer_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Arg dy, x, g, m, r, ws;
+    if (n != 6 || !take(a[1], x, false) || !here(*x.t) || x.t->dim() < 1 || x.t->numel() == 0) return none();
+    const int64_t cols = x.t->size(-1), rows = x.t->numel() / cols;
+    const auto type = x.t->scalar_type();
+    const auto lead = x.t->sizes().slice(0, x.t->dim() - 1);
+    int32_t dtype;
+    if (cols > INT32_MAX || !dtype_of(*x.t, &dtype) || !take_like(a[0], dy, x.t->sizes(), type, false) || !take_like(a[2], g, {cols}, type, true) ||
+        !take_like(a[3], m, lead, at::kFloat, false) || !take_like(a[4], r, lead, at::kFloat, false) || !take(a[5], ws, true) ||
+        (ws.t && !here(*ws.t))) return none();
+    const size_t bytes = ws.t ? ws.t->nbytes() : probsparse_layer_norm_bwd_workspace_bytes(rows, (int32_t)cols, dtype);
+    if (bytes == 0) return none();
+    at::Tensor room, dx, dg, db;
+    int rc;
+    {
+        const Unlocked unlocked;
+        if (!ws.t) { room = scratch(*x.t, bytes); ws.ptr = room.data_ptr(); }
+        dx = at::empty_like(*x.t);
+        dg = at::empty({cols}, x.t->options().dtype(at::kFloat));
+        db = at::empty({cols}, x.t->options().dtype(at::kFloat));
+        rc = probsparse_layer_norm_bwd(dy.ptr, x.ptr, g.ptr, static_cast<const float*>(m.ptr), static_cast<const float*>(r.ptr), dx.data_ptr(),
+                                       dg.data_ptr<float>(), db.data_ptr<float>(), rows, (int32_t)cols, dtype, ws.ptr, bytes, stream());
+    }
+    if (rc != PSA_OK) return failed(rc);
+    PyObject* const all[] = {THPVariable_Wrap(std::move(dx)), THPVariable_Wrap(std::move(dg)), THPVariable_Wrap(std::move(db))};
+    return tuple(all, 3);
+}
+
+// rotary(back, Q, K, rotary, positions, first, Q_out, K_out) -> Q_out or (Q_out, K_out)
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HeadsArg q, k, qo, ko;
+    Arg pos;
+    if (n != 8 || !take_heads(a[1], q, false) || !take_heads(a[2], k, true) || !take(a[4], pos, true) || !take_heads_like(a[6], qo, *q.t, true)) return none();
+    const int back = PyObject_IsTrue(a[0]);
+    const long first = PyLong_AsLong(a[5]);
+    if (PyErr_Occurred()) { PyErr_Clear(); return none(); }
+    const int64_t dim = q.t->dim(), B = dim == 4 ? q.t->size(0) : 1, H = q.t->size(dim - 3), L = q.t->size(dim - 2);
+    if (first != (int32_t)first || B > INT32_MAX || H > INT32_MAX || L > INT32_MAX) return none();
+    psa_shape_t s{(int32_t)B, (int32_t)H, (int32_t)L, (int32_t)L, 64, 1, 0};
+    if (!dtype_of(*q.t, &s.dtype)) return none();
+    if (k.t) {
+        if (k.t->dim() != dim || (dim == 4 && k.t->size(0) != B) || k.t->size(dim - 2) != L || k.t->scalar_type() != q.t->scalar_type() ||
+            !take_heads_like(a[7], ko, *k.t, true)) return none();
+    } else if (a[7] != Py_None) {
+        return none();
+    }
+    if (pos.t && (!here(*pos.t) || pos.t->scalar_type() != at::kInt || (pos.t->sizes() != at::IntArrayRef({L}) && pos.t->sizes() != at::IntArrayRef({B, L})))) return none();
+    Py_buffer view;
+    if (PyObject_GetBuffer(a[3], &view, PyBUF_SIMPLE) != 0) { PyErr_Clear(); return none(); }
+    psa_rotary_t o;
+    const bool whole = view.len == (Py_ssize_t)sizeof(o);
+    if (whole) o = *static_cast<const psa_rotary_t*>(view.buf);
+    PyBuffer_Release(&view);
+    if (!whole) return none();
+    at::Tensor q_made, k_made;
+    int rc;
+    {
+        const Unlocked unlocked;
+        make_heads(qo, q_made, *q.t);
+        if (k.t) make_heads(ko, k_made, *k.t);
+        rc = (back ? probsparse_rotary_bwd : probsparse_rotary_fwd)(&q.h, k.ptr(), k.t ? (int32_t)k.t->size(dim - 3) : 0, &o, static_cast<const int32_t*>(pos.ptr),
+                                                                    pos.t && pos.t->dim() == 2 ? L : 0, (int32_t)first, &qo.h, k.t ? &ko.h : nullptr, &s, stream());
+    }
+    if (rc != PSA_OK) return failed(rc);
+    PyObject* r = result(a[6], std::move(q_made));
+    if (!k.t) return r;
+    PyObject* const all[] = {r, result(a[7], std::move(k_made))};
+    return tuple(all, 2);
+}
+
+// Q, K, V, q_offsets, k_offsets, causal, scale
+struct Packed {
+    HeadsArg q, k, v;
+    Arg qo, ko;
+    psa_packed_shape_t s{};
+    bool take_all(PyObject* const* a, PyObject* qo_o, PyObject* ko_o, PyObject* causal, PyObject* scale) {
+        if (!take_heads(a[0], q, false) || !take_heads(a[1], k, false) || q.t->dim() != 3 || k.t->dim() != 3 || !take_heads_like(a[2], v, *k.t, false) ||
+            q.t->scalar_type() != k.t->scalar_type()) return false;
+        int64_t B = 1;
+        if (qo_o != Py_None) {
+            if (ko_o == Py_None && q.t->size(1) != k.t->size(1)) return false;
+            if (!take(qo_o, qo, false) || qo.t->dim() != 1 || qo.t->numel() < 2 || qo.t->scalar_type() != at::kInt || !here(*qo.t) ||
+                !take_like(ko_o == Py_None ? qo_o : ko_o, ko, qo.t->sizes(), at::kInt, false)) return false;
+            B = qo.t->numel() - 1;
+        } else if (ko_o != Py_None) {
+            return false;
+        }
+        const int c = PyObject_IsTrue(causal);
+        const double f = scale == Py_None ? 0.125 : PyFloat_AsDouble(scale);
+        if (PyErr_Occurred()) { PyErr_Clear(); return false; }
+        if (B > INT32_MAX || q.t->size(0) % k.t->size(0) != 0 || q.t->size(0) > INT32_MAX || q.t->size(1) > INT32_MAX || k.t->size(1) > INT32_MAX) return false;
+        s = psa_packed_shape_t{(int32_t)B, (int32_t)q.t->size(0), (int32_t)k.t->size(0), (int32_t)q.t->size(1), (int32_t)k.t->size(1), 64, 0, c, f};
+        return dtype_of(*q.t, &s.dtype);
+    }
+    const int32_t* q_offsets() const { return static_cast<const int32_t*>(qo.ptr); }
+    const int32_t* k_offsets() const { return static_cast<const int32_t*>(ko.ptr); }
+};
+
+// packed_fwd(Q, K, V, q_offsets, k_offsets, causal, scale, out, lse, workspace) -> out or (out, lse)
+PyObject* packed_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Packed p;
+    HeadsArg out;
+    Arg ws;
+    if (n != 10 || !p.take_all(a, a[3], a[4], a[5], a[6]) || !take_heads_like(a[7], out, *p.q.t, true) || !take(a[9], ws, true) || (ws.t && !here(*ws.t))) return none();
+    const int want_lse = PyObject_IsTrue(a[8]);
+    if (PyErr_Occurred()) { PyErr_Clear(); return none(); }
+    const size_t bytes = ws.t ? ws.t->nbytes() : dense_attn_packed_workspace_bytes(&p.s);
+    if (bytes == 0) return none();
+    at::Tensor made, lse, room;
+    int rc;
+    {
+        const Unlocked unlocked;
+        if (!ws.t) { room = scratch(*p.q.t, bytes); ws.ptr = room.data_ptr(); }
+        make_heads(out, made, *p.q.t);
+        if (want_lse) lse = at::empty({p.q.t->size(0), p.q.t->size(1)}, p.q.t->options().dtype(at::kFloat));
+        rc = dense_attn_packed_fwd(&p.q.h, &p.k.h, &p.v.h, p.q_offsets(), p.k_offsets(), &out.h, want_lse ? lse.data_ptr<float>() : nullptr, &p.s,
+                                   ws.ptr, bytes, stream());
+    }
+    if (rc != PSA_OK) return failed(rc);
+    PyObject* r = result(a[7], std::move(made));
+    if (!want_lse) return r;
+    PyObject* const all[] = {r, THPVariable_Wrap(std::move(lse))};
+    return tuple(all, 2);
+}
+
+// packed_bwd(Q, K, V, out, lse, dOut, q_offsets, k_offsets, causal, scale, dQ, dK, dV, workspace) -> (dQ, dK, dV)
+PyObject* packed_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Packed p;
+    HeadsArg out, g, dq, dk, dv;
+    Arg lse, ws;
+    if (n != 14 || !p.take_all(a, a[6], a[7], a[8], a[9]) || !take_heads_like(a[3], out, *p.q.t, false) ||
+        !take_like(a[4], lse, {p.q.t->size(0), p.q.t->size(1)}, at::kFloat, false) || !take_heads_like(a[5], g, *p.q.t, false) ||
+        !take_heads_like(a[10], dq, *p.q.t, true) || !take_heads_like(a[11], dk, *p.k.t, true) || !take_heads_like(a[12], dv, *p.k.t, true) ||
+        !take(a[13], ws, true) || (ws.t && !here(*ws.t))) return none();
+    const size_t bytes = ws.t ? ws.t->nbytes() : dense_attn_packed_bwd_workspace_bytes(&p.s);
+    if (bytes == 0) return none();
+    at::Tensor room, made[3];
+    int rc;
+    {
+        const Unlocked unlocked;
+        if (!ws.t) { room = scratch(*p.q.t, bytes); ws.ptr = room.data_ptr(); }
+        make_heads(dq, made[0], *p.q.t);
+        make_heads(dk, made[1], *p.k.t);
+        make_heads(dv, made[2], *p.v.t);
+        rc = dense_attn_packed_bwd(&p.q.h, &p.k.h, &p.v.h, p.q_offsets(), p.k_offsets(), &out.h, static_cast<const float*>(lse.ptr), &g.h, &dq.h, &dk.h,
+                                   &dv.h, &p.s, ws.ptr, bytes, stream());
+    }
+    if (rc != PSA_OK) return failed(rc);
+    PyObject* const all[] = {result(a[10], std::move(made[0])), result(a[11], std::move(made[1])), result(a[12], std::move(made[2]))};
+    return tuple(all, 3);
+}
+
 // exceptions of the tensor library (no memory, say) must not cross into the interpreter: the caller's path meets them
 // again and reports them
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
@@ -247,6 +487,11 @@ PyMethodDef methods[] = {
     {"attn_fwd_with_indices", entry<attn_fwd_with_indices>(), METH_FASTCALL, nullptr},
     {"attn_bwd", entry<attn_bwd>(), METH_FASTCALL, nullptr},
     {"mhsa_fwd", entry<mhsa_fwd>(), METH_FASTCALL, nullptr},
+    {"layer_norm_fwd", entry<layer_norm_fwd>(), METH_FASTCALL, nullptr},
+    {"layer_norm_bwd", entry<layer_norm_bwd>(), METH_FASTCALL, nullptr},
+    {"rotary", entry<rotary>(), METH_FASTCALL, nullptr},
+    {"packed_fwd", entry<packed_fwd>(), METH_FASTCALL, nullptr},
+    {"packed_bwd", entry<packed_bwd>(), METH_FASTCALL, nullptr},
     {"on_status", on_status, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -176,3 +176,25 @@ def test_binding_refuses_wrong_tensors():
             psa.probsparse_rotary_fwd(*args, **kw)
     with pytest.raises(TypeError):
         psa.probsparse_rotary_fwd(q, None, spec, positions=z(10, dtype=torch.int64))
+
+
+@pytest.mark.gpu
+def test_ctypes_path_gives_the_same(monkeypatch):
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16)
+    q, k, v, d, x, w = rand(4, 50, 64), rand(2, 50, 64), rand(2, 50, 64), rand(4, 50, 64), rand(9, 5, 96), rand(96)
+    off = torch.tensor([0, 20, 50], dtype=torch.int32, device="cuda")
+    pos = torch.arange(50, dtype=torch.int32, device="cuda")
+    spec = psa.make_rotary(64)
+
+    def calls():
+        y, mean, rstd = psa.probsparse_layer_norm_fwd(x, w, w, 1e-5)
+        out, lse = psa.dense_attn_packed_fwd(q, k, v, off, causal=True, scale=0.2, lse=True)
+        return [y, mean, rstd, psa.probsparse_layer_norm_fwd(x, w, None, stats=False), *psa.probsparse_layer_norm_bwd(x, x, w, mean, rstd),
+                *psa.probsparse_rotary_fwd(q, k, spec, positions=pos), psa.probsparse_rotary_bwd(q, None, spec, first=7), out, lse,
+                psa.dense_attn_packed_fwd(q, k, v), *psa.dense_attn_packed_bwd(q, k, v, out, lse, d, off, causal=True, scale=0.2)]
+    native = calls()
+    assert psa._native is not psa._CtypesOnly
+    monkeypatch.setattr(psa, "_native", psa._CtypesOnly)
+    other = calls()
+    assert all(a.shape == b.shape and a.dtype == b.dtype and torch.equal(a, b) for a, b in zip(native, other))

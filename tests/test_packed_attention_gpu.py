@@ -71,6 +71,16 @@ def test_whole_sequences(H, H_kv, lens, by_frame, causal, dtype):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("H,H_kv,q_lens,k_lens", [
+    (64, 32, [127, 0, 5, 128, 129, 65, 300], [127, 0, 5, 128, 129, 65, 300]), (96, 32, [111, 222, 1, 90], [70, 222, 150, 0]),
+    (64, 64, [260, 255, 256, 1], [257, 300, 256, 33])])
+def test_many_heads(H, H_kv, q_lens, k_lens, causal, dtype):
+    """Enough heads for work-groups of 128 rows (fewer leave the card idle, and rows are taken 32 at a time)."""
+    _check(*_case(H, H_kv, q_lens, k_lens, dtype, by_frame=causal, front=3, behind=200), causal)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("H,H_kv,q_lens,k_lens", [
     (8, 2, [1] * 5, [1, 40, 129, 600, 0]),              # single tokens; one stream without keys
     (4, 4, [1], [5000]), (8, 1, [3, 1], [2047, 2049]),  # long caches
     (4, 2, [20, 5, 64, 7], [10, 5, 300, 0]),            # more queries than keys: the first see none under the mask
@@ -98,10 +108,10 @@ def test_one_sequence_without_offsets(dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("q_lens,k_lens", [([200, 90], [200, 90]), ([4, 2], [300, 90])])
-def test_what_is_not_seen_has_no_part(q_lens, k_lens, dtype):
+@pytest.mark.parametrize("H,H_kv,q_lens,k_lens", [(4, 2, [200, 90], [200, 90]), (4, 2, [4, 2], [300, 90]), (64, 32, [200, 290], [200, 290])])
+def test_what_is_not_seen_has_no_part(H, H_kv, q_lens, k_lens, dtype):
     """Infinities and NaN in later keys and values, in other sequences and between them leave a row's output as it is."""
-    host, dev, q_off, k_off = _case(4, 2, q_lens, k_lens, dtype, front=20, behind=30)
+    host, dev, q_off, k_off = _case(H, H_kv, q_lens, k_lens, dtype, front=20, behind=30)
     Qd, Kd, Vd, _ = dev
     qo, ko = (torch.tensor(o, dtype=torch.int32, device="cuda") for o in (q_off, k_off))
     clean, clean_lse = psa.dense_attn_packed_fwd(Qd, Kd, Vd, qo, ko, causal=True, lse=True)
@@ -155,7 +165,7 @@ def test_offsets_out_of_range_are_clamped():
     a = psa.dense_attn_packed_fwd(Qd, Kd, Vd, bad, causal=True, lse=True)
     b = psa.dense_attn_packed_fwd(Qd, Kd, Vd, good, causal=True, lse=True)
     assert all(torch.equal(x, y) for x, y in zip(a, b))
-    # a sequence that would end before it begins is empty
+    # decreasing offsets: the first sequence's rows that no other claims
     back = torch.tensor([0, 30, 20, 64], dtype=torch.int32, device="cuda")
     out = psa.dense_attn_packed_fwd(Qd, Kd, Vd, back, causal=True)
     assert torch.equal(out[:, :20], b[0][:, :20])
