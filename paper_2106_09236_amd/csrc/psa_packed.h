@@ -36,9 +36,21 @@ struct Packing { const int* qo; const int* ko; int B, Tq, Tk, G; };
 // The tile a work-group takes: rows (or keys) tile * PER .. of the sequence; tile < 0: there is none.
 struct SeqTile { int q0, nq, k0, nk, tile; };
 
-// Tile x of the call, counted from the last tile of the last sequence (with a causal mask the last tiles of a sequence have
-// the most keys, and the longest work should start first).  64 sequences at a time: a prefix sum over the lanes of how many
-// tiles each has.  Every wave finds it for itself.
+// Sum over the lanes of a wave, in scalar registers
+__device__ __forceinline__ int wave_sum(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xF, 0xF, false);       // lanes 1, 2, 4 (mirrored), 8 apart
+    x += __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x141, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x140, 0xF, 0xF, false);
+    return __builtin_amdgcn_readlane(x, 0) + __builtin_amdgcn_readlane(x, 16) + __builtin_amdgcn_readlane(x, 32) + __builtin_amdgcn_readlane(x, 48);
+}
+
+// Tile x of the call.  Sequences are taken in groups of 16, last group first, and of a group's tiles those with the highest index in
+// their sequence come first (of tiles of keys the lowest: the index counts from the end): under a causal mask they have the most
+// work, and what starts last should be short.  Groups, not all
+// sequences, so that work-groups that run at one time share their keys in L2.  Every wave finds its tile for itself: 64 sequences
+// at a time, a prefix sum over the lanes for the group and a search for the index.
 template <int PER, bool KEYS>
 __device__ __forceinline__ SeqTile find_tile(const Packing& p, int x)
 {
@@ -46,7 +58,7 @@ __device__ __forceinline__ SeqTile find_tile(const Packing& p, int x)
     if (!p.qo) {
         f.nq = p.Tq; f.nk = p.Tk;
         const int n = ((KEYS ? p.Tk : p.Tq * p.G) + PER - 1) / PER;
-        f.tile = n - 1 - x;
+        f.tile = x >= n ? -1 : KEYS ? x : n - 1 - x;
         return f;
     }
     const int lane = threadIdx.x & 63;
@@ -57,22 +69,39 @@ __device__ __forceinline__ SeqTile find_tile(const Packing& p, int x)
             q0 = min(max(p.qo[s], 0), p.Tq); q1 = min(max(p.qo[s + 1], q0), p.Tq);
             k0 = min(max(p.ko[s], 0), p.Tk); k1 = min(max(p.ko[s + 1], k0), p.Tk);
         }
-        const int n = ((KEYS ? k1 - k0 : (q1 - q0) * p.G) + PER - 1) / PER;
-        int sum = n;
+        int n = ((KEYS ? k1 - k0 : (q1 - q0) * p.G) + PER - 1) / PER;
+        int sum = n;                                   // of this lane's group of 16, up to this lane
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int y = __shfl_up(sum, d, 64);
-            if (lane >= d) sum += y;
+        for (int d = 1; d < 16; d *= 2) {
+            const int y = __shfl_up(sum, d, 16);
+            if ((lane & 15) >= d) sum += y;
         }
-        const uint64_t hit = __builtin_amdgcn_ballot_w64(sum > x);
-        if (hit) {
-            const int l = __builtin_ctzll(hit);
-            f.q0 = __builtin_amdgcn_readlane(q0, l); f.nq = __builtin_amdgcn_readlane(q1, l) - f.q0;
-            f.k0 = __builtin_amdgcn_readlane(k0, l); f.nk = __builtin_amdgcn_readlane(k1, l) - f.k0;
-            f.tile = __builtin_amdgcn_readlane(sum, l) - 1 - x;
-            return f;
+        int group = -1;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int all = __builtin_amdgcn_readlane(sum, 16 * g + 15);
+            if (group < 0) {
+                if (x < all) group = g;
+                else x -= all;
+            }
         }
-        x -= __builtin_amdgcn_readlane(sum, 63);
+        if (group < 0) continue;
+        if ((lane >> 4) != group) n = 0;
+        // tiles of index >= t: sum of max(n - t, 0).  The t with more than x of them, of t + 1 at most x
+        int lo = 0, hi = 1;
+        while (wave_sum(max(n - hi, 0)) > x) { lo = hi; hi *= 2; }
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (wave_sum(max(n - mid, 0)) > x) lo = mid; else hi = mid;
+        }
+        const int k = x - wave_sum(max(n - hi, 0));    // of the sequences with more than lo tiles, which
+        const uint64_t with = __builtin_amdgcn_ballot_w64(n > lo);
+        const int rank = __builtin_popcountll(with & (((uint64_t)1 << lane) - 1));
+        const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(n > lo && rank == k));
+        f.q0 = __builtin_amdgcn_readlane(q0, l); f.nq = __builtin_amdgcn_readlane(q1, l) - f.q0;
+        f.k0 = __builtin_amdgcn_readlane(k0, l); f.nk = __builtin_amdgcn_readlane(k1, l) - f.k0;
+        f.tile = KEYS ? __builtin_amdgcn_readlane(n, l) - 1 - lo : lo;
+        return f;
     }
     return f;
 }
@@ -97,6 +126,17 @@ __device__ __forceinline__ void zero_outside(const Heads<T>& t, const int* offse
         if (k % CH == 0) each(h, row);
     }
 }
+
+// Row r = t G + g of a key head, moved on without divisions.
+struct RowAt {
+    int t, g;
+    __device__ __forceinline__ RowAt(int r, int G) : t(r / G), g(r - (r / G) * G) {}
+    // by n rows, given as n / G and n % G
+    __device__ __forceinline__ void add(int dt, int dg, int G) {
+        t += dt; g += dg;
+        if (g >= G) { g -= G; ++t; }
+    }
+};
 
 // Rows base .. base + n - 1 (n may be <= 0) of a head as a buffer: reads of rows behind them give zeros.  The base moves with the tile, so
 // that offsets into a long tensor stay small.
@@ -283,6 +323,26 @@ __device__ __forceinline__ void store_row(float* row, const floatx16 (&d)[2], fl
                 make_float4(d[dt][4 * k] * f, d[dt][4 * k + 1] * f, d[dt][4 * k + 2] * f, d[dt][4 * k + 3] * f);
 }
 
+// The sums of a work-group's 4 waves over D^T (32 columns of 64 elements each), 8 threads of 8 elements to a column: column tid / 8, elements
+// 8 (tid % 8) .. + 7, in the order of the waves.  `join` holds 4 * 32 * kJoinRow floats; barriers before and after belong to the caller.
+constexpr int kJoinRow = 68;               // floats of a column in the join: 64, and 16 bytes against bank conflicts
+__device__ __forceinline__ void join_columns(float (&v)[8], const float* join, int tid)
+{
+    const float* src = join + (tid >> 3) * kJoinRow + (tid & 7) * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = ((src[i] + src[32 * kJoinRow + i]) + src[2 * 32 * kJoinRow + i]) + src[3 * 32 * kJoinRow + i];
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* dst, const float (&v)[8], float f)
+{
+#pragma unroll
+    for (int k = 0; k < 8 / kVec<T>; ++k) {
+        float part[kVec<T>];
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) part[i] = v[k * kVec<T> + i] * f;
+        store_vec(dst + k * kVec<T>, part, kVec<T>);
+    }
+}
 __device__ __forceinline__ void store4(float* dst, float4 v) { *reinterpret_cast<float4*>(dst) = v; }
 __device__ __forceinline__ void store4(bf16_t* dst, float4 v) { *reinterpret_cast<uint2*>(dst) = make_uint2(cvt_pk_bf16(v.x, v.y), cvt_pk_bf16(v.z, v.w)); }
 // 8 elements of a row's sums over its weights' sum, 0 where that is 0 (no key)

@@ -54,7 +54,7 @@ struct Rows32 {
 
 // 4 waves of 32 rows each; tiles of KT keys and values go through LDS, the next tile's rows are on their way meanwhile.
 template <typename T, int KT>
-__global__ __launch_bounds__(256)
+__global__ __launch_bounds__(256, 2)
 void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Packing p, Heads<T> out, float* __restrict__ lse,
                         int H_kv, int causal, float scale, int n_tile)
 {
@@ -159,7 +159,7 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
 // sums at the end.  Keys come straight from memory as the first product's operand, values through LDS of the wave's own;
 // there is no barrier before the join.
 template <typename T>
-__global__ __launch_bounds__(256)
+__global__ __launch_bounds__(256, 2)
 void packed_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Packing p, Heads<T> out, float* __restrict__ lse,
                        int H_kv, int causal, float scale, int n_tile, int n_split, float* __restrict__ part_o, float2* __restrict__ part_ml)
 {
@@ -281,7 +281,7 @@ void packed_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pac
 // Joins the splits of each row that is in a sequence: a wave to a row, 16 lanes of 4 elements for every fourth split.  The loads of
 // several splits are in flight at once (8 threads to a row and one split after the other: 10.2 us for 15 splits of 256 rows).
 template <typename T>
-__global__ __launch_bounds__(256)
+__global__ __launch_bounds__(256, 2)
 void packed_merge_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, int n_split, Packing p, int H_kv, Heads<T> out,
                          float* __restrict__ lse)
 {
@@ -339,7 +339,7 @@ PackedPlan make_packed_plan(const psa_packed_shape_t& s)
     PackedPlan p{};
     const int64_t rows = (int64_t)s.T_q * (s.H / s.H_kv);
     const int64_t wide = (rows / 128 + s.B) * s.H_kv;
-    p.few = rows / s.B <= 64 || wide < 256;
+    p.few = s.dtype == PSA_F32 || rows / s.B <= 64 || wide < 256;
     p.rows = p.few ? 32 : 128;
     p.n_tile = (int)(rows / p.rows) + s.B;
     p.n_split = 1;

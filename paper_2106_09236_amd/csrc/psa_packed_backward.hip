@@ -10,7 +10,7 @@ namespace psa {
 
 // lse (base 2; +infinity for a row that sees no key, whose weights then are 0) and d of every row, [H_kv][T_q * G] each.
 template <typename T>
-__global__ __launch_bounds__(256)
+__global__ __launch_bounds__(256, 2)
 void packed_stats_kernel(Heads<const T> out, Heads<const T> dOut, const float* __restrict__ lse, Heads<T> dQ, Packing p, int H,
                          float* __restrict__ stat_l, float* __restrict__ stat_d)
 {
@@ -37,7 +37,7 @@ void packed_stats_kernel(Heads<const T> out, Heads<const T> dOut, const float* _
 
 // dK and dV of 128 keys: 4 waves of 32, tiles of 32 rows of Q and dOut through LDS.
 template <typename T>
-__global__ __launch_bounds__(256)
+__global__ __launch_bounds__(256, 2)
 void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, const float* __restrict__ stat_l,
                        const float* __restrict__ stat_d, Packing p, Heads<T> dK, Heads<T> dV, int H_kv, int causal, float scale,
                        float scale_log2, int n_tile)
@@ -135,7 +135,7 @@ void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Hea
 
 // dQ of 128 rows: 4 waves of 32, tiles of 32 keys and values through LDS.
 template <typename T>
-__global__ __launch_bounds__(256)
+__global__ __launch_bounds__(256, 2)
 void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, const float* __restrict__ stat_l,
                       const float* __restrict__ stat_d, Packing p, Heads<T> dQ, int H_kv, int causal, float scale, float scale_log2)
 {
@@ -209,11 +209,204 @@ void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Head
     store_row(dQ.at(head, f.q0 + t), dq, scale, h);
 }
 
+// ---- the same with 32 keys (rows) to a work-group, whose 4 waves divide the rows (keys) among themselves and join their sums in LDS at
+// the end.  Four times as many work-groups, each a quarter as long, no barrier before the join; a tile of rows is read by one wave
+// only, and 4 times as often.
+
+template <typename T>
+__global__ __launch_bounds__(256, 2)
+void packed_dkv_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, const float* __restrict__ stat_l,
+                           const float* __restrict__ stat_d, Packing p, Heads<T> dK, Heads<T> dV, int H_kv, int causal, float scale,
+                           float scale_log2, int n_tile)
+{
+    constexpr int CH = 64 * sizeof(T) / 16, NL = 32 * CH / 64, RL = 64 / CH;       // lanes of a row, chunks of a lane, rows of one load
+    constexpr int kTileBytes = 32 * LdsTile<T>::kRowBytes;
+    constexpr int kJoinBytes = 4 * 32 * kJoinRow * 4;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[8 * kTileBytes > kJoinBytes ? 8 * kTileBytes : kJoinBytes];
+    __shared__ __attribute__((aligned(16))) float sL[4][32], sD[4][32];
+    const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
+    zero_outside(dK, p.ko, p.B, p.Tk, hk, 1, x, n_tile, [](int, int) {});
+    zero_outside(dV, p.ko, p.B, p.Tk, hk, 1, x, n_tile, [](int, int) {});
+    const SeqTile f = find_tile<32, true>(p, x);
+    if (f.tile < 0) return;
+    const int n_rows = f.nq * p.G;
+    const int shift = f.nk - f.nq + 1;
+    auto first_row = [&](int j) { return causal ? max(j - shift + 1, 0) * p.G : 0; };
+    const int key0 = f.tile * 32, kc = min(key0 + c, f.nk - 1);
+    const int first = first_row(kc);
+    const int first_any = __builtin_amdgcn_readfirstlane(first_row(key0));
+    const int first_every = __builtin_amdgcn_readfirstlane(first_row(min(key0 + 31, f.nk - 1)));
+
+    ColOperand<T> k, v;
+    k.load(K.at(hk, f.k0 + kc), h);
+    v.load(V.at(hk, f.k0 + kc), h);
+    floatx16 dk[2], dv[2];
+    clear(dk[0]); clear(dk[1]); clear(dv[0]); clear(dv[1]);
+    unsigned char *sQ = lds + wave * 2 * kTileBytes, *sG = sQ + kTileBytes;
+    const int64_t stat0 = ((int64_t)hk * p.Tq + f.q0) * p.G;
+    const int lr = lane / CH, ch = lane % CH;
+
+    // one set of registers carries a tile of Q, then the tile of dOut, then the next tile of Q
+    uint4 x4[NL];
+    float l_next = INFINITY, d_next = 0.f;
+    auto fetch = [&](const Heads<const T>& t, int r0) {
+        RowAt at(r0 + lr, p.G);
+        const int dt = RL / p.G, dg = RL - dt * p.G;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            x4[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (r0 + lr + i * RL < n_rows) x4[i] = reinterpret_cast<const uint4*>(t.at(hk * p.G + at.g, f.q0 + at.t))[ch];
+            at.add(dt, dg, p.G);
+        }
+    };
+    auto keep = [&](unsigned char* s) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) *reinterpret_cast<uint4*>(s + LdsTile<T>::chunk_at(lr + i * RL, ch)) = x4[i];
+    };
+    auto fetch_stats = [&](int r0) {
+        const bool in = r0 + c < n_rows;
+        l_next = in ? stat_l[stat0 + r0 + c] : INFINITY;
+        d_next = in ? stat_d[stat0 + r0 + c] : 0.f;
+    };
+    int r0 = first_any / 32 * 32 + wave * 32;
+    if (r0 < n_rows) { fetch(Q, r0); fetch_stats(r0); }
+    for (; r0 < n_rows; r0 += 128) {
+        wave_lds_sync();
+        keep(sQ);
+        if (h == 0) { sL[wave][c] = l_next; sD[wave][c] = d_next; }
+        fetch(dOut, r0);
+        wave_lds_sync();
+        RowOperand<T> a;
+        floatx16 s, w;
+        clear(s); clear(w);
+        lds_rows(a, sQ, 0, c, h);
+        s = product(a, k, s);
+        keep(sG);
+        if (r0 + 128 < n_rows) { fetch(Q, r0 + 128); fetch_stats(r0 + 128); }
+        wave_lds_sync();
+        lds_rows(a, sG, 0, c, h);
+        w = product(a, v, w);
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+            const float4 l4 = *reinterpret_cast<const float4*>(&sL[wave][8 * r4 + 4 * h]), d4 = *reinterpret_cast<const float4*>(&sD[wave][8 * r4 + 4 * h]);
+            const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[4 * r4 + e] = fast_exp2(fmaf(s[4 * r4 + e], scale_log2, -l[e]));
+                w[4 * r4 + e] = s[4 * r4 + e] * (w[4 * r4 + e] - d[e]);
+            }
+        }
+        if (r0 < first_every) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (r0 + acc_row(r, h) < first) { s[r] = 0.f; w[r] = 0.f; }
+        }
+        accumulate(dv, sG, 0, s, c, h, T{});
+        accumulate(dk, sQ, 0, w, c, h, T{});
+    }
+    float* join = reinterpret_cast<float*>(lds);
+    const int key = key0 + (tid >> 3), e = (tid & 7) * 8;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        __syncthreads();
+        store_row(join + (wave * 32 + c) * kJoinRow, which ? dv : dk, 1.f, h);
+        __syncthreads();
+        float sum[8];
+        join_columns(sum, join, tid);
+        if (key < f.nk) store8((which ? dV : dK).at(hk, f.k0 + key) + e, sum, which ? 1.f : scale);
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256, 2)
+void packed_dq_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, const float* __restrict__ stat_l,
+                          const float* __restrict__ stat_d, Packing p, Heads<T> dQ, int H_kv, int causal, float scale, float scale_log2)
+{
+    constexpr int CH = 64 * sizeof(T) / 16, NL = 32 * CH / 64;
+    constexpr int kTileBytes = 32 * LdsTile<T>::kRowBytes;
+    constexpr int kJoinBytes = 4 * 32 * kJoinRow * 4;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kTileBytes > kJoinBytes ? 4 * kTileBytes : kJoinBytes];
+    const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
+    const SeqTile f = find_tile<32, false>(p, x);
+    if (f.tile < 0) return;
+    const int n_rows = f.nq * p.G;
+    const int shift = f.nk - f.nq + 1;
+    auto visible = [&](int r) { const int t = r / p.G; return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
+    const int row0 = f.tile * 32, rc = min(row0 + c, n_rows - 1);
+    const int t = rc / p.G, head = hk * p.G + (rc - t * p.G);
+    const int n_vis = visible(rc);
+    const int n_all = __builtin_amdgcn_readfirstlane(visible(min(row0 + 31, n_rows - 1)));
+    const int n_every = __builtin_amdgcn_readfirstlane(visible(row0));
+    ColOperand<T> q, g;
+    q.load(Q.at(head, f.q0 + t), h);
+    g.load(dOut.at(head, f.q0 + t), h);
+    const int64_t so = ((int64_t)hk * p.Tq + f.q0) * p.G + rc;
+    const float l = stat_l[so], d = stat_d[so];
+    floatx16 dq[2];
+    clear(dq[0]); clear(dq[1]);
+    const T* Kh = K.at(hk, f.k0);
+    const T* Vh = V.at(hk, f.k0);
+    unsigned char* sK = lds + wave * kTileBytes;
+    uint4 kn[NL];
+    RowOperand<T> vn;
+    auto fetch = [&](int j0) {
+        const int n = min(32, f.nk - j0);
+        const auto kb = tile_rows(Kh + j0 * K.row, K.row, n), vb = tile_rows(Vh + j0 * V.row, V.row, n);
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int id = i * 64 + lane;
+            kn[i] = buffer_load16<uint4>(kb, (int)((id / CH) * K.row * (int64_t)sizeof(T)) + (id % CH) * 16);
+        }
+        buffer_rows(vn, vb, (int)(c * V.row * (int64_t)sizeof(T)), h);
+    };
+    int j0 = wave * 32;
+    if (j0 < n_all) fetch(j0);
+    for (; j0 < n_all; j0 += 128) {
+        wave_lds_sync();
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int id = i * 64 + lane;
+            *reinterpret_cast<uint4*>(sK + LdsTile<T>::chunk_at(id / CH, id % CH)) = kn[i];
+        }
+        floatx16 s, w;
+        clear(s); clear(w);
+        w = product(vn, g, w);
+        wave_lds_sync();
+        if (j0 + 128 < n_all) fetch(j0 + 128);
+        RowOperand<T> a;
+        lds_rows(a, sK, 0, c, h);
+        s = product(a, q, s);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w[r] = fast_exp2(fmaf(s[r], scale_log2, -l)) * (w[r] - d);
+        if (j0 + 32 > n_every) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (j0 + acc_row(r, h) >= n_vis) w[r] = 0.f;
+        }
+        accumulate(dq, sK, 0, w, c, h, T{});
+    }
+    __syncthreads();
+    float* join = reinterpret_cast<float*>(lds);
+    store_row(join + (wave * 32 + c) * kJoinRow, dq, 1.f, h);
+    __syncthreads();
+    const int row = row0 + (tid >> 3);
+    if (row >= n_rows) return;
+    float sum[8];
+    join_columns(sum, join, tid);
+    const int rt = row / p.G;
+    store8(dQ.at(hk * p.G + (row - rt * p.G), f.q0 + rt) + (tid & 7) * 8, sum, scale);
+}
+
 PackedBwdPlan make_packed_bwd_plan(const psa_packed_shape_t& s)
 {
     PackedBwdPlan p{};
-    p.n_qtile = (int)((int64_t)s.T_q * (s.H / s.H_kv) / 128) + s.B;
-    p.n_ktile = s.T_k / 128 + s.B;
+    const int64_t rows = (int64_t)s.T_q * (s.H / s.H_kv);
+    p.few_q = s.dtype == PSA_F32 || (rows / 128 + s.B) * s.H_kv < 512;
+    p.few_k = s.dtype == PSA_F32 || (int64_t)(s.T_k / 128 + s.B) * s.H_kv < 512;
+    p.n_qtile = (int)(rows / (p.few_q ? 32 : 128)) + s.B;
+    p.n_ktile = s.T_k / (p.few_k ? 32 : 128) + s.B;
     p.total = 2 * (((size_t)s.T_q * s.H * sizeof(float) + 255) & ~(size_t)255);
     return p;
 }
@@ -229,10 +422,10 @@ static void packed_bwd_go(const PackedBwdPlan& p, const psa_packed_shape_t& s, c
     constexpr int rows = 256 / (64 / kVec<T>);
     packed_stats_kernel<T><<<(unsigned)(((int64_t)s.T_q * s.H + rows - 1) / rows), 256, 0, stream>>>(
         heads_of<const T>(out), heads_of<const T>(dOut), lse, heads_of<T>(dQ), pk, s.H, stat_l, stat_d);
-    packed_dkv_kernel<T><<<(unsigned)(p.n_ktile * s.H_kv), 256, 0, stream>>>(
+    (p.few_k ? packed_dkv_few_kernel<T> : packed_dkv_kernel<T>)<<<(unsigned)(p.n_ktile * s.H_kv), 256, 0, stream>>>(
         heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), heads_of<const T>(dOut), stat_l, stat_d, pk,
         heads_of<T>(dK), heads_of<T>(dV), s.H_kv, s.causal, scale, scale_log2, p.n_ktile);
-    packed_dq_kernel<T><<<(unsigned)(p.n_qtile * s.H_kv), 256, 0, stream>>>(
+    (p.few_q ? packed_dq_few_kernel<T> : packed_dq_kernel<T>)<<<(unsigned)(p.n_qtile * s.H_kv), 256, 0, stream>>>(
         heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), heads_of<const T>(dOut), stat_l, stat_d, pk,
         heads_of<T>(dQ), s.H_kv, s.causal, scale, scale_log2);
 }
