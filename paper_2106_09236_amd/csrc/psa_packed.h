@@ -191,116 +191,194 @@ __device__ __forceinline__ void clear(floatx16& a)
     for (int r = 0; r < 16; ++r) a[r] = 0.f;
 }
 
-// ---- a tile of rows in LDS, row-major with its 16-byte chunks permuted inside a row by the row's low bits, so that reads
-// of one chunk of many rows and of many chunks of one row both spread over the banks.
-template <typename T> struct LdsTile;
-template <> struct LdsTile<bf16_t> {
-    static constexpr int kRowBytes = 128;
-    static __device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ row) & 7) * 16; }
-};
-template <> struct LdsTile<float> {
-    static constexpr int kRowBytes = 256;
-    // rows 4 apart, which the two halves of a wave read at once in the second product, land in different halves of the banks
-    static __device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 256 + ((chunk ^ (row & 7) ^ ((row & 4) << 1)) & 15) * 16; }
-};
+// ---- float32 on the bfloat16 matrix units.  A float32 number is the sum of three bfloat16 numbers (each the rounding of what
+// the ones before it leave: 8 bits and a sign each), and a product of two is the six products of parts whose sizes are 2^-16 and
+// more of it; the others together are below 2^-23 of |a||b| (2^-25 as a rule), as a float32 product's own rounding.  Six bfloat16
+// products take 3/8 of the time of one on the float32 matrix unit (1024 against 64 flops a cycle of a SIMD).
+template <typename T> constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
 
-// ---- operands.  Q (or the columns' tensor of any product over the head's elements): this lane's column as B operand,
-// the elements a lane holds in the order that the rows' operand has them.
-template <typename T> struct ColOperand;
-template <> struct ColOperand<bf16_t> {
-    uint4 v[4];                            // elements 32 h + 8 k .. + 7
-    __device__ __forceinline__ void load(const bf16_t* row, int h) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = reinterpret_cast<const uint4*>(row)[4 * h + k];
-    }
-};
-template <> struct ColOperand<float> {
-    float4 v[8];                           // elements 8 k + 4 h .. + 3
-    __device__ __forceinline__ void load(const float* row, int h) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = reinterpret_cast<const float4*>(row)[2 * k + h];
-    }
-};
-// Rows of an LDS tile (32 from `row0`) as A operand, the same elements: lane (c, h) holds row row0 + c.
-template <typename T> using RowOperand = ColOperand<T>;
-__device__ __forceinline__ void lds_rows(RowOperand<bf16_t>& a, const unsigned char* s, int row0, int c, int h)
+// x[0], x[1] into parts (pairs of bfloat16, low half first).  The remainder p - hi is exact: a two-term dot product of the pair
+// with (-1, 0) or (0, -1).
+__device__ __forceinline__ void split_pair(float x0, float x1, uint32_t (&part)[3])
 {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) a.v[k] = *reinterpret_cast<const uint4*>(s + LdsTile<bf16_t>::chunk_at(row0 + c, 4 * h + k));
-}
-__device__ __forceinline__ void lds_rows(RowOperand<float>& a, const unsigned char* s, int row0, int c, int h)
-{
-#pragma unroll
-    for (int k = 0; k < 8; ++k) a.v[k] = *reinterpret_cast<const float4*>(s + LdsTile<float>::chunk_at(row0 + c, 2 * k + h));
-}
-// Row c of a tile in memory as A operand; `ofs` is the row's offset in the buffer.
-__device__ __forceinline__ void buffer_rows(RowOperand<bf16_t>& a, __amdgpu_buffer_rsrc_t b, int ofs, int h)
-{
-#pragma unroll
-    for (int k = 0; k < 4; ++k) a.v[k] = buffer_load16<uint4>(b, ofs + 64 * h + 16 * k);
-}
-__device__ __forceinline__ void buffer_rows(RowOperand<float>& a, __amdgpu_buffer_rsrc_t b, int ofs, int h)
-{
-#pragma unroll
-    for (int k = 0; k < 8; ++k) a.v[k] = buffer_load16<float4>(b, ofs + 16 * h + 32 * k);
-}
-// D[row][col] += sum over the head's 64 elements
-__device__ __forceinline__ floatx16 product(const RowOperand<bf16_t>& a, const ColOperand<bf16_t>& b, floatx16 d)
-{
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.v[k]), __builtin_bit_cast(bf16x8, b.v[k]), d, 0, 0, 0);
-    return d;
-}
-__device__ __forceinline__ floatx16 product(const RowOperand<float>& a, const ColOperand<float>& b, floatx16 d)
-{
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        d = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[k].x, b.v[k].x, d, 0, 0, 0);
-        d = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[k].y, b.v[k].y, d, 0, 0, 0);
-        d = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[k].z, b.v[k].z, d, 0, 0, 0);
-        d = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[k].w, b.v[k].w, d, 0, 0, 0);
-    }
-    return d;
+    // in scalar registers: as a literal the compiler encodes (-1, 0) as the inline constant -1.0, which the instruction reads as
+    // another pair
+    uint32_t minus_lo = 0x0000BF80u, minus_hi = 0xBF800000u;
+    asm("" : "+s"(minus_lo), "+s"(minus_hi));
+    part[0] = cvt_pk_bf16(x0, x1);
+    const bf16x2 a = __builtin_bit_cast(bf16x2, part[0]);
+    x0 = __builtin_amdgcn_fdot2_f32_bf16(a, __builtin_bit_cast(bf16x2, minus_lo), x0, false);
+    x1 = __builtin_amdgcn_fdot2_f32_bf16(a, __builtin_bit_cast(bf16x2, minus_hi), x1, false);
+    part[1] = cvt_pk_bf16(x0, x1);
+    const bf16x2 b = __builtin_bit_cast(bf16x2, part[1]);
+    x0 = __builtin_amdgcn_fdot2_f32_bf16(b, __builtin_bit_cast(bf16x2, minus_lo), x0, false);
+    x1 = __builtin_amdgcn_fdot2_f32_bf16(b, __builtin_bit_cast(bf16x2, minus_hi), x1, false);
+    part[2] = cvt_pk_bf16(x0, x1);
 }
 
-// D^T[e][col] += sum over 32 rows of the LDS tile from row0 of X[row][e] * w[row], w in accumulator order (row acc_row(r, h) in
-// w[r]); D in two accumulators of 32 elements e.
-// bfloat16: w is rounded to bfloat16; the tile is read through the transposing LDS read: of each group of 16 lanes, lane s
-// points at row s / 4 of four rows, columns 4 (s % 4) .., and lane i receives column i of the four rows.
-__device__ __forceinline__ void accumulate(floatx16 (&d)[2], const unsigned char* s, int row0, const floatx16& w, int c, int h, bf16_t)
+// Operand of 8 elements of the order of summation to a lane, in its parts.
+template <typename T> struct Operand { uint4 v[kParts<T>]; };
+__device__ __forceinline__ Operand<bf16_t> operand(const uint4& x, bf16_t) { return Operand<bf16_t>{{x}}; }
+__device__ __forceinline__ Operand<float> operand(const float (&x)[8])
 {
-    const int s16 = c & 15, row = row0 + 4 * h + (s16 >> 2), col = (c & 16) + 4 * (s16 & 3);
+    uint32_t p[4][3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split_pair(x[2 * i], x[2 * i + 1], p[i]);
+    Operand<float> o;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) o.v[k] = make_uint4(p[0][k], p[1][k], p[2][k], p[3][k]);
+    return o;
+}
+__device__ __forceinline__ floatx16 mfma(const uint4& a, const uint4& b, floatx16 d)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), d, 0, 0, 0);
+}
+__device__ __forceinline__ floatx16 mfma(const Operand<bf16_t>& a, const Operand<bf16_t>& b, floatx16 d) { return mfma(a.v[0], b.v[0], d); }
+__device__ __forceinline__ floatx16 mfma(const Operand<float>& a, const Operand<float>& b, floatx16 d)
+{
+    d = mfma(a.v[2], b.v[0], d);           // small ones first
+    d = mfma(a.v[0], b.v[2], d);
+    d = mfma(a.v[1], b.v[1], d);
+    d = mfma(a.v[1], b.v[0], d);
+    d = mfma(a.v[0], b.v[1], d);
+    return mfma(a.v[0], b.v[0], d);
+}
+
+// ---- a tile of ROWS rows in LDS: a plane of bfloat16 for each part, row-major, its 16-byte chunks permuted inside a row.  256 bytes of
+// banks are two rows, so the permutation comes from the row's bits 1 .. 3: one chunk of 16 rows in a row covers all banks (rows as first
+// operand), and so do 64 bytes of 4 rows (the transposing read), for which rows 2 apart have to differ in the chunk's high bit.
+constexpr int kTileRowBytes = 128;
+template <typename T, int ROWS> constexpr int kTileBytes = ROWS * kTileRowBytes * kParts<T>;
+__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * kTileRowBytes + ((chunk ^ ((row & 2) << 1) ^ ((row >> 2) & 3)) & 7) * 16; }
+
+// 16 bytes of a tensor's row (chunk `ch` of it) into the tile
+template <int ROWS>
+__device__ __forceinline__ void put(unsigned char* s, int row, int ch, const uint4& x, bf16_t) { *reinterpret_cast<uint4*>(s + chunk_at(row, ch)) = x; }
+template <int ROWS>
+__device__ __forceinline__ void put(unsigned char* s, int row, int ch, const uint4& x, float)
+{
+    uint32_t p[2][3];
+    split_pair(__uint_as_float(x.x), __uint_as_float(x.y), p[0]);
+    split_pair(__uint_as_float(x.z), __uint_as_float(x.w), p[1]);
+    unsigned char* dst = s + chunk_at(row, ch >> 1) + (ch & 1) * 8;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(dst + k * ROWS * kTileRowBytes) = make_uint2(p[0][k], p[1][k]);
+}
+
+// ---- operands over a head's 64 elements: lane (c, h) has elements 32 h + 8 k .. + 7 of row (or column) c in step k.
+template <typename T> struct HeadOperand {
+    Operand<T> v[4];
+    __device__ __forceinline__ void load(const T* row, int h);
+};
+template <> __device__ __forceinline__ void HeadOperand<bf16_t>::load(const bf16_t* row, int h)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k].v[0] = reinterpret_cast<const uint4*>(row)[4 * h + k];
+}
+template <> __device__ __forceinline__ void HeadOperand<float>::load(const float* row, int h)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        float x[8];
+        load_vec(reinterpret_cast<float (&)[4]>(x[0]), row + 32 * h + 8 * k, 4);
+        load_vec(reinterpret_cast<float (&)[4]>(x[4]), row + 32 * h + 8 * k + 4, 4);
+        v[k] = operand(x);
+    }
+}
+// A row on its way from memory to such an operand; `ofs` is the row's offset in the buffer.
+template <typename T> struct HeadRow {
+    static constexpr int N = 64 * sizeof(T) / 32;
+    uint4 x[N];
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t b, int ofs, int h) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = buffer_load16<uint4>(b, ofs + (16 * h * N) + 16 * i);
+    }
+    __device__ __forceinline__ Operand<T> step(int k) const;
+};
+template <> __device__ __forceinline__ Operand<bf16_t> HeadRow<bf16_t>::step(int k) const { return operand(x[k], bf16_t{}); }
+template <> __device__ __forceinline__ Operand<float> HeadRow<float>::step(int k) const
+{
+    const uint4 &a = x[2 * k], &b = x[2 * k + 1];
+    const float f[8] = {__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
+                        __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
+    return operand(f);
+}
+
+// D[row][col] = sum over the head's 64 elements, rows from memory
+template <typename T>
+__device__ __forceinline__ floatx16 product(const HeadRow<T>& a, const HeadOperand<T>& b)
+{
+    floatx16 d;
+    clear(d);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) d = mfma(a.step(k), b.v[k], d);
+    return d;
+}
+// ... the operand of one step from 32 rows from row0 of a tile of ROWS in LDS
+template <typename T, int ROWS>
+__device__ __forceinline__ Operand<T> tile_operand(const unsigned char* s, int row0, int k, int c, int h)
+{
+    Operand<T> a;
+#pragma unroll
+    for (int i = 0; i < kParts<T>; ++i) a.v[i] = *reinterpret_cast<const uint4*>(s + i * ROWS * kTileRowBytes + chunk_at(row0 + c, 4 * h + k));
+    return a;
+}
+template <typename T, int ROWS>
+__device__ __forceinline__ floatx16 product(const unsigned char* s, int row0, const HeadOperand<T>& b, int c, int h)
+{
+    floatx16 d;
+    clear(d);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        d = mfma(tile_operand<T, ROWS>(s, row0, k, c, h), b.v[k], d);
+    }
+    return d;
+}
+
+// The column operand of a product over 16 rows (step st of 32), from what a lane has in accumulator order: w[8 st] .. w[8 st + 7].
+// bfloat16: rounded.
+__device__ __forceinline__ Operand<bf16_t> weight_operand(const floatx16& w, int st, bf16_t)
+{
+    return Operand<bf16_t>{{make_uint4(cvt_pk_bf16(w[8 * st], w[8 * st + 1]), cvt_pk_bf16(w[8 * st + 2], w[8 * st + 3]),
+                                       cvt_pk_bf16(w[8 * st + 4], w[8 * st + 5]), cvt_pk_bf16(w[8 * st + 6], w[8 * st + 7]))}};
+}
+__device__ __forceinline__ Operand<float> weight_operand(const floatx16& w, int st, float)
+{
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = w[8 * st + i];
+    return operand(x);
+}
+// D^T[e][col] += sum over 32 rows of the tile from row0 of X[row][e] w[row], w in accumulator order (row acc_row(r, h) in w[r]); D in two
+// accumulators of 32 elements e.  The tile's operand for 16 rows (step st) and 32 elements (dt) comes through the transposing LDS
+// read: of each group of 16 lanes, lane s points at row s / 4 of four rows, columns 4 (s % 4) .., and lane i receives column i of
+// the four rows.
+template <typename T, int ROWS>
+__device__ __forceinline__ Operand<T> tile_transposed(const unsigned char* s, int row0, int st, int dt, int c, int h)
+{
+    const int s16 = c & 15, row = row0 + 4 * h + (s16 >> 2), byte = ((c & 16) + 4 * (s16 & 3) + 32 * dt) * 2;
+    Operand<T> a;
+#pragma unroll
+    for (int i = 0; i < kParts<T>; ++i) {
+        uint2 part[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const unsigned char* p = s + i * ROWS * kTileRowBytes + chunk_at(row + 16 * st + 8 * e, byte >> 4) + (byte & 15);
+            part[e] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((shortx4 __attribute__((address_space(3)))*)(p)));
+        }
+        a.v[i] = make_uint4(part[0].x, part[0].y, part[1].x, part[1].y);
+    }
+    return a;
+}
+template <typename T, int ROWS>
+__device__ __forceinline__ void accumulate(floatx16 (&d)[2], const unsigned char* s, int row0, const floatx16& w, int c, int h)
+{
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
-        uint4 b;
-        b.x = cvt_pk_bf16(w[8 * st], w[8 * st + 1]);
-        b.y = cvt_pk_bf16(w[8 * st + 2], w[8 * st + 3]);
-        b.z = cvt_pk_bf16(w[8 * st + 4], w[8 * st + 5]);
-        b.w = cvt_pk_bf16(w[8 * st + 6], w[8 * st + 7]);
+        const Operand<T> b = weight_operand(w, st, T{});
 #pragma unroll
-        for (int dt = 0; dt < 2; ++dt) {
-            uint2 part[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int r = row + 16 * st + 8 * e, byte = (col + 32 * dt) * 2;
-                const unsigned char* p = s + LdsTile<bf16_t>::chunk_at(r, byte >> 4) + (byte & 15);
-                part[e] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((shortx4 __attribute__((address_space(3)))*)(p)));
-            }
-            const uint4 a = make_uint4(part[0].x, part[0].y, part[1].x, part[1].y);
-            d[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), d[dt], 0, 0, 0);
-        }
+        for (int dt = 0; dt < 2; ++dt) d[dt] = mfma(tile_transposed<T, ROWS>(s, row0, st, dt, c, h), b, d[dt]);
     }
-}
-__device__ __forceinline__ void accumulate(floatx16 (&d)[2], const unsigned char* s, int row0, const floatx16& w, int c, int h, float)
-{
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-#pragma unroll
-        for (int dt = 0; dt < 2; ++dt) {
-            const float a = *reinterpret_cast<const float*>(s + LdsTile<float>::chunk_at(row0 + acc_row(r, h), (32 * dt + c) >> 2) + (c & 3) * 4);
-            d[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], d[dt], 0, 0, 0);
-        }
 }
 
 // Column c's 64 elements of D^T (elements 32 dt + acc_row(r, h) in d[dt][r]) times f, to its row of a tensor.

@@ -12,10 +12,10 @@ struct Rows32 {
     float m, l;
     floatx16 o[2];                         // element 32 dt + acc_row(r, h) of row c in o[dt][r]
     __device__ __forceinline__ void init() { m = kMaxInit; l = 0.f; clear(o[0]); clear(o[1]); }
-    // Scores of N x 32 keys to weights; the constant that is subtracted follows the maximum only when that has grown by
+    // Takes the maximum of the scores of N x 32 keys; the constant that is subtracted follows it only when that has grown by
     // more than 2^8 (kLagLog2): weights up to 2^8 are as exact as weights up to 1, and a change scales 32 accumulators.
     template <int N>
-    __device__ __forceinline__ void weights(floatx16 (&s)[N], float scale) {
+    __device__ __forceinline__ void follow(const floatx16 (&s)[N], float scale) {
         float t = s[0][0];
 #pragma unroll
         for (int n = 0; n < N; ++n)
@@ -23,20 +23,22 @@ struct Rows32 {
             for (int r = 0; r < 16; ++r) t = fmaxf(t, s[n][r]);
         t = max_xor32(t) * scale;
         const float m_new = t > m + kLagLog2 ? t : m;
-        const float alpha = fast_exp2(m - m_new);
-        float sum = 0.f;
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) { s[n][r] = fast_exp2(fmaf(s[n][r], scale, -m_new)); sum += s[n][r]; }
-        l = l * alpha + sum;
         if (__builtin_amdgcn_ballot_w64(m_new > m) != 0) {
+            const float alpha = fast_exp2(m - m_new);
+            l *= alpha;
 #pragma unroll
             for (int dt = 0; dt < 2; ++dt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
         }
         m = m_new;
+    }
+    // Scores to weights
+    __device__ __forceinline__ void weights(floatx16& s, float scale) {
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) { s[r] = fast_exp2(fmaf(s[r], scale, -m)); sum += s[r]; }
+        l += sum;
     }
     // The infinities and NaN of V rows j0 .. j0 + n - 1 that were left out of the tile: to the rows that see them.
     template <typename T>
@@ -53,15 +55,20 @@ struct Rows32 {
 };
 
 // 4 waves of 32 rows each; tiles of KT keys and values go through LDS, the next tile's rows are on their way meanwhile.
+// bfloat16 is bound by the vector unit (131 instructions and 32 exponentials to 16 matrix instructions: 65 % of its issue
+// cycles, the matrix unit 38 %) and, in long runs, by power: 16384 causal, 8 heads, 350 us at first (785 TFLOP/s), 390 when hot.  What
+// did not help: 64 rows to a wave (half the LDS reads, 2 waves to a SIMD: 530 us), 4 waves to a SIMD with 32 keys at a time
+// (430), the scores of a step formed between the weights of the one before (440), priorities (no change).
 template <typename T, int KT>
-__global__ __launch_bounds__(256, 2)
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3)
 void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Packing p, Heads<T> out, float* __restrict__ lse,
                         int H_kv, int causal, float scale, int n_tile)
 {
     constexpr int CH = 64 * sizeof(T) / 16;            // 16-byte chunks of a row
     constexpr int NL = KT * CH / 256;                  // of a tile, to a thread
-    constexpr int kTileBytes = KT * LdsTile<T>::kRowBytes;
-    __shared__ __attribute__((aligned(16))) unsigned char sK[2][kTileBytes], sV[2][kTileBytes];
+    constexpr int NS = KT / 32;
+    constexpr int kBytes = kTileBytes<T, KT>;
+    __shared__ __attribute__((aligned(16))) unsigned char sK[2][kBytes], sV[2][kBytes];
     __shared__ int s_bad[2][4];
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
@@ -72,26 +79,25 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
     const int n_rows = f.nq * p.G;
     const int shift = f.nk - f.nq + 1;                 // causal: query t sees the first t + shift keys
     auto visible = [&](int r) { const int t = r / p.G; return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
-    const int row = f.tile * 128 + wave * 32 + c, rc = min(row, n_rows - 1);
+    const int row0 = f.tile * 128 + wave * 32;
+    const int row = row0 + c, rc = min(row, n_rows - 1);
     const int t = rc / p.G, head = hk * p.G + (rc - t * p.G);
     const int n_vis = visible(rc);
     const int n_all = __builtin_amdgcn_readfirstlane(visible(min(f.tile * 128 + 127, n_rows - 1)));         // keys any row of the work-group sees
     const int n_every = __builtin_amdgcn_readfirstlane(visible(f.tile * 128));                              // ... and those that all see
-    const int row0 = f.tile * 128 + wave * 32;
     const int n_wave = __builtin_amdgcn_readfirstlane(row0 < n_rows ? visible(min(row0 + 31, n_rows - 1)) : 0);
     const int n_wave_every = __builtin_amdgcn_readfirstlane(visible(min(row0, n_rows - 1)));
 
-    ColOperand<T> q;
+    HeadOperand<T> q;
     q.load(Q.at(head, f.q0 + t), h);
     const T* Kh = K.at(hk, f.k0);
     const T* Vh = V.at(hk, f.k0);
-    int k_ofs[NL], v_ofs[NL], s_ofs[NL];
+    int k_ofs[NL], v_ofs[NL];
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
         const int id = i * 256 + tid, r = id / CH, ch = id % CH;
         k_ofs[i] = (int)(r * K.row * (int64_t)sizeof(T)) + ch * 16;
         v_ofs[i] = (int)(r * V.row * (int64_t)sizeof(T)) + ch * 16;
-        s_ofs[i] = LdsTile<T>::chunk_at(r, ch);
     }
     uint4 kr[NL], vr[NL];
     auto fetch = [&](int j0) {
@@ -106,9 +112,9 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
     int buf = 0;
     for (int j0 = 0; j0 < n_all; j0 += KT, buf ^= 1) {
         // a weight of 0 does not keep an infinity or NaN of a value that a row does not see out of its sum: in tiles that
-        // some row sees in part they are left out and added afterwards
-        const bool part = j0 + KT > n_every;
-        if (part) {
+        // some row sees in part they are left out and added afterwards (float32: in all, since an infinity has no parts)
+        const bool look = sizeof(T) == 4 || j0 + KT > n_every;
+        if (look) {
             bool bad = false;
 #pragma unroll
             for (int i = 0; i < NL; ++i) bad |= nonfinite(vr[i], T{});
@@ -120,33 +126,30 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
         }
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            *reinterpret_cast<uint4*>(sK[buf] + s_ofs[i]) = kr[i];
-            *reinterpret_cast<uint4*>(sV[buf] + s_ofs[i]) = vr[i];
+            const int id = i * 256 + tid;
+            put<KT>(sK[buf], id / CH, id % CH, kr[i], T{});
+            put<KT>(sV[buf], id / CH, id % CH, vr[i], T{});
         }
         if (j0 + KT < n_all) fetch(j0 + KT);
         lds_barrier();
-        if (j0 < n_wave) {
-            floatx16 s[KT / 32];
+        if (j0 >= n_wave) continue;
+        floatx16 s[NS];
 #pragma unroll
-            for (int n = 0; n < KT / 32; ++n) {
-                RowOperand<T> a;
-                lds_rows(a, sK[buf], 32 * n, c, h);
-                clear(s[n]);
-                s[n] = product(a, q, s[n]);
-            }
-            if (j0 + KT > n_wave_every) {
+        for (int n = 0; n < NS; ++n) s[n] = product<T, KT>(sK[buf], 32 * n, q, c, h);
+        if (j0 + KT > n_wave_every) {
 #pragma unroll
-                for (int n = 0; n < KT / 32; ++n)
+            for (int n = 0; n < NS; ++n)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        s[n][r] = j0 + 32 * n + acc_row(r, h) < n_vis ? s[n][r] : -INFINITY;
-            }
-            acc.weights(s, scale);
-#pragma unroll
-            for (int n = 0; n < KT / 32; ++n) accumulate(acc.o, sV[buf], 32 * n, s[n], c, h, T{});
-            if (part && (s_bad[buf][0] | s_bad[buf][1] | s_bad[buf][2] | s_bad[buf][3]))
-                acc.add_nonfinite(Vh + j0 * V.row, V.row, min(KT, f.nk - j0), n_vis - j0, h);
+                for (int r = 0; r < 16; ++r) s[n][r] = j0 + 32 * n + acc_row(r, h) < n_vis ? s[n][r] : -INFINITY;
         }
+        acc.follow(s, scale);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            acc.weights(s[n], scale);
+            accumulate<T, KT>(acc.o, sV[buf], 32 * n, s[n], c, h);
+        }
+        if (look && (s_bad[buf][0] | s_bad[buf][1] | s_bad[buf][2] | s_bad[buf][3]))
+            acc.add_nonfinite(Vh + j0 * V.row, V.row, min(KT, f.nk - j0), n_vis - j0, h);
     }
     if (row >= n_rows) return;
     float l = acc.l + swap_half(acc.l);
@@ -165,10 +168,10 @@ void packed_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pac
 {
     constexpr int CH = 64 * sizeof(T) / 16;
     constexpr int NL = 32 * CH / 64;                   // chunks of a tile of 32 rows, to a lane
-    constexpr int kTileBytes = 32 * LdsTile<T>::kRowBytes;
+    constexpr int kBytes = kTileBytes<T, 32>;
     constexpr int kRow = 68;                           // floats of a row of the join: 64, and 16 bytes against bank conflicts
     constexpr int kJoinBytes = 4 * 32 * kRow * 4;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kTileBytes > kJoinBytes ? 4 * kTileBytes : kJoinBytes];
+    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kBytes > kJoinBytes ? 4 * kBytes : kJoinBytes];
     __shared__ float s_m[4][32], s_l[4][32];
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv, split = blockIdx.y;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
@@ -188,17 +191,17 @@ void packed_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pac
     const int tiles = (n_all + 31) / 32, per = (tiles + n_split - 1) / n_split;
     const int end = min(n_all, (split + 1) * per * 32);
 
-    ColOperand<T> q;
+    HeadOperand<T> q;
     q.load(Q.at(head, f.q0 + t), h);
     const T* Kh = K.at(hk, f.k0);
     const T* Vh = V.at(hk, f.k0);
-    unsigned char* sV = lds + wave * kTileBytes;
-    RowOperand<T> kn;
+    unsigned char* sV = lds + wave * kBytes;
+    HeadRow<T> kn;
     uint4 vn[NL];
     auto fetch = [&](int j0) {
         const int n = min(32, f.nk - j0);
         const auto kb = tile_rows(Kh + j0 * K.row, K.row, n), vb = tile_rows(Vh + j0 * V.row, V.row, n);
-        buffer_rows(kn, kb, (int)(c * K.row * (int64_t)sizeof(T)), h);
+        kn.load(kb, (int)(c * K.row * (int64_t)sizeof(T)), h);
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int id = i * 64 + lane;
@@ -210,9 +213,9 @@ void packed_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pac
     int j0 = (split * per + wave) * 32;
     if (j0 < end) fetch(j0);
     for (; j0 < end; j0 += 128) {
-        const bool part = j0 + 32 > n_every;
+        const bool part = j0 + 32 > n_every, look = sizeof(T) == 4 || part;
         bool any = false;
-        if (part) {
+        if (look) {
             bool bad = false;
 #pragma unroll
             for (int i = 0; i < NL; ++i) bad |= nonfinite(vn[i], T{});
@@ -225,19 +228,19 @@ void packed_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pac
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int id = i * 64 + lane;
-            *reinterpret_cast<uint4*>(sV + LdsTile<T>::chunk_at(id / CH, id % CH)) = vn[i];
+            put<32>(sV, id / CH, id % CH, vn[i], T{});
         }
         floatx16 s[1];
-        clear(s[0]);
-        s[0] = product(kn, q, s[0]);
+        s[0] = product(kn, q);
         wave_lds_sync();
         if (j0 + 128 < end) fetch(j0 + 128);
         if (part) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[0][r] = j0 + acc_row(r, h) < n_vis ? s[0][r] : -INFINITY;
         }
-        acc.weights(s, scale);
-        accumulate(acc.o, sV, 0, s[0], c, h, T{});
+        acc.follow(s, scale);
+        acc.weights(s[0], scale);
+        accumulate<T, 32>(acc.o, sV, 0, s[0], c, h);
         if (any) acc.add_nonfinite(Vh + j0 * V.row, V.row, min(32, f.nk - j0), n_vis - j0, h);
     }
     // join: wave w's sums of row r at join[w][r]; a wave that saw no key has m = kMaxInit and sums of 0
@@ -339,7 +342,7 @@ PackedPlan make_packed_plan(const psa_packed_shape_t& s)
     PackedPlan p{};
     const int64_t rows = (int64_t)s.T_q * (s.H / s.H_kv);
     const int64_t wide = (rows / 128 + s.B) * s.H_kv;
-    p.few = s.dtype == PSA_F32 || rows / s.B <= 64 || wide < 256;
+    p.few = rows / s.B <= 64 || wide < 256;
     p.rows = p.few ? 32 : 128;
     p.n_tile = (int)(rows / p.rows) + s.B;
     p.n_split = 1;

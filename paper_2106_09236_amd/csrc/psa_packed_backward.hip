@@ -36,16 +36,15 @@ void packed_stats_kernel(Heads<const T> out, Heads<const T> dOut, const float* _
 }
 
 // dK and dV of 128 keys: 4 waves of 32, tiles of 32 rows of Q and dOut through LDS.
-template <typename T>
+template <typename T, int QT>
 __global__ __launch_bounds__(256, 2)
 void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, const float* __restrict__ stat_l,
                        const float* __restrict__ stat_d, Packing p, Heads<T> dK, Heads<T> dV, int H_kv, int causal, float scale,
                        float scale_log2, int n_tile)
 {
-    constexpr int QT = 32;
     constexpr int CH = 64 * sizeof(T) / 16, NL = QT * CH / 256;
-    constexpr int kTileBytes = QT * LdsTile<T>::kRowBytes;
-    __shared__ __attribute__((aligned(16))) unsigned char sQ[2][kTileBytes], sG[2][kTileBytes];
+    constexpr int kBytes = kTileBytes<T, QT>;
+    __shared__ __attribute__((aligned(16))) unsigned char sQ[2][kBytes], sG[2][kBytes];
     __shared__ __attribute__((aligned(16))) float sL[2][QT], sD[2][QT];
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
@@ -64,7 +63,7 @@ void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Hea
     const int first_wave = __builtin_amdgcn_readfirstlane(first_row(wave_key));
     const int first_every = __builtin_amdgcn_readfirstlane(first_row(min(wave_key + 31, f.nk - 1)));
 
-    ColOperand<T> k, v;
+    HeadOperand<T> k, v;
     k.load(K.at(hk, f.k0 + kc), h);
     v.load(V.at(hk, f.k0 + kc), h);
     floatx16 dk[2], dv[2];
@@ -73,16 +72,18 @@ void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Hea
     const int64_t stat0 = ((int64_t)hk * p.Tq + f.q0) * p.G;
     uint4 qr[NL], gr[NL];
     float lr = INFINITY, dr = 0.f;
+    int r0 = first_all / QT * QT;
+    const int ch = tid % CH, dt = 256 / CH / p.G, dg = 256 / CH - dt * p.G;     // (the thread's next chunk is 256 / CH rows on)
+    RowAt at(r0 + tid / CH, p.G);
     auto fetch = [&](int r0) {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            const int id = i * 256 + tid, r = r0 + id / CH, ch = id % CH;
             qr[i] = gr[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (r < n_rows) {
-                const int t = r / p.G, head = hk * p.G + (r - t * p.G);
-                qr[i] = reinterpret_cast<const uint4*>(Q.at(head, f.q0 + t))[ch];
-                gr[i] = reinterpret_cast<const uint4*>(dOut.at(head, f.q0 + t))[ch];
+            if (r0 + i * (256 / CH) + tid / CH < n_rows) {
+                qr[i] = reinterpret_cast<const uint4*>(Q.at(hk * p.G + at.g, f.q0 + at.t))[ch];
+                gr[i] = reinterpret_cast<const uint4*>(dOut.at(hk * p.G + at.g, f.q0 + at.t))[ch];
             }
+            at.add(dt, dg, p.G);
         }
         if (tid < QT) {
             const bool in = r0 + tid < n_rows;
@@ -90,43 +91,40 @@ void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Hea
             dr = in ? stat_d[stat0 + r0 + tid] : 0.f;
         }
     };
-    int r0 = first_all / QT * QT;
     if (r0 < n_rows) fetch(r0);
     for (int buf = 0; r0 < n_rows; r0 += QT, buf ^= 1) {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            const int id = i * 256 + tid, ofs = LdsTile<T>::chunk_at(id / CH, id % CH);
-            *reinterpret_cast<uint4*>(sQ[buf] + ofs) = qr[i];
-            *reinterpret_cast<uint4*>(sG[buf] + ofs) = gr[i];
+            const int id = i * 256 + tid;
+            put<QT>(sQ[buf], id / CH, id % CH, qr[i], T{});
+            put<QT>(sG[buf], id / CH, id % CH, gr[i], T{});
         }
         if (tid < QT) { sL[buf][tid] = lr; sD[buf][tid] = dr; }
         if (r0 + QT < n_rows) fetch(r0 + QT);
         lds_barrier();
-        if (r0 + QT <= first_wave) continue;
-        RowOperand<T> a;
-        floatx16 s, w;
-        clear(s); clear(w);
-        lds_rows(a, sQ[buf], 0, c, h);
-        s = product(a, k, s);
-        lds_rows(a, sG[buf], 0, c, h);
-        w = product(a, v, w);
 #pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-            const float4 l4 = *reinterpret_cast<const float4*>(&sL[buf][8 * r4 + 4 * h]), d4 = *reinterpret_cast<const float4*>(&sD[buf][8 * r4 + 4 * h]);
-            const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
+        for (int n = 0; n < QT / 32; ++n) {
+            const int r = r0 + 32 * n;
+            if (r + 32 <= first_wave || r >= n_rows) continue;
+            floatx16 s = product<T, QT>(sQ[buf], 32 * n, k, c, h), w = product<T, QT>(sG[buf], 32 * n, v, c, h);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[4 * r4 + e] = fast_exp2(fmaf(s[4 * r4 + e], scale_log2, -l[e]));
-                w[4 * r4 + e] = s[4 * r4 + e] * (w[4 * r4 + e] - d[e]);
+            for (int r4 = 0; r4 < 4; ++r4) {
+                const float4 l4 = *reinterpret_cast<const float4*>(&sL[buf][32 * n + 8 * r4 + 4 * h]), d4 = *reinterpret_cast<const float4*>(&sD[buf][32 * n + 8 * r4 + 4 * h]);
+                const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[4 * r4 + e] = fast_exp2(fmaf(s[4 * r4 + e], scale_log2, -l[e]));
+                    w[4 * r4 + e] = s[4 * r4 + e] * (w[4 * r4 + e] - d[e]);
+                }
             }
-        }
-        if (r0 < first_every) {
+            if (r < first_every) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (r0 + acc_row(r, h) < first) { s[r] = 0.f; w[r] = 0.f; }
+                for (int i = 0; i < 16; ++i)
+                    if (r + acc_row(i, h) < first) { s[i] = 0.f; w[i] = 0.f; }
+            }
+            accumulate<T, QT>(dv, sG[buf], 32 * n, s, c, h);
+            accumulate<T, QT>(dk, sQ[buf], 32 * n, w, c, h);
         }
-        accumulate(dv, sG[buf], 0, s, c, h, T{});
-        accumulate(dk, sQ[buf], 0, w, c, h, T{});
     }
     if (key >= f.nk) return;
     store_row(dK.at(hk, f.k0 + key), dk, scale, h);
@@ -134,15 +132,14 @@ void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Hea
 }
 
 // dQ of 128 rows: 4 waves of 32, tiles of 32 keys and values through LDS.
-template <typename T>
-__global__ __launch_bounds__(256, 2)
+template <typename T, int KT>
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3)
 void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, const float* __restrict__ stat_l,
                       const float* __restrict__ stat_d, Packing p, Heads<T> dQ, int H_kv, int causal, float scale, float scale_log2)
 {
-    constexpr int KT = 32;
     constexpr int CH = 64 * sizeof(T) / 16, NL = KT * CH / 256;
-    constexpr int kTileBytes = KT * LdsTile<T>::kRowBytes;
-    __shared__ __attribute__((aligned(16))) unsigned char sK[2][kTileBytes], sV[2][kTileBytes];
+    constexpr int kBytes = kTileBytes<T, KT>;
+    __shared__ __attribute__((aligned(16))) unsigned char sK[2][kBytes], sV[2][kBytes];
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
     const SeqTile f = find_tile<128, false>(p, x);
@@ -157,7 +154,7 @@ void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Head
     const int n_all = __builtin_amdgcn_readfirstlane(visible(min(f.tile * 128 + 127, n_rows - 1)));
     const int n_wave = __builtin_amdgcn_readfirstlane(row0 < n_rows ? visible(min(row0 + 31, n_rows - 1)) : 0);
     const int n_every = __builtin_amdgcn_readfirstlane(visible(min(row0, n_rows - 1)));
-    ColOperand<T> q, g;
+    HeadOperand<T> q, g;
     q.load(Q.at(head, f.q0 + t), h);
     g.load(dOut.at(head, f.q0 + t), h);
     const int64_t so = ((int64_t)hk * p.Tq + f.q0) * p.G + rc;
@@ -182,28 +179,27 @@ void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Head
     for (int j0 = 0; j0 < n_all; j0 += KT, buf ^= 1) {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            const int id = i * 256 + tid, ofs = LdsTile<T>::chunk_at(id / CH, id % CH);
-            *reinterpret_cast<uint4*>(sK[buf] + ofs) = kr[i];
-            *reinterpret_cast<uint4*>(sV[buf] + ofs) = vr[i];
+            const int id = i * 256 + tid;
+            put<KT>(sK[buf], id / CH, id % CH, kr[i], T{});
+            put<KT>(sV[buf], id / CH, id % CH, vr[i], T{});
         }
         if (j0 + KT < n_all) fetch(j0 + KT);
         lds_barrier();
-        if (j0 >= n_wave) continue;
-        RowOperand<T> a;
-        floatx16 s, w;
-        clear(s); clear(w);
-        lds_rows(a, sK[buf], 0, c, h);
-        s = product(a, q, s);
-        lds_rows(a, sV[buf], 0, c, h);
-        w = product(a, g, w);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) w[r] = fast_exp2(fmaf(s[r], scale_log2, -l)) * (w[r] - d);
-        if (j0 + KT > n_every) {
+        for (int n = 0; n < KT / 32; ++n) {
+            const int j = j0 + 32 * n;
+            if (j >= n_wave) break;
+            const floatx16 s = product<T, KT>(sK[buf], 32 * n, q, c, h);
+            floatx16 w = product<T, KT>(sV[buf], 32 * n, g, c, h);
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (j0 + acc_row(r, h) >= n_vis) w[r] = 0.f;
+            for (int r = 0; r < 16; ++r) w[r] = fast_exp2(fmaf(s[r], scale_log2, -l)) * (w[r] - d);
+            if (j + 32 > n_every) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (j + acc_row(r, h) >= n_vis) w[r] = 0.f;
+            }
+            accumulate<T, KT>(dq, sK[buf], 32 * n, w, c, h);
         }
-        accumulate(dq, sK[buf], 0, w, c, h, T{});
     }
     if (row >= n_rows) return;
     store_row(dQ.at(head, f.q0 + t), dq, scale, h);
@@ -220,9 +216,9 @@ void packed_dkv_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V,
                            float scale_log2, int n_tile)
 {
     constexpr int CH = 64 * sizeof(T) / 16, NL = 32 * CH / 64, RL = 64 / CH;       // lanes of a row, chunks of a lane, rows of one load
-    constexpr int kTileBytes = 32 * LdsTile<T>::kRowBytes;
+    constexpr int kBytes = kTileBytes<T, 32>;
     constexpr int kJoinBytes = 4 * 32 * kJoinRow * 4;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[8 * kTileBytes > kJoinBytes ? 8 * kTileBytes : kJoinBytes];
+    __shared__ __attribute__((aligned(16))) unsigned char lds[8 * kBytes > kJoinBytes ? 8 * kBytes : kJoinBytes];
     __shared__ __attribute__((aligned(16))) float sL[4][32], sD[4][32];
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
@@ -238,21 +234,23 @@ void packed_dkv_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V,
     const int first_any = __builtin_amdgcn_readfirstlane(first_row(key0));
     const int first_every = __builtin_amdgcn_readfirstlane(first_row(min(key0 + 31, f.nk - 1)));
 
-    ColOperand<T> k, v;
+    HeadOperand<T> k, v;
     k.load(K.at(hk, f.k0 + kc), h);
     v.load(V.at(hk, f.k0 + kc), h);
     floatx16 dk[2], dv[2];
     clear(dk[0]); clear(dk[1]); clear(dv[0]); clear(dv[1]);
-    unsigned char *sQ = lds + wave * 2 * kTileBytes, *sG = sQ + kTileBytes;
+    unsigned char *sQ = lds + wave * 2 * kBytes, *sG = sQ + kBytes;
     const int64_t stat0 = ((int64_t)hk * p.Tq + f.q0) * p.G;
     const int lr = lane / CH, ch = lane % CH;
 
     // one set of registers carries a tile of Q, then the tile of dOut, then the next tile of Q
     uint4 x4[NL];
     float l_next = INFINITY, d_next = 0.f;
+    int r0 = first_any / 32 * 32 + wave * 32;
+    const int dt = RL / p.G, dg = RL - dt * p.G, dt128 = 128 / p.G, dg128 = 128 - dt128 * p.G;
+    RowAt base(r0 + lr, p.G);                          // of the tile that is fetched
     auto fetch = [&](const Heads<const T>& t, int r0) {
-        RowAt at(r0 + lr, p.G);
-        const int dt = RL / p.G, dg = RL - dt * p.G;
+        RowAt at = base;
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             x4[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -262,14 +260,13 @@ void packed_dkv_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V,
     };
     auto keep = [&](unsigned char* s) {
 #pragma unroll
-        for (int i = 0; i < NL; ++i) *reinterpret_cast<uint4*>(s + LdsTile<T>::chunk_at(lr + i * RL, ch)) = x4[i];
+        for (int i = 0; i < NL; ++i) put<32>(s, lr + i * RL, ch, x4[i], T{});
     };
     auto fetch_stats = [&](int r0) {
         const bool in = r0 + c < n_rows;
         l_next = in ? stat_l[stat0 + r0 + c] : INFINITY;
         d_next = in ? stat_d[stat0 + r0 + c] : 0.f;
     };
-    int r0 = first_any / 32 * 32 + wave * 32;
     if (r0 < n_rows) { fetch(Q, r0); fetch_stats(r0); }
     for (; r0 < n_rows; r0 += 128) {
         wave_lds_sync();
@@ -277,16 +274,12 @@ void packed_dkv_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V,
         if (h == 0) { sL[wave][c] = l_next; sD[wave][c] = d_next; }
         fetch(dOut, r0);
         wave_lds_sync();
-        RowOperand<T> a;
-        floatx16 s, w;
-        clear(s); clear(w);
-        lds_rows(a, sQ, 0, c, h);
-        s = product(a, k, s);
+        floatx16 s = product<T, 32>(sQ, 0, k, c, h);
         keep(sG);
+        base.add(dt128, dg128, p.G);
         if (r0 + 128 < n_rows) { fetch(Q, r0 + 128); fetch_stats(r0 + 128); }
         wave_lds_sync();
-        lds_rows(a, sG, 0, c, h);
-        w = product(a, v, w);
+        floatx16 w = product<T, 32>(sG, 0, v, c, h);
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) {
             const float4 l4 = *reinterpret_cast<const float4*>(&sL[wave][8 * r4 + 4 * h]), d4 = *reinterpret_cast<const float4*>(&sD[wave][8 * r4 + 4 * h]);
@@ -302,8 +295,8 @@ void packed_dkv_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V,
             for (int r = 0; r < 16; ++r)
                 if (r0 + acc_row(r, h) < first) { s[r] = 0.f; w[r] = 0.f; }
         }
-        accumulate(dv, sG, 0, s, c, h, T{});
-        accumulate(dk, sQ, 0, w, c, h, T{});
+        accumulate<T, 32>(dv, sG, 0, s, c, h);
+        accumulate<T, 32>(dk, sQ, 0, w, c, h);
     }
     float* join = reinterpret_cast<float*>(lds);
     const int key = key0 + (tid >> 3), e = (tid & 7) * 8;
@@ -324,9 +317,9 @@ void packed_dq_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, 
                           const float* __restrict__ stat_d, Packing p, Heads<T> dQ, int H_kv, int causal, float scale, float scale_log2)
 {
     constexpr int CH = 64 * sizeof(T) / 16, NL = 32 * CH / 64;
-    constexpr int kTileBytes = 32 * LdsTile<T>::kRowBytes;
+    constexpr int kBytes = kTileBytes<T, 32>;
     constexpr int kJoinBytes = 4 * 32 * kJoinRow * 4;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kTileBytes > kJoinBytes ? 4 * kTileBytes : kJoinBytes];
+    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kBytes > kJoinBytes ? 4 * kBytes : kJoinBytes];
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
     const SeqTile f = find_tile<32, false>(p, x);
@@ -339,7 +332,7 @@ void packed_dq_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, 
     const int n_vis = visible(rc);
     const int n_all = __builtin_amdgcn_readfirstlane(visible(min(row0 + 31, n_rows - 1)));
     const int n_every = __builtin_amdgcn_readfirstlane(visible(row0));
-    ColOperand<T> q, g;
+    HeadOperand<T> q, g;
     q.load(Q.at(head, f.q0 + t), h);
     g.load(dOut.at(head, f.q0 + t), h);
     const int64_t so = ((int64_t)hk * p.Tq + f.q0) * p.G + rc;
@@ -348,9 +341,9 @@ void packed_dq_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, 
     clear(dq[0]); clear(dq[1]);
     const T* Kh = K.at(hk, f.k0);
     const T* Vh = V.at(hk, f.k0);
-    unsigned char* sK = lds + wave * kTileBytes;
+    unsigned char* sK = lds + wave * kBytes;
     uint4 kn[NL];
-    RowOperand<T> vn;
+    HeadRow<T> vn;
     auto fetch = [&](int j0) {
         const int n = min(32, f.nk - j0);
         const auto kb = tile_rows(Kh + j0 * K.row, K.row, n), vb = tile_rows(Vh + j0 * V.row, V.row, n);
@@ -359,7 +352,7 @@ void packed_dq_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, 
             const int id = i * 64 + lane;
             kn[i] = buffer_load16<uint4>(kb, (int)((id / CH) * K.row * (int64_t)sizeof(T)) + (id % CH) * 16);
         }
-        buffer_rows(vn, vb, (int)(c * V.row * (int64_t)sizeof(T)), h);
+        vn.load(vb, (int)(c * V.row * (int64_t)sizeof(T)), h);
     };
     int j0 = wave * 32;
     if (j0 < n_all) fetch(j0);
@@ -368,16 +361,12 @@ void packed_dq_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, 
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int id = i * 64 + lane;
-            *reinterpret_cast<uint4*>(sK + LdsTile<T>::chunk_at(id / CH, id % CH)) = kn[i];
+            put<32>(sK, id / CH, id % CH, kn[i], T{});
         }
-        floatx16 s, w;
-        clear(s); clear(w);
-        w = product(vn, g, w);
+        floatx16 w = product(vn, g);
         wave_lds_sync();
         if (j0 + 128 < n_all) fetch(j0 + 128);
-        RowOperand<T> a;
-        lds_rows(a, sK, 0, c, h);
-        s = product(a, q, s);
+        const floatx16 s = product<T, 32>(sK, 0, q, c, h);
 #pragma unroll
         for (int r = 0; r < 16; ++r) w[r] = fast_exp2(fmaf(s[r], scale_log2, -l)) * (w[r] - d);
         if (j0 + 32 > n_every) {
@@ -385,7 +374,7 @@ void packed_dq_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, 
             for (int r = 0; r < 16; ++r)
                 if (j0 + acc_row(r, h) >= n_vis) w[r] = 0.f;
         }
-        accumulate(dq, sK, 0, w, c, h, T{});
+        accumulate<T, 32>(dq, sK, 0, w, c, h);
     }
     __syncthreads();
     float* join = reinterpret_cast<float*>(lds);
@@ -403,8 +392,11 @@ PackedBwdPlan make_packed_bwd_plan(const psa_packed_shape_t& s)
 {
     PackedBwdPlan p{};
     const int64_t rows = (int64_t)s.T_q * (s.H / s.H_kv);
-    p.few_q = s.dtype == PSA_F32 || (rows / 128 + s.B) * s.H_kv < 512;
-    p.few_k = s.dtype == PSA_F32 || (int64_t)(s.T_k / 128 + s.B) * s.H_kv < 512;
+    // enough work-groups of 128 for every compute unit?  (bfloat16, 128 | 32: dQ of 24 ragged clips of 435 frames, 374 work-groups, 20.5 |
+    // 25.3 us, of 2 clips, 32 of them, 15 | 7.5; dK and dV, whose work-groups differ more in length, at 210 of them 48 | 26 us, at 280
+    // 36.9 | 31.4, at 320 23.6 | 28.9; float32 alike: 210: 168 | 107 us)
+    p.few_q = (rows / 128 + s.B) * s.H_kv < 256;
+    p.few_k = (int64_t)(s.T_k / 128 + s.B) * s.H_kv < 300;
     p.n_qtile = (int)(rows / (p.few_q ? 32 : 128)) + s.B;
     p.n_ktile = s.T_k / (p.few_k ? 32 : 128) + s.B;
     p.total = 2 * (((size_t)s.T_q * s.H * sizeof(float) + 255) & ~(size_t)255);
@@ -422,10 +414,10 @@ static void packed_bwd_go(const PackedBwdPlan& p, const psa_packed_shape_t& s, c
     constexpr int rows = 256 / (64 / kVec<T>);
     packed_stats_kernel<T><<<(unsigned)(((int64_t)s.T_q * s.H + rows - 1) / rows), 256, 0, stream>>>(
         heads_of<const T>(out), heads_of<const T>(dOut), lse, heads_of<T>(dQ), pk, s.H, stat_l, stat_d);
-    (p.few_k ? packed_dkv_few_kernel<T> : packed_dkv_kernel<T>)<<<(unsigned)(p.n_ktile * s.H_kv), 256, 0, stream>>>(
+    (p.few_k ? packed_dkv_few_kernel<T> : packed_dkv_kernel<T, sizeof(T) == 4 ? 32 : 64>)<<<(unsigned)(p.n_ktile * s.H_kv), 256, 0, stream>>>(
         heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), heads_of<const T>(dOut), stat_l, stat_d, pk,
         heads_of<T>(dK), heads_of<T>(dV), s.H_kv, s.causal, scale, scale_log2, p.n_ktile);
-    (p.few_q ? packed_dq_few_kernel<T> : packed_dq_kernel<T>)<<<(unsigned)(p.n_qtile * s.H_kv), 256, 0, stream>>>(
+    (p.few_q ? packed_dq_few_kernel<T> : packed_dq_kernel<T, sizeof(T) == 4 ? 32 : 64>)<<<(unsigned)(p.n_qtile * s.H_kv), 256, 0, stream>>>(
         heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), heads_of<const T>(dOut), stat_l, stat_d, pk,
         heads_of<T>(dQ), s.H_kv, s.causal, scale, scale_log2);
 }
