@@ -167,7 +167,7 @@ const char* project_route_name(const psa_shape_t& s, int n_mat);         // the 
 // Layer norm (psa_norm.hip): tpr threads with nv vectors of 16 bytes for a row, nv = 0 for rows too long to keep;
 // n_part partial rows of the weights' gradients.
 struct NormPlan { int tpr, nv, n_part; size_t off_part, total; };
-NormPlan make_norm_plan(int64_t rows, int cols, int dtype);
+NormPlan make_norm_plan(int64_t rows, int cols, int dtype, bool forward);
 hipError_t launch_norm_fwd(const NormPlan& p, const void* X, const void* gamma, const void* beta, float eps, void* Y, float* mean,
                            float* rstd, int64_t rows, int cols, int dtype, hipStream_t stream);
 hipError_t launch_norm_bwd(const NormPlan& p, const void* dY, const void* X, const void* gamma, const float* mean, const float* rstd,

@@ -126,13 +126,13 @@ int probsparse_layer_norm_fwd(const void* X, const void* gamma, const void* beta
     if (rc != PSA_OK) return rc;
     if (!(eps >= 0.0) || !isfinite((float)eps)) return PSA_ERR_ARG;
     if (off_by(X, 16) || off_by(Y, 16) || off_by(gamma, 16) || off_by(beta, 16) || off_by(mean, 4) || off_by(rstd, 4)) return PSA_ERR_ALIGN;
-    return launch_norm_fwd(make_norm_plan(rows, cols, dtype), X, gamma, beta, (float)eps, Y, mean, rstd, rows, cols, dtype,
+    return launch_norm_fwd(make_norm_plan(rows, cols, dtype, true), X, gamma, beta, (float)eps, Y, mean, rstd, rows, cols, dtype,
                            static_cast<hipStream_t>(stream)) == hipSuccess ? PSA_OK : PSA_ERR_HIP;
 }
 
 size_t probsparse_layer_norm_bwd_workspace_bytes(int64_t rows, int32_t cols, int32_t dtype)
 {
-    return psa::check_norm(rows, cols, dtype) == PSA_OK ? psa::make_norm_plan(rows, cols, dtype).total : 0;
+    return psa::check_norm(rows, cols, dtype) == PSA_OK ? psa::make_norm_plan(rows, cols, dtype, false).total : 0;
 }
 
 int probsparse_layer_norm_bwd(const void* dY, const void* X, const void* gamma, const float* mean, const float* rstd, void* dX,
@@ -145,7 +145,7 @@ int probsparse_layer_norm_bwd(const void* dY, const void* X, const void* gamma, 
     if (rc != PSA_OK) return rc;
     if (off_by(dY, 16) || off_by(X, 16) || off_by(gamma, 16) || off_by(dX, 16) || off_by(mean, 4) || off_by(rstd, 4) ||
         off_by(dgamma, 4) || off_by(dbeta, 4) || off_by(workspace, 256)) return PSA_ERR_ALIGN;
-    const NormPlan p = make_norm_plan(rows, cols, dtype);
+    const NormPlan p = make_norm_plan(rows, cols, dtype, false);
     if (workspace_bytes < p.total) return PSA_ERR_WORKSPACE;
     return launch_norm_bwd(p, dY, X, gamma, mean, rstd, dX, dgamma, dbeta, rows, cols, dtype, workspace,
                            static_cast<hipStream_t>(stream)) == hipSuccess ? PSA_OK : PSA_ERR_HIP;

@@ -72,9 +72,9 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
     __shared__ int s_bad[2][4];
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
-    zero_outside(out, p.qo, p.B, p.Tq, hk * p.G, p.G, x, n_tile, [&](int head, int row) { if (lse) lse[(int64_t)head * p.Tq + row] = -INFINITY; });
     const SeqTile f = find_tile<128, false>(p, x);
-    if (f.tile < 0) return;
+    auto outside = [&] { zero_outside(out, p.qo, p.B, p.Tq, hk * p.G, p.G, x, n_tile, [&](int head, int row) { if (lse) lse[(int64_t)head * p.Tq + row] = -INFINITY; }); };
+    if (f.tile < 0) { outside(); return; }
 
     const int n_rows = f.nq * p.G;
     const int shift = f.nk - f.nq + 1;                 // causal: query t sees the first t + shift keys
@@ -151,6 +151,7 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
         if (look && (s_bad[buf][0] | s_bad[buf][1] | s_bad[buf][2] | s_bad[buf][3]))
             acc.add_nonfinite(Vh + j0 * V.row, V.row, min(KT, f.nk - j0), n_vis - j0, h);
     }
+    outside();                                         // (last: its loads would delay the others)
     if (row >= n_rows) return;
     float l = acc.l + swap_half(acc.l);
     if (n_vis == 0) { l = 0.f; clear(acc.o[0]); clear(acc.o[1]); }
@@ -175,10 +176,11 @@ void packed_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pac
     __shared__ float s_m[4][32], s_l[4][32];
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv, split = blockIdx.y;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
-    if (split == 0)
-        zero_outside(out, p.qo, p.B, p.Tq, hk * p.G, p.G, x, n_tile, [&](int head, int row) { if (lse) lse[(int64_t)head * p.Tq + row] = -INFINITY; });
     const SeqTile f = find_tile<32, false>(p, x);
-    if (f.tile < 0) return;
+    auto outside = [&] {
+        if (split == 0) zero_outside(out, p.qo, p.B, p.Tq, hk * p.G, p.G, x, n_tile, [&](int head, int row) { if (lse) lse[(int64_t)head * p.Tq + row] = -INFINITY; });
+    };
+    if (f.tile < 0) { outside(); return; }
     const int n_rows = f.nq * p.G;
     const int shift = f.nk - f.nq + 1;
     auto visible = [&](int r) { const int t = r / p.G; return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
@@ -243,6 +245,7 @@ void packed_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pac
         accumulate<T, 32>(acc.o, sV, 0, s[0], c, h);
         if (any) acc.add_nonfinite(Vh + j0 * V.row, V.row, min(32, f.nk - j0), n_vis - j0, h);
     }
+    outside();                                         // (last: its loads would delay the others)
     // join: wave w's sums of row r at join[w][r]; a wave that saw no key has m = kMaxInit and sums of 0
     __syncthreads();
     float* join = reinterpret_cast<float*>(lds);
@@ -347,10 +350,12 @@ PackedPlan make_packed_plan(const psa_packed_shape_t& s)
     p.n_tile = (int)(rows / p.rows) + s.B;
     p.n_split = 1;
     if (p.few) {
-        // splits: until there are 4 work-groups to a compute unit, each with a round of its 4 waves at the least (by the mean length)
-        const int64_t wgs = (int64_t)p.n_tile * s.H_kv;
-        int64_t split = (1024 + wgs - 1) / wgs;
-        const int64_t most = ((int64_t)s.T_k / s.B + 127) / 128;
+        // splits: until there are 3 work-groups to a compute unit, each with a round of its 4 waves at the least (by the mean length);
+        // none for short sequences, where joining them costs more (4 us).  32 streams of 1 .. 4096 keys, 256 | 512 | 768 | 1024 | 2048
+        // work-groups: 15.2 | 13.3 | 11.9 | 12.2 | 12.8 us; 64 of 100 .. 500: 8.6 unsplit, 8.8 and more with the join on top
+        const int64_t wgs = (int64_t)p.n_tile * s.H_kv, mean = (int64_t)s.T_k / s.B;
+        int64_t split = (768 + wgs - 1) / wgs;
+        const int64_t most = mean <= 768 ? 1 : (mean + 127) / 128;
         if (split > most) split = most;
         if (split > 64) split = 64;
         p.n_split = (int)(split < 1 ? 1 : split);

@@ -2,14 +2,14 @@
 // p f_i (or back, in the backward), all heads of Q and K in one launch.
 //
 // Bound by memory: every element is read and written once.  The angle does not depend on the head, so a work-group takes
-// kRows rows of one batch item, forms their cosines and sines once in LDS (a product and a reduction in float64, which
+// up to 16 rows of one batch item, forms their cosines and sines once in LDS (a product and a reduction in float64, which
 // keeps a far position exact to float32, and one sine and cosine) and applies them to all heads.
 #include "psa_vec.h"
 
 namespace psa {
 
 constexpr int kRotaryThreads = 256;
-constexpr int kRotaryRows = 16;
+constexpr int kRotaryRows = 16;             // at the most
 
 struct RotaryTurns { double f[32]; };          // turns (of 2 pi) per position of each pair
 
@@ -21,13 +21,13 @@ struct RotaryHeads { const T* in; T* out; int64_t in_b, in_h, in_l, out_b, out_h
 template <typename T, int LAYOUT, bool WIDE>
 __global__ __launch_bounds__(kRotaryThreads)
 void rotary_kernel(RotaryHeads<T> q, RotaryHeads<T> k, RotaryTurns turns, const int* __restrict__ positions, int64_t positions_stride,
-                   int first, int dim, float magnitude, int L)
+                   int first, int dim, float magnitude, int L, int per)
 {
     constexpr int VEC = kVec<T>;
     __shared__ float2 cs[kRotaryRows][32];
     const int b = blockIdx.y;
-    const int l0 = blockIdx.x * kRotaryRows;
-    const int rows = min(kRotaryRows, L - l0);
+    const int l0 = blockIdx.x * per;
+    const int rows = min(per, L - l0);
     const int half = dim / 2;
     for (int i = threadIdx.x; i < rows * 32; i += kRotaryThreads) {
         const int r = i >> 5, p = i & 31;
@@ -123,14 +123,17 @@ static void rotary_go(const psa_heads_t* Q, const psa_heads_t* K, int H_kv, cons
     for (int i = 0; i < o.dim / 2; ++i) turns.f[i] = (back ? -freq[i] : freq[i]) * 0.15915494309189533577;
     const auto q = rotary_heads<T>(Q, Qo, s.H);
     const auto k = rotary_heads<T>(K, Ko, H_kv);
-    const dim3 grid((unsigned)((s.L_K + kRotaryRows - 1) / kRotaryRows), (unsigned)s.B);
+    // rows to a work-group: 16, or fewer where there would not be two work-groups to a compute unit (B=1, L=333, 6 heads: 6.7 -> 3.7 us)
+    int per = kRotaryRows;
+    while (per > 1 && (int64_t)s.B * ((s.L_K + per - 1) / per) < 512) per /= 2;
+    const dim3 grid((unsigned)((s.L_K + per - 1) / per), (unsigned)s.B);
     const bool half = o.layout == PSA_ROTARY_HALF;
     const bool wide = (half ? o.dim / 2 : o.dim) % kVec<T> == 0;
     const float mag = (float)o.magnitude;
-    if (half && wide) rotary_kernel<T, PSA_ROTARY_HALF, true><<<grid, kRotaryThreads, 0, stream>>>(q, k, turns, positions, positions_stride, first, o.dim, mag, s.L_K);
-    else if (half) rotary_kernel<T, PSA_ROTARY_HALF, false><<<grid, kRotaryThreads, 0, stream>>>(q, k, turns, positions, positions_stride, first, o.dim, mag, s.L_K);
-    else if (wide) rotary_kernel<T, PSA_ROTARY_INTERLEAVED, true><<<grid, kRotaryThreads, 0, stream>>>(q, k, turns, positions, positions_stride, first, o.dim, mag, s.L_K);
-    else rotary_kernel<T, PSA_ROTARY_INTERLEAVED, false><<<grid, kRotaryThreads, 0, stream>>>(q, k, turns, positions, positions_stride, first, o.dim, mag, s.L_K);
+    if (half && wide) rotary_kernel<T, PSA_ROTARY_HALF, true><<<grid, kRotaryThreads, 0, stream>>>(q, k, turns, positions, positions_stride, first, o.dim, mag, s.L_K, per);
+    else if (half) rotary_kernel<T, PSA_ROTARY_HALF, false><<<grid, kRotaryThreads, 0, stream>>>(q, k, turns, positions, positions_stride, first, o.dim, mag, s.L_K, per);
+    else if (wide) rotary_kernel<T, PSA_ROTARY_INTERLEAVED, true><<<grid, kRotaryThreads, 0, stream>>>(q, k, turns, positions, positions_stride, first, o.dim, mag, s.L_K, per);
+    else rotary_kernel<T, PSA_ROTARY_INTERLEAVED, false><<<grid, kRotaryThreads, 0, stream>>>(q, k, turns, positions, positions_stride, first, o.dim, mag, s.L_K, per);
 }
 hipError_t launch_rotary(const psa_heads_t* Q, const psa_heads_t* K, int H_kv, const psa_rotary_t& o, const double* freq, bool back,
                          const int* positions, int64_t positions_stride, int first, const psa_heads_t* Qo, const psa_heads_t* Ko,
