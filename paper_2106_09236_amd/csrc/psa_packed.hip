@@ -59,17 +59,22 @@ struct Rows32 {
 // cycles, the matrix unit 38 %) and, in long runs, by power: 16384 causal, 8 heads, 350 us at first (785 TFLOP/s), 390 when hot.  What
 // did not help: 64 rows to a wave (half the LDS reads, 2 waves to a SIMD: 530 us), 4 waves to a SIMD with 32 keys at a time
 // (430), the scores of a step formed between the weights of the one before (440), priorities (no change).
-template <typename T, int KT>
-__global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3)
+//
+// KW = 2 (float32): 8 waves, two to 32 rows, which take alternate tiles of KT keys and join their sums in LDS; see packed_halves().
+template <typename T, int KT, int KW>
+__global__ __launch_bounds__(256 * KW, sizeof(T) == 4 ? 2 : 3)
 void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Packing p, Heads<T> out, float* __restrict__ lse,
                         int H_kv, int causal, float scale, int n_tile)
 {
     constexpr int CH = 64 * sizeof(T) / 16;            // 16-byte chunks of a row
-    constexpr int NL = KT * CH / 256;                  // of a tile, to a thread
+    constexpr int NT = 256 * KW, TILE = KT * KW;       // threads; keys between barriers
+    constexpr int NL = TILE * CH / NT;                 // chunks of a tile, to a thread
     constexpr int NS = KT / 32;
-    constexpr int kBytes = kTileBytes<T, KT>;
-    __shared__ __attribute__((aligned(16))) unsigned char sK[2][kBytes], sV[2][kBytes];
-    __shared__ int s_bad[2][4];
+    constexpr int kBytes = kTileBytes<T, TILE>;
+    static_assert(KW == 1 || 4 * kBytes >= 128 * (kJoinRow + 2) * 4, "the join of 128 rows does not fit the tiles");
+    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kBytes];
+    __shared__ int s_bad[2][4 * KW];
+    unsigned char *const sK = lds, *const sV = lds + 2 * kBytes;
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
     const SeqTile f = find_tile<128, false>(p, x);
@@ -79,7 +84,8 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
     const int n_rows = f.nq * p.G;
     const int shift = f.nk - f.nq + 1;                 // causal: query t sees the first t + shift keys
     auto visible = [&](int r) { const int t = r / p.G; return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
-    const int row0 = f.tile * 128 + wave * 32;
+    const int rw = wave & 3, kg = KW == 1 ? 0 : wave >> 2;         // which rows, which keys
+    const int row0 = f.tile * 128 + rw * 32;
     const int row = row0 + c, rc = min(row, n_rows - 1);
     const int t = rc / p.G, head = hk * p.G + (rc - t * p.G);
     const int n_vis = visible(rc);
@@ -95,13 +101,13 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
     int k_ofs[NL], v_ofs[NL];
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-        const int id = i * 256 + tid, r = id / CH, ch = id % CH;
+        const int id = i * NT + tid, r = id / CH, ch = id % CH;
         k_ofs[i] = (int)(r * K.row * (int64_t)sizeof(T)) + ch * 16;
         v_ofs[i] = (int)(r * V.row * (int64_t)sizeof(T)) + ch * 16;
     }
     uint4 kr[NL], vr[NL];
     auto fetch = [&](int j0) {
-        const int n = min(KT, f.nk - j0);
+        const int n = min(TILE, f.nk - j0);
         const auto kb = tile_rows(Kh + j0 * K.row, K.row, n), vb = tile_rows(Vh + j0 * V.row, V.row, n);
 #pragma unroll
         for (int i = 0; i < NL; ++i) { kr[i] = buffer_load16<uint4>(kb, k_ofs[i]); vr[i] = buffer_load16<uint4>(vb, v_ofs[i]); }
@@ -110,10 +116,10 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
     acc.init();
     if (n_all > 0) fetch(0);
     int buf = 0;
-    for (int j0 = 0; j0 < n_all; j0 += KT, buf ^= 1) {
+    for (int j0 = 0; j0 < n_all; j0 += TILE, buf ^= 1) {
         // a weight of 0 does not keep an infinity or NaN of a value that a row does not see out of its sum: in tiles that
         // some row sees in part they are left out and added afterwards (float32: in all, since an infinity has no parts)
-        const bool look = sizeof(T) == 4 || j0 + KT > n_every;
+        const bool look = sizeof(T) == 4 || j0 + TILE > n_every;
         if (look) {
             bool bad = false;
 #pragma unroll
@@ -126,34 +132,58 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
         }
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            const int id = i * 256 + tid;
-            put<KT>(sK[buf], id / CH, id % CH, kr[i], T{});
-            put<KT>(sV[buf], id / CH, id % CH, vr[i], T{});
+            const int id = i * NT + tid;
+            put<TILE>(sK + buf * kBytes, id / CH, id % CH, kr[i], T{});
+            put<TILE>(sV + buf * kBytes, id / CH, id % CH, vr[i], T{});
         }
-        if (j0 + KT < n_all) fetch(j0 + KT);
+        if (j0 + TILE < n_all) fetch(j0 + TILE);
         lds_barrier();
-        if (j0 >= n_wave) continue;
+        const int j = j0 + kg * KT;
+        if (j >= n_wave) continue;
         floatx16 s[NS];
 #pragma unroll
-        for (int n = 0; n < NS; ++n) s[n] = product<T, KT>(sK[buf], 32 * n, q, c, h);
-        if (j0 + KT > n_wave_every) {
+        for (int n = 0; n < NS; ++n) s[n] = product<T, TILE>(sK + buf * kBytes, kg * KT + 32 * n, q, c, h);
+        if (j + KT > n_wave_every) {
 #pragma unroll
             for (int n = 0; n < NS; ++n)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[n][r] = j0 + 32 * n + acc_row(r, h) < n_vis ? s[n][r] : -INFINITY;
+                for (int r = 0; r < 16; ++r) s[n][r] = j + 32 * n + acc_row(r, h) < n_vis ? s[n][r] : -INFINITY;
         }
         acc.follow(s, scale);
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
             acc.weights(s[n], scale);
-            accumulate<T, KT>(acc.o, sV[buf], 32 * n, s[n], c, h);
+            accumulate<T, TILE>(acc.o, sV + buf * kBytes, kg * KT + 32 * n, s[n], c, h);
         }
-        if (look && (s_bad[buf][0] | s_bad[buf][1] | s_bad[buf][2] | s_bad[buf][3]))
-            acc.add_nonfinite(Vh + j0 * V.row, V.row, min(KT, f.nk - j0), n_vis - j0, h);
+        if (look) {
+            int any = 0;
+#pragma unroll
+            for (int w = 0; w < 4 * KW; ++w) any |= s_bad[buf][w];
+            if (any) acc.add_nonfinite(Vh + j * V.row, V.row, min(KT, f.nk - j), n_vis - j, h);
+        }
     }
     outside();                                         // (last: its loads would delay the others)
-    if (row >= n_rows) return;
     float l = acc.l + swap_half(acc.l);
+    if (KW == 2) {
+        float* join = reinterpret_cast<float*>(lds) + (rw * 32 + c) * kJoinRow;
+        float* join_ml = reinterpret_cast<float*>(lds) + 128 * kJoinRow + (rw * 32 + c) * 2;
+        __syncthreads();
+        if (kg == 1) {
+            store_row(join, acc.o, 1.f, h);
+            if (h == 0) { join_ml[0] = acc.m; join_ml[1] = l; }
+        }
+        __syncthreads();
+        if (kg == 1) return;
+        const float m1 = join_ml[0], l1 = join_ml[1], m = fmaxf(acc.m, m1);
+        const float a0 = fast_exp2(acc.m - m), a1 = fast_exp2(m1 - m);
+        l = l * a0 + l1 * a1;
+        acc.m = m;
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc.o[dt][r] = acc.o[dt][r] * a0 + join[32 * dt + acc_row(r, h)] * a1;
+    }
+    if (row >= n_rows) return;
     if (n_vis == 0) { l = 0.f; clear(acc.o[0]); clear(acc.o[1]); }
     store_row(out.at(head, f.q0 + t), acc.o, l != 0.f ? 1.f / l : 0.f, h);
     if (lse && h == 0) lse[(int64_t)head * p.Tq + f.q0 + t] = n_vis > 0 ? acc.m * kLn2 + logf(l) : -INFINITY;
@@ -338,6 +368,13 @@ void packed_merge_kernel(const float* __restrict__ part_o, const float2* __restr
     if (lse && e == 0) lse[(int64_t)head * p.Tq + t] = sum == 0.f ? -INFINITY : m * kLn2 + logf(sum);
 }
 
+// float32, two waves to 32 rows?  One work-group of them fills a compute unit, and a wave's chain of steps is half as long: for calls
+// with few work-groups (`wide` of 128 rows) and long sequences.  1 | 2 waves, forward: 16 x 512 (4 heads, 320 work-groups) 41 | 35 us, 24
+// ragged clips of 435 causal (374) 55 | 41, 8 x 1000 causal (8 heads, 531) 83 | 77; but 32 of 40 .. 500 (400) 50 | 54, 64 of 450 (1120)
+// 135 | 154, 8 x 2048 causal (8 heads, 1088) 240 | 246.  dQ alike.  (bfloat16, which has two work-groups of 4 waves to a unit: 32 ragged
+// clips 17.6 | 21.6, 8 x 2048 64 | 83.)
+bool packed_halves(const psa_packed_shape_t& s, int64_t wide) { return s.dtype == PSA_F32 && wide < 640 && s.T_k / s.B >= 400; }
+
 // Few rows or many?  A wave owns 32 rows either way.  Work-groups of 128 rows read K and V a quarter as often but leave waves idle
 // in sequences of fewer rows, and there must be enough of them.
 PackedPlan make_packed_plan(const psa_packed_shape_t& s)
@@ -346,6 +383,7 @@ PackedPlan make_packed_plan(const psa_packed_shape_t& s)
     const int64_t rows = (int64_t)s.T_q * (s.H / s.H_kv);
     const int64_t wide = (rows / 128 + s.B) * s.H_kv;
     p.few = rows / s.B <= 64 || wide < 256;
+    p.halves = !p.few && packed_halves(s, wide);
     p.rows = p.few ? 32 : 128;
     p.n_tile = (int)(rows / p.rows) + s.B;
     p.n_split = 1;
@@ -377,8 +415,9 @@ static void packed_go(const PackedPlan& p, const psa_packed_shape_t& s, const ps
     const float scale = (float)(s.scale * 1.4426950408889634);
     const dim3 grid((unsigned)(p.n_tile * s.H_kv), (unsigned)p.n_split);
     if (!p.few) {
-        packed_rows_kernel<T, KT><<<grid, 256, 0, stream>>>(heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), pk, heads_of<T>(out),
-                                                            lse, s.H_kv, s.causal, scale, p.n_tile);
+        constexpr int KW = sizeof(T) == 4 ? 2 : 1;
+        (p.halves ? packed_rows_kernel<T, KT, KW> : packed_rows_kernel<T, KT, 1>)<<<grid, p.halves ? 512 : 256, 0, stream>>>(
+            heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), pk, heads_of<T>(out), lse, s.H_kv, s.causal, scale, p.n_tile);
         return;
     }
     float2* part_ml = static_cast<float2*>(workspace);

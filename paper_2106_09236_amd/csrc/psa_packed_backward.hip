@@ -132,14 +132,17 @@ void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Hea
 }
 
 // dQ of 128 rows: 4 waves of 32, tiles of 32 keys and values through LDS.
-template <typename T, int KT>
-__global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3)
+template <typename T, int KT, int KW>
+__global__ __launch_bounds__(256 * KW, sizeof(T) == 4 ? 2 : 3)
 void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, const float* __restrict__ stat_l,
                       const float* __restrict__ stat_d, Packing p, Heads<T> dQ, int H_kv, int causal, float scale, float scale_log2)
 {
-    constexpr int CH = 64 * sizeof(T) / 16, NL = KT * CH / 256;
-    constexpr int kBytes = kTileBytes<T, KT>;
-    __shared__ __attribute__((aligned(16))) unsigned char sK[2][kBytes], sV[2][kBytes];
+    constexpr int NT = 256 * KW, TILE = KT * KW;       // KW = 2: 8 waves, two to 32 rows, with alternate tiles of KT keys (as in the forward)
+    constexpr int CH = 64 * sizeof(T) / 16, NL = TILE * CH / NT;
+    constexpr int kBytes = kTileBytes<T, TILE>;
+    static_assert(KW == 1 || 4 * kBytes >= 128 * kJoinRow * 4, "the join of 128 rows does not fit the tiles");
+    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kBytes];
+    unsigned char *const sK = lds, *const sV = lds + 2 * kBytes;
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
     const SeqTile f = find_tile<128, false>(p, x);
@@ -147,7 +150,8 @@ void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Head
     const int n_rows = f.nq * p.G;
     const int shift = f.nk - f.nq + 1;
     auto visible = [&](int r) { const int t = r / p.G; return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
-    const int row0 = f.tile * 128 + wave * 32;
+    const int rw = wave & 3, kg = KW == 1 ? 0 : wave >> 2;
+    const int row0 = f.tile * 128 + rw * 32;
     const int row = row0 + c, rc = min(row, n_rows - 1);
     const int t = rc / p.G, head = hk * p.G + (rc - t * p.G);
     const int n_vis = visible(rc);
@@ -165,32 +169,32 @@ void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Head
     const T* Vh = V.at(hk, f.k0);
     uint4 kr[NL], vr[NL];
     auto fetch = [&](int j0) {
-        const int n = min(KT, f.nk - j0);
+        const int n = min(TILE, f.nk - j0);
         const auto kb = tile_rows(Kh + j0 * K.row, K.row, n), vb = tile_rows(Vh + j0 * V.row, V.row, n);
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            const int id = i * 256 + tid, r = id / CH, ch = id % CH;
+            const int id = i * NT + tid, r = id / CH, ch = id % CH;
             kr[i] = buffer_load16<uint4>(kb, (int)(r * K.row * (int64_t)sizeof(T)) + ch * 16);
             vr[i] = buffer_load16<uint4>(vb, (int)(r * V.row * (int64_t)sizeof(T)) + ch * 16);
         }
     };
     if (n_all > 0) fetch(0);
     int buf = 0;
-    for (int j0 = 0; j0 < n_all; j0 += KT, buf ^= 1) {
+    for (int j0 = 0; j0 < n_all; j0 += TILE, buf ^= 1) {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            const int id = i * 256 + tid;
-            put<KT>(sK[buf], id / CH, id % CH, kr[i], T{});
-            put<KT>(sV[buf], id / CH, id % CH, vr[i], T{});
+            const int id = i * NT + tid;
+            put<TILE>(sK + buf * kBytes, id / CH, id % CH, kr[i], T{});
+            put<TILE>(sV + buf * kBytes, id / CH, id % CH, vr[i], T{});
         }
-        if (j0 + KT < n_all) fetch(j0 + KT);
+        if (j0 + TILE < n_all) fetch(j0 + TILE);
         lds_barrier();
 #pragma unroll
         for (int n = 0; n < KT / 32; ++n) {
-            const int j = j0 + 32 * n;
+            const int in = kg * KT + 32 * n, j = j0 + in;
             if (j >= n_wave) break;
-            const floatx16 s = product<T, KT>(sK[buf], 32 * n, q, c, h);
-            floatx16 w = product<T, KT>(sV[buf], 32 * n, g, c, h);
+            const floatx16 s = product<T, TILE>(sK + buf * kBytes, in, q, c, h);
+            floatx16 w = product<T, TILE>(sV + buf * kBytes, in, g, c, h);
 #pragma unroll
             for (int r = 0; r < 16; ++r) w[r] = fast_exp2(fmaf(s[r], scale_log2, -l)) * (w[r] - d);
             if (j + 32 > n_every) {
@@ -198,8 +202,19 @@ void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Head
                 for (int r = 0; r < 16; ++r)
                     if (j + acc_row(r, h) >= n_vis) w[r] = 0.f;
             }
-            accumulate<T, KT>(dq, sK[buf], 32 * n, w, c, h);
+            accumulate<T, TILE>(dq, sK + buf * kBytes, in, w, c, h);
         }
+    }
+    if (KW == 2) {
+        float* join = reinterpret_cast<float*>(lds) + (rw * 32 + c) * kJoinRow;
+        __syncthreads();
+        if (kg == 1) store_row(join, dq, 1.f, h);
+        __syncthreads();
+        if (kg == 1) return;
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dq[dt][r] += join[32 * dt + acc_row(r, h)];
     }
     if (row >= n_rows) return;
     store_row(dQ.at(head, f.q0 + t), dq, scale, h);
@@ -395,7 +410,9 @@ PackedBwdPlan make_packed_bwd_plan(const psa_packed_shape_t& s)
     // enough work-groups of 128 for every compute unit?  (bfloat16, 128 | 32: dQ of 24 ragged clips of 435 frames, 374 work-groups, 20.5 |
     // 25.3 us, of 2 clips, 32 of them, 15 | 7.5; dK and dV, whose work-groups differ more in length, at 210 of them 48 | 26 us, at 280
     // 36.9 | 31.4, at 320 23.6 | 28.9; float32 alike: 210: 168 | 107 us)
-    p.few_q = (rows / 128 + s.B) * s.H_kv < 256;
+    const int64_t wide = (rows / 128 + s.B) * s.H_kv;
+    p.few_q = wide < 256;
+    p.halves_q = !p.few_q && packed_halves(s, wide);
     p.few_k = (int64_t)(s.T_k / 128 + s.B) * s.H_kv < 300;
     p.n_qtile = (int)(rows / (p.few_q ? 32 : 128)) + s.B;
     p.n_ktile = s.T_k / (p.few_k ? 32 : 128) + s.B;
@@ -417,7 +434,9 @@ static void packed_bwd_go(const PackedBwdPlan& p, const psa_packed_shape_t& s, c
     (p.few_k ? packed_dkv_few_kernel<T> : packed_dkv_kernel<T, sizeof(T) == 4 ? 32 : 64>)<<<(unsigned)(p.n_ktile * s.H_kv), 256, 0, stream>>>(
         heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), heads_of<const T>(dOut), stat_l, stat_d, pk,
         heads_of<T>(dK), heads_of<T>(dV), s.H_kv, s.causal, scale, scale_log2, p.n_ktile);
-    (p.few_q ? packed_dq_few_kernel<T> : packed_dq_kernel<T, sizeof(T) == 4 ? 32 : 64>)<<<(unsigned)(p.n_qtile * s.H_kv), 256, 0, stream>>>(
+    constexpr int KT = sizeof(T) == 4 ? 32 : 64, KW = sizeof(T) == 4 ? 2 : 1;
+    (p.few_q ? packed_dq_few_kernel<T> : p.halves_q ? packed_dq_kernel<T, KT, KW> : packed_dq_kernel<T, KT, 1>)<<<
+        (unsigned)(p.n_qtile * s.H_kv), p.halves_q ? 512 : 256, 0, stream>>>(
         heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), heads_of<const T>(dOut), stat_l, stat_d, pk,
         heads_of<T>(dQ), s.H_kv, s.causal, scale, scale_log2);
 }

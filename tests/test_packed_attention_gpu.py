@@ -72,7 +72,7 @@ def test_whole_sequences(H, H_kv, lens, by_frame, causal, dtype):
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("H,H_kv,q_lens,k_lens", [
     (128, 64, [127, 0, 5, 128, 129, 65, 300], [127, 0, 5, 128, 129, 65, 300]), (96, 32, [111, 222, 1, 90], [70, 222, 150, 0]),
-    (64, 64, [260, 255, 256, 1], [257, 300, 256, 33])])
+    (64, 64, [260, 255, 256, 1], [257, 300, 256, 33]), (32, 16, [500, 401, 390], [500, 401, 390]), (32, 32, [300, 1, 400], [700, 300, 401])])
 def test_many_heads(H, H_kv, q_lens, k_lens, causal, dtype):
     """Enough heads for work-groups of 128 rows (fewer leave the card idle, and rows are taken 32 at a time)."""
     _check(*_case(H, H_kv, q_lens, k_lens, dtype, by_frame=causal, front=3, behind=200), causal)
