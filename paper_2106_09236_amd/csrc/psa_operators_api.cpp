@@ -100,7 +100,7 @@ static int check_packed(const psa_packed_shape_t* s)
     if (s->B > (1 << 20) || s->H > 65535 || s->T_q > (1 << 28) || s->T_k > (1 << 28)) return PSA_ERR_SHAPE;
     if ((int64_t)s->T_q * (s->H / s->H_kv) > INT32_MAX - 65536) return PSA_ERR_SHAPE;
     // work-groups of a launch: tiles of 32 rows at the least
-    if (((int64_t)s->T_q * (s->H / s->H_kv) / 32 + s->T_k / 32 + s->B) * s->H_kv > INT32_MAX) return PSA_ERR_SHAPE;
+    if (((int64_t)s->T_q * (s->H / s->H_kv) / 32 + s->T_k / 32 + 2 * s->B) * s->H_kv > INT32_MAX) return PSA_ERR_SHAPE;
     if ((s->causal != 0 && s->causal != 1) || !positive(s->scale)) return PSA_ERR_ARG;
     return PSA_OK;
 }

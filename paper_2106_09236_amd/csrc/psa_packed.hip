@@ -388,11 +388,12 @@ PackedPlan make_packed_plan(const psa_packed_shape_t& s)
     p.n_tile = (int)(rows / p.rows) + s.B;
     p.n_split = 1;
     if (p.few) {
-        // splits: until there are 3 work-groups to a compute unit, each with a round of its 4 waves at the least (by the mean length);
-        // none for short sequences, where joining them costs more (4 us).  32 streams of 1 .. 4096 keys, 256 | 512 | 768 | 1024 | 2048
-        // work-groups: 15.2 | 13.3 | 11.9 | 12.2 | 12.8 us; 64 of 100 .. 500: 8.6 unsplit, 8.8 and more with the join on top
+        // splits: towards 3 work-groups to a compute unit, each with a round of its 4 waves at the least (by the mean length); none
+        // where every unit has a work-group or sequences are short, and joining them costs more (4 us and more with many rows).  32
+        // streams of 1 .. 4096 keys, 256 | 512 | 768 | 1024 | 2048 work-groups: 15.2 | 13.3 | 11.9 | 12.2 | 12.8 us; 64 of 100 .. 500:
+        // 8.6 unsplit, 8.8 and more with the join on top; 2000 causal, 8 heads, 512 work-groups: 2 splits 22.4 and 9.6 for the join
         const int64_t wgs = (int64_t)p.n_tile * s.H_kv, mean = (int64_t)s.T_k / s.B;
-        int64_t split = (768 + wgs - 1) / wgs;
+        int64_t split = wgs >= 256 ? 1 : 768 / wgs;
         const int64_t most = mean <= 768 ? 1 : (mean + 127) / 128;
         if (split > most) split = most;
         if (split > 64) split = 64;

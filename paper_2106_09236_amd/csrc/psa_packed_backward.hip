@@ -1,22 +1,44 @@
 // Dense attention over packed sequences, backward.  With p the weights, recomputed from Q, K and the forward's lse, G = dOut
 // and d_t = G[t].out[t]:
 //   ds_tj = p_tj (G[t].V[j] - d_t),  dQ[t] = scale sum_j ds_tj K[j],  dK[j] = scale sum_t ds_tj Q[t],  dV[j] = sum_t p_tj G[t]
-// Three launches: d_t and lse row by row (bound by memory); dK and dV with a work-group's keys held and the rows passing by;
-// dQ with the rows held and the keys passing by.  The scores and G.V are computed in both of the latter, seven products
+// Two launches: dQ with a work-group's rows held and the keys passing by, which also leaves d_t and lse where the other finds them;
+// dK and dV with the keys held and the rows passing by.  (Small calls take one launch for both, and one before it for d_t.)  The scores and G.V are computed in both of the latter, seven products
 // where five would do if dQ were added up in memory by atomics, whose order would change the result.
 #include "psa_packed.h"
 
 namespace psa {
 
-// lse (base 2; +infinity for a row that sees no key, whose weights then are 0) and d of every row, [H_kv][T_q * G] each.
+// lse in base 2; +infinity for a row that sees no key, whose weights then are 0
+__device__ __forceinline__ float stat_of(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+// Where a row's lse and d lie, [H_kv][T_q * G] each
+struct Stats {
+    float *l, *d;
+    const float* lse;
+    __device__ __forceinline__ static int64_t at(const Packing& p, int hk, int64_t row) { return (int64_t)hk * p.Tq * p.G + row; }
+};
+// Half of a row's d: a lane's 32 of its 64 products
+template <typename T>
+__device__ __forceinline__ float half_row_dot(const T* a, const T* b, int h)
+{
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 32 / kVec<T>; ++k) {
+        float x[kVec<T>], y[kVec<T>];
+        load_vec(x, a + 32 * h + k * kVec<T>, kVec<T>);
+        load_vec(y, b + 32 * h + k * kVec<T>, kVec<T>);
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) sum = fmaf(x[i], y[i], sum);
+    }
+    return sum;
+}
+
+// Both of every row, for calls whose two kernels run at once.
 template <typename T>
 __global__ __launch_bounds__(256, 2)
-void packed_stats_kernel(Heads<const T> out, Heads<const T> dOut, const float* __restrict__ lse, Heads<T> dQ, Packing p, int H,
+void packed_stats_kernel(Heads<const T> out, Heads<const T> dOut, const float* __restrict__ lse, Packing p, int H,
                          float* __restrict__ stat_l, float* __restrict__ stat_d)
 {
     constexpr int VEC = kVec<T>, CH = 64 / VEC;        // lanes of a row
-    const int n_wg = gridDim.x;
-    zero_outside(dQ, p.qo, p.B, p.Tq, 0, H, blockIdx.x, n_wg, [](int, int) {});
     const int64_t id = (int64_t)blockIdx.x * (256 / CH) + threadIdx.x / CH;
     if (id >= (int64_t)p.Tq * H) return;
     const int head = (int)(id / p.Tq), t = (int)(id % p.Tq), ch = threadIdx.x % CH;
@@ -29,8 +51,8 @@ void packed_stats_kernel(Heads<const T> out, Heads<const T> dOut, const float* _
     for (int k = 1; k < CH; k *= 2) sum += __shfl_xor(sum, k, 64);
     if (ch == 0) {
         const float l = lse[(int64_t)head * p.Tq + t];
-        const int64_t o = (int64_t)(head / p.G) * p.Tq * p.G + (int64_t)t * p.G + head % p.G;
-        stat_l[o] = l == -INFINITY ? INFINITY : l * kLog2e;
+        const int64_t o = Stats::at(p, head / p.G, (int64_t)t * p.G + head % p.G);
+        stat_l[o] = stat_of(l);
         stat_d[o] = sum;
     }
 }
@@ -48,10 +70,12 @@ void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Hea
     __shared__ __attribute__((aligned(16))) float sL[2][QT], sD[2][QT];
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
-    zero_outside(dK, p.ko, p.B, p.Tk, hk, 1, x, n_tile, [](int, int) {});
-    zero_outside(dV, p.ko, p.B, p.Tk, hk, 1, x, n_tile, [](int, int) {});
     const SeqTile f = find_tile<128, true>(p, x);
-    if (f.tile < 0) return;
+    auto outside = [&] {
+        zero_outside(dK, p.ko, p.B, p.Tk, hk, 1, x, n_tile, [](int, int) {});
+        zero_outside(dV, p.ko, p.B, p.Tk, hk, 1, x, n_tile, [](int, int) {});
+    };
+    if (f.tile < 0) { outside(); return; }
     const int n_rows = f.nq * p.G;
     const int shift = f.nk - f.nq + 1;
     // the first row that sees key j (rows are in the order of their queries)
@@ -126,6 +150,7 @@ void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Hea
             accumulate<T, QT>(dk, sQ[buf], 32 * n, w, c, h);
         }
     }
+    outside();
     if (key >= f.nk) return;
     store_row(dK.at(hk, f.k0 + key), dk, scale, h);
     store_row(dV.at(hk, f.k0 + key), dv, 1.f, h);
@@ -134,8 +159,8 @@ void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Hea
 // dQ of 128 rows: 4 waves of 32, tiles of 32 keys and values through LDS.
 template <typename T, int KT, int KW>
 __global__ __launch_bounds__(256 * KW, sizeof(T) == 4 ? 2 : 3)
-void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, const float* __restrict__ stat_l,
-                      const float* __restrict__ stat_d, Packing p, Heads<T> dQ, int H_kv, int causal, float scale, float scale_log2)
+void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, Heads<const T> out, Stats stats, Packing p,
+                      Heads<T> dQ, int H_kv, int causal, float scale, float scale_log2, int n_tile)
 {
     constexpr int NT = 256 * KW, TILE = KT * KW;       // KW = 2: 8 waves, two to 32 rows, with alternate tiles of KT keys (as in the forward)
     constexpr int CH = 64 * sizeof(T) / 16, NL = TILE * CH / NT;
@@ -146,7 +171,8 @@ void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Head
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
     const SeqTile f = find_tile<128, false>(p, x);
-    if (f.tile < 0) return;
+    auto outside = [&] { zero_outside(dQ, p.qo, p.B, p.Tq, hk * p.G, p.G, x, n_tile, [](int, int) {}); };
+    if (f.tile < 0) { outside(); return; }
     const int n_rows = f.nq * p.G;
     const int shift = f.nk - f.nq + 1;
     auto visible = [&](int r) { const int t = r / p.G; return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
@@ -161,8 +187,14 @@ void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Head
     HeadOperand<T> q, g;
     q.load(Q.at(head, f.q0 + t), h);
     g.load(dOut.at(head, f.q0 + t), h);
-    const int64_t so = ((int64_t)hk * p.Tq + f.q0) * p.G + rc;
-    const float l = stat_l[so], d = stat_d[so];
+    const float l = stat_of(stats.lse[(int64_t)head * p.Tq + f.q0 + t]);
+    float d = half_row_dot(out.at(head, f.q0 + t), dOut.at(head, f.q0 + t), h);
+    d += swap_half(d);
+    if (kg == 0 && h == 0 && row < n_rows) {
+        const int64_t so = Stats::at(p, hk, (int64_t)f.q0 * p.G + row);
+        stats.l[so] = l;
+        stats.d[so] = d;
+    }
     floatx16 dq[2];
     clear(dq[0]); clear(dq[1]);
     const T* Kh = K.at(hk, f.k0);
@@ -205,6 +237,7 @@ void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Head
             accumulate<T, TILE>(dq, sK + buf * kBytes, in, w, c, h);
         }
     }
+    outside();                                         // (last: its loads would delay the others)
     if (KW == 2) {
         float* join = reinterpret_cast<float*>(lds) + (rw * 32 + c) * kJoinRow;
         __syncthreads();
@@ -223,24 +256,26 @@ void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Head
 // ---- the same with 32 keys (rows) to a work-group, whose 4 waves divide the rows (keys) among themselves and join their sums in LDS at
 // the end.  Four times as many work-groups, each a quarter as long, no barrier before the join; a tile of rows is read by one wave
 // only, and 4 times as often.
+constexpr int kJoinBytes = 4 * 32 * kJoinRow * 4;
+template <typename T> constexpr int kDkvLds = (8 * kTileBytes<T, 32> > kJoinBytes ? 8 * kTileBytes<T, 32> : kJoinBytes) + 4 * 2 * 32 * 4;
+template <typename T> constexpr int kDqLds = 4 * kTileBytes<T, 32> > kJoinBytes ? 4 * kTileBytes<T, 32> : kJoinBytes;
 
 template <typename T>
-__global__ __launch_bounds__(256, 2)
-void packed_dkv_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, const float* __restrict__ stat_l,
-                           const float* __restrict__ stat_d, Packing p, Heads<T> dK, Heads<T> dV, int H_kv, int causal, float scale,
+__device__ __forceinline__
+void dkv_few(unsigned char* lds, int hk, int x, Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, const float* __restrict__ stat_l,
+                           const float* __restrict__ stat_d, const Packing& p, Heads<T> dK, Heads<T> dV, int causal, float scale,
                            float scale_log2, int n_tile)
 {
     constexpr int CH = 64 * sizeof(T) / 16, NL = 32 * CH / 64, RL = 64 / CH;       // lanes of a row, chunks of a lane, rows of one load
     constexpr int kBytes = kTileBytes<T, 32>;
-    constexpr int kJoinBytes = 4 * 32 * kJoinRow * 4;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[8 * kBytes > kJoinBytes ? 8 * kBytes : kJoinBytes];
-    __shared__ __attribute__((aligned(16))) float sL[4][32], sD[4][32];
-    const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
+    float(*const sL)[32] = reinterpret_cast<float(*)[32]>(lds + kDkvLds<T> - 4 * 2 * 32 * 4), (*const sD)[32] = sL + 4;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
-    zero_outside(dK, p.ko, p.B, p.Tk, hk, 1, x, n_tile, [](int, int) {});
-    zero_outside(dV, p.ko, p.B, p.Tk, hk, 1, x, n_tile, [](int, int) {});
     const SeqTile f = find_tile<32, true>(p, x);
-    if (f.tile < 0) return;
+    auto outside = [&] {
+        zero_outside(dK, p.ko, p.B, p.Tk, hk, 1, x, n_tile, [](int, int) {});
+        zero_outside(dV, p.ko, p.B, p.Tk, hk, 1, x, n_tile, [](int, int) {});
+    };
+    if (f.tile < 0) { outside(); return; }
     const int n_rows = f.nq * p.G;
     const int shift = f.nk - f.nq + 1;
     auto first_row = [&](int j) { return causal ? max(j - shift + 1, 0) * p.G : 0; };
@@ -313,6 +348,7 @@ void packed_dkv_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V,
         accumulate<T, 32>(dv, sG, 0, s, c, h);
         accumulate<T, 32>(dk, sQ, 0, w, c, h);
     }
+    outside();
     float* join = reinterpret_cast<float*>(lds);
     const int key = key0 + (tid >> 3), e = (tid & 7) * 8;
 #pragma unroll
@@ -326,19 +362,17 @@ void packed_dkv_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V,
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(256, 2)
-void packed_dq_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, const float* __restrict__ stat_l,
-                          const float* __restrict__ stat_d, Packing p, Heads<T> dQ, int H_kv, int causal, float scale, float scale_log2)
+template <typename T, bool FIND_STATS>
+__device__ __forceinline__
+void dq_few(unsigned char* lds, int hk, int x, Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, Heads<const T> out,
+            const Stats& stats, const Packing& p, Heads<T> dQ, int causal, float scale, float scale_log2, int n_tile)
 {
     constexpr int CH = 64 * sizeof(T) / 16, NL = 32 * CH / 64;
     constexpr int kBytes = kTileBytes<T, 32>;
-    constexpr int kJoinBytes = 4 * 32 * kJoinRow * 4;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kBytes > kJoinBytes ? 4 * kBytes : kJoinBytes];
-    const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
     const SeqTile f = find_tile<32, false>(p, x);
-    if (f.tile < 0) return;
+    auto outside = [&] { zero_outside(dQ, p.qo, p.B, p.Tq, hk * p.G, p.G, x, n_tile, [](int, int) {}); };
+    if (f.tile < 0) { outside(); return; }
     const int n_rows = f.nq * p.G;
     const int shift = f.nk - f.nq + 1;
     auto visible = [&](int r) { const int t = r / p.G; return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
@@ -350,8 +384,17 @@ void packed_dq_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, 
     HeadOperand<T> q, g;
     q.load(Q.at(head, f.q0 + t), h);
     g.load(dOut.at(head, f.q0 + t), h);
-    const int64_t so = ((int64_t)hk * p.Tq + f.q0) * p.G + rc;
-    const float l = stat_l[so], d = stat_d[so];
+    const int64_t so = Stats::at(p, hk, (int64_t)f.q0 * p.G + rc);
+    float l, d;
+    if (FIND_STATS) {
+        l = stat_of(stats.lse[(int64_t)head * p.Tq + f.q0 + t]);
+        d = half_row_dot(out.at(head, f.q0 + t), dOut.at(head, f.q0 + t), h);
+        d += swap_half(d);
+        if (wave == 0 && h == 0 && row0 + c < n_rows) { stats.l[so] = l; stats.d[so] = d; }
+    } else {
+        l = stats.l[so];
+        d = stats.d[so];
+    }
     floatx16 dq[2];
     clear(dq[0]); clear(dq[1]);
     const T* Kh = K.at(hk, f.k0);
@@ -391,6 +434,7 @@ void packed_dq_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, 
         }
         accumulate<T, 32>(dq, sK, 0, w, c, h);
     }
+    outside();
     __syncthreads();
     float* join = reinterpret_cast<float*>(lds);
     store_row(join + (wave * 32 + c) * kJoinRow, dq, 1.f, h);
@@ -401,6 +445,21 @@ void packed_dq_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, 
     join_columns(sum, join, tid);
     const int rt = row / p.G;
     store8(dQ.at(hk * p.G + (row - rt * p.G), f.q0 + rt) + (tid & 7) * 8, sum, scale);
+}
+
+// The first n_k work-groups form dK and dV, the others dQ: both or (n_k = 0, or as many as there are) one of them.  One launch where both take
+// few keys and rows: such calls leave the card idle, and the two do not depend on each other.
+template <typename T, bool DKV, bool DQ>
+__global__ __launch_bounds__(256, 2)
+void packed_grads_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, Heads<const T> out, Stats stats, Packing p,
+                             Heads<T> dQ, Heads<T> dK, Heads<T> dV, int H_kv, int causal, float scale, float scale_log2, int n_ktile, int n_qtile)
+{
+    __shared__ __attribute__((aligned(16))) unsigned char lds[DKV ? kDkvLds<T> : kDqLds<T>];
+    const int n_k = DKV ? n_ktile * H_kv : 0, id = (int)blockIdx.x;
+    if (DKV && (!DQ || id < n_k))
+        dkv_few<T>(lds, id % H_kv, id / H_kv, Q, K, V, dOut, stats.l, stats.d, p, dK, dV, causal, scale, scale_log2, n_ktile);
+    else if (DQ)
+        dq_few<T, !DKV>(lds, (id - n_k) % H_kv, (id - n_k) / H_kv, Q, K, V, dOut, out, stats, p, dQ, causal, scale, scale_log2, n_qtile);
 }
 
 PackedBwdPlan make_packed_bwd_plan(const psa_packed_shape_t& s)
@@ -425,20 +484,27 @@ static void packed_bwd_go(const PackedBwdPlan& p, const psa_packed_shape_t& s, c
                           const Packing& pk, const psa_heads_t& out, const float* lse, const psa_heads_t& dOut, const psa_heads_t& dQ,
                           const psa_heads_t& dK, const psa_heads_t& dV, void* workspace, hipStream_t stream)
 {
-    float* stat_l = static_cast<float*>(workspace);
-    float* stat_d = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.total / 2);
+    const Stats st{static_cast<float*>(workspace), reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.total / 2), lse};
     const float scale = (float)s.scale, scale_log2 = (float)(s.scale * 1.4426950408889634);
-    constexpr int rows = 256 / (64 / kVec<T>);
-    packed_stats_kernel<T><<<(unsigned)(((int64_t)s.T_q * s.H + rows - 1) / rows), 256, 0, stream>>>(
-        heads_of<const T>(out), heads_of<const T>(dOut), lse, heads_of<T>(dQ), pk, s.H, stat_l, stat_d);
-    (p.few_k ? packed_dkv_few_kernel<T> : packed_dkv_kernel<T, sizeof(T) == 4 ? 32 : 64>)<<<(unsigned)(p.n_ktile * s.H_kv), 256, 0, stream>>>(
-        heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), heads_of<const T>(dOut), stat_l, stat_d, pk,
-        heads_of<T>(dK), heads_of<T>(dV), s.H_kv, s.causal, scale, scale_log2, p.n_ktile);
+    const auto q = heads_of<const T>(Q), k = heads_of<const T>(K), v = heads_of<const T>(V), g = heads_of<const T>(dOut), o = heads_of<const T>(out);
+    const auto dq = heads_of<T>(dQ), dk = heads_of<T>(dK), dv = heads_of<T>(dV);
+    const unsigned n_k = (unsigned)(p.n_ktile * s.H_kv), n_q = (unsigned)(p.n_qtile * s.H_kv);
     constexpr int KT = sizeof(T) == 4 ? 32 : 64, KW = sizeof(T) == 4 ? 2 : 1;
-    (p.few_q ? packed_dq_few_kernel<T> : p.halves_q ? packed_dq_kernel<T, KT, KW> : packed_dq_kernel<T, KT, 1>)<<<
-        (unsigned)(p.n_qtile * s.H_kv), p.halves_q ? 512 : 256, 0, stream>>>(
-        heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), heads_of<const T>(dOut), stat_l, stat_d, pk,
-        heads_of<T>(dQ), s.H_kv, s.causal, scale, scale_log2);
+    if (p.few_k && p.few_q) {
+        constexpr int rows = 256 / (64 / kVec<T>);
+        packed_stats_kernel<T><<<(unsigned)(((int64_t)s.T_q * s.H + rows - 1) / rows), 256, 0, stream>>>(o, g, lse, pk, s.H, st.l, st.d);
+        packed_grads_few_kernel<T, true, true><<<n_k + n_q, 256, 0, stream>>>(q, k, v, g, o, st, pk, dq, dk, dv, s.H_kv, s.causal, scale, scale_log2, p.n_ktile, p.n_qtile);
+        return;
+    }
+    if (p.few_q)
+        packed_grads_few_kernel<T, false, true><<<n_q, 256, 0, stream>>>(q, k, v, g, o, st, pk, dq, dk, dv, s.H_kv, s.causal, scale, scale_log2, p.n_ktile, p.n_qtile);
+    else
+        (p.halves_q ? packed_dq_kernel<T, KT, KW> : packed_dq_kernel<T, KT, 1>)<<<n_q, p.halves_q ? 512 : 256, 0, stream>>>(
+            q, k, v, g, o, st, pk, dq, s.H_kv, s.causal, scale, scale_log2, p.n_qtile);
+    if (p.few_k)
+        packed_grads_few_kernel<T, true, false><<<n_k, 256, 0, stream>>>(q, k, v, g, o, st, pk, dq, dk, dv, s.H_kv, s.causal, scale, scale_log2, p.n_ktile, p.n_qtile);
+    else
+        packed_dkv_kernel<T, KT><<<n_k, 256, 0, stream>>>(q, k, v, g, st.l, st.d, pk, dk, dv, s.H_kv, s.causal, scale, scale_log2, p.n_ktile);
 }
 hipError_t launch_packed_bwd(const PackedBwdPlan& p, const psa_packed_shape_t& s, const psa_heads_t& Q, const psa_heads_t& K, const psa_heads_t& V,
                              const int* q_offsets, const int* k_offsets, const psa_heads_t& out, const float* lse, const psa_heads_t& dOut,
