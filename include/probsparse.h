@@ -373,8 +373,10 @@ int probsparse_rotary_bwd(const psa_heads_t* dQ_out, const psa_heads_t* dK_out, 
  *   Q, out    H heads of T_q rows;  K, V: H_kv heads of T_k rows; batch_stride is ignored
  *   lse       [H, T_q] float32 DEVICE, or NULL
  * Arithmetic: bfloat16 operands are multiplied exactly and summed in float32; the weights p are
- * rounded to bfloat16 before they are multiplied with V.  float32 operands are multiplied and
- * summed in float32.  Softmax statistics are float32. */
+ * rounded to bfloat16 before they are multiplied with V (calls with few rows: kept to 16 bits).
+ * float32 operands are multiplied as sums of three bfloat16 parts each (error 2^-23 of |a||b| at
+ * the most, 2^-25 as a rule) and summed in float32; an infinity has no such parts, so that one in
+ * Q or K makes the scores it takes part in NaN.  Softmax statistics are float32. */
 typedef struct psa_packed_shape {
     int32_t B, H, H_kv;           /* sequences; heads, H a multiple of H_kv */
     int32_t T_q, T_k;             /* rows of Q and of K and V; T_q * (H / H_kv) <= 2^31 - 2^16 */
@@ -393,7 +395,8 @@ int dense_attn_packed_fwd(const psa_heads_t* Q, const psa_heads_t* K, const psa_
  *   dQ[t] = scale * sum_j ds_tj K[j],  dK[j] = scale * sum_t ds_tj Q[t],  dV[j] = sum_t p_tj G[t]
  * the sums over t also over the query heads that share the key head.  Every element of dQ, dK
  * and dV is written; rows in no sequence get zeros.  p and ds are rounded to bfloat16 before
- * they are multiplied where the tensors are bfloat16.  The order of all sums is fixed.
+ * they are multiplied where the tensors are bfloat16 (calls with few rows or keys: kept to 16
+ * bits), and d is corrected for the rounding of out.  The order of all sums is fixed.
  * Infinities and NaN stay within the gradients of their own sequence. */
 size_t dense_attn_packed_bwd_workspace_bytes(const psa_packed_shape_t* shape);
 int dense_attn_packed_bwd(const psa_heads_t* Q, const psa_heads_t* K, const psa_heads_t* V,

@@ -335,20 +335,33 @@ __device__ __forceinline__ floatx16 product(const unsigned char* s, int row0, co
     return d;
 }
 
-// The column operand of a product over 16 rows (step st of 32), from what a lane has in accumulator order: w[8 st] .. w[8 st + 7].
-// bfloat16: rounded.
-__device__ __forceinline__ Operand<bf16_t> weight_operand(const floatx16& w, int st, bf16_t)
+// The column operands of a product over 16 rows (step st of 32), from what a lane has in accumulator order: w[8 st] .. w[8 st + 7].  bfloat16:
+// rounded, or (N = 2) in two parts of 16 bits and a sign each.  Rounded weights cost a result as much as its own rounding (1.4 times the
+// error with both); kernels that wait for memory or for each other rather than for the matrix unit take two parts.
+template <int N>
+__device__ __forceinline__ void weight_operand(Operand<bf16_t> (&b)[N], const floatx16& w, int st)
 {
-    return Operand<bf16_t>{{make_uint4(cvt_pk_bf16(w[8 * st], w[8 * st + 1]), cvt_pk_bf16(w[8 * st + 2], w[8 * st + 3]),
-                                       cvt_pk_bf16(w[8 * st + 4], w[8 * st + 5]), cvt_pk_bf16(w[8 * st + 6], w[8 * st + 7]))}};
+    if constexpr (N == 1) {
+        b[0].v[0] = make_uint4(cvt_pk_bf16(w[8 * st], w[8 * st + 1]), cvt_pk_bf16(w[8 * st + 2], w[8 * st + 3]),
+                               cvt_pk_bf16(w[8 * st + 4], w[8 * st + 5]), cvt_pk_bf16(w[8 * st + 6], w[8 * st + 7]));
+    } else {
+        uint32_t part[4][3];               // (the third parts are not used, and not computed)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) split_pair(w[8 * st + 2 * i], w[8 * st + 2 * i + 1], part[i]);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) b[n].v[0] = make_uint4(part[0][1 - n], part[1][1 - n], part[2][1 - n], part[3][1 - n]);      // the small one first
+    }
 }
-__device__ __forceinline__ Operand<float> weight_operand(const floatx16& w, int st, float)
+template <int N>
+__device__ __forceinline__ void weight_operand(Operand<float> (&b)[N], const floatx16& w, int st)
 {
     float x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = w[8 * st + i];
-    return operand(x);
+    b[0] = operand(x);
 }
+template <typename T, bool FINE> constexpr int kWeightParts = FINE && sizeof(T) == 2 ? 2 : 1;
+
 // D^T[e][col] += sum over 32 rows of the tile from row0 of X[row][e] w[row], w in accumulator order (row acc_row(r, h) in w[r]); D in two
 // accumulators of 32 elements e.  The tile's operand for 16 rows (step st) and 32 elements (dt) comes through the transposing LDS
 // read: of each group of 16 lanes, lane s points at row s / 4 of four rows, columns 4 (s % 4) .., and lane i receives column i of
@@ -370,14 +383,39 @@ __device__ __forceinline__ Operand<T> tile_transposed(const unsigned char* s, in
     }
     return a;
 }
-template <typename T, int ROWS>
+template <typename T, int ROWS, bool FINE>
 __device__ __forceinline__ void accumulate(floatx16 (&d)[2], const unsigned char* s, int row0, const floatx16& w, int c, int h)
 {
+    constexpr int N = kWeightParts<T, FINE>;
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
-        const Operand<T> b = weight_operand(w, st, T{});
+        Operand<T> b[N];
+        weight_operand(b, w, st);
 #pragma unroll
-        for (int dt = 0; dt < 2; ++dt) d[dt] = mfma(tile_transposed<T, ROWS>(s, row0, st, dt, c, h), b, d[dt]);
+        for (int dt = 0; dt < 2; ++dt) {
+            const Operand<T> a = tile_transposed<T, ROWS>(s, row0, st, dt, c, h);
+#pragma unroll
+            for (int n = 0; n < N; ++n) d[dt] = mfma(a, b[n], d[dt]);
+        }
+    }
+}
+// The same for a second set of weights at once (rounded)
+template <typename T, int ROWS, bool FINE>
+__device__ __forceinline__ void accumulate_two(floatx16 (&d)[2], const floatx16& w, floatx16 (&d2)[2], const floatx16& w2, const unsigned char* s, int row0, int c, int h)
+{
+    constexpr int N = kWeightParts<T, FINE>;
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+        Operand<T> b[N], b2[1];
+        weight_operand(b, w, st);
+        weight_operand(b2, w2, st);
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt) {
+            const Operand<T> a = tile_transposed<T, ROWS>(s, row0, st, dt, c, h);
+#pragma unroll
+            for (int n = 0; n < N; ++n) d[dt] = mfma(a, b[n], d[dt]);
+            d2[dt] = mfma(a, b2[0], d2[dt]);
+        }
     }
 }
 

@@ -153,7 +153,7 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
             acc.weights(s[n], scale);
-            accumulate<T, TILE>(acc.o, sV + buf * kBytes, kg * KT + 32 * n, s[n], c, h);
+            accumulate<T, TILE, false>(acc.o, sV + buf * kBytes, kg * KT + 32 * n, s[n], c, h);
         }
         if (look) {
             int any = 0;
@@ -272,7 +272,7 @@ void packed_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pac
         }
         acc.follow(s, scale);
         acc.weights(s[0], scale);
-        accumulate<T, 32>(acc.o, sV, 0, s[0], c, h);
+        accumulate<T, 32, true>(acc.o, sV, 0, s[0], c, h);
         if (any) acc.add_nonfinite(Vh + j0 * V.row, V.row, min(32, f.nk - j0), n_vis - j0, h);
     }
     outside();                                         // (last: its loads would delay the others)

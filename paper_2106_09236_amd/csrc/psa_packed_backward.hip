@@ -2,7 +2,7 @@
 // and d_t = G[t].out[t]:
 //   ds_tj = p_tj (G[t].V[j] - d_t),  dQ[t] = scale sum_j ds_tj K[j],  dK[j] = scale sum_t ds_tj Q[t],  dV[j] = sum_t p_tj G[t]
 // Two launches: dQ with a work-group's rows held and the keys passing by, which also leaves d_t and lse where the other finds them;
-// dK and dV with the keys held and the rows passing by.  (Small calls take one launch for both, and one before it for d_t.)  The scores and G.V are computed in both of the latter, seven products
+// dK and dV with the keys held and the rows passing by.  (Small calls of float32 take one launch for both, and one before it for d_t.)  The scores and G.V are computed in both of the latter, seven products
 // where five would do if dQ were added up in memory by atomics, whose order would change the result.
 #include "psa_packed.h"
 
@@ -32,7 +32,51 @@ __device__ __forceinline__ float half_row_dot(const T* a, const T* b, int h)
     return sum;
 }
 
-// Both of every row, for calls whose two kernels run at once.
+// What a wave keeps of dQ for 32 rows.  out has been rounded, so d formed from it is off by 2^-8 of its terms for bfloat16 tensors, more than
+// the rounding of dS where a few keys have the weight (dQ and dK then had twice the error of their own rounding).  But d is also
+// sum_j p_j (G.V[j]): with d0 the value from out, e = sum_j p_j (G.V[j] - d0) is what d0 is off by, and
+//     sum_j p_j (G.V[j] - d0 - e) K[j] = sum_j p_j (G.V[j] - d0) K[j] - e sum_j p_j K[j],
+// one product more (of weights rounded once: e is small) and d = d0 + e for dK.  float32 tensors need none of it.
+template <typename T> struct RowGradient;
+template <> struct RowGradient<float> {
+    floatx16 dq[2];
+    __device__ __forceinline__ void init() { clear(dq[0]); clear(dq[1]); }
+    static __device__ __forceinline__ void weights(floatx16& s, floatx16& w, float scale, float l, float d) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w[r] = fast_exp2(fmaf(s[r], scale, -l)) * (w[r] - d);
+    }
+    template <int ROWS, bool FINE>
+    __device__ __forceinline__ void add(const floatx16&, const floatx16& w, const unsigned char* k, int row0, int c, int h) { accumulate<float, ROWS, false>(dq, k, row0, w, c, h); }
+    __device__ __forceinline__ float finish() { return 0.f; }
+};
+template <> struct RowGradient<bf16_t> {
+    floatx16 dq[2], pk[2];
+    float e;
+    __device__ __forceinline__ void init() { clear(dq[0]); clear(dq[1]); clear(pk[0]); clear(pk[1]); e = 0.f; }
+    // s: scores to weights; w: G.V to dS
+    static __device__ __forceinline__ void weights(floatx16& s, floatx16& w, float scale, float l, float d) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) { s[r] = fast_exp2(fmaf(s[r], scale, -l)); w[r] = s[r] * (w[r] - d); }
+    }
+    template <int ROWS, bool FINE>
+    __device__ __forceinline__ void add(const floatx16& s, const floatx16& w, const unsigned char* k, int row0, int c, int h) {
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += w[r];
+        e += sum;
+        accumulate_two<bf16_t, ROWS, FINE>(dq, w, pk, s, k, row0, c, h);
+    }
+    __device__ __forceinline__ float finish() {
+        e += swap_half(e);
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dq[dt][r] = fmaf(-e, pk[dt][r], dq[dt][r]);
+        return e;
+    }
+};
+
+// Both of every row, for calls whose two kernels run at once (float32).
 template <typename T>
 __global__ __launch_bounds__(256, 2)
 void packed_stats_kernel(Heads<const T> out, Heads<const T> dOut, const float* __restrict__ lse, Packing p, int H,
@@ -141,13 +185,14 @@ void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Hea
                     w[4 * r4 + e] = s[4 * r4 + e] * (w[4 * r4 + e] - d[e]);
                 }
             }
+            if (f.nk == 1) clear(w);                   // (an only key)
             if (r < first_every) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (r + acc_row(i, h) < first) { s[i] = 0.f; w[i] = 0.f; }
             }
-            accumulate<T, QT>(dv, sG[buf], 32 * n, s, c, h);
-            accumulate<T, QT>(dk, sQ[buf], 32 * n, w, c, h);
+            accumulate<T, QT, false>(dv, sG[buf], 32 * n, s, c, h);
+            accumulate<T, QT, false>(dk, sQ[buf], 32 * n, w, c, h);
         }
     }
     outside();
@@ -158,7 +203,7 @@ void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Hea
 
 // dQ of 128 rows: 4 waves of 32, tiles of 32 keys and values through LDS.
 template <typename T, int KT, int KW>
-__global__ __launch_bounds__(256 * KW, sizeof(T) == 4 ? 2 : 3)
+__global__ __launch_bounds__(256 * KW, 2)
 void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, Heads<const T> out, Stats stats, Packing p,
                       Heads<T> dQ, int H_kv, int causal, float scale, float scale_log2, int n_tile)
 {
@@ -190,13 +235,8 @@ void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Head
     const float l = stat_of(stats.lse[(int64_t)head * p.Tq + f.q0 + t]);
     float d = half_row_dot(out.at(head, f.q0 + t), dOut.at(head, f.q0 + t), h);
     d += swap_half(d);
-    if (kg == 0 && h == 0 && row < n_rows) {
-        const int64_t so = Stats::at(p, hk, (int64_t)f.q0 * p.G + row);
-        stats.l[so] = l;
-        stats.d[so] = d;
-    }
-    floatx16 dq[2];
-    clear(dq[0]); clear(dq[1]);
+    RowGradient<T> grad;
+    grad.init();
     const T* Kh = K.at(hk, f.k0);
     const T* Vh = V.at(hk, f.k0);
     uint4 kr[NL], vr[NL];
@@ -225,32 +265,39 @@ void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Head
         for (int n = 0; n < KT / 32; ++n) {
             const int in = kg * KT + 32 * n, j = j0 + in;
             if (j >= n_wave) break;
-            const floatx16 s = product<T, TILE>(sK + buf * kBytes, in, q, c, h);
+            floatx16 s = product<T, TILE>(sK + buf * kBytes, in, q, c, h);
             floatx16 w = product<T, TILE>(sV + buf * kBytes, in, g, c, h);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) w[r] = fast_exp2(fmaf(s[r], scale_log2, -l)) * (w[r] - d);
+            grad.weights(s, w, scale_log2, l, d);
             if (j + 32 > n_every) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (j + acc_row(r, h) >= n_vis) w[r] = 0.f;
+                for (int r = 0; r < 16; ++r) {
+                    if (j + acc_row(r, h) >= n_vis) s[r] = w[r] = 0.f;
+                    if (n_vis == 1) w[r] = 0.f;        // the weight of an only key is 1 whatever the scores are
+                }
             }
-            accumulate<T, TILE>(dq, sK + buf * kBytes, in, w, c, h);
+            grad.template add<TILE, false>(s, w, sK + buf * kBytes, in, c, h);
         }
     }
     outside();                                         // (last: its loads would delay the others)
     if (KW == 2) {
         float* join = reinterpret_cast<float*>(lds) + (rw * 32 + c) * kJoinRow;
         __syncthreads();
-        if (kg == 1) store_row(join, dq, 1.f, h);
+        if (kg == 1) store_row(join, grad.dq, 1.f, h);
         __syncthreads();
         if (kg == 1) return;
 #pragma unroll
         for (int dt = 0; dt < 2; ++dt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) dq[dt][r] += join[32 * dt + acc_row(r, h)];
+            for (int r = 0; r < 16; ++r) grad.dq[dt][r] += join[32 * dt + acc_row(r, h)];
     }
     if (row >= n_rows) return;
-    store_row(dQ.at(head, f.q0 + t), dq, scale, h);
+    d += grad.finish();
+    store_row(dQ.at(head, f.q0 + t), grad.dq, scale, h);
+    if (h == 0) {
+        const int64_t so = Stats::at(p, hk, (int64_t)f.q0 * p.G + row);
+        stats.l[so] = l;
+        stats.d[so] = d;
+    }
 }
 
 // ---- the same with 32 keys (rows) to a work-group, whose 4 waves divide the rows (keys) among themselves and join their sums in LDS at
@@ -258,7 +305,7 @@ void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Head
 // only, and 4 times as often.
 constexpr int kJoinBytes = 4 * 32 * kJoinRow * 4;
 template <typename T> constexpr int kDkvLds = (8 * kTileBytes<T, 32> > kJoinBytes ? 8 * kTileBytes<T, 32> : kJoinBytes) + 4 * 2 * 32 * 4;
-template <typename T> constexpr int kDqLds = 4 * kTileBytes<T, 32> > kJoinBytes ? 4 * kTileBytes<T, 32> : kJoinBytes;
+template <typename T> constexpr int kDqLds = 4 * kTileBytes<T, 32> > kJoinBytes + 4 * 32 * 4 ? 4 * kTileBytes<T, 32> : kJoinBytes + 4 * 32 * 4;
 
 template <typename T>
 __device__ __forceinline__
@@ -340,13 +387,14 @@ void dkv_few(unsigned char* lds, int hk, int x, Heads<const T> Q, Heads<const T>
                 w[4 * r4 + e] = s[4 * r4 + e] * (w[4 * r4 + e] - d[e]);
             }
         }
+        if (f.nk == 1) clear(w);                       // (an only key)
         if (r0 < first_every) {
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 if (r0 + acc_row(r, h) < first) { s[r] = 0.f; w[r] = 0.f; }
         }
-        accumulate<T, 32>(dv, sG, 0, s, c, h);
-        accumulate<T, 32>(dk, sQ, 0, w, c, h);
+        accumulate<T, 32, true>(dv, sG, 0, s, c, h);
+        accumulate<T, 32, true>(dk, sQ, 0, w, c, h);
     }
     outside();
     float* join = reinterpret_cast<float*>(lds);
@@ -390,13 +438,12 @@ void dq_few(unsigned char* lds, int hk, int x, Heads<const T> Q, Heads<const T> 
         l = stat_of(stats.lse[(int64_t)head * p.Tq + f.q0 + t]);
         d = half_row_dot(out.at(head, f.q0 + t), dOut.at(head, f.q0 + t), h);
         d += swap_half(d);
-        if (wave == 0 && h == 0 && row0 + c < n_rows) { stats.l[so] = l; stats.d[so] = d; }
     } else {
         l = stats.l[so];
         d = stats.d[so];
     }
-    floatx16 dq[2];
-    clear(dq[0]); clear(dq[1]);
+    RowGradient<T> grad;
+    grad.init();
     const T* Kh = K.at(hk, f.k0);
     const T* Vh = V.at(hk, f.k0);
     unsigned char* sK = lds + wave * kBytes;
@@ -424,31 +471,49 @@ void dq_few(unsigned char* lds, int hk, int x, Heads<const T> Q, Heads<const T> 
         floatx16 w = product(vn, g);
         wave_lds_sync();
         if (j0 + 128 < n_all) fetch(j0 + 128);
-        const floatx16 s = product<T, 32>(sK, 0, q, c, h);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) w[r] = fast_exp2(fmaf(s[r], scale_log2, -l)) * (w[r] - d);
+        floatx16 s = product<T, 32>(sK, 0, q, c, h);
+        grad.weights(s, w, scale_log2, l, d);
         if (j0 + 32 > n_every) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (j0 + acc_row(r, h) >= n_vis) w[r] = 0.f;
+            for (int r = 0; r < 16; ++r) {
+                if (j0 + acc_row(r, h) >= n_vis) s[r] = w[r] = 0.f;
+                if (n_vis == 1) w[r] = 0.f;            // the weight of an only key is 1 whatever the scores are
+            }
         }
-        accumulate<T, 32>(dq, sK, 0, w, c, h);
+        grad.template add<32, true>(s, w, sK, 0, c, h);
     }
     outside();
     __syncthreads();
     float* join = reinterpret_cast<float*>(lds);
-    store_row(join + (wave * 32 + c) * kJoinRow, dq, 1.f, h);
+    const int jr = tid >> 3, row = row0 + jr, rt = min(row, n_rows - 1) / p.G;
+    store_row(join + (wave * 32 + c) * kJoinRow, grad.dq, 1.f, h);
     __syncthreads();
-    const int row = row0 + (tid >> 3);
-    if (row >= n_rows) return;
     float sum[8];
     join_columns(sum, join, tid);
-    const int rt = row / p.G;
+    if constexpr (sizeof(T) == 2) {
+        // e is the sum of the waves' parts, then d and sum_j p_j K[j] as in RowGradient::finish()
+        float* join_e = reinterpret_cast<float*>(lds + kJoinBytes);
+        const float e = grad.e + swap_half(grad.e);
+        __syncthreads();
+        store_row(join + (wave * 32 + c) * kJoinRow, grad.pk, 1.f, h);
+        if (h == 0) join_e[wave * 32 + c] = e;
+        __syncthreads();
+        float pk[8];
+        join_columns(pk, join, tid);
+        auto whole = [&](int r) { return ((join_e[r] + join_e[32 + r]) + join_e[64 + r]) + join_e[96 + r]; };
+        const float er = whole(jr);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] = fmaf(-er, pk[i], sum[i]);
+        d += whole(c);
+    }
+    if (FIND_STATS && wave == 0 && h == 0 && row0 + c < n_rows) { stats.l[so] = l; stats.d[so] = d; }
+    if (row >= n_rows) return;
     store8(dQ.at(hk * p.G + (row - rt * p.G), f.q0 + rt) + (tid & 7) * 8, sum, scale);
 }
 
 // The first n_k work-groups form dK and dV, the others dQ: both or (n_k = 0, or as many as there are) one of them.  One launch where both take
-// few keys and rows: such calls leave the card idle, and the two do not depend on each other.
+// few keys and rows of float32: such calls leave the card idle, and with d from a launch of its own the two do not depend on each other (2 clips
+// of 400: 43.7 | 24.4 us).
 template <typename T, bool DKV, bool DQ>
 __global__ __launch_bounds__(256, 2)
 void packed_grads_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, Heads<const T> out, Stats stats, Packing p,
@@ -490,11 +555,13 @@ static void packed_bwd_go(const PackedBwdPlan& p, const psa_packed_shape_t& s, c
     const auto dq = heads_of<T>(dQ), dk = heads_of<T>(dK), dv = heads_of<T>(dV);
     const unsigned n_k = (unsigned)(p.n_ktile * s.H_kv), n_q = (unsigned)(p.n_qtile * s.H_kv);
     constexpr int KT = sizeof(T) == 4 ? 32 : 64, KW = sizeof(T) == 4 ? 2 : 1;
-    if (p.few_k && p.few_q) {
-        constexpr int rows = 256 / (64 / kVec<T>);
-        packed_stats_kernel<T><<<(unsigned)(((int64_t)s.T_q * s.H + rows - 1) / rows), 256, 0, stream>>>(o, g, lse, pk, s.H, st.l, st.d);
-        packed_grads_few_kernel<T, true, true><<<n_k + n_q, 256, 0, stream>>>(q, k, v, g, o, st, pk, dq, dk, dv, s.H_kv, s.causal, scale, scale_log2, p.n_ktile, p.n_qtile);
-        return;
+    if constexpr (sizeof(T) == 4) {
+        if (p.few_k && p.few_q) {
+            constexpr int rows = 256 / (64 / kVec<T>);
+            packed_stats_kernel<T><<<(unsigned)(((int64_t)s.T_q * s.H + rows - 1) / rows), 256, 0, stream>>>(o, g, lse, pk, s.H, st.l, st.d);
+            packed_grads_few_kernel<T, true, true><<<n_k + n_q, 256, 0, stream>>>(q, k, v, g, o, st, pk, dq, dk, dv, s.H_kv, s.causal, scale, scale_log2, p.n_ktile, p.n_qtile);
+            return;
+        }
     }
     if (p.few_q)
         packed_grads_few_kernel<T, false, true><<<n_q, 256, 0, stream>>>(q, k, v, g, o, st, pk, dq, dk, dv, s.H_kv, s.causal, scale, scale_log2, p.n_ktile, p.n_qtile);
