@@ -348,7 +348,7 @@ int probsparse_rotary_frequencies(const psa_rotary_t* rotary, double* freq);
  *   positions  DEVICE int32, 4-byte aligned: row l of item b stands at
  *              positions[b * positions_stride + l]; positions_stride 0: the same for every
  *              item, else >= L.  NULL: row l stands at first + l (first + L <= 2^31 - 1)
- *   shape      L_Q = L_K = L; U is ignored
+ *   shape      L_Q = L_K = L, 1 .. 2^22; U is ignored
  * The backward turns the gradients of Q_out and K_out the other way (and multiplies by the same
  * magnitude), which makes them those of Q and K. */
 int probsparse_rotary_fwd(const psa_heads_t* Q, const psa_heads_t* K, int32_t H_kv, const psa_rotary_t* rotary,
@@ -378,12 +378,12 @@ int probsparse_rotary_bwd(const psa_heads_t* dQ_out, const psa_heads_t* dK_out, 
  * the most, 2^-25 as a rule) and summed in float32; an infinity has no such parts, so that one in
  * Q or K makes the scores it takes part in NaN.  Softmax statistics are float32. */
 typedef struct psa_packed_shape {
-    int32_t B, H, H_kv;           /* sequences; heads, H a multiple of H_kv */
+    int32_t B, H, H_kv;           /* sequences, at most 2^20; heads, H a multiple of H_kv */
     int32_t T_q, T_k;             /* rows of Q and of K and V; T_q * (H / H_kv) <= 2^31 - 2^16 */
     int32_t D;                    /* 64 */
     int32_t dtype;                /* psa_dtype_t */
     int32_t causal;               /* 0 or 1 */
-    double  scale;                /* finite, > 0; 1 / sqrt(64) as a rule */
+    double  scale;                /* 1e-30 .. 1e30; 1 / sqrt(64) as a rule */
 } psa_packed_shape_t;
 size_t dense_attn_packed_workspace_bytes(const psa_packed_shape_t* shape);
 int dense_attn_packed_fwd(const psa_heads_t* Q, const psa_heads_t* K, const psa_heads_t* V,

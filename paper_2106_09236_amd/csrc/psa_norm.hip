@@ -435,7 +435,6 @@ static void norm_fwd_pick(const NormPlan& p, const void* X, const void* gamma, c
 hipError_t launch_norm_fwd(const NormPlan& p, const void* X, const void* gamma, const void* beta, float eps, void* Y, float* mean,
                            float* rstd, int64_t rows, int cols, int dtype, hipStream_t stream)
 {
-    (void)hipGetLastError();
     if (dtype == PSA_F32) norm_fwd_pick<float>(p, X, gamma, beta, eps, Y, mean, rstd, rows, cols, stream);
     else norm_fwd_pick<bf16_t>(p, X, gamma, beta, eps, Y, mean, rstd, rows, cols, stream);
     return hipGetLastError();
@@ -476,7 +475,6 @@ static void norm_bwd_pick(const NormPlan& p, const void* dY, const void* X, cons
 hipError_t launch_norm_bwd(const NormPlan& p, const void* dY, const void* X, const void* gamma, const float* mean, const float* rstd,
                            void* dX, float* dgamma, float* dbeta, int64_t rows, int cols, int dtype, void* workspace, hipStream_t stream)
 {
-    (void)hipGetLastError();
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     float* off = reinterpret_cast<float*>(ws);
     float* part = dgamma ? reinterpret_cast<float*>(ws + p.off_part) : nullptr;

@@ -101,7 +101,8 @@ static int check_packed(const psa_packed_shape_t* s)
     if ((int64_t)s->T_q * (s->H / s->H_kv) > INT32_MAX - 65536) return PSA_ERR_SHAPE;
     // work-groups of a launch: tiles of 32 rows at the least
     if (((int64_t)s->T_q * (s->H / s->H_kv) / 32 + s->T_k / 32 + 2 * s->B) * s->H_kv > INT32_MAX) return PSA_ERR_SHAPE;
-    if ((s->causal != 0 && s->causal != 1) || !positive(s->scale)) return PSA_ERR_ARG;
+    // (the kernels hold scale * log2(e) in float32: 0 there would make NaN of a masked score)
+    if ((s->causal != 0 && s->causal != 1) || !(s->scale >= 1e-30) || !(s->scale <= 1e30)) return PSA_ERR_ARG;
     return PSA_OK;
 }
 static int check_offsets(const psa_packed_shape_t& s, const int32_t* qo, const int32_t* ko)

@@ -30,8 +30,24 @@ struct Heads {
 template <typename T>
 inline Heads<T> heads_of(const psa_heads_t& t) { return Heads<T>{static_cast<T*>(t.data), t.head_stride, t.row_stride}; }
 
-// The sequences of a call: offsets and what they are clamped to.
-struct Packing { const int* qo; const int* ko; int B, Tq, Tk, G; };
+// The sequences of a call: offsets and what they are clamped to; of calls with many, the tiles before each 64 of them (see below).
+struct Packing { const int* qo; const int* ko; int B, Tq, Tk, G; const int* q_before; const int* k_before; };
+
+// Sequence s's rows and keys
+struct SeqRange { int q0, q1, k0, k1; };
+__device__ __forceinline__ SeqRange seq_range(const Packing& p, int s)
+{
+    SeqRange r{0, 0, 0, 0};
+    if (s >= 0) {
+        r.q0 = min(max(p.qo[s], 0), p.Tq); r.q1 = min(max(p.qo[s + 1], r.q0), p.Tq);
+        r.k0 = min(max(p.ko[s], 0), p.Tk); r.k1 = min(max(p.ko[s + 1], r.k0), p.Tk);
+    }
+    return r;
+}
+__device__ __forceinline__ int seq_tiles(const SeqRange& r, int G, int per, bool keys) { return ((keys ? r.k1 - r.k0 : (r.q1 - r.q0) * G) + per - 1) / per; }
+
+constexpr int kManySequences = 256;
+inline size_t packed_before_bytes(int B) { return B > kManySequences ? (((size_t)(B + 63) / 64 * sizeof(int)) + 255) & ~(size_t)255 : 0; }
 
 // The tile a work-group takes: rows (or keys) tile * PER .. of the sequence; tile < 0: there is none.
 struct SeqTile { int q0, nq, k0, nk, tile; };
@@ -50,7 +66,9 @@ __device__ __forceinline__ int wave_sum(int x)
 // their sequence come first (of tiles of keys the lowest: the index counts from the end): under a causal mask they have the most
 // work, and what starts last should be short.  Groups, not all
 // sequences, so that work-groups that run at one time share their keys in L2.  Every wave finds its tile for itself: 64 sequences
-// at a time, a prefix sum over the lanes for the group and a search for the index.
+// at a time, a prefix sum over the lanes for the group and a search for the index.  Beyond kManySequences a kernel of its own has
+// summed up the tiles before each 64 of them (packed_before_kernel): work-groups that each walk all of them would take a time that
+// grows with the square of their number.
 template <int PER, bool KEYS>
 __device__ __forceinline__ SeqTile find_tile(const Packing& p, int x)
 {
@@ -62,14 +80,24 @@ __device__ __forceinline__ SeqTile find_tile(const Packing& p, int x)
         return f;
     }
     const int lane = threadIdx.x & 63;
-    for (int base = 0; base < p.B; base += 64) {
-        const int s = p.B - 1 - base - lane;
-        int q0 = 0, q1 = 0, k0 = 0, k1 = 0;
-        if (s >= 0) {
-            q0 = min(max(p.qo[s], 0), p.Tq); q1 = min(max(p.qo[s + 1], q0), p.Tq);
-            k0 = min(max(p.ko[s], 0), p.Tk); k1 = min(max(p.ko[s + 1], k0), p.Tk);
+    int base = 0, end = p.B;
+    if (const int* before = KEYS ? p.k_before : p.q_before) {
+        // the last 64 sequences with at most x tiles before them: 64 candidates at a time
+        int lo = 0, n = (p.B + 63) / 64;
+        while (n > 1) {
+            const int step = (n + 63) / 64, i = lane * step;
+            const int k = __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < n && before[min(lo + i, (p.B + 63) / 64 - 1)] <= x)) - 1;
+            lo += k * step;
+            n = min(step, n - k * step);
         }
-        int n = ((KEYS ? k1 - k0 : (q1 - q0) * p.G) + PER - 1) / PER;
+        x -= before[lo];
+        base = lo * 64;
+        end = min(end, base + 64);
+    }
+    for (; base < end; base += 64) {
+        const SeqRange r = seq_range(p, p.B - 1 - base - lane);
+        const int q0 = r.q0, q1 = r.q1, k0 = r.k0, k1 = r.k1;
+        int n = seq_tiles(r, p.G, PER, KEYS);
         int sum = n;                                   // of this lane's group of 16, up to this lane
 #pragma unroll
         for (int d = 1; d < 16; d *= 2) {
@@ -105,6 +133,10 @@ __device__ __forceinline__ SeqTile find_tile(const Packing& p, int x)
     }
     return f;
 }
+
+// The sequences of a call; where there are many, with a launch that sums up their tiles (of per_q rows and, `keys`, per_k keys) in `room`,
+// 2 packed_before_bytes().
+Packing make_packing(const psa_packed_shape_t& s, const int* q_offsets, const int* k_offsets, int per_q, int per_k, void* room, bool keys, hipStream_t stream);
 
 // Zeros in the rows of `t` that belong to no sequence (before the first offset, from the last one on), the share `x` of
 // `n` work-groups; `each(head, row)` is called by one thread of the work-group for each head.

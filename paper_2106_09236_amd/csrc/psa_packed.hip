@@ -368,6 +368,44 @@ void packed_merge_kernel(const float* __restrict__ part_o, const float2* __restr
     if (lse && e == 0) lse[(int64_t)head * p.Tq + t] = sum == 0.f ? -INFINITY : m * kLn2 + logf(sum);
 }
 
+// Tiles before each 64 sequences, counted from the last (find_tile): of rows in work-group 0, of keys in work-group 1.  16 waves with 64
+// sequences each at a time.
+__global__ __launch_bounds__(1024)
+void packed_before_kernel(Packing p, int per_q, int per_k, int* __restrict__ q_before, int* __restrict__ k_before)
+{
+    __shared__ int s[2][16];
+    const bool keys = blockIdx.x == 1;
+    int* out = keys ? k_before : q_before;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, groups = (p.B + 63) / 64;
+    int sum = 0;                                       // of all before these 16
+    for (int g0 = 0, buf = 0; g0 < groups; g0 += 16, buf ^= 1) {
+        const int g = g0 + wave;
+        const int n = wave_sum(g < groups ? seq_tiles(seq_range(p, p.B - 1 - 64 * g - lane), p.G, keys ? per_k : per_q, keys) : 0);
+        if (lane == 0) s[buf][wave] = n;
+        __syncthreads();
+        int mine = sum, all = sum;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) mine += s[buf][w];
+            all += s[buf][w];
+        }
+        if (g < groups && lane == 0) out[g] = mine;
+        sum = all;
+    }
+}
+Packing make_packing(const psa_packed_shape_t& s, const int* q_offsets, const int* k_offsets, int per_q, int per_k, void* room, bool keys, hipStream_t stream)
+{
+    Packing p{q_offsets, k_offsets, s.B, s.T_q, s.T_k, s.H / s.H_kv, nullptr, nullptr};
+    if (const size_t bytes = packed_before_bytes(s.B)) {
+        int* q = static_cast<int*>(room);
+        int* k = reinterpret_cast<int*>(static_cast<unsigned char*>(room) + bytes);
+        packed_before_kernel<<<keys ? 2 : 1, 1024, 0, stream>>>(p, per_q, per_k, q, k);
+        p.q_before = q;
+        p.k_before = keys ? k : nullptr;
+    }
+    return p;
+}
+
 // float32, two waves to 32 rows?  One work-group of them fills a compute unit, and a wave's chain of steps is half as long: for calls
 // with few work-groups (`wide` of 128 rows) and long sequences.  1 | 2 waves, forward: 16 x 512 (4 heads, 320 work-groups) 41 | 35 us, 24
 // ragged clips of 435 causal (374) 55 | 41, 8 x 1000 causal (8 heads, 531) 83 | 77; but 32 of 40 .. 500 (400) 50 | 54, 64 of 450 (1120)
@@ -399,12 +437,13 @@ PackedPlan make_packed_plan(const psa_packed_shape_t& s)
         if (split > 64) split = 64;
         p.n_split = (int)(split < 1 ? 1 : split);
     }
-    p.off_part = 0;
+    p.off_ml = packed_before_bytes(s.B);
+    p.off_part = p.off_ml;
     if (p.n_split > 1) {
-        p.off_part = ((size_t)p.n_split * (size_t)rows * s.H_kv * sizeof(float2) + 255) & ~(size_t)255;
+        p.off_part += ((size_t)p.n_split * (size_t)rows * s.H_kv * sizeof(float2) + 255) & ~(size_t)255;
         p.total = p.off_part + (size_t)p.n_split * (size_t)rows * s.H_kv * 64 * sizeof(float);
     } else {
-        p.total = 256;
+        p.total = p.off_part > 256 ? p.off_part : 256;
     }
     return p;
 }
@@ -421,7 +460,7 @@ static void packed_go(const PackedPlan& p, const psa_packed_shape_t& s, const ps
             heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), pk, heads_of<T>(out), lse, s.H_kv, s.causal, scale, p.n_tile);
         return;
     }
-    float2* part_ml = static_cast<float2*>(workspace);
+    float2* part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(workspace) + p.off_ml);
     float* part_o = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.off_part);
     packed_few_kernel<T><<<grid, 256, 0, stream>>>(heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), pk, heads_of<T>(out), lse,
                                                    s.H_kv, s.causal, scale, p.n_tile, p.n_split, part_o, part_ml);
@@ -433,8 +472,7 @@ static void packed_go(const PackedPlan& p, const psa_packed_shape_t& s, const ps
 hipError_t launch_packed(const PackedPlan& p, const psa_packed_shape_t& s, const psa_heads_t& Q, const psa_heads_t& K, const psa_heads_t& V,
                          const int* q_offsets, const int* k_offsets, const psa_heads_t& out, float* lse, void* workspace, hipStream_t stream)
 {
-    (void)hipGetLastError();
-    const Packing pk{q_offsets, k_offsets, s.B, s.T_q, s.T_k, s.H / s.H_kv};
+    const Packing pk = make_packing(s, q_offsets, k_offsets, p.rows, 0, workspace, false, stream);
     if (s.dtype == PSA_F32) packed_go<float, 32>(p, s, Q, K, V, pk, out, lse, workspace, stream);
     else packed_go<bf16_t, 64>(p, s, Q, K, V, pk, out, lse, workspace, stream);
     return hipGetLastError();

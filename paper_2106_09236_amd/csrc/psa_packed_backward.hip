@@ -540,7 +540,8 @@ PackedBwdPlan make_packed_bwd_plan(const psa_packed_shape_t& s)
     p.few_k = (int64_t)(s.T_k / 128 + s.B) * s.H_kv < 300;
     p.n_qtile = (int)(rows / (p.few_q ? 32 : 128)) + s.B;
     p.n_ktile = s.T_k / (p.few_k ? 32 : 128) + s.B;
-    p.total = 2 * (((size_t)s.T_q * s.H * sizeof(float) + 255) & ~(size_t)255);
+    p.stat_bytes = ((size_t)s.T_q * s.H * sizeof(float) + 255) & ~(size_t)255;
+    p.total = 2 * (p.stat_bytes + packed_before_bytes(s.B));
     return p;
 }
 
@@ -549,7 +550,7 @@ static void packed_bwd_go(const PackedBwdPlan& p, const psa_packed_shape_t& s, c
                           const Packing& pk, const psa_heads_t& out, const float* lse, const psa_heads_t& dOut, const psa_heads_t& dQ,
                           const psa_heads_t& dK, const psa_heads_t& dV, void* workspace, hipStream_t stream)
 {
-    const Stats st{static_cast<float*>(workspace), reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.total / 2), lse};
+    const Stats st{static_cast<float*>(workspace), reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.stat_bytes), lse};
     const float scale = (float)s.scale, scale_log2 = (float)(s.scale * 1.4426950408889634);
     const auto q = heads_of<const T>(Q), k = heads_of<const T>(K), v = heads_of<const T>(V), g = heads_of<const T>(dOut), o = heads_of<const T>(out);
     const auto dq = heads_of<T>(dQ), dk = heads_of<T>(dK), dv = heads_of<T>(dV);
@@ -577,8 +578,8 @@ hipError_t launch_packed_bwd(const PackedBwdPlan& p, const psa_packed_shape_t& s
                              const int* q_offsets, const int* k_offsets, const psa_heads_t& out, const float* lse, const psa_heads_t& dOut,
                              const psa_heads_t& dQ, const psa_heads_t& dK, const psa_heads_t& dV, void* workspace, hipStream_t stream)
 {
-    (void)hipGetLastError();
-    const Packing pk{q_offsets, k_offsets, s.B, s.T_q, s.T_k, s.H / s.H_kv};
+    const Packing pk = make_packing(s, q_offsets, k_offsets, p.few_q ? 32 : 128, p.few_k ? 32 : 128, static_cast<unsigned char*>(workspace) + 2 * p.stat_bytes,
+                                    true, stream);
     if (s.dtype == PSA_F32) packed_bwd_go<float>(p, s, Q, K, V, pk, out, lse, dOut, dQ, dK, dV, workspace, stream);
     else packed_bwd_go<bf16_t>(p, s, Q, K, V, pk, out, lse, dOut, dQ, dK, dV, workspace, stream);
     return hipGetLastError();

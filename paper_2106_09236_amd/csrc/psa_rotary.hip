@@ -139,7 +139,6 @@ hipError_t launch_rotary(const psa_heads_t* Q, const psa_heads_t* K, int H_kv, c
                          const int* positions, int64_t positions_stride, int first, const psa_heads_t* Qo, const psa_heads_t* Ko,
                          const psa_shape_t& s, hipStream_t stream)
 {
-    (void)hipGetLastError();
     if (s.dtype == PSA_F32) rotary_go<float>(Q, K, H_kv, o, freq, back, positions, positions_stride, first, Qo, Ko, s, stream);
     else rotary_go<bf16_t>(Q, K, H_kv, o, freq, back, positions, positions_stride, first, Qo, Ko, s, stream);
     return hipGetLastError();

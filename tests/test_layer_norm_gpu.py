@@ -39,7 +39,7 @@ def test_norm_and_gradients(rows, cols, dtype):
     assert all(torch.equal(a, b) for a, b in zip(again, (dX, dgamma, dbeta)))
 
 
-@pytest.mark.parametrize("rows,cols", [(40000, 256), (9000, 512), (66000, 24)])
+@pytest.mark.parametrize("rows,cols", [(40000, 256), (9000, 512), (66000, 24), (66000, 300)])
 def test_many_rows(rows, cols):
     X, dY, gamma, beta = _inputs(rows, cols, torch.bfloat16, rows + cols)
     Xd, dYd, gd, bd = (t.cuda() for t in (X, dY, gamma, beta))

@@ -119,7 +119,7 @@ def test_packed_attention_refusals(backward):
         assert call(shape=_packed(**kw)) == SHAPE, kw
     assert call(shape=_packed(H=64, H_kv=1, T_q=1 << 26)) == SHAPE           # rows of a key head beyond 31 bits
     assert call(shape=_packed(dtype=9)) == DTYPE
-    for kw in (dict(causal=2), dict(causal=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf)):
+    for kw in (dict(causal=2), dict(causal=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(scale=1e-40), dict(scale=1e40)):
         assert call(shape=_packed(**kw)) == ARG, kw
     assert call(qo=0x101) == call(lse=0x302) == call(ws=0x10080) == ALIGN
     assert call(n=0) == WORKSPACE

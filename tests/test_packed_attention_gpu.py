@@ -91,6 +91,81 @@ def test_queries_and_keys_of_other_lengths(H, H_kv, q_lens, k_lens, causal, dtyp
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("H,H_kv,B,longest", [(2, 1, 256, 5), (2, 1, 257, 5), (2, 2, 700, 9), (1, 1, 5000, 3), (32, 32, 300, 70)])
+def test_many_sequences(H, H_kv, B, longest, causal, dtype):
+    """Hundreds of sequences, empty ones and a long one among them, the last group of 64 not full."""
+    g = torch.Generator().manual_seed(B)
+    q_lens = torch.randint(0, longest + 1, (B,), generator=g).tolist()
+    k_lens = [n + int(e) for n, e in zip(q_lens, torch.randint(0, 3, (B,), generator=g))]
+    q_lens[B // 3] = k_lens[B // 3] = 300 if H < 32 else 100
+    k_lens[2] = 0
+    _check(*_case(H, H_kv, q_lens, k_lens, dtype, behind=7), causal)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_few_queries_of_many_keys_with_gradients(dtype):
+    """Rows taken 32 at a time, keys 128 at a time."""
+    _check(*_case(16, 16, [40], [2500], dtype), True)
+
+
+def test_offsets_beyond_31_bits():
+    """K and V as columns of a cache whose rows are 8 MB apart: element offsets up to 2^32."""
+    n, wide = 1024, 1 << 22
+    cache = torch.empty(n, wide, dtype=torch.bfloat16, device="cuda")
+    (Q, K, V, G), (Qd, Kd, Vd, Gd), q_off, k_off = _case(2, 1, [3, 70], [600, n - 600], torch.bfloat16)
+    kv = cache[:, wide - 128:].unflatten(1, (2, 64))
+    kv[:, 0], kv[:, 1] = Kd[0], Vd[0]
+    Kc, Vc = kv[:, :1].transpose(0, 1), kv[:, 1:].transpose(0, 1)
+    qo, ko = (torch.tensor(o, dtype=torch.int32, device="cuda") for o in (q_off, k_off))
+    out, lse = psa.dense_attn_packed_fwd(Qd, Kc, Vc, qo, ko, causal=True, lse=True)
+    want = packed_attention(Q, K, V, q_off, k_off, True, 0.125, G)
+    grads = psa.dense_attn_packed_bwd(Qd, Kc, Vc, out, lse, Gd, qo, ko, causal=True)
+    for g, (w, e) in zip((out, lse, *grads), want):
+        assert_within(g, w, e)
+    with pytest.raises(psa.ProbSparseError):          # a wider row would pass the limit of offsets within a tile
+        psa.dense_attn_packed_fwd(Qd, cache.view(-1)[:64 * 2].view(1, 2, 64).as_strided((1, 2, 64), (0, wide + 8, 1)), Vc[:, :2], torch.tensor([0, 73], dtype=torch.int32, device="cuda"),
+                                  torch.tensor([0, 2], dtype=torch.int32, device="cuda"))
+
+
+def test_two_streams_at_once():
+    """Calls on two streams, each with a workspace of its own, give what they give alone."""
+    a = _case(8, 2, [1] * 9, [2000] * 9, torch.bfloat16)
+    b = _case(4, 4, [300, 500], [300, 500], torch.float32)
+    def run(case, causal=True):
+        _, (Qd, Kd, Vd, Gd), q_off, k_off = case
+        qo, ko = case_offsets[id(case)]
+        out, lse = psa.dense_attn_packed_fwd(Qd, Kd, Vd, qo, ko, causal=causal, lse=True)
+        return (out, lse, *psa.dense_attn_packed_bwd(Qd, Kd, Vd, out, lse, Gd, qo, ko, causal=causal))
+    case_offsets = {id(c): [torch.tensor(o, dtype=torch.int32, device="cuda") for o in c[2:]] for c in (a, b)}
+    ref = [run(a), run(b)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        for s, c in zip(streams, (a, b)):
+            with torch.cuda.stream(s):
+                got.append(run(c))
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert all(torch.equal(x, y) for x, y in zip(g, ref[i % 2]))
+
+
+def test_one_key_has_no_gradient_but_its_value():
+    for dtype in (torch.float32, torch.bfloat16):
+        for H, H_kv, lens in ((4, 2, [1] * 7), (64, 64, [1] * 300)):
+            host, (Qd, Kd, Vd, Gd), q_off, k_off = _case(H, H_kv, lens, lens, dtype)
+            off = torch.tensor(q_off, dtype=torch.int32, device="cuda")
+            out, lse = psa.dense_attn_packed_fwd(Qd, Kd, Vd, off, causal=True, lse=True)
+            dQ, dK, dV = psa.dense_attn_packed_bwd(Qd, Kd, Vd, out, lse, Gd, off, causal=True)
+            assert not dQ.any() and not dK.any()
+            # p is 1 but for the rounding of the score that is subtracted, and its sum is p: p V and 1 / p are left.  In half steps
+            # of float32: 2 for the parts of a product, 1 for their sum, 1 for the reciprocal, 1 for the product with it; then the tensor's own
+            v = Vd.repeat_interleave(H // H_kv, 0).cpu().double()
+            assert_within(out, v, (5 * 2.0 ** -24 + HALF[dtype]) * v.abs())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_rows_in_no_sequence(dtype):
     _check(*_case(4, 2, [40, 9], [60, 30], dtype, by_frame=True, front=150, behind=300), True)
     _check(*_case(2, 2, [0, 0], [0, 0], dtype, behind=5), False)
