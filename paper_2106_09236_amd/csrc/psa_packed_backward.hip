@@ -304,7 +304,10 @@ void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Head
 // the end.  Four times as many work-groups, each a quarter as long, no barrier before the join; a tile of rows is read by one wave
 // only, and 4 times as often.
 constexpr int kJoinBytes = 4 * 32 * kJoinRow * 4;
-template <typename T> constexpr int kDkvLds = (8 * kTileBytes<T, 32> > kJoinBytes ? 8 * kTileBytes<T, 32> : kJoinBytes) + 4 * 2 * 32 * 4;
+// float32 tiles are 12 KB.  With K and V in registers and a tile of Q and one of dOut to each wave, a compute unit held one work-group, a wave
+// to a SIMD; so K and V lie in LDS, and one tile of a wave holds Q, then dOut, then Q again (24 ragged clips of 435: 101 -> 73 us).
+template <typename T> constexpr int kDkvTiles = sizeof(T) == 4 ? 6 : 8;
+template <typename T> constexpr int kDkvLds = (kDkvTiles<T> * kTileBytes<T, 32> > kJoinBytes ? kDkvTiles<T> * kTileBytes<T, 32> : kJoinBytes) + 4 * 2 * 32 * 4;
 template <typename T> constexpr int kDqLds = 4 * kTileBytes<T, 32> > kJoinBytes + 4 * 32 * 4 ? 4 * kTileBytes<T, 32> : kJoinBytes + 4 * 32 * 4;
 
 template <typename T>
@@ -331,22 +334,35 @@ void dkv_few(unsigned char* lds, int hk, int x, Heads<const T> Q, Heads<const T>
     const int first_any = __builtin_amdgcn_readfirstlane(first_row(key0));
     const int first_every = __builtin_amdgcn_readfirstlane(first_row(min(key0 + 31, f.nk - 1)));
 
-    HeadOperand<T> k, v;
-    k.load(K.at(hk, f.k0 + kc), h);
-    v.load(V.at(hk, f.k0 + kc), h);
+    constexpr bool kOneTile = sizeof(T) == 4;
     floatx16 dk[2], dv[2];
     clear(dk[0]); clear(dk[1]); clear(dv[0]); clear(dv[1]);
-    unsigned char *sQ = lds + wave * 2 * kBytes, *sG = sQ + kBytes;
+    unsigned char *sK = lds, *sV = lds + kBytes;
+    unsigned char *sQ = lds + (kOneTile ? 2 + wave : 2 * wave) * kBytes, *sG = kOneTile ? sQ : sQ + kBytes;
     const int64_t stat0 = ((int64_t)hk * p.Tq + f.q0) * p.G;
     const int lr = lane / CH, ch = lane % CH;
+    HeadOperand<T> k, v;
+    if constexpr (kOneTile) {
+        const auto kb = tile_rows(K.at(hk, f.k0 + key0), K.row, f.nk - key0), vb = tile_rows(V.at(hk, f.k0 + key0), V.row, f.nk - key0);
+#pragma unroll
+        for (int i = 0; i < 32 * CH / 256; ++i) {
+            const int r = (i * 256 + tid) / CH, kc4 = (i * 256 + tid) % CH;
+            put<32>(sK, r, kc4, buffer_load16<uint4>(kb, (int)(r * K.row * (int64_t)sizeof(T)) + kc4 * 16), T{});
+            put<32>(sV, r, kc4, buffer_load16<uint4>(vb, (int)(r * V.row * (int64_t)sizeof(T)) + kc4 * 16), T{});
+        }
+        __syncthreads();
+    } else {
+        k.load(K.at(hk, f.k0 + kc), h);
+        v.load(V.at(hk, f.k0 + kc), h);
+    }
 
-    // one set of registers carries a tile of Q, then the tile of dOut, then the next tile of Q
-    uint4 x4[NL];
+    // one set of registers carries a tile of Q, then the tile of dOut, then the next tile of Q (float32: one of Q, one of dOut)
+    uint4 x4[NL], g4[NL];
     float l_next = INFINITY, d_next = 0.f;
     int r0 = first_any / 32 * 32 + wave * 32;
     const int dt = RL / p.G, dg = RL - dt * p.G, dt128 = 128 / p.G, dg128 = 128 - dt128 * p.G;
     RowAt base(r0 + lr, p.G);                          // of the tile that is fetched
-    auto fetch = [&](const Heads<const T>& t, int r0) {
+    auto fetch = [&](const Heads<const T>& t, uint4 (&x4)[NL], int r0) {
         RowAt at = base;
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
@@ -355,7 +371,7 @@ void dkv_few(unsigned char* lds, int hk, int x, Heads<const T> Q, Heads<const T>
             at.add(dt, dg, p.G);
         }
     };
-    auto keep = [&](unsigned char* s) {
+    auto keep = [&](unsigned char* s, const uint4 (&x4)[NL]) {
 #pragma unroll
         for (int i = 0; i < NL; ++i) put<32>(s, lr + i * RL, ch, x4[i], T{});
     };
@@ -364,19 +380,24 @@ void dkv_few(unsigned char* lds, int hk, int x, Heads<const T> Q, Heads<const T>
         l_next = in ? stat_l[stat0 + r0 + c] : INFINITY;
         d_next = in ? stat_d[stat0 + r0 + c] : 0.f;
     };
-    if (r0 < n_rows) { fetch(Q, r0); fetch_stats(r0); }
+    if (r0 < n_rows) { fetch(Q, x4, r0); fetch_stats(r0); }
     for (; r0 < n_rows; r0 += 128) {
         wave_lds_sync();
-        keep(sQ);
+        keep(sQ, x4);
         if (h == 0) { sL[wave][c] = l_next; sD[wave][c] = d_next; }
-        fetch(dOut, r0);
+        fetch(dOut, kOneTile ? g4 : x4, r0);
         wave_lds_sync();
-        floatx16 s = product<T, 32>(sQ, 0, k, c, h);
-        keep(sG);
+        floatx16 s, w;
+        if constexpr (kOneTile) s = product<T, 32>(sQ, 0, sK, c, h); else s = product<T, 32>(sQ, 0, k, c, h);
+        wave_lds_sync();
+        keep(sG, kOneTile ? g4 : x4);
         base.add(dt128, dg128, p.G);
-        if (r0 + 128 < n_rows) { fetch(Q, r0 + 128); fetch_stats(r0 + 128); }
+        if (r0 + 128 < n_rows) {
+            if (!kOneTile) fetch(Q, x4, r0 + 128);
+            fetch_stats(r0 + 128);
+        }
         wave_lds_sync();
-        floatx16 w = product<T, 32>(sG, 0, v, c, h);
+        if constexpr (kOneTile) w = product<T, 32>(sG, 0, sV, c, h); else w = product<T, 32>(sG, 0, v, c, h);
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) {
             const float4 l4 = *reinterpret_cast<const float4*>(&sL[wave][8 * r4 + 4 * h]), d4 = *reinterpret_cast<const float4*>(&sD[wave][8 * r4 + 4 * h]);
@@ -394,6 +415,12 @@ void dkv_few(unsigned char* lds, int hk, int x, Heads<const T> Q, Heads<const T>
                 if (r0 + acc_row(r, h) < first) { s[r] = 0.f; w[r] = 0.f; }
         }
         accumulate<T, 32, true>(dv, sG, 0, s, c, h);
+        if (kOneTile) {
+            wave_lds_sync();
+            keep(sQ, x4);
+            if (r0 + 128 < n_rows) fetch(Q, x4, r0 + 128);
+            wave_lds_sync();
+        }
         accumulate<T, 32, true>(dk, sQ, 0, w, c, h);
     }
     outside();
