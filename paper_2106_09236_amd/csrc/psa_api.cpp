@@ -725,10 +725,10 @@ const char* probsparse_strerror(int code)
     switch (code) {
         case PSA_OK:            return "ok";
         case PSA_ERR_NULL:      return "a required pointer is NULL";
-        case PSA_ERR_SHAPE:     return "unsupported shape (need B,H,L,U >= 1, D == 64, L_Q == L_K, B*H <= 65535)";
+        case PSA_ERR_SHAPE:     return "unsupported shape (need B,H,L,U >= 1, D == 64, L_Q == L_K, B*H <= 65535; packed attention: H a multiple of H_kv; layer norm: rows, cols >= 1)";
         case PSA_ERR_DTYPE:     return "unsupported dtype (PSA_F32 or PSA_BF16)";
-        case PSA_ERR_ARG:       return "invalid argument (factor must be finite and positive; stage mask within PSA_STAGE_ALL; known rule and fill; 1 <= u_stride <= L)";
-        case PSA_ERR_WORKSPACE: return "workspace smaller than probsparse_attn_workspace_bytes() (or, for probsparse_attn_fwd_static, the shape needs more than probsparse_static_workspace_bytes())";
+        case PSA_ERR_ARG:       return "invalid argument (factor must be finite and positive; stage mask within PSA_STAGE_ALL; known rule and fill; 1 <= u_stride <= L; eps, scale, rotary options and strides as in the header)";
+        case PSA_ERR_WORKSPACE: return "workspace smaller than the entry point's workspace_bytes() (or, for probsparse_attn_fwd_static, the shape needs more than probsparse_static_workspace_bytes())";
         case PSA_ERR_HIP:       return "HIP runtime error on launch or copy";
         case PSA_ERR_ALIGN:     return "device pointer not sufficiently aligned (16 B tensors, 256 B workspace)";
         default:                return "unknown status";
