@@ -418,6 +418,31 @@ __device__ __forceinline__ Operand<T> tile_transposed(const unsigned char* s, in
     }
     return a;
 }
+template <typename T> struct Transposed { Operand<T> v[2][2]; };
+template <typename T, int ROWS>
+__device__ __forceinline__ Transposed<T> transposed(const unsigned char* s, int row0, int c, int h)
+{
+    Transposed<T> a;
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt) a.v[st][dt] = tile_transposed<T, ROWS>(s, row0, st, dt, c, h);
+    return a;
+}
+template <typename T, bool FINE>
+__device__ __forceinline__ void accumulate(floatx16 (&d)[2], const Transposed<T>& a, const floatx16& w)
+{
+    constexpr int N = kWeightParts<T, FINE>;
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+        Operand<T> b[N];
+        weight_operand(b, w, st);
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+            for (int n = 0; n < N; ++n) d[dt] = mfma(a.v[st][dt], b[n], d[dt]);
+    }
+}
 template <typename T, int ROWS, bool FINE>
 __device__ __forceinline__ void accumulate(floatx16 (&d)[2], const unsigned char* s, int row0, const floatx16& w, int c, int h)
 {
@@ -434,6 +459,15 @@ __device__ __forceinline__ void accumulate(floatx16 (&d)[2], const unsigned char
         }
     }
 }
+// Order of a step's instructions: N reads of LDS together, then M matrix instructions.  Left to itself the compiler asks for an operand
+// right before the instruction that takes it, and each waits for its own.
+template <int N, int M>
+__device__ __forceinline__ void reads_first()
+{
+    __builtin_amdgcn_sched_group_barrier(0x100, N, 0);
+    if (M > 0) __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
+}
+
 // The same for a second set of weights at once (rounded)
 template <typename T, int ROWS, bool FINE>
 __device__ __forceinline__ void accumulate_two(floatx16 (&d)[2], const floatx16& w, floatx16 (&d2)[2], const floatx16& w2, const unsigned char* s, int row0, int c, int h)

@@ -57,7 +57,8 @@ struct Rows32 {
 // 4 waves of 32 rows each; tiles of KT keys and values go through LDS, the next tile's rows are on their way meanwhile.
 // bfloat16 is bound by the vector unit (131 instructions and 32 exponentials to 16 matrix instructions: 65 % of its issue
 // cycles, the matrix unit 38 %) and, in long runs, by power: 16384 causal, 8 heads, 350 us at first (785 TFLOP/s), 390 when hot.  What
-// did not help: 64 rows to a wave (half the LDS reads, 2 waves to a SIMD: 530 us), 4 waves to a SIMD with 32 keys at a time
+// helped: a step's LDS reads before the instructions that take them (8 x 2048 causal 56.8 -> 55.2 us, 32 clips 17.4 -> 17.0).  What
+// did not: 64 rows to a wave (half the LDS reads, 2 waves to a SIMD: 530 us), 4 waves to a SIMD with 32 keys at a time
 // (430), the scores of a step formed between the weights of the one before (440), priorities (no change).
 //
 // KW = 2 (float32): 8 waves, two to 32 rows, which take alternate tiles of KT keys and join their sums in LDS; see packed_halves().
@@ -143,6 +144,7 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
         floatx16 s[NS];
 #pragma unroll
         for (int n = 0; n < NS; ++n) s[n] = product<T, TILE>(sK + buf * kBytes, kg * KT + 32 * n, q, c, h);
+        reads_first<4 * NS * kParts<T>, 4 * NS * (sizeof(T) == 4 ? 6 : 1)>();
         if (j + KT > n_wave_every) {
 #pragma unroll
             for (int n = 0; n < NS; ++n)
@@ -150,10 +152,14 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
                 for (int r = 0; r < 16; ++r) s[n][r] = j + 32 * n + acc_row(r, h) < n_vis ? s[n][r] : -INFINITY;
         }
         acc.follow(s, scale);
+        Transposed<T> v[NS];
+#pragma unroll
+        for (int n = 0; n < NS; ++n) v[n] = transposed<T, TILE>(sV + buf * kBytes, kg * KT + 32 * n, c, h);
+        reads_first<8 * NS * kParts<T>, 0>();
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
             acc.weights(s[n], scale);
-            accumulate<T, TILE, false>(acc.o, sV + buf * kBytes, kg * KT + 32 * n, s[n], c, h);
+            accumulate<T, false>(acc.o, v[n], s[n]);
         }
         if (look) {
             int any = 0;
