@@ -206,8 +206,7 @@ void packed_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pac
     constexpr int CH = 64 * sizeof(T) / 16;
     constexpr int NL = 32 * CH / 64;                   // chunks of a tile of 32 rows, to a lane
     constexpr int kBytes = kTileBytes<T, 32>;
-    constexpr int kRow = 68;                           // floats of a row of the join: 64, and 16 bytes against bank conflicts
-    constexpr int kJoinBytes = 4 * 32 * kRow * 4;
+    constexpr int kJoinBytes = 4 * 32 * kJoinRow * 4;
     __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kBytes > kJoinBytes ? 4 * kBytes : kJoinBytes];
     __shared__ float s_m[4][32], s_l[4][32];
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv, split = blockIdx.y;
@@ -287,7 +286,7 @@ void packed_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pac
     float* join = reinterpret_cast<float*>(lds);
     const float l = acc.l + swap_half(acc.l);
     if (h == 0) { s_m[wave][c] = acc.m; s_l[wave][c] = l; }
-    store_row(join + (wave * 32 + c) * kRow, acc.o, 1.f, h);
+    store_row(join + (wave * 32 + c) * kJoinRow, acc.o, 1.f, h);
     __syncthreads();
     // 8 threads of 8 elements to a row
     const int r = tid >> 3, e = (tid & 7) * 8;
@@ -303,7 +302,7 @@ void packed_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pac
         if (s_m[w][r] == kMaxInit && s_l[w][r] == 0.f) continue;       // (saw no key: its accumulators may hold 0 * NaN)
         const float a = fast_exp2(s_m[w][r] - m);
         sum = fmaf(s_l[w][r], a, sum);
-        const float* src = join + (w * 32 + r) * kRow + e;
+        const float* src = join + (w * 32 + r) * kJoinRow + e;
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = fmaf(src[i], a, o[i]);
     }
@@ -375,7 +374,9 @@ void packed_merge_kernel(const float* __restrict__ part_o, const float2* __restr
 }
 
 // Tiles before each 64 sequences, counted from the last (find_tile): of rows in work-group 0, of keys in work-group 1.  16 waves with 64
-// sequences each at a time.
+// sequences each at a time.  A call has fewer than 2^28 tiles (2^31 rows in tiles of 32, and one more to a sequence), but where offsets
+// decrease each sequence may claim all of its rows; sums stop at kMostTiles, so that they do not overflow and stay in order.
+constexpr int kMostTiles = 1 << 29;
 __global__ __launch_bounds__(1024)
 void packed_before_kernel(Packing p, int per_q, int per_k, int* __restrict__ q_before, int* __restrict__ k_before)
 {
@@ -386,14 +387,15 @@ void packed_before_kernel(Packing p, int per_q, int per_k, int* __restrict__ q_b
     int sum = 0;                                       // of all before these 16
     for (int g0 = 0, buf = 0; g0 < groups; g0 += 16, buf ^= 1) {
         const int g = g0 + wave;
-        const int n = wave_sum(g < groups ? seq_tiles(seq_range(p, p.B - 1 - 64 * g - lane), p.G, keys ? per_k : per_q, keys) : 0);
+        const int tiles = g < groups ? seq_tiles(seq_range(p, p.B - 1 - 64 * g - lane), p.G, keys ? per_k : per_q, keys) : 0;
+        const int n = wave_sum(tiles >> 6) >= kMostTiles >> 6 ? kMostTiles : wave_sum(tiles);    // (64 x 2^26 may be; the second sum then is not)
         if (lane == 0) s[buf][wave] = n;
         __syncthreads();
         int mine = sum, all = sum;
 #pragma unroll
         for (int w = 0; w < 16; ++w) {
-            if (w < wave) mine += s[buf][w];
-            all += s[buf][w];
+            if (w < wave) mine = min(mine + s[buf][w], kMostTiles);
+            all = min(all + s[buf][w], kMostTiles);
         }
         if (g < groups && lane == 0) out[g] = mine;
         sum = all;

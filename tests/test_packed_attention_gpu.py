@@ -247,6 +247,25 @@ def test_offsets_out_of_range_are_clamped():
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_decreasing_offsets_of_many_sequences(dtype):
+    """600 sequences of which every other claims all rows: together more tiles than there are work-groups.  The tensors are parts of
+    larger ones, and what lies around them stays as it was; the next call is as ever."""
+    T, B = 500, 600
+    host, dev, q_off, _ = _case(4, 2, [T], [T], dtype)
+    off = torch.tensor([0, T] * (B // 2) + [0], dtype=torch.int32, device="cuda")
+
+    def around(heads):
+        whole = torch.full((heads, T + 64, 64), 7.0, dtype=dtype, device="cuda")
+        return whole, whole[:, 32:32 + T]
+    (o_all, out), *grads = around(4), around(4), around(2), around(2)
+    _, lse = psa.dense_attn_packed_fwd(*dev[:3], off, causal=True, out=out, lse=True)
+    psa.dense_attn_packed_bwd(*dev[:3], out, lse, dev[3], off, causal=True, **{n: g[1] for n, g in zip(("dQ", "dK", "dV"), grads)})
+    for whole in (o_all, *(g[0] for g in grads)):
+        assert (whole[:, :32] == 7).all() and (whole[:, 32 + T:] == 7).all()
+    _check(host, dev, q_off, q_off, True)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_repeated_keys_and_fused_layout(dtype):
     """K and V of one head repeated by a stride of 0, and Q, K, V and their gradients inside [T, 3, H, 64] arrays."""
     T, H = 90, 4
