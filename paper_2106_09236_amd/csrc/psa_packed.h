@@ -170,8 +170,8 @@ struct RowAt {
     }
 };
 
-// Rows base .. base + n - 1 (n may be <= 0) of a head as a buffer: reads of rows behind them give zeros.  The base moves with the tile, so
-// that offsets into a long tensor stay small.
+// Rows base .. base + n - 1 (n <= 128, and may be <= 0) of a head as a buffer: reads of rows behind them give zeros.  The base moves with
+// the tile, so that offsets into a long tensor stay small: 127 rows of at most 2^22 elements are within 31 bits.
 template <typename T>
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rows(const T* base, int64_t row_stride, int n)
 {

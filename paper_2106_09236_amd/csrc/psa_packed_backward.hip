@@ -359,7 +359,8 @@ void dkv_few(unsigned char* lds, int hk, int x, Heads<const T> Q, Heads<const T>
     const int lr = lane / CH, ch = lane % CH;
     HeadOperand<T> k, v;
     if constexpr (kOneTile) {
-        const auto kb = tile_rows(K.at(hk, f.k0 + key0), K.row, f.nk - key0), vb = tile_rows(V.at(hk, f.k0 + key0), V.row, f.nk - key0);
+        const int n = min(32, f.nk - key0);
+        const auto kb = tile_rows(K.at(hk, f.k0 + key0), K.row, n), vb = tile_rows(V.at(hk, f.k0 + key0), V.row, n);
 #pragma unroll
         for (int i = 0; i < 32 * CH / 256; ++i) {
             const int r = (i * 256 + tid) / CH, kc4 = (i * 256 + tid) % CH;

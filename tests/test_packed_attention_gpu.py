@@ -128,6 +128,17 @@ def test_offsets_beyond_31_bits():
                                   torch.tensor([0, 2], dtype=torch.int32, device="cuda"))
 
 
+@pytest.mark.parametrize("lens", [[270], [40, 130]])
+def test_rows_far_apart_float32(lens):
+    """K and V with rows 16 MB apart: 270 rows are beyond 32 bits of bytes, 129 beyond 31."""
+    wide = 1 << 22
+    (Q, K, V, G), (Qd, Kd, Vd, Gd), q_off, k_off = _case(2, 1, lens, lens, torch.float32)
+    cache = torch.empty(k_off[-1], wide, device="cuda")
+    kv = cache[:, wide - 128:].unflatten(1, (2, 64))
+    kv[:, 0], kv[:, 1] = Kd[0], Vd[0]
+    _check((Q, K, V, G), (Qd, kv[:, :1].transpose(0, 1), kv[:, 1:].transpose(0, 1), Gd), q_off, k_off, True)
+
+
 def test_two_streams_at_once():
     """Calls on two streams, each with a workspace of its own, give what they give alone."""
     a = _case(8, 2, [1] * 9, [2000] * 9, torch.bfloat16)
