@@ -409,9 +409,13 @@ template <typename T, int TPR, int NV>
 static void norm_fwd_go(const void* X, const void* gamma, const void* beta, float eps, void* Y, float* mean, float* rstd,
                         int64_t rows, int cols, hipStream_t stream)
 {
-    const int64_t grid = (rows + kNormThreads / TPR - 1) / (kNormThreads / TPR);
-    norm_fwd_kernel<T, TPR, NV><<<(unsigned)grid, kNormThreads, 0, stream>>>(
-        static_cast<const T*>(X), static_cast<const T*>(gamma), static_cast<const T*>(beta), eps, static_cast<T*>(Y), mean, rstd, rows, cols);
+    constexpr int64_t kMost = (int64_t)(1 << 23) * (kNormThreads / TPR);       // rows of a launch, which has fewer than 2^32 threads
+    for (int64_t r0 = 0; r0 < rows; r0 += kMost) {
+        const int64_t n = rows - r0 < kMost ? rows - r0 : kMost, grid = (n + kNormThreads / TPR - 1) / (kNormThreads / TPR);
+        norm_fwd_kernel<T, TPR, NV><<<(unsigned)grid, kNormThreads, 0, stream>>>(
+            static_cast<const T*>(X) + r0 * cols, static_cast<const T*>(gamma), static_cast<const T*>(beta), eps, static_cast<T*>(Y) + r0 * cols,
+            mean ? mean + r0 : nullptr, rstd ? rstd + r0 : nullptr, n, cols);
+    }
 }
 template <typename T>
 static void norm_fwd_pick(const NormPlan& p, const void* X, const void* gamma, const void* beta, float eps, void* Y, float* mean,

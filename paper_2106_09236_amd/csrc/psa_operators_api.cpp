@@ -92,6 +92,7 @@ static int run_rotary(const psa_heads_t* Q, const psa_heads_t* K, int32_t H_kv, 
 }
 
 // ---- packed attention
+constexpr int64_t kMostGroups = (1 << 24) - 1;         // work-groups of 256 threads
 static int check_packed(const psa_packed_shape_t* s)
 {
     if (!s) return PSA_ERR_NULL;
@@ -99,10 +100,11 @@ static int check_packed(const psa_packed_shape_t* s)
     if (s->B < 1 || s->H < 1 || s->H_kv < 1 || s->T_q < 1 || s->T_k < 1 || s->D != kD || s->H % s->H_kv != 0) return PSA_ERR_SHAPE;
     if (s->B > (1 << 20) || s->H > 65535 || s->T_q > (1 << 28) || s->T_k > (1 << 28)) return PSA_ERR_SHAPE;
     if ((int64_t)s->T_q * (s->H / s->H_kv) > INT32_MAX - 65536) return PSA_ERR_SHAPE;
-    // work-groups of a launch: tiles of 32 rows at the least
-    if (((int64_t)s->T_q * (s->H / s->H_kv) / 32 + s->T_k / 32 + 2 * s->B) * s->H_kv > INT32_MAX) return PSA_ERR_SHAPE;
     // (the kernels hold scale * log2(e) in float32: 0 there would make NaN of a masked score)
     if ((s->causal != 0 && s->causal != 1) || !(s->scale >= 1e-30) || !(s->scale <= 1e30)) return PSA_ERR_ARG;
+    // a launch has fewer than 2^32 threads
+    const PackedBwdPlan b = make_packed_bwd_plan(*s);
+    if ((int64_t)make_packed_plan(*s).n_tile * s->H_kv > kMostGroups || ((int64_t)b.n_qtile + b.n_ktile) * s->H_kv > kMostGroups) return PSA_ERR_SHAPE;
     return PSA_OK;
 }
 static int check_offsets(const psa_packed_shape_t& s, const int32_t* qo, const int32_t* ko)

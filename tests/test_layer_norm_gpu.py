@@ -52,6 +52,19 @@ def test_many_rows(rows, cols):
         assert_within(g, w, e, what)
 
 
+def test_more_rows_than_one_launch_takes():
+    """2^28 + 77 rows of two columns (16 rows to a work-group of 256 threads: 2^32 threads), in place; the rows repeat every 1013."""
+    rows, period = (1 << 28) + 77, 1013
+    X, _, gamma, beta = _inputs(period, 2, torch.bfloat16, 9)
+    Xd = X.cuda().repeat((rows + period - 1) // period, 1)[:rows].contiguous()
+    psa.probsparse_layer_norm_fwd(Xd, gamma.cuda(), beta.cuda(), EPS, Y=Xd, stats=False)
+    y, _, _, e_y, _, _ = layer_norm(X, gamma, beta, EPS)
+    assert_within(Xd[:period], y, e_y, "Y")
+    whole = rows // period * period
+    assert (Xd[:whole].view(-1, period, 2) == Xd[:period]).all()
+    assert torch.equal(Xd[whole:], Xd[:rows - whole])
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("cols", [24, 600, 9000])
 def test_without_weights_and_in_place(cols, dtype):

@@ -118,6 +118,8 @@ def test_packed_attention_refusals(backward):
     for kw in (dict(B=0), dict(H=0), dict(H_kv=0), dict(H=3), dict(T_q=0), dict(T_k=0), dict(D=128), dict(H=70000, H_kv=1), dict(T_q=1 << 29)):
         assert call(shape=_packed(**kw)) == SHAPE, kw
     assert call(shape=_packed(H=64, H_kv=1, T_q=1 << 26)) == SHAPE           # rows of a key head beyond 31 bits
+    assert call(shape=_packed(B=1 << 20, H=64, H_kv=64, T_q=1 << 20, T_k=1 << 20)) == SHAPE      # 2^32 threads and more
+    assert call(shape=_packed(B=1 << 20, H=16, H_kv=4, T_q=1 << 20, T_k=1 << 20), n=0) == WORKSPACE
     assert call(shape=_packed(dtype=9)) == DTYPE
     for kw in (dict(causal=2), dict(causal=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(scale=1e-40), dict(scale=1e40)):
         assert call(shape=_packed(**kw)) == ARG, kw
