@@ -334,10 +334,10 @@ typedef enum psa_rotary_scaling {
 typedef struct psa_rotary {
     int32_t dim;                  /* even, 2 .. 64 */
     int32_t layout, scaling;      /* psa_rotary_layout_t, psa_rotary_scaling_t */
-    double  base, factor;         /* finite, > 0; base >= 1 */
+    double  base, factor;         /* finite, > 0, 1 / factor too; base >= 1 */
     double  original_length;      /* PSA_ROTARY_PARTS alone: finite, > 0 */
     double  fast_turns, slow_turns;   /* PSA_ROTARY_PARTS alone: finite, fast_turns > slow_turns */
-    double  magnitude;            /* finite, > 0 */
+    double  magnitude;            /* finite, > 0, in float32 too */
 } psa_rotary_t;
 
 /* The frequencies f_i in radians per position into freq[dim / 2] (HOST); no GPU needed. */

@@ -43,6 +43,8 @@ static int check_rotary(const psa_rotary_t& o)
     if (o.layout != PSA_ROTARY_HALF && o.layout != PSA_ROTARY_INTERLEAVED) return PSA_ERR_ARG;
     if (o.scaling < PSA_ROTARY_PLAIN || o.scaling > PSA_ROTARY_PARTS) return PSA_ERR_ARG;
     if (!positive(o.base) || o.base < 1.0 || !positive(o.factor) || !positive(o.magnitude)) return PSA_ERR_ARG;
+    // (a frequency beyond float64, or a magnitude beyond float32, would make infinities and NaN of every element)
+    if (!positive(1.0 / o.factor) || !positive((float)o.magnitude)) return PSA_ERR_ARG;
     if (o.scaling == PSA_ROTARY_BASE && o.dim > 2 && !positive(o.base * pow(o.factor, (double)o.dim / (o.dim - 2)))) return PSA_ERR_ARG;
     if (o.scaling == PSA_ROTARY_PARTS &&
         (!positive(o.original_length) || !isfinite(o.fast_turns) || !isfinite(o.slow_turns) || !(o.fast_turns > o.slow_turns))) return PSA_ERR_ARG;

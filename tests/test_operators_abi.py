@@ -43,7 +43,7 @@ def test_layer_norm_refusals():
 
 def test_rotary_options():
     bad = [dict(dim=0), dict(dim=3), dict(dim=66), dict(layout=2), dict(scaling=4), dict(base=0.5), dict(base=math.inf), dict(factor=0.0),
-           dict(factor=-1.0), dict(factor=math.nan), dict(magnitude=0.0), dict(magnitude=math.inf),
+           dict(factor=-1.0), dict(factor=math.nan), dict(magnitude=0.0), dict(magnitude=math.inf), dict(magnitude=1e39), dict(magnitude=1e-50), dict(factor=1e-310),
            dict(scaling=psa.ROTARY_PARTS), dict(scaling=psa.ROTARY_PARTS, original_length=100.0, fast_turns=1.0, slow_turns=1.0),
            dict(scaling=psa.ROTARY_BASE, dim=4, base=1e200, factor=1e100)]
     for kw in bad:
