@@ -380,7 +380,7 @@ int probsparse_rotary_bwd(const psa_heads_t* dQ_out, const psa_heads_t* dK_out, 
 typedef struct psa_packed_shape {
     int32_t B, H, H_kv;           /* sequences, at most 2^20; heads, H a multiple of H_kv */
     int32_t T_q, T_k;             /* rows of Q and of K and V, at most 2^28; T_q * (H / H_kv) <= 2^31 - 2^16.  Tiles of 128
-                                   * rows (of 32 where sequences have 64 or fewer on average) and of 128 keys, one more of
+                                   * rows (of 32 where sequences have 32 or fewer on average) and of 128 keys, one more of
                                    * each to a sequence, times H_kv: fewer than 2^24 (else PSA_ERR_SHAPE) */
     int32_t D;                    /* 64 */
     int32_t dtype;                /* psa_dtype_t */
