@@ -422,16 +422,18 @@ Packing make_packing(const psa_packed_shape_t& s, const int* q_offsets, const in
 bool packed_halves(const psa_packed_shape_t& s, int64_t wide) { return s.dtype == PSA_F32 && wide < 640 && s.T_k / s.B >= 400; }
 
 // Few rows or many?  A wave owns 32 rows either way.  Work-groups of 128 rows read K and V a quarter as often but leave waves idle
-// in sequences of fewer rows, and there must be enough of them; those of 32 rows divide the keys among their waves, which pays for 32 rows
-// and less with 100 keys and more.  32 | 128 rows, 4 or 8 heads: 256 sequences of 1 row and up to 4096 keys 50 | 61 us, 64 of 20 rows and 500
+// in sequences of fewer rows, and there must be enough of them, unless sequences are over in a step of 64 keys; those of 32 rows divide
+// the keys among their waves, which pays for 32 rows and less with 100 keys and more.  32 | 128 rows, 4 or 8 heads: 256 sequences of 1 row and up to 4096 keys 50 | 61 us, 64 of 20 rows and 500
 // to 2000 keys 26.7 | 32.5, 128 of 16 and 100 to 1000 float32 91 | 112; but 5000 of 1 to 40 rows, as many keys 181 | 140, 1000 of 20 to
-// 60 float32 113 | 67, 2000 of 30 to 64 114 | 65, 64 of 64 rows and 500 to 2000 keys 52 | 45.
+// 60 float32 113 | 67, 2000 of 30 to 64 114 | 65, 64 of 64 rows and 500 to 2000 keys 52 | 45.  Calls with few
+// work-groups: 50 sequences of 1 to 60 rows 7.1 | 5.9, one row and 20 keys 6.0 | 5.5, 4 of 30 float32 8.4 | 6.5, 20 of 20 to 100 7.5 | 7.2, but
+// 8 of 60 to 130 6.4 | 7.2 and in float32 9.8 | 12.0.
 PackedPlan make_packed_plan(const psa_packed_shape_t& s)
 {
     PackedPlan p{};
     const int64_t rows = (int64_t)s.T_q * (s.H / s.H_kv);
     const int64_t wide = (rows / 128 + s.B) * s.H_kv;
-    p.few = wide < 256 || (rows / s.B <= 32 && s.T_k / s.B >= 100);
+    p.few = s.T_k / s.B > 64 && (wide < 256 || (rows / s.B <= 32 && s.T_k / s.B >= 100));
     p.halves = !p.few && packed_halves(s, wide);
     p.rows = p.few ? 32 : 128;
     p.n_tile = (int)(rows / p.rows) + s.B;
