@@ -2,8 +2,9 @@
 // and d_t = G[t].out[t]:
 //   ds_tj = p_tj (G[t].V[j] - d_t),  dQ[t] = scale sum_j ds_tj K[j],  dK[j] = scale sum_t ds_tj Q[t],  dV[j] = sum_t p_tj G[t]
 // Two launches: dQ with a work-group's rows held and the keys passing by, which also leaves d_t and lse where the other finds them;
-// dK and dV with the keys held and the rows passing by.  (Small calls of float32 take one launch for both, and one before it for d_t.)  The scores and G.V are computed in both of the latter, seven products
-// where five would do if dQ were added up in memory by atomics, whose order would change the result.
+// dK and dV with the keys held and the rows passing by.  (Small calls of float32 take one launch for both, and one before it for
+// d_t; few keys that many rows read take one after them, which joins the parts of dK and dV.)  The scores and G.V are computed in both,
+// seven products where five would do if dQ were added up in memory by atomics, whose order would change the result.
 #include <type_traits>
 
 #include "psa_packed.h"
@@ -103,12 +104,13 @@ void packed_stats_kernel(Heads<const T> out, Heads<const T> dOut, const float* _
     }
 }
 
-// dK and dV of 128 keys: 4 waves of 32, tiles of 32 rows of Q and dOut through LDS.
+// dK and dV of 128 keys: 4 waves of 32, tiles of QT rows of Q and dOut through LDS.  Where few work-groups would pass many rows each (the
+// rows of all query heads of a group), blockIdx.y takes a part of the rows and leaves its sums in `part` [n_split, H_kv, T_k, 2, 64].
 template <typename T, int QT>
 __global__ __launch_bounds__(256, 2)
 void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, const float* __restrict__ stat_l,
                        const float* __restrict__ stat_d, Packing p, Heads<T> dK, Heads<T> dV, int H_kv, int causal, float scale,
-                       float scale_log2, int n_tile)
+                       float scale_log2, int n_tile, int n_split, float* __restrict__ part)
 {
     constexpr int CH = 64 * sizeof(T) / 16, NL = QT * CH / 256;
     constexpr int kBytes = kTileBytes<T, QT>;
@@ -118,11 +120,11 @@ void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Hea
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
     const SeqTile f = find_tile<128, true>(p, x);
     auto outside = [&] {
+        if (blockIdx.y != 0) return;
         zero_outside(dK, p.ko, p.B, p.Tk, hk, 1, x, n_tile, [](int, int) {});
         zero_outside(dV, p.ko, p.B, p.Tk, hk, 1, x, n_tile, [](int, int) {});
     };
     if (f.tile < 0) { outside(); return; }
-    const int n_rows = f.nq * p.G;
     const int shift = f.nk - f.nq + 1;
     // the first row that sees key j (rows are in the order of their queries)
     auto first_row = [&](int j) { return causal ? max(j - shift + 1, 0) * p.G : 0; };
@@ -142,7 +144,12 @@ void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Hea
     const int64_t stat0 = ((int64_t)hk * p.Tq + f.q0) * p.G;
     uint4 qr[NL], gr[NL];
     float lr = INFINITY, dr = 0.f;
-    int r0 = first_all / QT * QT;
+    int r0 = first_all / QT * QT, n_rows = f.nq * p.G;
+    if (n_split > 1) {                                 // this part's rows
+        const int steps = max((n_rows - r0 + QT - 1) / QT, 0), per = (steps + n_split - 1) / n_split * QT;
+        r0 = (int)min((int64_t)r0 + (int64_t)blockIdx.y * per, (int64_t)n_rows);
+        n_rows = (int)min((int64_t)r0 + per, (int64_t)n_rows);
+    }
     const int ch = tid % CH, dt = 256 / CH / p.G, dg = 256 / CH - dt * p.G;     // (the thread's next chunk is 256 / CH rows on)
     RowAt at(r0 + tid / CH, p.G);
     auto fetch = [&](int r0) {
@@ -214,8 +221,34 @@ void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Hea
     }
     outside();
     if (key >= f.nk) return;
+    if (n_split > 1) {
+        float* sums = part + (((int64_t)blockIdx.y * H_kv + hk) * p.Tk + f.k0 + key) * 128;
+        store_row(sums, dk, f.nk == 1 ? 0.f : 1.f, h);
+        store_row(sums + 64, dv, 1.f, h);
+        return;
+    }
     store_row(dK.at(hk, f.k0 + key), dk, f.nk == 1 ? 0.f : scale, h);       // (the weight of an only key is 1 whatever the scores are)
     store_row(dV.at(hk, f.k0 + key), dv, 1.f, h);
+}
+
+// The parts' sums, 4 elements to a thread, in the order of the parts; 8 keys to a work-group.  (Keys in no sequence have been cleared.)
+template <typename T>
+__global__ __launch_bounds__(256)
+void packed_join_keys_kernel(const float* __restrict__ part, int n_split, Packing p, Heads<T> dK, Heads<T> dV, int H_kv, float scale)
+{
+    const int64_t id = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+    const int e = threadIdx.x % 32 * 4;                // of dK's 64 elements, then dV's
+    if (id >= (int64_t)p.Tk * H_kv) return;
+    const int hk = (int)(id / p.Tk), key = (int)(id % p.Tk);
+    if (p.ko && (key < p.ko[0] || key >= p.ko[p.B])) return;
+    const float* src = part + id * 128 + e;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < n_split; ++s) {
+        const float4 x = *reinterpret_cast<const float4*>(src + (int64_t)s * H_kv * p.Tk * 128);
+        sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+    }
+    if (e < 64) store4(dK.at(hk, key) + e, make_float4(sum.x * scale, sum.y * scale, sum.z * scale, sum.w * scale));
+    else store4(dV.at(hk, key) + e - 64, sum);
 }
 
 // dQ of 128 rows: 4 waves of 32, tiles of 32 keys and values through LDS.
@@ -582,10 +615,20 @@ PackedBwdPlan make_packed_bwd_plan(const psa_packed_shape_t& s)
     p.few_q = wide < 256 && (one || s.T_k / s.B > 64);
     p.halves_q = !p.few_q && packed_halves(s, wide);
     p.few_k = (int64_t)(s.T_k / 128 + s.B) * s.H_kv < 300 && (one || rows / s.B > 64);
+    // Many rows to a key head (several heads, long sequences): 128 keys and a part of the rows each, towards two work-groups to a compute unit.
+    // 32 keys | so, with the join: 13 sequences of 539 to 1079, 4 heads to a key head, 57 | 38 us (towards three: 44), 8 of 1000 to 2000, 2 times
+    // 4, 116 | 92, one of 16000 838 | 450; float32 173 | 122.  But one of 1863, a head each, 31 | 34, 9 of 280, 2 to a key head, 11.6 | 20.
+    p.n_split = 1;
+    if (p.few_k && rows / s.B >= 2048) {
+        const int64_t wgs = (int64_t)(s.T_k / 128 + s.B) * s.H_kv, split = (511 + wgs) / wgs;
+        p.n_split = (int)(split < 16 ? split : 16);
+        p.few_k = 0;
+    }
     p.n_qtile = (int)(rows / (p.few_q ? 32 : 128)) + s.B;
     p.n_ktile = s.T_k / (p.few_k ? 32 : 128) + s.B;
     p.stat_bytes = ((size_t)s.T_q * s.H * sizeof(float) + 255) & ~(size_t)255;
-    p.total = 2 * (p.stat_bytes + packed_before_bytes(s.B));
+    p.off_part = 2 * (p.stat_bytes + packed_before_bytes(s.B));
+    p.total = p.off_part + (p.n_split > 1 ? (size_t)p.n_split * s.H_kv * s.T_k * 128 * sizeof(float) : 0);
     return p;
 }
 
@@ -615,8 +658,13 @@ static void packed_bwd_go(const PackedBwdPlan& p, const psa_packed_shape_t& s, c
             q, k, v, g, o, st, pk, dq, s.H_kv, s.causal, scale, scale_log2, p.n_qtile);
     if (p.few_k)
         packed_grads_few_kernel<T, true, false><<<n_k, 256, 0, stream>>>(q, k, v, g, o, st, pk, dq, dk, dv, s.H_kv, s.causal, scale, scale_log2, p.n_ktile, p.n_qtile);
-    else
-        packed_dkv_kernel<T, KT><<<n_k, 256, 0, stream>>>(q, k, v, g, st.l, st.d, pk, dk, dv, s.H_kv, s.causal, scale, scale_log2, p.n_ktile);
+    else {
+        float* part = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.off_part);
+        packed_dkv_kernel<T, KT><<<dim3(n_k, p.n_split), 256, 0, stream>>>(q, k, v, g, st.l, st.d, pk, dk, dv, s.H_kv, s.causal, scale, scale_log2, p.n_ktile,
+                                                                          p.n_split, part);
+        if (p.n_split > 1)
+            packed_join_keys_kernel<T><<<(unsigned)(((int64_t)s.T_k * s.H_kv + 7) / 8), 256, 0, stream>>>(part, p.n_split, pk, dk, dv, s.H_kv, scale);
+    }
 }
 hipError_t launch_packed_bwd(const PackedBwdPlan& p, const psa_packed_shape_t& s, const psa_heads_t& Q, const psa_heads_t& K, const psa_heads_t& V,
                              const int* q_offsets, const int* k_offsets, const psa_heads_t& out, const float* lse, const psa_heads_t& dOut,

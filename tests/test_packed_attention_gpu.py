@@ -109,6 +109,17 @@ def test_few_queries_of_many_keys_with_gradients(dtype):
     _check(*_case(16, 16, [40], [2500], dtype), True)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("H,H_kv,q_lens,k_lens", [
+    (8, 1, [700, 0, 1, 333], [700, 5, 1, 333]), (4, 1, [1500], [1500]), (6, 2, [1900, 260], [300, 40]), (64, 2, [1, 40, 511], [130, 300, 511]),
+    (2, 2, [2100], [2100])])
+def test_keys_of_many_rows(H, H_kv, q_lens, k_lens, causal, dtype):
+    """Few keys that many rows read, those of a group's heads together: the rows are divided among work-groups.  Sequences of one
+    key, without rows or without keys among them, and rows of no sequence before and behind."""
+    _check(*_case(H, H_kv, q_lens, k_lens, dtype, by_frame=causal, front=5, behind=40), causal)
+
+
 def test_offsets_beyond_31_bits():
     """K and V as columns of a cache whose rows are 8 MB apart: element offsets up to 2^32."""
     n, wide = 1024, 1 << 22
