@@ -189,6 +189,7 @@ struct PackedPlan {
 };
 PackedPlan make_packed_plan(const psa_packed_shape_t& s);
 bool packed_halves(const psa_packed_shape_t& s, int64_t wide);
+bool packed_enough(const psa_packed_shape_t& s, int64_t wide);
 hipError_t launch_packed(const PackedPlan& p, const psa_packed_shape_t& s, const psa_heads_t& Q, const psa_heads_t& K, const psa_heads_t& V,
                          const int* q_offsets, const int* k_offsets, const psa_heads_t& out, float* lse, void* workspace, hipStream_t stream);
 struct PackedBwdPlan { int few_q, halves_q, few_k, n_split, n_qtile, n_ktile; size_t stat_bytes, off_part, total; };

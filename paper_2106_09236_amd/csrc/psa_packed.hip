@@ -421,6 +421,11 @@ Packing make_packing(const psa_packed_shape_t& s, const int* q_offsets, const in
 // clips 17.6 | 21.6, 8 x 2048 64 | 83.)
 bool packed_halves(const psa_packed_shape_t& s, int64_t wide) { return s.dtype == PSA_F32 && wide < 640 && s.T_k / s.B >= 400; }
 
+// Enough work-groups of 128 rows (`wide` of them)?  Causal tiles differ in length, so more of them.  32 | 128 rows, bfloat16: 7146 keys, 4
+// heads to 2, 226 work-groups, 171 | 110 us, dQ 202 | 145; 5000, 158, 92 | 77 and 115 | 100 (float32 272 | 205, 361 | 263); 8 of 512, 160, 12.0 |
+// 11.9; causal: 12 of 300 to 700, 234, 15.3 | 14.6 and 24.1 | 17.9; one of 3000, 8 heads, 192, 41 | 46 and 50 | 59 (float32 107 | 120, 130 | 155).
+bool packed_enough(const psa_packed_shape_t& s, int64_t wide) { return wide >= (s.causal ? 224 : 152); }
+
 // Few rows or many?  A wave owns 32 rows either way.  Work-groups of 128 rows read K and V a quarter as often but leave waves idle
 // in sequences of fewer rows, and there must be enough of them, unless sequences are over in a step of 64 keys; those of 32 rows divide
 // the keys among their waves, which pays for 32 rows and less with 100 keys and more.  32 | 128 rows, 4 or 8 heads: 256 sequences of 1 row and up to 4096 keys 50 | 61 us, 64 of 20 rows and 500
@@ -433,7 +438,7 @@ PackedPlan make_packed_plan(const psa_packed_shape_t& s)
     PackedPlan p{};
     const int64_t rows = (int64_t)s.T_q * (s.H / s.H_kv);
     const int64_t wide = (rows / 128 + s.B) * s.H_kv;
-    p.few = s.T_k / s.B > 64 && (wide < 256 || (rows / s.B <= 32 && s.T_k / s.B >= 100));
+    p.few = s.T_k / s.B > 64 && (!packed_enough(s, wide) || (rows / s.B <= 32 && s.T_k / s.B >= 100));
     p.halves = !p.few && packed_halves(s, wide);
     p.rows = p.few ? 32 : 128;
     p.n_tile = (int)(rows / p.rows) + s.B;

@@ -605,15 +605,13 @@ PackedBwdPlan make_packed_bwd_plan(const psa_packed_shape_t& s)
 {
     PackedBwdPlan p{};
     const int64_t rows = (int64_t)s.T_q * (s.H / s.H_kv);
-    // enough work-groups of 128 for every compute unit?  (bfloat16, 128 | 32: dQ of 24 ragged clips of 435 frames, 374 work-groups, 20.5 |
-    // 25.3 us, of 2 clips, 32 of them, 15 | 7.5; dK and dV, whose work-groups differ more in length, at 210 of them 48 | 26 us, at 280
-    // 36.9 | 31.4, at 320 23.6 | 28.9; float32 alike: 210: 168 | 107 us.)
-    // Not in bfloat16 where the other axis is over in a step of 64: 50 sequences of 1 to 60 frames, 4 heads, 32 | 128: dQ 8.8 | 6.5, dK and dV
+    // dQ: enough work-groups of 128 rows, as in the forward.  (24 ragged clips of 435 frames, 374 work-groups, 128 | 32: 20.5 | 25.3 us, 2 clips,
+    // 32 of them, 15 | 7.5.)  dK and dV, whose work-groups differ more in length: at 210 of them 48 | 26 us, at 280 36.9 | 31.4, at 320
+    // 23.6 | 28.9, float32 at 210 168 | 107.
+    // 32 not in bfloat16 where the other axis is over in a step of 64: 50 sequences of 1 to 60 frames, 4 heads, 32 | 128: dQ 8.8 | 6.5, dK and dV
     // 7.4 | 6.1 us; 8 of 60 to 130: 7.9 | 8.9 and 6.6 | 8.0.  (float32, one launch for both: 17.0 and 3.1 for d | 22.6)
     const int64_t wide = (rows / 128 + s.B) * s.H_kv;
-    const bool one = s.dtype == PSA_F32;
-    p.few_q = wide < 256 && (one || s.T_k / s.B > 64);
-    p.halves_q = !p.few_q && packed_halves(s, wide);
+    const bool one = s.dtype == PSA_F32;               // (may take one launch for both)
     p.few_k = (int64_t)(s.T_k / 128 + s.B) * s.H_kv < 300 && (one || rows / s.B > 64);
     // Many rows to a key head (several heads, long sequences): 128 keys and a part of the rows each, towards two work-groups to a compute unit.
     // 32 keys | so, with the join: 13 sequences of 539 to 1079, 4 heads to a key head, 57 | 38 us (towards three: 44), 8 of 1000 to 2000, 2 times
@@ -624,6 +622,8 @@ PackedBwdPlan make_packed_bwd_plan(const psa_packed_shape_t& s)
         p.n_split = (int)(split < 16 ? split : 16);
         p.few_k = 0;
     }
+    p.few_q = one && p.few_k ? wide < 256 : !packed_enough(s, wide) && s.T_k / s.B > 64;
+    p.halves_q = !p.few_q && packed_halves(s, wide);
     p.n_qtile = (int)(rows / (p.few_q ? 32 : 128)) + s.B;
     p.n_ktile = s.T_k / (p.few_k ? 32 : 128) + s.B;
     p.stat_bytes = ((size_t)s.T_q * s.H * sizeof(float) + 255) & ~(size_t)255;
