@@ -229,11 +229,14 @@ __device__ __forceinline__ void clear(floatx16& a)
 // products take 3/8 of the time of one on the float32 matrix unit (1024 against 64 flops a cycle of a SIMD).
 template <typename T> constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
 
-// x0, x1 into parts (pairs of bfloat16, low half first); the remainders are exact.  (A two-term dot product of the pair with (-1, 0) and (0, -1)
+// x0, x1 into parts (pairs of bfloat16, low half first); the remainders are exact.  Finite numbers beyond the largest of bfloat16 would round to
+// an infinity, whose remainders are an infinity and NaN: the first part is at most that largest and the others have the rest, 2^-8 of
+// it at the most (24 ragged clips of 435, forward and backward, 152 -> 157 us).  (A two-term dot product of the pair with (-1, 0) and (0, -1)
 // forms them in one instruction instead of two, on the matrix unit's time: 16 x 512 float32 35.6 | 34.4 us.)
 __device__ __forceinline__ void split_pair(float x0, float x1, uint32_t (&part)[3])
 {
-    part[0] = cvt_pk_bf16(x0, x1);
+    constexpr float kMost = 0x1.FEp127f;
+    part[0] = cvt_pk_bf16(__builtin_amdgcn_fmed3f(x0, -kMost, kMost), __builtin_amdgcn_fmed3f(x1, -kMost, kMost));
     x0 -= bf16_lo(part[0]); x1 -= bf16_hi(part[0]);
     part[1] = cvt_pk_bf16(x0, x1);
     x0 -= bf16_lo(part[1]); x1 -= bf16_hi(part[1]);
