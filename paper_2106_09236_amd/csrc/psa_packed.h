@@ -16,6 +16,7 @@
 namespace psa {
 
 typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -179,22 +180,31 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rows(const T* base, int64
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, bytes, 0x00020000);
 }
 
-// Any infinity or NaN among the elements of 16 bytes?
-__device__ __forceinline__ bool nonfinite(const uint4& x, float)
+// Any infinity or NaN among the elements of N times 16 bytes?  (bfloat16: the largest of them without their signs, two at a time; 32 streams of one
+// new frame, the test in every tile instead of the last, 16.5 -> 16.9 us, with a test of each element 17.7.)
+template <int N>
+__device__ __forceinline__ bool nonfinite(const uint4 (&x)[N], float)
 {
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
     bool b = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) b |= (w[i] & 0x7F800000u) == 0x7F800000u;
+    for (int k = 0; k < N; ++k) {
+        const uint32_t w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b |= (w[i] & 0x7F800000u) == 0x7F800000u;
+    }
     return b;
 }
-__device__ __forceinline__ bool nonfinite(const uint4& x, bf16_t)
+template <int N>
+__device__ __forceinline__ bool nonfinite(const uint4 (&x)[N], bf16_t)
 {
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    bool b = false;
+    ushortx2 most = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) b |= (w[i] & 0x7F80u) == 0x7F80u || (w[i] & 0x7F800000u) == 0x7F800000u;
-    return b;
+    for (int k = 0; k < N; ++k) {
+        const uint32_t w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(ushortx2, w[i] & 0x7FFF7FFFu));
+    }
+    return most.x >= 0x7F80 || most.y >= 0x7F80;
 }
 __device__ __forceinline__ uint4 finite_only(const uint4& x, float)
 {

@@ -122,10 +122,7 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
         // some row sees in part they are left out and added afterwards (float32: in all, since an infinity has no parts)
         const bool look = sizeof(T) == 4 || j0 + TILE > n_every;
         if (look) {
-            bool bad = false;
-#pragma unroll
-            for (int i = 0; i < NL; ++i) bad |= nonfinite(vr[i], T{});
-            const bool any = __builtin_amdgcn_ballot_w64(bad) != 0;
+            const bool any = __builtin_amdgcn_ballot_w64(nonfinite(vr, T{})) != 0;
             if (lane == 0) s_bad[buf][wave] = any;
             if (any)
 #pragma unroll
@@ -250,17 +247,12 @@ void packed_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pac
     int j0 = (split * per + wave) * 32;
     if (j0 < end) fetch(j0);
     for (; j0 < end; j0 += 128) {
-        const bool part = j0 + 32 > n_every, look = sizeof(T) == 4 || part;
-        bool any = false;
-        if (look) {
-            bool bad = false;
+        // infinities and NaN of V are left out of the product and added afterwards, in whole tiles too: the weights have parts of either
+        // sign and of 0
+        const bool any = __builtin_amdgcn_ballot_w64(nonfinite(vn, T{})) != 0;
+        if (any)
 #pragma unroll
-            for (int i = 0; i < NL; ++i) bad |= nonfinite(vn[i], T{});
-            any = __builtin_amdgcn_ballot_w64(bad) != 0;
-            if (any)
-#pragma unroll
-                for (int i = 0; i < NL; ++i) vn[i] = finite_only(vn[i], T{});
-        }
+            for (int i = 0; i < NL; ++i) vn[i] = finite_only(vn[i], T{});
         wave_lds_sync();
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
@@ -271,7 +263,7 @@ void packed_few_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pac
         s[0] = product(kn, q);
         wave_lds_sync();
         if (j0 + 128 < end) fetch(j0 + 128);
-        if (part) {
+        if (j0 + 32 > n_every) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[0][r] = j0 + acc_row(r, h) < n_vis ? s[0][r] : -INFINITY;
         }

@@ -1,4 +1,4 @@
-"""Packed attention at the ends of the number range: the largest float32 numbers."""
+"""Packed attention at the ends of the number range: the largest float32 numbers, and infinities of V wherever they stand."""
 import pytest
 import torch
 
@@ -81,3 +81,24 @@ def test_largest_numbers_that_are_seen(H, H_kv, q_lens, k_lens, which):
         elif empty.any():
             got, w, bound = got.masked_fill(empty, 0.0), w.masked_fill(empty, 0.0), bound.masked_fill(empty, 1.0)
         assert_within(got, w, bound, what)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("H,H_kv,q_lens,k_lens", [(4, 2, [3, 2], [300, 200]), (4, 2, [1], [3000]), (4, 2, [20, 6], [40, 6]),
+                                                  (32, 32, [500, 401, 390], [500, 401, 390])])
+def test_infinite_value_wherever_it_stands(H, H_kv, q_lens, k_lens, causal, dtype):
+    """An infinity in one element of the first key, which every query of its sequence sees, is that element of their outputs; the other
+    elements and the other sequences stay as they are."""
+    q_off, k_off = _offsets(q_lens), _offsets(k_lens)
+    Q, K, V, _ = (t.cuda() for t in _tensors(H, H_kv, q_off[-1], k_off[-1], dtype, 5))
+    qo, ko = _device_offsets(q_off, k_off)
+    clean = psa.dense_attn_packed_fwd(Q, K, V, qo, ko, causal=causal)
+    for value in (float("inf"), -float("inf"), float("nan")):
+        V2 = V.clone()
+        V2[:, 0, 5] = value
+        out = psa.dense_attn_packed_fwd(Q, K, V2, qo, ko, causal=causal)
+        hit = out[:, :q_off[1], 5].float()
+        assert (hit.isnan() if value != value else hit == value).all()
+        out[:, :q_off[1], 5] = clean[:, :q_off[1], 5]
+        assert torch.equal(out, clean)
