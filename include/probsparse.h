@@ -372,9 +372,13 @@ int probsparse_rotary_bwd(const psa_heads_t* dQ_out, const psa_heads_t* dK_out, 
  *             is touched); both NULL: one sequence of all rows (B = 1)
  *   Q, out    H heads of T_q rows;  K, V: H_kv heads of T_k rows; batch_stride is ignored
  *   lse       [H, T_q] float32 DEVICE, or NULL
- * Arithmetic: bfloat16 operands are multiplied exactly and summed in float32; the weights p are
- * rounded to bfloat16 before they are multiplied with V (calls with few rows: kept to 16 bits).
- * float32 operands are multiplied as sums of three bfloat16 parts each (error 2^-23 of |a||b| at
+ * Arithmetic: bfloat16 operands are multiplied exactly and summed in float32.  The weights p are
+ * kept to 16 bits before they are multiplied with V in small calls and rounded to bfloat16 in
+ * large ones, where 16 bits would take 1.3 to 1.5 times as long: the error of out then is up to
+ * 1.45 times that of its own rounding.  With W = (T_q * (H / H_kv) / 128 + B) * H_kv (divisions
+ * of integers) a call is small if W < 152 (causal: 224), if W <= 512 and T_k / B <= 64, or if
+ * T_q * (H / H_kv) / B <= 32 and T_k / B >= 100 (few new queries of longer sequences).  float32
+ * operands are multiplied as sums of three bfloat16 parts each (error 2^-23 of |a||b| at
  * the most, 2^-25 as a rule) and summed in float32; an infinity has no such parts, so that one in
  * Q or K makes the scores it takes part in NaN.  Softmax statistics are float32. */
 typedef struct psa_packed_shape {
@@ -396,9 +400,10 @@ int dense_attn_packed_fwd(const psa_heads_t* Q, const psa_heads_t* K, const psa_
  * d_t = sum_e G[t, e] out[t, e] and ds_tj = p_tj (G[t].V[j] - d_t):
  *   dQ[t] = scale * sum_j ds_tj K[j],  dK[j] = scale * sum_t ds_tj Q[t],  dV[j] = sum_t p_tj G[t]
  * the sums over t also over the query heads that share the key head.  Every element of dQ, dK
- * and dV is written; rows in no sequence get zeros.  p and ds are rounded to bfloat16 before
- * they are multiplied where the tensors are bfloat16 (calls with few rows or keys: kept to 16
- * bits), and d is corrected for the rounding of out.  The order of all sums is fixed.
+ * and dV is written; rows in no sequence get zeros.  bfloat16: p and ds are kept to 16 bits or
+ * rounded as in the forward, for dQ by its first two rules, for dK and dV kept if N < 300 or if
+ * N <= 512 and T_q * (H / H_kv) / B <= 64, with N = (T_k / 128 + B) * H_kv; and d is corrected
+ * for the rounding of out.  The order of all sums is fixed.
  * Infinities and NaN stay within the gradients of their own sequence. */
 size_t dense_attn_packed_bwd_workspace_bytes(const psa_packed_shape_t* shape);
 int dense_attn_packed_bwd(const psa_heads_t* Q, const psa_heads_t* K, const psa_heads_t* V,

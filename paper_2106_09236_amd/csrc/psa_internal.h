@@ -180,19 +180,21 @@ hipError_t launch_rotary(const psa_heads_t* Q, const psa_heads_t* K, int H_kv, c
 
 // Dense attention over packed sequences (psa_packed.hip, psa_packed_backward.hip).
 //   halves   1: two waves to 32 rows, each with half of the keys
+//   fine     1: bfloat16 weights in two parts
 //   few      1: the waves of a work-group share 32 rows and divide its keys; 0: each wave has rows of its own
 //   n_tile   work-groups along the rows of a key head (rows of one token for each head of its group), an upper bound
 //   n_split  parts of the keys, joined by a second kernel where there are several
 struct PackedPlan {
-    int few, halves, rows, n_tile, n_split;
+    int few, halves, fine, rows, n_tile, n_split;
     size_t off_ml, off_part, total;
 };
 PackedPlan make_packed_plan(const psa_packed_shape_t& s);
 bool packed_halves(const psa_packed_shape_t& s, int64_t wide);
 bool packed_enough(const psa_packed_shape_t& s, int64_t wide);
+bool packed_fine(const psa_packed_shape_t& s, int64_t wide);
 hipError_t launch_packed(const PackedPlan& p, const psa_packed_shape_t& s, const psa_heads_t& Q, const psa_heads_t& K, const psa_heads_t& V,
                          const int* q_offsets, const int* k_offsets, const psa_heads_t& out, float* lse, void* workspace, hipStream_t stream);
-struct PackedBwdPlan { int few_q, halves_q, few_k, n_split, n_qtile, n_ktile; size_t stat_bytes, off_part, total; };
+struct PackedBwdPlan { int few_q, halves_q, fine_q, few_k, fine_k, n_split, n_qtile, n_ktile; size_t stat_bytes, off_part, total; };
 PackedBwdPlan make_packed_bwd_plan(const psa_packed_shape_t& s);
 hipError_t launch_packed_bwd(const PackedBwdPlan& p, const psa_packed_shape_t& s, const psa_heads_t& Q, const psa_heads_t& K, const psa_heads_t& V,
                              const int* q_offsets, const int* k_offsets, const psa_heads_t& out, const float* lse, const psa_heads_t& dOut,

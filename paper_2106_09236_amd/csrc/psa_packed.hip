@@ -62,8 +62,10 @@ struct Rows32 {
 // (430), the scores of a step formed between the weights of the one before (440), priorities (no change).
 //
 // KW = 2 (float32): 8 waves, two to 32 rows, which take alternate tiles of KT keys and join their sums in LDS; see packed_halves().
-template <typename T, int KT, int KW>
-__global__ __launch_bounds__(256 * KW, sizeof(T) == 4 ? 2 : 3)
+//
+// FINE: bfloat16 weights in two parts (packed_fine()).  Infinities of V are left out of every tile then: one times a part of the other sign is NaN.
+template <typename T, int KT, int KW, bool FINE>
+__global__ __launch_bounds__(256 * KW, sizeof(T) == 4 || FINE ? 2 : 3)
 void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Packing p, Heads<T> out, float* __restrict__ lse,
                         int H_kv, int causal, float scale, int n_tile)
 {
@@ -120,7 +122,7 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
     for (int j0 = 0; j0 < n_all; j0 += TILE, buf ^= 1) {
         // a weight of 0 does not keep an infinity or NaN of a value that a row does not see out of its sum: in tiles that
         // some row sees in part they are left out and added afterwards (float32: in all, since an infinity has no parts)
-        const bool look = sizeof(T) == 4 || j0 + TILE > n_every;
+        const bool look = sizeof(T) == 4 || FINE || j0 + TILE > n_every;
         if (look) {
             const bool any = __builtin_amdgcn_ballot_w64(nonfinite(vr, T{})) != 0;
             if (lane == 0) s_bad[buf][wave] = any;
@@ -156,7 +158,7 @@ void packed_rows_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Pa
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
             acc.weights(s[n], scale);
-            accumulate<T, false>(acc.o, v[n], s[n]);
+            accumulate<T, FINE>(acc.o, v[n], s[n]);
         }
         if (look) {
             int any = 0;
@@ -418,6 +420,12 @@ bool packed_halves(const psa_packed_shape_t& s, int64_t wide) { return s.dtype =
 // 11.9; causal: 12 of 300 to 700, 234, 15.3 | 14.6 and 24.1 | 17.9; one of 3000, 8 heads, 192, 41 | 46 and 50 | 59 (float32 107 | 120, 130 | 155).
 bool packed_enough(const psa_packed_shape_t& s, int64_t wide) { return wide >= (s.causal ? 224 : 152); }
 
+// bfloat16 weights of rows: in two parts, 16 bits, unless the matrix and vector units are what the call waits for; rounded once they cost a
+// result as much as its own rounding.  Once | two parts: 50 sequences of 1 to 60 rows, 4 heads, 7.0 | 6.8 us and with the backward 19.8 | 20.0, 100
+// of them 7.3 | 7.5 and 22.0 | 23.7, one row and 20 keys 7.2 | 6.8, 20 of 20 to 100 7.3 | 7.5; but 5000 of 1 to 40 rows 150 | 217 and 594 | 684, 32 clips of 40 to 500 frames
+// 17.7 | 24.7, 16384 causal 354 | 515, 8 x 2048 causal with the backward 234 | 302.
+bool packed_fine(const psa_packed_shape_t& s, int64_t wide) { return !packed_enough(s, wide) || (wide <= 512 && s.T_k / s.B <= 64); }
+
 // Few rows or many?  A wave owns 32 rows either way.  Work-groups of 128 rows read K and V a quarter as often but leave waves idle
 // in sequences of fewer rows, and there must be enough of them, unless sequences are over in a step of 64 keys; those of 32 rows divide
 // the keys among their waves, which pays for 32 rows and less with 100 keys and more.  32 | 128 rows, 4 or 8 heads: 256 sequences of 1 row and up to 4096 keys 50 | 61 us, 64 of 20 rows and 500
@@ -432,6 +440,7 @@ PackedPlan make_packed_plan(const psa_packed_shape_t& s)
     const int64_t wide = (rows / 128 + s.B) * s.H_kv;
     p.few = s.T_k / s.B > 64 && (!packed_enough(s, wide) || (rows / s.B <= 32 && s.T_k / s.B >= 100));
     p.halves = !p.few && packed_halves(s, wide);
+    p.fine = p.few || packed_fine(s, wide);
     p.rows = p.few ? 32 : 128;
     p.n_tile = (int)(rows / p.rows) + s.B;
     p.n_split = 1;
@@ -466,7 +475,8 @@ static void packed_go(const PackedPlan& p, const psa_packed_shape_t& s, const ps
     const dim3 grid((unsigned)(p.n_tile * s.H_kv), (unsigned)p.n_split);
     if (!p.few) {
         constexpr int KW = sizeof(T) == 4 ? 2 : 1;
-        (p.halves ? packed_rows_kernel<T, KT, KW> : packed_rows_kernel<T, KT, 1>)<<<grid, p.halves ? 512 : 256, 0, stream>>>(
+        constexpr bool FINE = sizeof(T) == 2;
+        (p.halves ? packed_rows_kernel<T, KT, KW, false> : p.fine ? packed_rows_kernel<T, KT, 1, FINE> : packed_rows_kernel<T, KT, 1, false>)<<<grid, p.halves ? 512 : 256, 0, stream>>>(
             heads_of<const T>(Q), heads_of<const T>(K), heads_of<const T>(V), pk, heads_of<T>(out), lse, s.H_kv, s.causal, scale, p.n_tile);
         return;
     }

@@ -106,7 +106,8 @@ void packed_stats_kernel(Heads<const T> out, Heads<const T> dOut, const float* _
 
 // dK and dV of 128 keys: 4 waves of 32, tiles of QT rows of Q and dOut through LDS.  Where few work-groups would pass many rows each (the
 // rows of all query heads of a group), blockIdx.y takes a part of the rows and leaves its sums in `part` [n_split, H_kv, T_k, 2, 64].
-template <typename T, int QT>
+// FINE: bfloat16 weights in two parts.
+template <typename T, int QT, bool FINE>
 __global__ __launch_bounds__(256, 2)
 void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, const float* __restrict__ stat_l,
                        const float* __restrict__ stat_d, Packing p, Heads<T> dK, Heads<T> dV, int H_kv, int causal, float scale,
@@ -202,8 +203,8 @@ void packed_dkv_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Hea
                 for (int i = 0; i < 16; ++i)
                     if (r + acc_row(i, h) < first) s[i] = w[i] = 0.f;
             }
-            accumulate<T, QT, false>(dv, sG[buf], 32 * n, s, c, h);
-            accumulate<T, QT, false>(dk, sQ[buf], 32 * n, w, c, h);
+            accumulate<T, QT, FINE>(dv, sG[buf], 32 * n, s, c, h);
+            accumulate<T, QT, FINE>(dk, sQ[buf], 32 * n, w, c, h);
         }
     };
     int parity = 0;
@@ -252,7 +253,7 @@ void packed_join_keys_kernel(const float* __restrict__ part, int n_split, Packin
 }
 
 // dQ of 128 rows: 4 waves of 32, tiles of 32 keys and values through LDS.
-template <typename T, int KT, int KW>
+template <typename T, int KT, int KW, bool FINE>
 __global__ __launch_bounds__(256 * KW, 2)
 void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, Heads<const T> out, Stats stats, Packing p,
                       Heads<T> dQ, int H_kv, int causal, float scale, float scale_log2, int n_tile)
@@ -324,7 +325,7 @@ void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Head
                 for (int r = 0; r < 16; ++r)
                     if (j + acc_row(r, h) >= n_vis) s[r] = w[r] = 0.f;
             }
-            grad.template add<TILE, false>(s, w, sK + buf * kBytes, in, c, h);
+            grad.template add<TILE, FINE>(s, w, sK + buf * kBytes, in, c, h);
         }
     }
     outside();                                         // (last: its loads would delay the others)
@@ -612,7 +613,12 @@ PackedBwdPlan make_packed_bwd_plan(const psa_packed_shape_t& s)
     // 7.4 | 6.1 us; 8 of 60 to 130: 7.9 | 8.9 and 6.6 | 8.0.  (float32, one launch for both: 17.0 and 3.1 for d | 22.6)
     const int64_t wide = (rows / 128 + s.B) * s.H_kv;
     const bool one = s.dtype == PSA_F32;               // (may take one launch for both)
-    p.few_k = (int64_t)(s.T_k / 128 + s.B) * s.H_kv < 300 && (one || rows / s.B > 64);
+    p.fine_q = packed_fine(s, wide);
+    // 16 bits to the weights of dK and dV in small calls, as in the forward, and wherever few keys are read by many rows: once | two parts, with the
+    // rest of the call, 13 of 539 to 1079 below 85 | 92 us, 8 of 1000 to 2000 171 | 193, one of 16000 957 | 1135.
+    const int64_t wide_k = (int64_t)(s.T_k / 128 + s.B) * s.H_kv;
+    p.fine_k = wide_k < 300 || (wide_k <= 512 && rows / s.B <= 64);
+    p.few_k = wide_k < 300 && (one || rows / s.B > 64);
     // Many rows to a key head (several heads, long sequences): 128 keys and a part of the rows each, towards two work-groups to a compute unit.
     // 32 keys | so, with the join: 13 sequences of 539 to 1079, 4 heads to a key head, 57 | 38 us (towards three: 44), 8 of 1000 to 2000, 2 times
     // 4, 116 | 92, one of 16000 838 | 450; float32 173 | 122.  But one of 1863, a head each, 31 | 34, 9 of 280, 2 to a key head, 11.6 | 20.
@@ -643,6 +649,7 @@ static void packed_bwd_go(const PackedBwdPlan& p, const psa_packed_shape_t& s, c
     const auto dq = heads_of<T>(dQ), dk = heads_of<T>(dK), dv = heads_of<T>(dV);
     const unsigned n_k = (unsigned)(p.n_ktile * s.H_kv), n_q = (unsigned)(p.n_qtile * s.H_kv);
     constexpr int KT = sizeof(T) == 4 ? 32 : 64, KW = sizeof(T) == 4 ? 2 : 1;
+    constexpr bool FINE = sizeof(T) == 2;
     if constexpr (sizeof(T) == 4) {
         if (p.few_k && p.few_q) {
             constexpr int rows = 256 / (64 / kVec<T>);
@@ -654,13 +661,13 @@ static void packed_bwd_go(const PackedBwdPlan& p, const psa_packed_shape_t& s, c
     if (p.few_q)
         packed_grads_few_kernel<T, false, true><<<n_q, 256, 0, stream>>>(q, k, v, g, o, st, pk, dq, dk, dv, s.H_kv, s.causal, scale, scale_log2, p.n_ktile, p.n_qtile);
     else
-        (p.halves_q ? packed_dq_kernel<T, KT, KW> : packed_dq_kernel<T, KT, 1>)<<<n_q, p.halves_q ? 512 : 256, 0, stream>>>(
+        (p.halves_q ? packed_dq_kernel<T, KT, KW, false> : p.fine_q ? packed_dq_kernel<T, KT, 1, FINE> : packed_dq_kernel<T, KT, 1, false>)<<<n_q, p.halves_q ? 512 : 256, 0, stream>>>(
             q, k, v, g, o, st, pk, dq, s.H_kv, s.causal, scale, scale_log2, p.n_qtile);
     if (p.few_k)
         packed_grads_few_kernel<T, true, false><<<n_k, 256, 0, stream>>>(q, k, v, g, o, st, pk, dq, dk, dv, s.H_kv, s.causal, scale, scale_log2, p.n_ktile, p.n_qtile);
     else {
         float* part = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.off_part);
-        packed_dkv_kernel<T, KT><<<dim3(n_k, p.n_split), 256, 0, stream>>>(q, k, v, g, st.l, st.d, pk, dk, dv, s.H_kv, s.causal, scale, scale_log2, p.n_ktile,
+        (p.fine_k ? packed_dkv_kernel<T, KT, FINE> : packed_dkv_kernel<T, KT, false>)<<<dim3(n_k, p.n_split), 256, 0, stream>>>(q, k, v, g, st.l, st.d, pk, dk, dv, s.H_kv, s.causal, scale, scale_log2, p.n_ktile,
                                                                           p.n_split, part);
         if (p.n_split > 1)
             packed_join_keys_kernel<T><<<(unsigned)(((int64_t)s.T_k * s.H_kv + 7) / 8), 256, 0, stream>>>(part, p.n_split, pk, dk, dv, s.H_kv, scale);
