@@ -96,48 +96,51 @@ void norm_fwd_kernel(const T* X, const T* __restrict__ gamma, const T* __restric
     }
 }
 
-// Rows of any length, a work-group each: the row is read again for each step instead of kept.
+// Rows of any length, a work-group each: the row is read again for each step instead of kept.  kNormLongGroups work-groups at the most, which take
+// several rows then: a launch has fewer than 2^32 threads.
+constexpr int kNormLongGroups = 1 << 17;
 template <typename T>
 __global__ __launch_bounds__(kNormThreads)
 void norm_fwd_long_kernel(const T* X, const T* __restrict__ gamma, const T* __restrict__ beta, float eps,
-                          T* Y, float* __restrict__ mean_out, float* __restrict__ rstd_out, int cols)
+                          T* Y, float* __restrict__ mean_out, float* __restrict__ rstd_out, int64_t rows, int cols)
 {
     constexpr int VEC = kVec<T>;
     __shared__ float s[8];
-    const int64_t row = blockIdx.x;
-    const T* x = X + row * cols;
-    float v[VEC];
-    float sum[1] = {0.f};
-    for (int c = threadIdx.x * VEC; c < cols; c += kNormThreads * VEC) {
-        load_vec(v, x + c, cols - c);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) sum[0] += v[i];
-    }
-    row_sum<kNormThreads>(sum, s);
     const float inv = 1.f / (float)cols;
-    const float m0 = sum[0] * inv;
-    float dev[2] = {0.f, 0.f};
-    for (int c = threadIdx.x * VEC; c < cols; c += kNormThreads * VEC) {
-        load_vec(v, x + c, cols - c);
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const T* x = X + row * cols;
+        float v[VEC];
+        float sum[1] = {0.f};
+        for (int c = threadIdx.x * VEC; c < cols; c += kNormThreads * VEC) {
+            load_vec(v, x + c, cols - c);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i)
-            if (c + i < cols) { const float d = v[i] - m0; dev[0] += d; dev[1] += d * d; }
-    }
-    row_sum<kNormThreads>(dev, s);
-    const float off = dev[0] * inv;
-    const float rstd = 1.f / sqrtf(fmaxf(dev[1] * inv - off * off, 0.f) + eps);
-    if (threadIdx.x == 0 && mean_out) { mean_out[row] = m0 + off; rstd_out[row] = rstd; }
-    T* y = Y + row * cols;
-    for (int c = threadIdx.x * VEC; c < cols; c += kNormThreads * VEC) {
-        float g[VEC], b[VEC];
+            for (int i = 0; i < VEC; ++i) sum[0] += v[i];
+        }
+        row_sum<kNormThreads>(sum, s);
+        const float m0 = sum[0] * inv;
+        float dev[2] = {0.f, 0.f};
+        for (int c = threadIdx.x * VEC; c < cols; c += kNormThreads * VEC) {
+            load_vec(v, x + c, cols - c);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) { g[i] = 1.f; b[i] = 0.f; }
-        load_vec(v, x + c, cols - c);                  // (Y may be X: a thread reads what it writes)
-        if (gamma) load_vec(g, gamma + c, cols - c);
-        if (beta) load_vec(b, beta + c, cols - c);
+            for (int i = 0; i < VEC; ++i)
+                if (c + i < cols) { const float d = v[i] - m0; dev[0] += d; dev[1] += d * d; }
+        }
+        row_sum<kNormThreads>(dev, s);
+        const float off = dev[0] * inv;
+        const float rstd = 1.f / sqrtf(fmaxf(dev[1] * inv - off * off, 0.f) + eps);
+        if (threadIdx.x == 0 && mean_out) { mean_out[row] = m0 + off; rstd_out[row] = rstd; }
+        T* y = Y + row * cols;
+        for (int c = threadIdx.x * VEC; c < cols; c += kNormThreads * VEC) {
+            float g[VEC], b[VEC];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) v[i] = fmaf((v[i] - m0 - off) * rstd, g[i], b[i]);
-        store_vec(y + c, v, cols - c);
+            for (int i = 0; i < VEC; ++i) { g[i] = 1.f; b[i] = 0.f; }
+            load_vec(v, x + c, cols - c);              // (Y may be X: a thread reads what it writes)
+            if (gamma) load_vec(g, gamma + c, cols - c);
+            if (beta) load_vec(b, beta + c, cols - c);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = fmaf((v[i] - m0 - off) * rstd, g[i], b[i]);
+            store_vec(y + c, v, cols - c);
+        }
     }
 }
 
@@ -260,48 +263,49 @@ void norm_bwd_kernel(const T* __restrict__ dY, const T* __restrict__ X, const T*
     }
 }
 
-// Rows of any length: dX as above with the row read again, and the column sums in a kernel of their own.
+// Rows of any length: dX as above with the row read again (work-groups as in the forward), and the column sums in a kernel of their own.
 template <typename T>
 __global__ __launch_bounds__(kNormThreads)
 void norm_bwd_long_kernel(const T* __restrict__ dY, const T* __restrict__ X, const T* __restrict__ gamma, const float* __restrict__ mean,
-                          float* __restrict__ off_out, const float* __restrict__ rstd_in, T* __restrict__ dX, int cols)
+                          float* __restrict__ off_out, const float* __restrict__ rstd_in, T* __restrict__ dX, int64_t rows, int cols)
 {
     constexpr int VEC = kVec<T>;
     __shared__ float s[12];
-    const int64_t row = blockIdx.x;
-    const T* x = X + row * cols;
-    const T* dy = dY + row * cols;
-    const float m = mean[row], rstd = rstd_in[row];
-    float sum[3] = {0.f, 0.f, 0.f};
-    for (int c = threadIdx.x * VEC; c < cols; c += kNormThreads * VEC) {
-        float d[VEC], g[VEC], w[VEC];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) w[i] = 1.f;
-        load_vec(d, x + c, cols - c);
-        load_vec(g, dy + c, cols - c);
-        if (gamma) load_vec(w, gamma + c, cols - c);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const float dev = c + i < cols ? d[i] - m : 0.f, gw = g[i] * w[i];
-            sum[0] += dev;
-            sum[1] += gw;
-            sum[2] = fmaf(gw, dev, sum[2]);
-        }
-    }
-    row_sum<kNormThreads>(sum, s);
     const float inv = 1.f / (float)cols;
-    const float off = sum[0] * inv, c1 = sum[1] * inv, c2 = (sum[2] - off * sum[1]) * rstd * inv;
-    if (threadIdx.x == 0 && off_out) off_out[row] = off;
-    for (int c = threadIdx.x * VEC; c < cols; c += kNormThreads * VEC) {
-        float d[VEC], g[VEC], w[VEC];
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const T* x = X + row * cols;
+        const T* dy = dY + row * cols;
+        const float m = mean[row], rstd = rstd_in[row];
+        float sum[3] = {0.f, 0.f, 0.f};
+        for (int c = threadIdx.x * VEC; c < cols; c += kNormThreads * VEC) {
+            float d[VEC], g[VEC], w[VEC];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) w[i] = 1.f;
-        load_vec(d, x + c, cols - c);
-        load_vec(g, dy + c, cols - c);
-        if (gamma) load_vec(w, gamma + c, cols - c);
+            for (int i = 0; i < VEC; ++i) w[i] = 1.f;
+            load_vec(d, x + c, cols - c);
+            load_vec(g, dy + c, cols - c);
+            if (gamma) load_vec(w, gamma + c, cols - c);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) d[i] = rstd * (g[i] * w[i] - c1 - (d[i] - m - off) * rstd * c2);
-        store_vec(dX + row * cols + c, d, cols - c);
+            for (int i = 0; i < VEC; ++i) {
+                const float dev = c + i < cols ? d[i] - m : 0.f, gw = g[i] * w[i];
+                sum[0] += dev;
+                sum[1] += gw;
+                sum[2] = fmaf(gw, dev, sum[2]);
+            }
+        }
+        row_sum<kNormThreads>(sum, s);
+        const float off = sum[0] * inv, c1 = sum[1] * inv, c2 = (sum[2] - off * sum[1]) * rstd * inv;
+        if (threadIdx.x == 0 && off_out) off_out[row] = off;
+        for (int c = threadIdx.x * VEC; c < cols; c += kNormThreads * VEC) {
+            float d[VEC], g[VEC], w[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) w[i] = 1.f;
+            load_vec(d, x + c, cols - c);
+            load_vec(g, dy + c, cols - c);
+            if (gamma) load_vec(w, gamma + c, cols - c);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) d[i] = rstd * (g[i] * w[i] - c1 - (d[i] - m - off) * rstd * c2);
+            store_vec(dX + row * cols + c, d, cols - c);
+        }
     }
 }
 // Column sums of the rows blockIdx.y * per .. + per, a vector of columns to a thread.
@@ -405,6 +409,8 @@ NormPlan make_norm_plan(int64_t rows, int cols, int dtype, bool forward)
     return p;
 }
 
+static unsigned norm_long_groups(int64_t rows) { return (unsigned)(rows < kNormLongGroups ? rows : kNormLongGroups); }
+
 template <typename T, int TPR, int NV>
 static void norm_fwd_go(const void* X, const void* gamma, const void* beta, float eps, void* Y, float* mean, float* rstd,
                         int64_t rows, int cols, hipStream_t stream)
@@ -432,8 +438,8 @@ static void norm_fwd_pick(const NormPlan& p, const void* X, const void* gamma, c
         case 256 * 16 + 4: return norm_fwd_go<T, 256, 4>(X, gamma, beta, eps, Y, mean, rstd, rows, cols, stream);
         case 256 * 16 + 8: return norm_fwd_go<T, 256, kVec<T> == 4 ? 8 : 4>(X, gamma, beta, eps, Y, mean, rstd, rows, cols, stream);
         default:
-            norm_fwd_long_kernel<T><<<(unsigned)rows, kNormThreads, 0, stream>>>(
-                static_cast<const T*>(X), static_cast<const T*>(gamma), static_cast<const T*>(beta), eps, static_cast<T*>(Y), mean, rstd, cols);
+            norm_fwd_long_kernel<T><<<norm_long_groups(rows), kNormThreads, 0, stream>>>(
+                static_cast<const T*>(X), static_cast<const T*>(gamma), static_cast<const T*>(beta), eps, static_cast<T*>(Y), mean, rstd, rows, cols);
     }
 }
 hipError_t launch_norm_fwd(const NormPlan& p, const void* X, const void* gamma, const void* beta, float eps, void* Y, float* mean,
@@ -467,8 +473,8 @@ static void norm_bwd_pick(const NormPlan& p, const void* dY, const void* X, cons
         default: {
             const T *dy = static_cast<const T*>(dY), *x = static_cast<const T*>(X);
             // (the row kernel leaves what the rounded means are off by for the column sums)
-            norm_bwd_long_kernel<T><<<(unsigned)rows, kNormThreads, 0, stream>>>(dy, x, static_cast<const T*>(gamma), mean, part ? off : nullptr, rstd,
-                                                                                 static_cast<T*>(dX), cols);
+            norm_bwd_long_kernel<T><<<norm_long_groups(rows), kNormThreads, 0, stream>>>(dy, x, static_cast<const T*>(gamma), mean, part ? off : nullptr,
+                                                                                         rstd, static_cast<T*>(dX), rows, cols);
             if (!part) return;
             const int64_t per = (rows + p.n_part - 1) / p.n_part;
             norm_cols_kernel<T><<<dim3((unsigned)((cols + 64 * kVec<T> - 1) / (64 * kVec<T>)), (unsigned)p.n_part), 64, 0, stream>>>(
