@@ -378,16 +378,17 @@ void norm_sum_kernel(const float* __restrict__ part, int n, int cols, float* __r
 }
 
 // How a row of `cols` elements is shared: TPR threads with NV vectors each, or (nv = 0) the kernels for long rows.  One vector to a
-// thread while a wave covers the row.  The forward takes two from 65536 rows on, where the latency of a row's reductions is hidden by
-// others and two rows to a wave keep more loads in flight (131072 x 512 bfloat16, 1 | 2: 64 | 59 us; 18000 x 256 float32 11.1 | 12.4, one row 2.3 | 3.1); the
-// backward, which asks for the next row ahead, does not (75 | 90 us).
+// thread while a wave covers the row.  The forward takes two where there are many rows: the latency of a row's reductions is hidden by
+// others and two rows to a wave keep more loads in flight.  1 | 2, a call among others: bfloat16 x 512, 16384 rows 9.9 | 10.0 us, 32768 16.1 | 14.8, 65536
+// 28.6 | 24.2, 131072 60.1 | 53.0, 131072 x 300 71 | 51; float32 x 256, 18000 11.1 | 12.4, 32768 15.2 | 16.5, 65536 26.0 | 27.9, 131072 58.0 | 56.7, 262144
+// 117 | 114.5; one row 2.3 | 3.1.  The backward, which asks for the next row ahead, does not (131072 x 512 bfloat16 75 | 90 us).
 struct NormShape { int tpr, nv; };
 static NormShape norm_shape(int64_t rows, int cols, int dtype, bool forward)
 {
     const int vec = dtype == PSA_F32 ? 4 : 8;
     const int chunks = (cols + vec - 1) / vec;
     int tpr = chunks <= 16 ? 16 : chunks <= 32 ? 32 : chunks <= 64 * 4 ? 64 : 256;
-    if (forward && tpr == 64 && chunks <= 64 && rows >= 65536) tpr = 32;
+    if (forward && tpr == 64 && chunks <= 64 && rows >= (dtype == PSA_F32 ? 131072 : 32768)) tpr = 32;
     int nv = 1;
     while (nv * tpr < chunks) nv *= 2;
     return NormShape{tpr, cols <= kNormMaxCols ? nv : 0};
