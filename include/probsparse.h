@@ -323,7 +323,8 @@ int probsparse_layer_norm_bwd(const void* dY, const void* X, const void* gamma, 
  *   PSA_ROTARY_PARTS   with r = original_length * f_i / (2 pi), the turns of pair i over the
  *                      length that the model was trained on, and s = clamp((r - slow_turns) /
  *                      (fast_turns - slow_turns), 0, 1):  f_i * s + f_i / factor * (1 - s)
- * Angles are formed and reduced in float64, so far positions lose nothing. */
+ * Angles are formed and reduced in float64 and off by 2^-50 of themselves at the most: no more than
+ * a rounding to float32 for angles up to 2^26 radians. */
 typedef enum psa_rotary_layout {
     PSA_ROTARY_HALF        = 0,   /* pair i is elements i and i + dim / 2 */
     PSA_ROTARY_INTERLEAVED = 1    /* pair i is elements 2 i and 2 i + 1   */
@@ -383,9 +384,10 @@ int probsparse_rotary_bwd(const psa_heads_t* dQ_out, const psa_heads_t* dK_out, 
  * Q or K makes the scores it takes part in NaN.  Softmax statistics are float32. */
 typedef struct psa_packed_shape {
     int32_t B, H, H_kv;           /* sequences, at most 2^20; heads, H a multiple of H_kv */
-    int32_t T_q, T_k;             /* rows of Q and of K and V, at most 2^28; T_q * (H / H_kv) <= 2^31 - 2^16.  Tiles of 128
-                                   * rows (of 32 where sequences have 32 or fewer on average) and of 128 keys, one more of
-                                   * each to a sequence, times H_kv: fewer than 2^24 (else PSA_ERR_SHAPE) */
+    int32_t T_q, T_k;             /* rows of Q and of K and V, 1 .. 2^28; T_q * (H / H_kv) <= 2^31 - 2^16.  Tiles of 128
+                                   * rows (of 32 where sequences have at most 32 rows and at least 100 keys on average)
+                                   * and of 128 keys, one more of each to a sequence, times H_kv: fewer than 2^24 (else
+                                   * PSA_ERR_SHAPE) */
     int32_t D;                    /* 64 */
     int32_t dtype;                /* psa_dtype_t */
     int32_t causal;               /* 0 or 1 */

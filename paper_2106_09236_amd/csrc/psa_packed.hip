@@ -56,8 +56,8 @@ struct Rows32 {
 
 // 4 waves of 32 rows each; tiles of KT keys and values go through LDS, the next tile's rows are on their way meanwhile.
 // bfloat16 is bound by the vector unit (131 instructions and 32 exponentials to 16 matrix instructions: 65 % of its issue
-// cycles, the matrix unit 38 %) and, in long runs, by power: 16384 causal, 8 heads, 350 us at first (785 TFLOP/s), 390 when hot.  What
-// helped: a step's LDS reads before the instructions that take them (8 x 2048 causal 56.8 -> 55.2 us, 32 clips 17.4 -> 17.0).  What
+// cycles, the matrix unit 38 %) and, in long runs, by power: 16384 causal, 8 heads, 335 to 355 us a call in 200 of them (820 to 775 TFLOP/s,
+// from card to card), 377 to 408 in 20 traced ones.  What helped: a step's LDS reads before the instructions that take them (8 x 2048 causal 56.8 -> 55.2 us, 32 clips 17.4 -> 17.0).  What
 // did not: 64 rows to a wave (half the LDS reads, 2 waves to a SIMD: 530 us), 4 waves to a SIMD with 32 keys at a time
 // (430), the scores of a step formed between the weights of the one before (440), priorities (no change).
 //

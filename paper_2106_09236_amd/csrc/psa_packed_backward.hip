@@ -252,7 +252,7 @@ void packed_join_keys_kernel(const float* __restrict__ part, int n_split, Packin
     else store4(dV.at(hk, key) + e - 64, sum);
 }
 
-// dQ of 128 rows: 4 waves of 32, tiles of 32 keys and values through LDS.
+// dQ of 128 rows: 4 waves of 32, tiles of KT keys and values (64, float32: 32 to each of the KW) through LDS.
 template <typename T, int KT, int KW, bool FINE>
 __global__ __launch_bounds__(256 * KW, 2)
 void packed_dq_kernel(Heads<const T> Q, Heads<const T> K, Heads<const T> V, Heads<const T> dOut, Heads<const T> out, Stats stats, Packing p,

@@ -3,7 +3,7 @@
 //
 // Bound by memory: every element is read and written once.  The angle does not depend on the head, so a work-group takes
 // up to 16 rows of one batch item, forms their cosines and sines once in LDS (a product and a reduction in float64, which
-// keeps a far position exact to float32, and one sine and cosine) and applies them to all heads.
+// keeps angles up to 2^26 exact to float32, and one sine and cosine) and applies them to all heads.
 #include "psa_vec.h"
 
 namespace psa {
@@ -16,8 +16,10 @@ struct RotaryTurns { double f[32]; };          // turns (of 2 pi) per position o
 template <typename T>
 struct RotaryHeads { const T* in; T* out; int64_t in_b, in_h, in_l, out_b, out_h, out_l; int H; };
 
+// 8 x (8 + 8) x 2048, dim 64: bfloat16 12.4 us (5.4 TB/s), float32 23.5 (5.7).
+//
 // LAYOUT: psa_rotary_layout_t.  WIDE: dim / 2 is a multiple of the elements of 16 bytes (HALF), or dim of it (INTERLEAVED);
-// else elements are taken one pair at a time.
+// else elements are taken one pair at a time, 2 or 4 bytes to an access (bfloat16, dim 62: 38 us, dim 24 by halves 37).
 template <typename T, int LAYOUT, bool WIDE>
 __global__ __launch_bounds__(kRotaryThreads)
 void rotary_kernel(RotaryHeads<T> q, RotaryHeads<T> k, RotaryTurns turns, const int* __restrict__ positions, int64_t positions_stride,

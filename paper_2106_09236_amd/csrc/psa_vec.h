@@ -1,8 +1,6 @@
 // Vectors of VEC tensor elements as float32: 16 bytes of either type, for the kernels that pass over rows.
 #pragma once
 
-#include <string.h>
-
 #include "psa_device.h"
 #include "psa_internal.h"
 
