@@ -381,7 +381,8 @@ int probsparse_rotary_bwd(const psa_heads_t* dQ_out, const psa_heads_t* dK_out, 
  * T_q * (H / H_kv) / B <= 32 and T_k / B >= 100 (few new queries of longer sequences).  float32
  * operands are multiplied as sums of three bfloat16 parts each (error 2^-23 of |a||b| at
  * the most, 2^-25 as a rule) and summed in float32; an infinity has no such parts, so that one in
- * Q or K makes the scores it takes part in NaN.  Softmax statistics are float32. */
+ * Q or K makes the scores it takes part in NaN.  Softmax statistics are float32.  Weights are up
+ * to 2^8 until their sum divides the result: beyond 2^119 / n_k elements of V may overflow. */
 typedef struct psa_packed_shape {
     int32_t B, H, H_kv;           /* sequences, at most 2^20; heads, H a multiple of H_kv */
     int32_t T_q, T_k;             /* rows of Q and of K and V, 1 .. 2^28; T_q * (H / H_kv) <= 2^31 - 2^16.  Tiles of 128
