@@ -414,6 +414,103 @@ int dense_attn_packed_bwd(const psa_heads_t* Q, const psa_heads_t* K, const psa_
                           const psa_heads_t* dOut, const psa_heads_t* dQ, const psa_heads_t* dK, const psa_heads_t* dV,
                           const psa_packed_shape_t* shape, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * A cache in pages: keys and values of running sequences, kept where they were written.
+ *
+ * A pool holds n_pages pages of `page_rows` rows (a power of two) of H_kv heads.  Row j of sequence s, its position from
+ * the sequence's start, is row j % page_rows of page table[s * max_pages + j / page_rows]; lengths[s] rows exist.  An
+ * entry outside [0, n_pages) names no page (-1 as a rule): its rows cannot be written and are not seen, as if a mask left
+ * them out, so that pages of rows too old to matter may be freed.  Sequences may share pages.
+ *   K, V      psa_heads_t with pages in the place of batch items: element e of row r of head h of page p is
+ *             data[p * batch_stride + h * head_stride + r * row_stride + e].  By head, by frame, K and V side by side in a
+ *             page or apart, several layers in a page: whatever the strides say
+ *   format    PSA_CACHE_PLAIN: elements of the call's dtype.  PSA_CACHE_MX: 8-bit floats (e4m3, without infinities),
+ *             and for each 32 elements of a row a byte b: an element is its code's value times 2^(b - 127), exactly
+ *             representable in bfloat16.  probsparse_cache_append takes the least power that brings the largest finite
+ *             magnitude of the 32 to at most 448, within 2^-117 .. 2^119, and rounds to nearest, ties to even;
+ *             infinities and NaN become NaN.  Bytes outside [10, 246] give unspecified values
+ *   K_scales, V_scales   PSA_CACHE_MX alone: these bytes, two to a row, 2-byte aligned, strides in bytes and even
+ * table and lengths are DEVICE int32, 4-byte aligned, lengths clamped to [0, max_pages * page_rows]. */
+typedef enum psa_cache_format { PSA_CACHE_PLAIN = 0, PSA_CACHE_MX = 1 } psa_cache_format_t;
+typedef struct psa_cache {
+    psa_heads_t K, V, K_scales, V_scales;
+    const int32_t* table;         /* [B, max_pages] */
+    const int32_t* lengths;       /* [B] */
+    int32_t n_pages;              /* 1 .. 2^28 */
+    int32_t page_rows;            /* a power of two, 1 .. 2^16 */
+    int32_t max_pages;            /* of a sequence; max_pages * page_rows <= 2^28 */
+    int32_t format;               /* psa_cache_format_t */
+} psa_cache_t;
+typedef struct psa_paged_shape {
+    int32_t B, H, H_kv;           /* sequences, at most 2^20; heads, H a multiple of H_kv */
+    int32_t T;                    /* new rows of all sequences, 1 .. 2^28; T * (H / H_kv) <= 2^31 - 2^16 */
+    int32_t D;                    /* 64 */
+    int32_t dtype;                /* psa_dtype_t, of Q and out, or of the rows that are appended */
+    int32_t causal;               /* 0 or 1 */
+    double  scale;                /* 1e-30 .. 1e30; 1 / sqrt(64) as a rule */
+} psa_paged_shape_t;
+
+/* The new rows of sequence s are rows offsets[s] .. offsets[s + 1] - 1 of every head (int32 [B + 1] DEVICE, not
+ * decreasing, clamped to [0, T]; NULL: T / B rows each), n of them, and its rows lengths[s] - n .. lengths[s] - 1 in the
+ * cache: lengths count them already.
+ *
+ * probsparse_cache_append writes K and V [H_kv, T, 64] there.  Rows whose position would be negative, and rows without a page, are
+ * left out.  H, causal and scale are ignored.  No two sequences may hold the page that one of them writes to
+ * (probsparse_cache_update sees to that); where they do the order is unspecified. */
+int probsparse_cache_append(const psa_heads_t* K, const psa_heads_t* V, const int32_t* offsets, const psa_cache_t* cache,
+                            const psa_paged_shape_t* shape, void* stream);
+
+/* Attention of the new rows Q [H, T, 64] over the cache: as dense_attn_packed_fwd where a sequence's keys are its rows in
+ * the cache (new query t sees all of them or, `causal`, rows j <= t + lengths[s] - n), those on a page.
+ * A query that sees no key, and a row of Q in no sequence, get zeros in out and -infinity in lse [H, T] float32 DEVICE
+ * (may be NULL).  What a query does not see, rows behind a sequence's last among it, has no part in its output, whatever lies there.
+ * Arithmetic as there: 8-bit elements are taken exactly; bfloat16 weights are kept to 16 bits where sequences have few new
+ * rows (T * (H / H_kv) / B <= 32) or where W < 152 (causal: 224) with W = (T * (H / H_kv) / 128 + B) * H_kv, else rounded.
+ * The keys of long sequences are divided among work-groups by the lengths that the device finds, so a captured call serves while sequences grow.
+ * The order of all sums is fixed by the shape and the lengths. */
+size_t dense_attn_paged_workspace_bytes(const psa_cache_t* cache, const psa_paged_shape_t* shape);
+int dense_attn_paged_fwd(const psa_heads_t* Q, const int32_t* offsets, const psa_cache_t* cache, const psa_heads_t* out,
+                         float* lse, const psa_paged_shape_t* shape, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Pages and who holds them.  refs [n_pages] counts the entries of tables that name a page (0: free; zeros at first), within the first
+ * ceil(lengths[s] / page_rows) entries of each row; entries behind them are -1.
+ *
+ * probsparse_cache_update makes the sequences of the next step in one pass:
+ *   forked   sequence i of the B_out new ones continues sequence parents[i] (several may continue one; outside [0, B): it starts
+ *            empty).  parents NULL: i continues i (B_out = B)
+ *   freed    what no sequence continues: pages that nobody holds any more are free, for this call too
+ *   grown    it gets pages for grow[i] more rows (negative: 0; grow NULL: 0), the lowest free ones in order of (i, position)
+ *   copied   the last, partly filled page of a sequence that grows, unless it alone holds the page or all who hold it
+ *            grow in this call and it is the first of them: the page is replaced by a new one, allocated before those it
+ *            grows into, and (page, new page) goes into `pairs`, in order of i, for probsparse_cache_copy
+ * Outputs (DEVICE int32; they must not alias inputs): table_out [B_out, max_pages], lengths_out [B_out] (grown, at most
+ * max_pages * page_rows), refs_out [n_pages], pairs [B_out, 2] (-1 behind the last), counts [2]: pairs, and pages that were
+ * missing.  Where pages run out, or rows pass max_pages, entries stay -1 and are counted there (a page that could not be copied is
+ * given up): look at it before the rows are needed.
+ * B, B_out 1 .. 2^20, n_pages 1 .. 2^28, max_pages * page_rows <= 2^28, B * max_pages and B_out * max_pages <= 2^30 (PSA_ERR_SHAPE).
+ * Other tables may hold pages of the same pool: refs counts theirs too. */
+size_t probsparse_cache_update_workspace_bytes(int32_t B, int32_t B_out, int32_t n_pages);
+int probsparse_cache_update(const int32_t* table, const int32_t* lengths, const int32_t* refs, int32_t B, const int32_t* parents,
+                            const int32_t* grow, int32_t B_out, int32_t n_pages, int32_t page_rows, int32_t max_pages,
+                            int32_t* table_out, int32_t* lengths_out, int32_t* refs_out, int32_t* pairs, int32_t* counts,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* The pages in use (refs not 0, n of them) to the front: those at n or behind go to the free ones before n, both in ascending order.
+ * table_out [B, max_pages] (may be table) and refs_out [n_pages] (must not alias refs) follow; pairs [n_pages / 2, 2] (-1
+ * behind the last; NULL where n_pages is 1) for probsparse_cache_copy, counts [2]: pairs, and n.  Every table that holds pages
+ * of the pool has to be in `table`. */
+size_t probsparse_cache_compact_workspace_bytes(int32_t n_pages);
+int probsparse_cache_compact(const int32_t* table, const int32_t* refs, int32_t B, int32_t n_pages, int32_t max_pages,
+                             int32_t* table_out, int32_t* refs_out, int32_t* pairs, int32_t* counts, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Copies page pairs[i][0] to page pairs[i][1] of every pool (i < counts[0], or i < n_pairs where counts is NULL; at most
+ * n_pairs), page p of a pool being the page_bytes at data + p * page_stride.  Pairs with a page outside [0, n_pages), or twice the same, are left out.
+ * No page may be written by two pairs, or written by one and read by another. */
+typedef struct psa_pool { void* data; int64_t page_stride, page_bytes; } psa_pool_t;    /* data DEVICE; bytes */
+int probsparse_cache_copy(const psa_pool_t* pools, int32_t n_pools, int32_t n_pages, const int32_t* pairs, const int32_t* counts,
+                          int32_t n_pairs, void* stream);
+
 /* Host only, no GPU needed: which kernels a call with this shape would launch, as
  * one line of `key=value` words in `buf` (NUL-terminated), e.g. which measure kernel
  * (`measure=lds|lds_half|stream|none`; `measure_parts` > 0: the keys of streamed heads go

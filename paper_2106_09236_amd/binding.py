@@ -28,6 +28,7 @@ U_LOG, U_RATIO = 0, 1
 FILL_MEAN, FILL_VALUE = 0, 1
 ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
+CACHE_PLAIN, CACHE_MX = 0, 1
 
 EXPORTS = [
     "probsparse_attn_workspace_bytes", "probsparse_attn_fwd", "probsparse_attn_fwd_debug",
@@ -43,6 +44,9 @@ EXPORTS = [
     "probsparse_rotary_frequencies", "probsparse_rotary_fwd", "probsparse_rotary_bwd",
     "dense_attn_packed_workspace_bytes", "dense_attn_packed_fwd",
     "dense_attn_packed_bwd_workspace_bytes", "dense_attn_packed_bwd",
+    "probsparse_cache_append", "dense_attn_paged_workspace_bytes", "dense_attn_paged_fwd",
+    "probsparse_cache_update_workspace_bytes", "probsparse_cache_update",
+    "probsparse_cache_compact_workspace_bytes", "probsparse_cache_compact", "probsparse_cache_copy",
 ]
 
 
@@ -76,6 +80,21 @@ class PsaPackedShape(ctypes.Structure):
                 ("scale", ctypes.c_double)]
 
 
+class PsaCache(ctypes.Structure):
+    _fields_ = [("K", PsaHeads), ("V", PsaHeads), ("K_scales", PsaHeads), ("V_scales", PsaHeads), ("table", ctypes.c_void_p),
+                ("lengths", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("format", ctypes.c_int32)]
+
+
+class PsaPagedShape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("T", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32), ("scale", ctypes.c_double)]
+
+
+class PsaPool(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("page_bytes", ctypes.c_int64)]
+
+
 class ProbSparseError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"libprobsparse: {msg} (status {code})")
@@ -89,6 +108,7 @@ class _CtypesOnly:
         return None
     attn_fwd_opt = attn_fwd_with_indices = attn_bwd = mhsa_fwd = attn_fwd
     layer_norm_fwd = layer_norm_bwd = rotary = packed_fwd = packed_bwd = attn_fwd
+    cache_append = paged_fwd = cache_update = cache_compact = cache_copy = attn_fwd
 
 
 _lib = None
@@ -194,6 +214,23 @@ def load() -> ctypes.CDLL:
     lib.dense_attn_packed_fwd.argtypes = [hp, hp, hp, i32p, i32p, hp, f32p, kp, vp, ctypes.c_size_t, vp]
     lib.dense_attn_packed_bwd.restype = ctypes.c_int
     lib.dense_attn_packed_bwd.argtypes = [hp, hp, hp, i32p, i32p, hp, f32p, hp, hp, hp, hp, kp, vp, ctypes.c_size_t, vp]
+    cp, gp, pp = ctypes.POINTER(PsaCache), ctypes.POINTER(PsaPagedShape), ctypes.POINTER(PsaPool)
+    lib.probsparse_cache_append.restype = ctypes.c_int
+    lib.probsparse_cache_append.argtypes = [hp, hp, i32p, cp, gp, vp]
+    lib.dense_attn_paged_workspace_bytes.restype = ctypes.c_size_t
+    lib.dense_attn_paged_workspace_bytes.argtypes = [cp, gp]
+    lib.dense_attn_paged_fwd.restype = ctypes.c_int
+    lib.dense_attn_paged_fwd.argtypes = [hp, i32p, cp, hp, f32p, gp, vp, ctypes.c_size_t, vp]
+    lib.probsparse_cache_update_workspace_bytes.restype = ctypes.c_size_t
+    lib.probsparse_cache_update_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.probsparse_cache_update.restype = ctypes.c_int
+    lib.probsparse_cache_update.argtypes = [i32p, i32p, i32p, i32, i32p, i32p, i32, i32, i32, i32, i32p, i32p, i32p, i32p, i32p, vp, ctypes.c_size_t, vp]
+    lib.probsparse_cache_compact_workspace_bytes.restype = ctypes.c_size_t
+    lib.probsparse_cache_compact_workspace_bytes.argtypes = [i32]
+    lib.probsparse_cache_compact.restype = ctypes.c_int
+    lib.probsparse_cache_compact.argtypes = [i32p, i32p, i32, i32, i32, i32p, i32p, i32p, i32p, vp, ctypes.c_size_t, vp]
+    lib.probsparse_cache_copy.restype = ctypes.c_int
+    lib.probsparse_cache_copy.argtypes = [pp, i32, i32, i32p, i32p, i32, vp]
     lib.probsparse_describe_plan.restype = ctypes.c_int
     lib.probsparse_describe_plan.argtypes = [shp, optp, ctypes.c_int32, ctypes.c_char_p, ctypes.c_size_t]
     _lib, _native = lib, _load_native()
@@ -690,6 +727,146 @@ def dense_attn_packed_bwd(Q, K, V, out, lse, dOut, q_offsets=None, k_offsets=Non
     _launch(device, lib.dense_attn_packed_bwd, *heads[:3], _ptr(q_offsets), _ptr(k_offsets), heads[3], _ptr(lse), *heads[4:],
             ctypes.byref(shape), _ptr(workspace), workspace.numel() * workspace.element_size())
     return dQ, dK, dV
+
+
+# ---- a cache in pages.  K_pages and V_pages [n_pages, H_kv, page_rows, 64] may have any strides the library takes: views of
+# pools that lie by head or by frame, K and V side by side or apart.  An 8-bit cache is torch.float8_e4m3fn with K_scales and
+# V_scales, uint8 [n_pages, H_kv, page_rows, 2] (see psa_cache_t).  table int32 [B, max_pages], lengths int32 [B].
+
+def _cache(rows, H_kv, K_pages, V_pages, table, lengths, offsets, K_scales, V_scales):
+    """The cache, sequences and new rows of a call for rows [heads, T, 64]."""
+    _require(K_pages.dim() == 4 and K_pages.shape[-1] == 64, "K_pages must be [n_pages, H_kv, page_rows, 64]")
+    _require(K_pages.numel() > 0 and K_pages.shape[1] == H_kv, f"K_pages must have {H_kv} heads and not be empty")
+    mx = K_pages.dtype == torch.float8_e4m3fn
+    kind = torch.float8_e4m3fn if mx else rows.dtype
+    _require_like(K_pages, K_pages.shape, kind, "K_pages", contiguous=False)
+    _require_like(V_pages, K_pages.shape, kind, "V_pages", contiguous=False)
+    _require((K_scales is not None) == mx and (V_scales is not None) == mx, "an 8-bit cache, and no other, has K_scales and V_scales")
+    for t, what in ((K_scales, "K_scales"), (V_scales, "V_scales")):
+        _require_like(t, (*K_pages.shape[:-1], 2), torch.uint8, what, contiguous=False)
+    _require(table.dim() == 2 and table.numel() > 0, "table must be [B, max_pages]")
+    B = table.shape[0]
+    _require_like(table, table.shape, torch.int32, "table")
+    _require_like(lengths, (B,), torch.int32, "lengths")
+    _require_like(offsets, (B + 1,), torch.int32, "offsets")
+    _require(offsets is not None or rows.shape[1] % B == 0, "without offsets every sequence has as many new rows")
+    none = PsaHeads(None, 0, 0, 0)
+    scales = [_heads(t) if mx else none for t in (K_scales, V_scales)]
+    return B, PsaCache(_heads(K_pages), _heads(V_pages), *scales, _ptr(table), _ptr(lengths), K_pages.shape[0], K_pages.shape[2], table.shape[1],
+                       CACHE_MX if mx else CACHE_PLAIN)
+
+
+def probsparse_cache_append(K, V, K_pages, V_pages, table, lengths, offsets=None, K_scales=None, V_scales=None):
+    """Writes the new rows K and V [H_kv, T, 64] into the cache: rows offsets[s] .. offsets[s + 1] - 1 (int32 [B + 1]; None: T / B
+    each) become the last of the lengths[s] rows of sequence s."""
+    if (_native or _fast()).cache_append(K, V, K_pages, V_pages, table, lengths, offsets, K_scales, V_scales) is not None:
+        return
+    device = _device_of(K, V, K_pages, V_pages, table, lengths, offsets, K_scales, V_scales)
+    _require(K.dim() == 3 and K.shape[-1] == 64 and K.numel() > 0, "K must be [H_kv, T, 64] and not empty")
+    _require_like(K, K.shape, K.dtype, "K", contiguous=False)
+    _require_like(V, K.shape, K.dtype, "V", contiguous=False)
+    dtype = _dtype_code(K)
+    B, cache = _cache(K, K.shape[0], K_pages, V_pages, table, lengths, offsets, K_scales, V_scales)
+    shape = PsaPagedShape(B, K.shape[0], K.shape[0], K.shape[1], 64, dtype, 0, 0.125)
+    k, v = _heads(K), _heads(V)
+    _launch(device, load().probsparse_cache_append, ctypes.byref(k), ctypes.byref(v), _ptr(offsets), ctypes.byref(cache), ctypes.byref(shape))
+
+
+def dense_attn_paged_fwd(Q, K_pages, V_pages, table, lengths, offsets=None, causal: bool = False, scale: Optional[float] = None,
+                         K_scales=None, V_scales=None, out=None, lse: bool = False, workspace=None):
+    """Attention of the new rows Q [H, T, 64] over the cache, whose lengths count them: dense_attn_packed_fwd with keys in pages.
+    `scale` is 1 / 8 unless given.  Returns out, or (out, lse) with lse [H, T] float32."""
+    done = (_native or _fast()).paged_fwd(Q, K_pages, V_pages, table, lengths, offsets, causal, scale, K_scales, V_scales, out, lse, workspace)
+    if done is not None:
+        return done
+    device = _device_of(Q, K_pages, V_pages, table, lengths, offsets, K_scales, V_scales, out, workspace)
+    _require(Q.dim() == 3 and Q.shape[-1] == 64 and Q.numel() > 0, "Q must be [H, T, 64] and not empty")
+    _require_like(Q, Q.shape, Q.dtype, "Q", contiguous=False)
+    dtype = _dtype_code(Q)
+    H_kv = K_pages.shape[1] if K_pages.dim() == 4 else 0
+    _require(H_kv > 0 and Q.shape[0] % H_kv == 0, "the heads of Q must be a multiple of those of K_pages")
+    B, cache = _cache(Q, H_kv, K_pages, V_pages, table, lengths, offsets, K_scales, V_scales)
+    _require_like(out, Q.shape, Q.dtype, "out", contiguous=False)
+    shape = PsaPagedShape(B, Q.shape[0], H_kv, Q.shape[1], 64, dtype, int(bool(causal)), 0.125 if scale is None else scale)
+    lib = load()
+    workspace = _room(lib.dense_attn_paged_workspace_bytes(ctypes.byref(cache), ctypes.byref(shape)), device, workspace)
+    if out is None:
+        out = torch.empty_like(Q)
+    norm = torch.empty(Q.shape[:2], dtype=torch.float32, device=device) if lse else None
+    q, o = _heads(Q), _heads(out)
+    _launch(device, lib.dense_attn_paged_fwd, ctypes.byref(q), _ptr(offsets), ctypes.byref(cache), ctypes.byref(o), _ptr(norm), ctypes.byref(shape),
+            _ptr(workspace), workspace.numel() * workspace.element_size())
+    return (out, norm) if lse else out
+
+
+def probsparse_cache_update(table, lengths, refs, page_rows: int, parents=None, grow=None, table_out=None, lengths_out=None, refs_out=None,
+                            pairs=None, counts=None, workspace=None):
+    """The sequences of the next step: sequence i continues parents[i] (int32 [B_out]; outside [0, B): nobody; None: itself) and gets
+    pages for grow[i] more rows (int32 [B_out]; None: 0); what nobody continues is freed.  Returns (table, lengths, refs, pairs, counts):
+    pairs [B_out, 2] are the pages that probsparse_cache_copy has to copy, counts [2] how many, and pages that were missing."""
+    done = (_native or _fast()).cache_update(table, lengths, refs, page_rows, parents, grow, table_out, lengths_out, refs_out, pairs, counts, workspace)
+    if done is not None:
+        return done
+    device = _device_of(table, lengths, refs, parents, grow, table_out, lengths_out, refs_out, pairs, counts, workspace)
+    _require(table.dim() == 2 and table.numel() > 0, "table must be [B, max_pages]")
+    _require(refs.dim() == 1 and refs.numel() > 0, "refs must be [n_pages]")
+    (B, max_pages), n_pages = table.shape, refs.numel()
+    B_out = B if parents is None else parents.numel()
+    _require(B_out > 0, "parents must not be empty")
+    for t, shape, what in ((table, (B, max_pages), "table"), (lengths, (B,), "lengths"), (refs, (n_pages,), "refs"), (parents, (B_out,), "parents"),
+                           (grow, (B_out,), "grow"), (table_out, (B_out, max_pages), "table_out"), (lengths_out, (B_out,), "lengths_out"),
+                           (refs_out, (n_pages,), "refs_out"), (pairs, (B_out, 2), "pairs"), (counts, (2,), "counts")):
+        _require_like(t, shape, torch.int32, what)
+    lib = load()
+    workspace = _room(lib.probsparse_cache_update_workspace_bytes(B, B_out, n_pages), device, workspace)
+    made = lambda t, *shape: torch.empty(shape, dtype=torch.int32, device=device) if t is None else t
+    table_out, lengths_out, refs_out = made(table_out, B_out, max_pages), made(lengths_out, B_out), made(refs_out, n_pages)
+    pairs, counts = made(pairs, B_out, 2), made(counts, 2)
+    _launch(device, lib.probsparse_cache_update, _ptr(table), _ptr(lengths), _ptr(refs), B, _ptr(parents), _ptr(grow), B_out, n_pages, page_rows, max_pages,
+            _ptr(table_out), _ptr(lengths_out), _ptr(refs_out), _ptr(pairs), _ptr(counts), _ptr(workspace), workspace.numel() * workspace.element_size())
+    return table_out, lengths_out, refs_out, pairs, counts
+
+
+def probsparse_cache_compact(table, refs, table_out=None, refs_out=None, pairs=None, counts=None, workspace=None):
+    """The pages in use to the front of the pools.  Returns (table, refs, pairs, counts): pairs [n_pages / 2, 2] are the pages that
+    probsparse_cache_copy has to move, counts [2] how many, and pages in use.  table_out may be table."""
+    done = (_native or _fast()).cache_compact(table, refs, table_out, refs_out, pairs, counts, workspace)
+    if done is not None:
+        return done
+    device = _device_of(table, refs, table_out, refs_out, pairs, counts, workspace)
+    _require(table.dim() == 2 and table.numel() > 0, "table must be [B, max_pages]")
+    _require(refs.dim() == 1 and refs.numel() > 0, "refs must be [n_pages]")
+    (B, max_pages), n_pages = table.shape, refs.numel()
+    for t, shape, what in ((table, (B, max_pages), "table"), (refs, (n_pages,), "refs"), (table_out, (B, max_pages), "table_out"),
+                           (refs_out, (n_pages,), "refs_out"), (pairs, (n_pages // 2, 2), "pairs"), (counts, (2,), "counts")):
+        _require_like(t, shape, torch.int32, what)
+    lib = load()
+    workspace = _room(lib.probsparse_cache_compact_workspace_bytes(n_pages), device, workspace)
+    made = lambda t, *shape: torch.empty(shape, dtype=torch.int32, device=device) if t is None else t
+    table_out, refs_out, pairs, counts = made(table_out, B, max_pages), made(refs_out, n_pages), made(pairs, n_pages // 2, 2), made(counts, 2)
+    _launch(device, lib.probsparse_cache_compact, _ptr(table), _ptr(refs), B, n_pages, max_pages, _ptr(table_out), _ptr(refs_out), _ptr(pairs), _ptr(counts),
+            _ptr(workspace), workspace.numel() * workspace.element_size())
+    return table_out, refs_out, pairs, counts
+
+
+def probsparse_cache_copy(pools, pairs, counts=None):
+    """Copies page pairs[i, 0] to page pairs[i, 1] of every pool for the first counts[0] pairs (None: all).  A pool is a tensor [n_pages, ..]
+    whose pages are contiguous (all layers' K and V, and the scales of 8-bit ones)."""
+    if (_native or _fast()).cache_copy(pools, pairs, counts) is not None:
+        return
+    _require(len(pools) > 0, "there must be a pool")
+    device = _device_of(*pools, pairs, counts)
+    n_pages = pools[0].shape[0] if pools[0].dim() > 0 else 0
+    descriptions = (PsaPool * len(pools))()
+    for d, t in zip(descriptions, pools):
+        _require(t.dim() >= 2 and t.numel() > 0 and t.shape[0] == n_pages and t[0].is_contiguous(), "pools must be [n_pages, ..] with contiguous pages, and not empty")
+        d.data, d.page_stride, d.page_bytes = t.data_ptr(), t.stride(0) * t.element_size(), t[0].numel() * t.element_size()
+    _require(pairs.dim() == 2 and pairs.shape[1] == 2, "pairs must be [n, 2]")
+    _require_like(pairs, pairs.shape, torch.int32, "pairs")
+    _require(counts is None or counts.numel() > 0, "counts must not be empty")
+    if counts is not None:
+        _require_like(counts, counts.shape, torch.int32, "counts")
+    _launch(device, load().probsparse_cache_copy, descriptions, len(pools), n_pages, _ptr(pairs), _ptr(counts), pairs.shape[0])
 
 
 def version() -> int:

@@ -1,0 +1,457 @@
+// A cache in pages: new rows into it, who holds its pages, compaction, and copies of pages.
+//
+// All of it is bound by memory, or, for the few rows and the few thousand integers of a step, by latency: the length of a chain
+// of dependent loads and the number of launches.
+#include <limits.h>
+
+#include "psa_paged.h"
+
+namespace psa {
+
+// ---- new rows
+// A wave takes one row of all heads, K and V.  Which sequence it belongs to is found by all lanes, 64 candidates at a time.
+__device__ __forceinline__ int sequence_of(const int* offsets, int B, int row)
+{
+    // the last sequence whose offset is at most `row` (offsets do not decrease); -1: none
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = B + 1;                             // candidates lo .. lo + n - 1
+    while (true) {
+        const int step = (n + 63) / 64, i = lo + lane * step;
+        const uint64_t at_most = __builtin_amdgcn_ballot_w64(lane * step < n && offsets[min(i, B)] <= row);
+        if (at_most == 0) return -1;
+        const int k = 63 - __builtin_clzll(at_most);
+        lo += k * step;
+        if (step == 1) return lo;
+        n = min(step, n - k * step);
+    }
+}
+
+// 16 bytes of a row, chunk `ch` of head `hk`, to where the row lies in the cache.  8-bit: every lane of the 32 elements that share a
+// power of two has to be here.
+template <typename T>
+__device__ __forceinline__ void put_chunk(const uint4& x, const PageHeads<T>& to, const PageScales&, int hk, int64_t page, int slot, int ch)
+{
+    *reinterpret_cast<uint4*>(to.data + hk * to.head + page * to.page + slot * to.row + ch * (16 / (int)sizeof(T))) = x;
+}
+// largest of the lanes of one block of 32 elements: 4 lanes of 8 elements, or 8 of 4
+__device__ __forceinline__ float block_max(float a, bf16_t) { a = fmaxf(a, dpp_mov<0xB1>(a)); return fmaxf(a, dpp_mov<0x4E>(a)); }
+__device__ __forceinline__ float block_max(float a, float) { a = block_max(a, bf16_t{}); return fmaxf(a, dpp_mov<0x141>(a)); }
+template <typename T>
+__device__ __forceinline__ void put_chunk(const uint4& x, const PageHeads<mx8_t>& to, const PageScales& scales, int hk, int64_t page, int slot, int ch)
+{
+    constexpr int N = kVec<T>;                         // elements of a chunk
+    constexpr int LANES = 32 / N;                      // lanes of a block
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    float v[N], most = 0.f;
+    unpack(w, v, T{});
+#pragma unroll
+    for (int i = 0; i < N; ++i) most = fmaxf(most, isfinite(v[i]) ? fabsf(v[i]) : 0.f);
+    const uint32_t bits = __float_as_uint(block_max(most, T{}));
+    // floor(log2) - 8, one more where the largest would pass 1.75 * 2^8 = 448, the largest code
+    const int e = min(max((int)(bits >> 23) - 127 - 8 + ((bits & 0x7FFFFF) > 0x600000 ? 1 : 0), -117), 119);
+    const float inverse = __uint_as_float((uint32_t)(127 - e) << 23);
+    uint32_t code[N / 4];
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        float y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] = __builtin_amdgcn_fmed3f(v[i + k] * inverse, -448.f, 448.f);
+        int c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+        c = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], c, true);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (!isfinite(v[i + k])) c |= 0x7F << (8 * k);
+        code[i / 4] = (uint32_t)c;
+    }
+    mx8_t* dst = to.data + hk * to.head + page * to.page + slot * to.row + ch * N;
+    if constexpr (N == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(code[0], code[1]);
+    else *reinterpret_cast<uint32_t*>(dst) = code[0];
+    if (ch % LANES == 0) *(scales.at(hk, (int)page, slot) + ch / LANES) = (uint8_t)(e + 127);
+}
+
+template <typename T, typename C>
+__global__ __launch_bounds__(256)
+void cache_append_kernel(Heads<const T> K, Heads<const T> V, PagedSeqs p, PageHeads<C> Kc, PageHeads<C> Vc, PageScales ks, PageScales vs, int H_kv)
+{
+    constexpr int CH = 64 * sizeof(T) / 16;
+    const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (row >= p.T) return;
+    int s, first, n;
+    if (p.offsets) {
+        s = sequence_of(p.offsets, p.B, row);
+        if (s < 0 || s >= p.B) return;                 // in no sequence
+        first = max(p.offsets[s], 0);
+        n = min(p.offsets[s + 1], p.T) - first;
+    } else {
+        s = row / p.uniform;
+        first = s * p.uniform;
+        n = p.uniform;
+    }
+    const int j = min(max(p.lengths[s], 0), p.capacity) - n + (row - first);
+    if (row - first >= n || j < 0) return;             // (the first only where offsets decrease)
+    const int page = p.table[(int64_t)s * p.max_pages + (j >> p.shift)], slot = j & ((1 << p.shift) - 1);
+    if ((unsigned)page >= (unsigned)p.n_pages) return;
+    for (int i = lane; i < H_kv * CH; i += 64) {
+        const int hk = i / CH, ch = i % CH;
+        const uint4 k = *reinterpret_cast<const uint4*>(K.at(hk, row) + ch * kVec<T>);
+        const uint4 v = *reinterpret_cast<const uint4*>(V.at(hk, row) + ch * kVec<T>);
+        put_chunk<T>(k, Kc, ks, hk, page, slot, ch);
+        put_chunk<T>(v, Vc, vs, hk, page, slot, ch);
+    }
+}
+
+template <typename T, typename C>
+static void append_go(const psa_heads_t& K, const psa_heads_t& V, const PagedSeqs& seqs, const psa_cache_t& cache, int H_kv, hipStream_t stream)
+{
+    cache_append_kernel<T, C><<<(unsigned)((seqs.T + 3) / 4), 256, 0, stream>>>(heads_of<const T>(K), heads_of<const T>(V), seqs, page_heads_of<C>(cache.K), page_heads_of<C>(cache.V),
+                                                                               page_scales_of(cache.K_scales), page_scales_of(cache.V_scales), H_kv);
+}
+hipError_t launch_cache_append(const psa_heads_t& K, const psa_heads_t& V, const int* offsets, const psa_cache_t& cache, const psa_paged_shape_t& s, hipStream_t stream)
+{
+    const PagedSeqs seqs{offsets, cache.lengths, cache.table, s.B, s.T, s.T / s.B, 1, cache.max_pages * cache.page_rows, page_shift(cache.page_rows), cache.n_pages,
+                         cache.max_pages, 0, 1, nullptr};
+    const bool mx = cache.format == PSA_CACHE_MX;
+    if (s.dtype == PSA_F32) {
+        if (mx) append_go<float, mx8_t>(K, V, seqs, cache, s.H_kv, stream);
+        else append_go<float, float>(K, V, seqs, cache, s.H_kv, stream);
+    } else {
+        if (mx) append_go<bf16_t, mx8_t>(K, V, seqs, cache, s.H_kv, stream);
+        else append_go<bf16_t, bf16_t>(K, V, seqs, cache, s.H_kv, stream);
+    }
+    return hipGetLastError();
+}
+
+// ---- the sequences of the next step
+// Three launches: refs and the workspace; the tables' rows, with the changes of refs that they make; one work-group for what
+// depends on all of them, which is little: the pages that are given away, in ascending order.
+constexpr int kScanParents = 4096;         // new sequences up to which each old one looks through all of them for those that continue it
+struct UpdateRoom {
+    int *growers, *first, *given;          // [n_pages]: sequences that write to a page next, the first of them; free pages in order of need
+    int *at, *copied;                      // [B_out]: pages needed before it; whether its last page is copied
+    int *children;                         // [B], beyond kScanParents: sequences that continue it
+};
+static UpdateRoom update_room(const CacheUpdate& u, void* room)
+{
+    int* p = static_cast<int*>(room);
+    UpdateRoom w{};
+    w.growers = p; p += u.n_pages;
+    w.first = p; p += u.n_pages;
+    w.given = p; p += u.n_pages;
+    w.at = p; p += u.B_out;
+    w.copied = p; p += u.B_out;
+    if (u.B_out > kScanParents) w.children = p;
+    return w;
+}
+size_t cache_update_bytes(int B, int B_out, int n_pages) { return ((3 * (size_t)n_pages + 2 * (size_t)B_out + (B_out > kScanParents ? B : 0)) * sizeof(int) + 255) & ~(size_t)255; }
+
+// Sequence i of the new ones: whom it continues (-1: nobody), the rows and pages it has from there, the rows and pages it will have, and the
+// pages that a row of the table cannot hold
+struct Child { int parent, n, had, n_out, want; int64_t over; };
+__device__ __forceinline__ Child child_of(const CacheUpdate& u, int i)
+{
+    Child c;
+    c.parent = u.parents ? u.parents[i] : i;
+    if ((unsigned)c.parent >= (unsigned)u.B) c.parent = -1;
+    const int most = u.max_pages * u.page_rows, shift = __builtin_ctz((unsigned)u.page_rows);
+    c.n = c.parent < 0 ? 0 : min(max(u.lengths[c.parent], 0), most);
+    const int64_t grown = (int64_t)c.n + (u.grow ? max(u.grow[i], 0) : 0);
+    c.had = (c.n + u.page_rows - 1) >> shift;
+    c.n_out = (int)min(grown, (int64_t)most);
+    c.want = (c.n_out + u.page_rows - 1) >> shift;
+    c.over = ((grown + u.page_rows - 1) >> shift) - c.want;
+    return c;
+}
+// The last page of a sequence that will write to it; -1: none
+__device__ __forceinline__ int partial_page(const CacheUpdate& u, const Child& c)
+{
+    if (c.n_out == c.n || (c.n & (u.page_rows - 1)) == 0) return -1;
+    const int page = u.table[(int64_t)c.parent * u.max_pages + c.had - 1];
+    return (unsigned)page < (unsigned)u.n_pages ? page : -1;
+}
+
+__global__ __launch_bounds__(256)
+void update_begin_kernel(CacheUpdate u, UpdateRoom w)
+{
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i < u.n_pages) {
+        u.refs_out[i] = u.refs[i];
+        w.growers[i] = 0;
+        w.first[i] = INT_MAX;
+    }
+    if (w.children && i < u.B) w.children[i] = 0;
+}
+__global__ __launch_bounds__(256)
+void update_children_kernel(CacheUpdate u, UpdateRoom w)
+{
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i < u.B_out && (unsigned)u.parents[i] < (unsigned)u.B) atomicAdd(w.children + u.parents[i], 1);
+}
+// Work-groups 0 .. B - 1: refs follow the number of sequences that continue one; the others: a row of the new table each
+__global__ __launch_bounds__(256)
+void update_rows_kernel(CacheUpdate u, UpdateRoom w)
+{
+    const int tid = threadIdx.x;
+    if ((int)blockIdx.x < u.B) {
+        if (!u.parents) return;
+        const int b = blockIdx.x;
+        int more = -1;
+        if (w.children) {
+            more += w.children[b];
+        } else {
+            for (int i0 = 0; i0 < u.B_out; i0 += 64) {
+                const int i = i0 + (tid & 63);
+                more += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < u.B_out && u.parents[min(i, u.B_out - 1)] == b));
+            }
+        }
+        if (more == 0) return;
+        const int had = (min(max(u.lengths[b], 0), u.max_pages * u.page_rows) + u.page_rows - 1) / u.page_rows;
+        for (int j = tid; j < had; j += 256) {
+            const int page = u.table[(int64_t)b * u.max_pages + j];
+            if ((unsigned)page < (unsigned)u.n_pages) atomicAdd(u.refs_out + page, more);
+        }
+        return;
+    }
+    const int i = blockIdx.x - u.B;
+    const Child c = child_of(u, i);
+    for (int j = tid; j < u.max_pages; j += 256) {
+        int page = -1;
+        if (j < c.had) {
+            page = u.table[(int64_t)c.parent * u.max_pages + j];
+            if ((unsigned)page >= (unsigned)u.n_pages) page = -1;
+        }
+        u.table_out[(int64_t)i * u.max_pages + j] = page;
+    }
+    if (tid == 0) {
+        u.lengths_out[i] = c.n_out;
+        const int page = partial_page(u, c);
+        if (page >= 0) {
+            atomicAdd(w.growers + page, 1);
+            atomicMin(w.first + page, i);
+        }
+    }
+}
+
+// Exclusive prefix over a work-group of 1024 threads of one number each, and the sum of all.  `s` holds 16 ints; calls take two of them in turn.
+__device__ __forceinline__ int group_scan(int x, int* s, int& all)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int sum = wave_scan(x);
+    if (lane == 63) s[wave] = sum;
+    __syncthreads();
+    int before = 0;
+    all = 0;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        if (k < wave) before += s[k];
+        all += s[k];
+    }
+    return before + sum - x;
+}
+__global__ __launch_bounds__(1024)
+void update_end_kernel(CacheUpdate u, UpdateRoom w)
+{
+    __shared__ int s[2][16];
+    __shared__ unsigned long long s_over;
+    const int tid = threadIdx.x;
+    int buf = 0, all;
+    if (tid == 0) s_over = 0;
+    __syncthreads();
+    // pages that are needed: as many free ones are looked for
+    int need = 0;
+    for (int i0 = 0; i0 < u.B_out; i0 += 1024, buf ^= 1) {
+        const int i = i0 + tid;
+        int n = 0, copied = 0;
+        if (i < u.B_out) {
+            const Child c = child_of(u, i);
+            const int page = partial_page(u, c);
+            copied = page >= 0 && !(u.refs_out[page] == w.growers[page] && w.first[page] == i);
+            n = c.want - c.had + copied;
+            if (c.over > 0) atomicAdd(&s_over, (unsigned long long)c.over);
+        }
+        const int at = need + group_scan(n, s[buf], all);
+        if (i < u.B_out) { w.at[i] = at; w.copied[i] = copied; }
+        need += all;                                   // (at most B_out * max_pages <= 2^30)
+    }
+    int found = 0;
+    for (int p0 = 0; p0 < u.n_pages && found < need; p0 += 4096, buf ^= 1) {
+        const int p = p0 + 4 * tid;
+        bool is_free[4];
+        int n = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            is_free[k] = p + k < u.n_pages && u.refs_out[min(p + k, u.n_pages - 1)] == 0;
+            n += is_free[k];
+        }
+        int at = found + group_scan(n, s[buf], all);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (is_free[k]) w.given[at++] = p + k;     // (each page once: at most n_pages)
+        found += all;
+    }
+    __syncthreads();                                   // (all of `given` is written, and refs have been read)
+    int pairs = 0;
+    for (int i0 = 0; i0 < u.B_out; i0 += 1024, buf ^= 1) {
+        const int i = i0 + tid;
+        int copied = 0, at = 0;
+        if (i < u.B_out) { copied = w.copied[i]; at = w.at[i]; }
+        const bool with_page = copied && at < found;
+        const int pair = pairs + group_scan(with_page, s[buf], all);
+        pairs += all;
+        if (i < u.B_out) {
+            const Child c = child_of(u, i);
+            int* row = u.table_out + (int64_t)i * u.max_pages;
+            if (copied) {
+                const int old = partial_page(u, c);
+                atomicAdd(u.refs_out + old, -1);
+                if (with_page) { u.pairs[2 * pair] = old; u.pairs[2 * pair + 1] = w.given[at]; }
+            }
+            for (int j = c.had - copied; j < c.want; ++j, ++at) {
+                const int page = at < found ? w.given[at] : -1;
+                row[j] = page;
+                if (page >= 0) u.refs_out[page] = 1;   // (it was 0: nobody else's)
+            }
+        }
+    }
+    for (int i = pairs + tid; i < u.B_out; i += 1024) u.pairs[2 * i] = u.pairs[2 * i + 1] = -1;
+    if (tid == 0) {
+        u.counts[0] = pairs;
+        u.counts[1] = (int)min((unsigned long long)max(need - found, 0) + s_over, (unsigned long long)INT_MAX);
+    }
+}
+hipError_t launch_cache_update(const CacheUpdate& u, void* workspace, hipStream_t stream)
+{
+    const UpdateRoom w = update_room(u, workspace);
+    const int n = w.children && u.B > u.n_pages ? u.B : u.n_pages;
+    update_begin_kernel<<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(u, w);
+    if (w.children && u.parents) update_children_kernel<<<(unsigned)((u.B_out + 255) / 256), 256, 0, stream>>>(u, w);
+    update_rows_kernel<<<(unsigned)(u.B + u.B_out), 256, 0, stream>>>(u, w);
+    update_end_kernel<<<1, 1024, 0, stream>>>(u, w);
+    return hipGetLastError();
+}
+
+// ---- compaction
+// One work-group counts the pages in use and ranks those that move and the holes they move to; then all pages and entries follow.
+// workspace: [n_pages], where a page at n or behind goes
+size_t cache_compact_bytes(int n_pages) { return ((size_t)n_pages * sizeof(int) + 255) & ~(size_t)255; }
+__global__ __launch_bounds__(1024)
+void compact_rank_kernel(const int* __restrict__ refs, int n_pages, int* __restrict__ pairs, int* __restrict__ counts)
+{
+    __shared__ int s[2][2][16];
+    const int tid = threadIdx.x;
+    int all, used = 0;
+    for (int p = tid; p < n_pages; p += 1024) used += refs[p] != 0;
+    group_scan(used, s[0][0], used);
+    int holes = 0, moved = 0, buf = 1;
+    for (int p0 = 0; p0 < n_pages; p0 += 4096, buf ^= 1) {
+        const int p = p0 + 4 * tid;
+        int hole = 0, move = 0;
+        bool taken[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            taken[k] = p + k < n_pages && refs[min(p + k, n_pages - 1)] != 0;
+            hole += p + k < used && !taken[k];
+            move += p + k >= used && taken[k];
+        }
+        int h = holes + group_scan(hole, s[buf][0], all);
+        holes += all;
+        int m = moved + group_scan(move, s[buf][1], all);
+        moved += all;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (p + k < used && !taken[k]) pairs[2 * h++ + 1] = p + k;
+            if (p + k >= used && taken[k]) pairs[2 * m++] = p + k;
+        }
+    }
+    // (as many holes as pages to move: `used` pages are taken)
+    for (int i = moved + tid; i < n_pages / 2; i += 1024) pairs[2 * i] = pairs[2 * i + 1] = -1;
+    if (tid == 0) { counts[0] = moved; counts[1] = used; }
+}
+__global__ __launch_bounds__(256)
+void compact_map_kernel(const int* __restrict__ refs, int n_pages, const int* __restrict__ pairs, const int* __restrict__ counts, int* __restrict__ refs_out, int* __restrict__ to)
+{
+    const int p = blockIdx.x * 256 + threadIdx.x, moved = counts[0], used = counts[1];
+    if (p < moved) to[pairs[2 * p]] = pairs[2 * p + 1];
+    if (p < moved) refs_out[pairs[2 * p + 1]] = refs[pairs[2 * p]];
+    if (p < n_pages && (p >= used || refs[p] != 0)) refs_out[p] = p < used ? refs[p] : 0;
+}
+__global__ __launch_bounds__(256)
+void compact_table_kernel(const int* table, int64_t entries, int n_pages, const int* __restrict__ refs, const int* __restrict__ counts, const int* __restrict__ to, int* table_out)
+{
+    const int used = counts[1];
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < entries; i += (int64_t)gridDim.x * 256) {
+        const int page = table[i];
+        const bool moves = page >= used && page < n_pages && refs[page] != 0;
+        table_out[i] = moves ? to[page] : page;
+    }
+}
+hipError_t launch_cache_compact(const int* table, const int* refs, int B, int n_pages, int max_pages, int* table_out, int* refs_out, int* pairs, int* counts, void* workspace, hipStream_t stream)
+{
+    int* to = static_cast<int*>(workspace);
+    compact_rank_kernel<<<1, 1024, 0, stream>>>(refs, n_pages, pairs, counts);
+    compact_map_kernel<<<(unsigned)((n_pages + 255) / 256), 256, 0, stream>>>(refs, n_pages, pairs, counts, refs_out, to);
+    const int64_t entries = (int64_t)B * max_pages, groups = (entries + 255) / 256;
+    compact_table_kernel<<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, stream>>>(table, entries, n_pages, refs, counts, to, table_out);
+    return hipGetLastError();
+}
+
+// ---- copies of pages
+constexpr int kPools = 64;                 // of a launch
+constexpr int kCopyBytes = 16384;          // of a page that a work-group takes at a time
+struct Pools { unsigned char* data[kPools]; int64_t stride[kPools], bytes[kPools]; int unit[kPools]; };
+template <typename W>
+__device__ __forceinline__ void copy_bytes(unsigned char* to, const unsigned char* from, int bytes)
+{
+    W* dst = reinterpret_cast<W*>(to);
+    const W* src = reinterpret_cast<const W*>(from);
+    const int n = bytes / (int)sizeof(W);
+    for (int i = threadIdx.x; i < n; i += 1024) {
+        const int last = n - 1;                        // (loads of four in flight: those behind the end read its last again)
+        const W a = src[i], b = src[min(i + 256, last)], c = src[min(i + 512, last)], d = src[min(i + 768, last)];
+        dst[i] = a;
+        if (i + 256 < n) dst[i + 256] = b;
+        if (i + 512 < n) dst[i + 512] = c;
+        if (i + 768 < n) dst[i + 768] = d;
+    }
+}
+__global__ __launch_bounds__(256)
+void cache_copy_kernel(Pools pools, int n_pools, int parts, int n_pages, const int* __restrict__ pairs, const int* __restrict__ counts, int n_pairs)
+{
+    const int n = counts ? min(max(counts[0], 0), n_pairs) : n_pairs;
+    const int64_t items = (int64_t)n * n_pools * parts;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int part = (int)(item % parts), pool = (int)(item / parts % n_pools);
+        const int64_t pair = item / parts / n_pools;
+        const int from = pairs[2 * pair], to = pairs[2 * pair + 1];
+        if ((unsigned)from >= (unsigned)n_pages || (unsigned)to >= (unsigned)n_pages || from == to) continue;
+        const int64_t at = (int64_t)part * kCopyBytes;
+        const int bytes = (int)min((int64_t)kCopyBytes, pools.bytes[pool] - at);
+        if (bytes <= 0) continue;
+        unsigned char* dst = pools.data[pool] + to * pools.stride[pool] + at;
+        const unsigned char* src = pools.data[pool] + from * pools.stride[pool] + at;
+        if (pools.unit[pool] == 16) copy_bytes<uint4>(dst, src, bytes);
+        else if (pools.unit[pool] == 4) copy_bytes<uint32_t>(dst, src, bytes);
+        else copy_bytes<uint8_t>(dst, src, bytes);
+    }
+}
+hipError_t launch_cache_copy(const psa_pool_t* pools, int n_pools, int n_pages, const int* pairs, const int* counts, int n_pairs, hipStream_t stream)
+{
+    for (int first = 0; first < n_pools; first += kPools) {
+        const int n = n_pools - first < kPools ? n_pools - first : kPools;
+        Pools p{};
+        int64_t most = 0;
+        for (int i = 0; i < n; ++i) {
+            const psa_pool_t& t = pools[first + i];
+            p.data[i] = static_cast<unsigned char*>(t.data);
+            p.stride[i] = t.page_stride;
+            p.bytes[i] = t.page_bytes;
+            const uintptr_t bits = reinterpret_cast<uintptr_t>(t.data) | (uintptr_t)t.page_stride | (uintptr_t)t.page_bytes;
+            p.unit[i] = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 1;
+            if (t.page_bytes > most) most = t.page_bytes;
+        }
+        const int64_t parts = (most + kCopyBytes - 1) / kCopyBytes, items = n_pairs * parts * n;
+        cache_copy_kernel<<<(unsigned)(items < 2048 ? items : 2048), 256, 0, stream>>>(p, n, (int)parts, n_pages, pairs, counts, n_pairs);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace psa

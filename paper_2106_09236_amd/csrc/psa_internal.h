@@ -200,4 +200,32 @@ hipError_t launch_packed_bwd(const PackedBwdPlan& p, const psa_packed_shape_t& s
                              const int* q_offsets, const int* k_offsets, const psa_heads_t& out, const float* lse, const psa_heads_t& dOut,
                              const psa_heads_t& dQ, const psa_heads_t& dK, const psa_heads_t& dV, void* workspace, hipStream_t stream);
 
+// Dense attention over a cache in pages (psa_paged.hip).
+//   few       1: 32 rows to a work-group, whose waves divide its keys; 0: 128 rows, 32 to a wave
+//   fine      1: bfloat16 weights in two parts
+//   per_head  work-groups of a key head that the work is divided into, beside one for each tile of rows; n_part: the most there are
+//   join      1: sequences may be divided; n_join: parts of 32 rows to join, at most
+struct PagedPlan { int few, fine, rows, join; int64_t per_head, n_part, n_join; size_t off_ml, off_part, total; };
+PagedPlan make_paged_plan(const psa_cache_t& cache, const psa_paged_shape_t& s);
+hipError_t launch_paged(const PagedPlan& p, const psa_paged_shape_t& s, const psa_heads_t& Q, const int* offsets, const psa_cache_t& cache, const psa_heads_t& out,
+                        float* lse, void* workspace, hipStream_t stream);
+
+// Rows into a cache, its pages' holders, compaction and copies (psa_cache.hip).
+hipError_t launch_cache_append(const psa_heads_t& K, const psa_heads_t& V, const int* offsets, const psa_cache_t& cache, const psa_paged_shape_t& s, hipStream_t stream);
+struct CacheUpdate {
+    const int *table, *lengths, *refs, *parents, *grow;
+    int B, B_out, n_pages, page_rows, max_pages;
+    int *table_out, *lengths_out, *refs_out, *pairs, *counts;
+};
+size_t cache_update_bytes(int B, int B_out, int n_pages);
+hipError_t launch_cache_update(const CacheUpdate& u, void* workspace, hipStream_t stream);
+size_t cache_compact_bytes(int n_pages);
+hipError_t launch_cache_compact(const int* table, const int* refs, int B, int n_pages, int max_pages, int* table_out, int* refs_out, int* pairs, int* counts,
+                                void* workspace, hipStream_t stream);
+hipError_t launch_cache_copy(const psa_pool_t* pools, int n_pools, int n_pages, const int* pairs, const int* counts, int n_pairs, hipStream_t stream);
+
+// Strides of a tensor of heads (psa_operators_api.cpp): multiples of `unit` elements, rows of `width` elements,
+// data aligned to `align` bytes; `out`: rows must not overlap.
+int check_heads(const psa_heads_t& t, int64_t unit, int64_t width, size_t align, int64_t batches, int64_t heads, int64_t rows, bool out);
+
 }  // namespace psa

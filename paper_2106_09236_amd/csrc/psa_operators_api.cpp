@@ -19,20 +19,23 @@ static int check_norm(int64_t rows, int32_t cols, int32_t dtype)
 
 // ---- heads
 // Strides (and limits that keep offsets inside a tile of rows within 31 bits), `out`: rows of an output must not overlap.
-static int check_heads(const psa_heads_t& t, int dtype, int64_t batches, int64_t heads, int64_t rows, bool out)
+int check_heads(const psa_heads_t& t, int64_t unit, int64_t width, size_t align, int64_t batches, int64_t heads, int64_t rows, bool out)
 {
-    const int64_t unit = dtype == PSA_F32 ? 4 : 8;
     const int64_t stride[3] = {t.batch_stride, t.head_stride, t.row_stride}, count[3] = {batches, heads, rows};
     for (int i = 0; i < 3; ++i) {
         if (stride[i] < 0) return PSA_ERR_ARG;
-        if (count[i] > 1 && out && stride[i] < 64) return PSA_ERR_ARG;
+        if (count[i] > 1 && out && stride[i] < width) return PSA_ERR_ARG;
         // the last element's offset within 62 bits
         if (count[i] > 1 && stride[i] > (INT64_MAX >> 3) / count[i]) return PSA_ERR_ARG;
     }
     if (rows > 1 && t.row_stride > (1 << 22)) return PSA_ERR_ARG;
     for (int i = 0; i < 3; ++i) if (stride[i] % unit != 0 && count[i] > 1) return PSA_ERR_ALIGN;
-    if (off_by(t.data, 16)) return PSA_ERR_ALIGN;
+    if (off_by(t.data, align)) return PSA_ERR_ALIGN;
     return PSA_OK;
+}
+static int check_heads(const psa_heads_t& t, int dtype, int64_t batches, int64_t heads, int64_t rows, bool out)
+{
+    return check_heads(t, dtype == PSA_F32 ? 4 : 8, 64, 16, batches, heads, rows, out);
 }
 
 // ---- rotary positions

@@ -7,53 +7,6 @@
 
 namespace psa {
 
-// What a wave keeps for 32 rows: running maximum (in base 2, scaled), sum and the output's accumulators.
-struct Rows32 {
-    float m, l;
-    floatx16 o[2];                         // element 32 dt + acc_row(r, h) of row c in o[dt][r]
-    __device__ __forceinline__ void init() { m = kMaxInit; l = 0.f; clear(o[0]); clear(o[1]); }
-    // Takes the maximum of the scores of N x 32 keys; the constant that is subtracted follows it only when that has grown by
-    // more than 2^8 (kLagLog2): weights up to 2^8 are as exact as weights up to 1, and a change scales 32 accumulators.
-    template <int N>
-    __device__ __forceinline__ void follow(const floatx16 (&s)[N], float scale) {
-        float t = s[0][0];
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) t = fmaxf(t, s[n][r]);
-        t = max_xor32(t) * scale;
-        const float m_new = t > m + kLagLog2 ? t : m;
-        if (__builtin_amdgcn_ballot_w64(m_new > m) != 0) {
-            const float alpha = fast_exp2(m - m_new);
-            l *= alpha;
-#pragma unroll
-            for (int dt = 0; dt < 2; ++dt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
-        }
-        m = m_new;
-    }
-    // Scores to weights
-    __device__ __forceinline__ void weights(floatx16& s, float scale) {
-        float sum = 0.f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) { s[r] = fast_exp2(fmaf(s[r], scale, -m)); sum += s[r]; }
-        l += sum;
-    }
-    // The infinities and NaN of V rows j0 .. j0 + n - 1 that were left out of the tile: to the rows that see them.
-    template <typename T>
-    __device__ __forceinline__ void add_nonfinite(const T* v, int64_t row_stride, int n, int n_vis, int h) {
-        for (int j = 0; j < n; ++j)
-#pragma unroll
-            for (int dt = 0; dt < 2; ++dt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float x = to_f32(v[j * row_stride + 32 * dt + acc_row(r, h)]);
-                    if (j < n_vis && !isfinite(x)) o[dt][r] += x;
-                }
-    }
-};
-
 // 4 waves of 32 rows each; tiles of KT keys and values go through LDS, the next tile's rows are on their way meanwhile.
 // bfloat16 is bound by the vector unit (131 instructions and 32 exponentials to 16 matrix instructions: 65 % of its issue
 // cycles, the matrix unit 38 %) and, in long runs, by power: 16384 causal, 8 heads, 335 to 355 us a call in 200 of them (820 to 775 TFLOP/s,

@@ -467,6 +467,207 @@ PyObject* packed_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
     return tuple(all, 3);
 }
 
+// ---- a cache in pages
+// K_pages, V_pages, table, lengths, offsets, K_scales, V_scales, of new rows `rows`
+struct CacheArg {
+    HeadsArg k, v;
+    Arg table, lengths, offsets;
+    psa_cache_t c{};
+    int64_t B = 0;
+    static bool scales(PyObject* o, const at::Tensor& pages, psa_heads_t& h) {
+        if (!THPVariable_Check(o)) return false;
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (t.dim() != 4 || t.scalar_type() != at::kByte || !here(t) || t.stride(3) != 1 || t.size(3) != 2) return false;
+        for (int i = 0; i < 3; ++i) if (t.size(i) != pages.size(i)) return false;
+        h = psa_heads_t{t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)};
+        return true;
+    }
+    bool take_all(const at::Tensor& rows, PyObject* k_o, PyObject* v_o, PyObject* table_o, PyObject* lengths_o, PyObject* offsets_o, PyObject* ks_o, PyObject* vs_o) {
+        if (!take_heads(k_o, k, false) || k.t->dim() != 4 || !take_heads_like(v_o, v, *k.t, false)) return false;
+        const bool mx = k.t->scalar_type() == at::kFloat8_e4m3fn;
+        if (!mx && (k.t->scalar_type() != rows.scalar_type() || ks_o != Py_None || vs_o != Py_None)) return false;
+        if (mx && (!scales(ks_o, *k.t, c.K_scales) || !scales(vs_o, *k.t, c.V_scales))) return false;
+        if (!take(table_o, table, false) || table.t->dim() != 2 || table.t->numel() == 0 || table.t->scalar_type() != at::kInt || !here(*table.t)) return false;
+        B = table.t->size(0);
+        if (!take_like(lengths_o, lengths, {B}, at::kInt, false) || !take_like(offsets_o, offsets, {B + 1}, at::kInt, true)) return false;
+        if (B > INT32_MAX || table.t->size(1) > INT32_MAX || k.t->size(0) > INT32_MAX || k.t->size(1) > INT32_MAX || k.t->size(2) > INT32_MAX ||
+            rows.size(1) > INT32_MAX || rows.size(0) > INT32_MAX || (!offsets.t && rows.size(1) % B != 0)) return false;
+        c.K = k.h;
+        c.V = v.h;
+        c.table = static_cast<const int32_t*>(table.ptr);
+        c.lengths = static_cast<const int32_t*>(lengths.ptr);
+        c.n_pages = (int32_t)k.t->size(0);
+        c.page_rows = (int32_t)k.t->size(2);
+        c.max_pages = (int32_t)table.t->size(1);
+        c.format = mx ? PSA_CACHE_MX : PSA_CACHE_PLAIN;
+        return true;
+    }
+    const int32_t* rows_of() const { return static_cast<const int32_t*>(offsets.ptr); }
+};
+
+// cache_append(K, V, K_pages, V_pages, table, lengths, offsets, K_scales, V_scales) -> True
+PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HeadsArg k, v;
+    CacheArg c;
+    psa_paged_shape_t s{};
+    if (n != 9 || !take_heads(a[0], k, false) || k.t->dim() != 3 || !take_heads_like(a[1], v, *k.t, false) || !dtype_of(*k.t, &s.dtype) ||
+        !c.take_all(*k.t, a[2], a[3], a[4], a[5], a[6], a[7], a[8]) || c.k.t->size(1) != k.t->size(0)) return none();
+    s.B = (int32_t)c.B; s.H = s.H_kv = (int32_t)k.t->size(0); s.T = (int32_t)k.t->size(1); s.D = 64; s.scale = 0.125;
+    int rc;
+    {
+        const Unlocked unlocked;
+        rc = probsparse_cache_append(&k.h, &v.h, c.rows_of(), &c.c, &s, stream());
+    }
+    if (rc != PSA_OK) return failed(rc);
+    Py_RETURN_TRUE;
+}
+
+// paged_fwd(Q, K_pages, V_pages, table, lengths, offsets, causal, scale, K_scales, V_scales, out, lse, workspace) -> out or (out, lse)
+PyObject* paged_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HeadsArg q, out;
+    CacheArg c;
+    Arg ws;
+    psa_paged_shape_t s{};
+    if (n != 13 || !take_heads(a[0], q, false) || q.t->dim() != 3 || !dtype_of(*q.t, &s.dtype) || !c.take_all(*q.t, a[1], a[2], a[3], a[4], a[5], a[8], a[9]) ||
+        q.t->size(0) % c.k.t->size(1) != 0 || !take_heads_like(a[10], out, *q.t, true) || !take(a[12], ws, true) || (ws.t && !here(*ws.t))) return none();
+    s.causal = PyObject_IsTrue(a[6]);
+    s.scale = a[7] == Py_None ? 0.125 : PyFloat_AsDouble(a[7]);
+    const int want_lse = PyObject_IsTrue(a[11]);
+    if (PyErr_Occurred()) { PyErr_Clear(); return none(); }
+    s.B = (int32_t)c.B; s.H = (int32_t)q.t->size(0); s.H_kv = (int32_t)c.k.t->size(1); s.T = (int32_t)q.t->size(1); s.D = 64;
+    const size_t bytes = ws.t ? ws.t->nbytes() : dense_attn_paged_workspace_bytes(&c.c, &s);
+    if (bytes == 0) return none();
+    at::Tensor made, lse, room;
+    int rc;
+    {
+        const Unlocked unlocked;
+        if (!ws.t) { room = scratch(*q.t, bytes); ws.ptr = room.data_ptr(); }
+        make_heads(out, made, *q.t);
+        if (want_lse) lse = at::empty({q.t->size(0), q.t->size(1)}, q.t->options().dtype(at::kFloat));
+        rc = dense_attn_paged_fwd(&q.h, c.rows_of(), &c.c, &out.h, want_lse ? lse.data_ptr<float>() : nullptr, &s, ws.ptr, bytes, stream());
+    }
+    if (rc != PSA_OK) return failed(rc);
+    PyObject* r = result(a[10], std::move(made));
+    if (!want_lse) return r;
+    PyObject* const all[] = {r, THPVariable_Wrap(std::move(lse))};
+    return tuple(all, 2);
+}
+
+int32_t* ints(const Arg& a) { return static_cast<int32_t*>(a.ptr); }
+void make_ints(Arg& a, at::Tensor& made, const at::Tensor& like, at::IntArrayRef sizes)
+{
+    if (a.t) return;
+    made = at::empty(sizes, like.options());
+    a.ptr = made.data_ptr();
+}
+bool int_arg(PyObject* o, int32_t* x)
+{
+    const long v = PyLong_AsLong(o);
+    if (PyErr_Occurred()) { PyErr_Clear(); return false; }
+    *x = (int32_t)v;
+    return v >= INT32_MIN && v <= INT32_MAX;
+}
+
+// cache_update(table, lengths, refs, page_rows, parents, grow, table_out, lengths_out, refs_out, pairs, counts, workspace) -> the five outputs
+PyObject* cache_update(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Arg table, lengths, refs, parents, grow, out[5], ws;
+    int32_t page_rows;
+    if (n != 12 || !take(a[0], table, false) || table.t->dim() != 2 || table.t->numel() == 0 || table.t->scalar_type() != at::kInt || !here(*table.t)) return none();
+    const int64_t B = table.t->size(0), max_pages = table.t->size(1);
+    if (!take_like(a[1], lengths, {B}, at::kInt, false) || !take(a[2], refs, false) || refs.t->dim() != 1 || refs.t->numel() == 0 || refs.t->scalar_type() != at::kInt ||
+        !here(*refs.t) || !int_arg(a[3], &page_rows) || !take(a[4], parents, true)) return none();
+    const int64_t n_pages = refs.t->numel(), B_out = parents.t ? parents.t->numel() : B;
+    if (B_out == 0 || (parents.t && (parents.t->dim() != 1 || parents.t->scalar_type() != at::kInt || !here(*parents.t))) || !take_like(a[5], grow, {B_out}, at::kInt, true) ||
+        !take_like(a[6], out[0], {B_out, max_pages}, at::kInt, true) || !take_like(a[7], out[1], {B_out}, at::kInt, true) || !take_like(a[8], out[2], {n_pages}, at::kInt, true) ||
+        !take_like(a[9], out[3], {B_out, 2}, at::kInt, true) || !take_like(a[10], out[4], {2}, at::kInt, true) || !take(a[11], ws, true) || (ws.t && !here(*ws.t)) ||
+        B > INT32_MAX || B_out > INT32_MAX || n_pages > INT32_MAX || max_pages > INT32_MAX) return none();
+    const size_t bytes = ws.t ? ws.t->nbytes() : probsparse_cache_update_workspace_bytes((int32_t)B, (int32_t)B_out, (int32_t)n_pages);
+    if (bytes == 0) return none();
+    at::Tensor made[5], room;
+    int rc;
+    {
+        const Unlocked unlocked;
+        if (!ws.t) { room = at::empty({(int64_t)bytes}, table.t->options().dtype(at::kByte)); ws.ptr = room.data_ptr(); }
+        make_ints(out[0], made[0], *table.t, {B_out, max_pages});
+        make_ints(out[1], made[1], *table.t, {B_out});
+        make_ints(out[2], made[2], *table.t, {n_pages});
+        make_ints(out[3], made[3], *table.t, {B_out, 2});
+        make_ints(out[4], made[4], *table.t, {2});
+        rc = probsparse_cache_update(ints(table), ints(lengths), ints(refs), (int32_t)B, ints(parents), ints(grow), (int32_t)B_out, (int32_t)n_pages, page_rows, (int32_t)max_pages,
+                                     ints(out[0]), ints(out[1]), ints(out[2]), ints(out[3]), ints(out[4]), ws.ptr, bytes, stream());
+    }
+    if (rc != PSA_OK) return failed(rc);
+    PyObject* all[5];
+    for (int i = 0; i < 5; ++i) all[i] = result(a[6 + i], std::move(made[i]));
+    return tuple(all, 5);
+}
+
+// cache_compact(table, refs, table_out, refs_out, pairs, counts, workspace) -> the four outputs
+PyObject* cache_compact(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Arg table, refs, out[4], ws;
+    if (n != 7 || !take(a[0], table, false) || table.t->dim() != 2 || table.t->numel() == 0 || table.t->scalar_type() != at::kInt || !here(*table.t) || !take(a[1], refs, false) ||
+        refs.t->dim() != 1 || refs.t->numel() == 0 || refs.t->scalar_type() != at::kInt || !here(*refs.t)) return none();
+    const int64_t B = table.t->size(0), max_pages = table.t->size(1), n_pages = refs.t->numel();
+    if (!take_like(a[2], out[0], {B, max_pages}, at::kInt, true) || !take_like(a[3], out[1], {n_pages}, at::kInt, true) || !take_like(a[4], out[2], {n_pages / 2, 2}, at::kInt, true) ||
+        !take_like(a[5], out[3], {2}, at::kInt, true) || !take(a[6], ws, true) || (ws.t && !here(*ws.t)) || B > INT32_MAX || n_pages > INT32_MAX || max_pages > INT32_MAX) return none();
+    const size_t bytes = ws.t ? ws.t->nbytes() : probsparse_cache_compact_workspace_bytes((int32_t)n_pages);
+    if (bytes == 0) return none();
+    at::Tensor made[4], room;
+    int rc;
+    {
+        const Unlocked unlocked;
+        if (!ws.t) { room = at::empty({(int64_t)bytes}, table.t->options().dtype(at::kByte)); ws.ptr = room.data_ptr(); }
+        make_ints(out[0], made[0], *table.t, {B, max_pages});
+        make_ints(out[1], made[1], *table.t, {n_pages});
+        make_ints(out[2], made[2], *table.t, {n_pages / 2, 2});
+        make_ints(out[3], made[3], *table.t, {2});
+        rc = probsparse_cache_compact(ints(table), ints(refs), (int32_t)B, (int32_t)n_pages, (int32_t)max_pages, ints(out[0]), ints(out[1]), ints(out[2]), ints(out[3]), ws.ptr,
+                                      bytes, stream());
+    }
+    if (rc != PSA_OK) return failed(rc);
+    PyObject* all[4];
+    for (int i = 0; i < 4; ++i) all[i] = result(a[2 + i], std::move(made[i]));
+    return tuple(all, 4);
+}
+
+// cache_copy(pools, pairs, counts) -> True
+PyObject* cache_copy(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    constexpr Py_ssize_t kMost = 64;
+    Arg pairs, counts;
+    if (n != 3 || !(PyList_Check(a[0]) || PyTuple_Check(a[0])) || !take(a[1], pairs, false) || pairs.t->dim() != 2 || pairs.t->size(1) != 2 ||
+        pairs.t->scalar_type() != at::kInt || !here(*pairs.t) || pairs.t->size(0) > INT32_MAX || !take(a[2], counts, true) ||
+        (counts.t && (counts.t->scalar_type() != at::kInt || counts.t->numel() == 0 || !here(*counts.t)))) return none();
+    const Py_ssize_t n_pools = PySequence_Fast_GET_SIZE(a[0]);
+    if (n_pools < 1 || n_pools > kMost) return none();
+    psa_pool_t pools[kMost];
+    int64_t n_pages = 0;
+    for (Py_ssize_t i = 0; i < n_pools; ++i) {
+        PyObject* o = PySequence_Fast_GET_ITEM(a[0], i);
+        if (!THPVariable_Check(o)) return none();
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (t.dim() < 2 || t.numel() == 0 || !here(t) || (i > 0 && t.size(0) != n_pages) || t.size(0) > INT32_MAX) return none();
+        n_pages = t.size(0);
+        int64_t elements = 1;                          // of a page, which is contiguous
+        for (int64_t d = t.dim() - 1; d > 0; --d) {
+            if (t.size(d) != 1 && t.stride(d) != elements) return none();
+            elements *= t.size(d);
+        }
+        pools[i] = psa_pool_t{t.data_ptr(), t.stride(0) * (int64_t)t.element_size(), elements * (int64_t)t.element_size()};
+    }
+    int rc;
+    {
+        const Unlocked unlocked;
+        rc = probsparse_cache_copy(pools, (int32_t)n_pools, (int32_t)n_pages, ints(pairs), ints(counts), (int32_t)pairs.t->size(0), stream());
+    }
+    if (rc != PSA_OK) return failed(rc);
+    Py_RETURN_TRUE;
+}
+
 // exceptions of the tensor library (no memory, say) must not cross into the interpreter: the caller's path meets them
 // again and reports them
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
@@ -492,6 +693,11 @@ PyMethodDef methods[] = {
     {"rotary", entry<rotary>(), METH_FASTCALL, nullptr},
     {"packed_fwd", entry<packed_fwd>(), METH_FASTCALL, nullptr},
     {"packed_bwd", entry<packed_bwd>(), METH_FASTCALL, nullptr},
+    {"cache_append", entry<cache_append>(), METH_FASTCALL, nullptr},
+    {"paged_fwd", entry<paged_fwd>(), METH_FASTCALL, nullptr},
+    {"cache_update", entry<cache_update>(), METH_FASTCALL, nullptr},
+    {"cache_compact", entry<cache_compact>(), METH_FASTCALL, nullptr},
+    {"cache_copy", entry<cache_copy>(), METH_FASTCALL, nullptr},
     {"on_status", on_status, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

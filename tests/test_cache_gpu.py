@@ -1,0 +1,466 @@
+"""A cache in pages: rows written to it, attention over it, forks, growth, compaction and copies, against float64 and plain lists."""
+import math
+
+import pytest
+import torch
+
+from paper_2106_09236_amd import binding as psa
+from tests import cache_oracle as O
+from tests.operator_bounds import assert_within
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+class Cache:
+    """Pools on the GPU, filled with NaN where nothing has been written, and tables."""
+
+    def __init__(self, H_kv, page_rows, lengths, dtype, mx=False, by_frame=False, together=True, spare=3, width=None, holes=(), seed=0):
+        g = torch.Generator().manual_seed(seed + sum(lengths) + page_rows)
+        self.H_kv, self.P, self.dtype, self.mx, self.lengths_host = H_kv, page_rows, dtype, mx, list(lengths)
+        per = [-(-n // page_rows) for n in lengths]
+        self.n_pages = sum(per) + spare
+        width = width or max(max(per), 1) + 1
+        order = torch.randperm(self.n_pages, generator=g).tolist()
+        self.table_host = torch.full((len(lengths), width), -1, dtype=torch.int32)
+        for s, n in enumerate(per):
+            self.table_host[s, :n] = torch.tensor(order[:n], dtype=torch.int32)
+            order = order[n:]
+        for s, j, value in holes:
+            self.table_host[s, j] = value
+        self.table, self.lengths = self.table_host.cuda(), torch.tensor(lengths, dtype=torch.int32, device="cuda")
+        kind = torch.float8_e4m3fn if mx else dtype
+        nan = 0x7F if mx else 0xFF
+        self.K, self.V = self._views(64, kind, by_frame, together, nan)
+        self.scales = self._views(2, torch.uint8, by_frame, together, 127) if mx else (None, None)
+        self.kw = dict(K_scales=self.scales[0], V_scales=self.scales[1]) if mx else {}
+
+    def _views(self, cols, kind, by_frame, together, fill):
+        rows = (self.P, self.H_kv, cols) if by_frame else (self.H_kv, self.P, cols)
+        shape = (self.n_pages, 2, *rows) if together else (2, self.n_pages, *rows)
+        pool = torch.full((*shape[:-1], cols * torch.empty(0, dtype=kind).element_size()), fill, dtype=torch.uint8, device="cuda").view(kind)
+        k, v = (pool[:, 0], pool[:, 1]) if together else pool
+        return (k.transpose(1, 2), v.transpose(1, 2)) if by_frame else (k, v)
+
+    def rows(self, page, slot):
+        """K and V of rows, [H_kv, n, 64] float64, from what lies in the pools."""
+        out = []
+        for x, s in zip((self.K, self.V), self.scales):
+            raw = x.contiguous().cpu()
+            if self.mx:
+                raw = raw.view(torch.uint8)[page, :, slot].view(torch.float8_e4m3fn)
+                out.append(O.mx_decode(raw, s.contiguous().cpu()[page, :, slot]).transpose(0, 1))
+            else:
+                out.append(raw[page, :, slot].double().transpose(0, 1))
+        return out
+
+    def append(self, K, V, offsets=None):
+        psa.probsparse_cache_append(K, V, self.K, self.V, self.table, self.lengths, offsets, **self.kw)
+
+    def fill(self, seed=1, wide=False):
+        """All rows of all sequences, written by one call; the rows [H_kv, sum of lengths, 64]."""
+        g = torch.Generator().manual_seed(seed)
+        T = sum(self.lengths_host)
+        K, V = (torch.randn((self.H_kv, T, 64), generator=g) for _ in range(2))
+        K, V = K.to(self.dtype), V.to(self.dtype)
+        self.append(K.cuda(), V.cuda(), _offsets(self.lengths_host))
+        return K, V
+
+    def attend(self, Q, offsets=None, **kw):
+        return psa.dense_attn_paged_fwd(Q, self.K, self.V, self.table, self.lengths, offsets, **self.kw, **kw)
+
+
+def _offsets(lens, front=0):
+    return torch.tensor([front] + lens, dtype=torch.int32).cumsum(0).int().cuda()
+
+
+def _queries(H, T, dtype, by_frame=False, wide=True, seed=2):
+    g = torch.Generator().manual_seed(seed + T)
+    x = torch.randn((T, H, 64) if by_frame else (H, T, 64), generator=g)
+    if wide:
+        x = x * (1 + 5 * (torch.rand(x.shape[:-1], generator=g) < 0.1).unsqueeze(-1))
+    x = x.to(dtype)
+    return (x.transpose(0, 1), x.cuda().transpose(0, 1)) if by_frame else (x, x.cuda())
+
+
+def _check(cache, H, new, causal, by_frame=False, uniform=False, scale=0.125):
+    Q, Qd = _queries(H, sum(new), cache.dtype, by_frame)
+    off = None if uniform else _offsets(new)
+    out = torch.full_like(Qd, math.nan)
+    _, lse = cache.attend(Qd, off, causal=causal, scale=scale, out=out, lse=True)
+    want, e_out, want_lse, e_lse = O.attention(Q, cache.rows, cache.table_host, cache.lengths_host, new, cache.P, causal, scale, cache.dtype, cache.n_pages)
+    assert_within(out, want, e_out, "out")
+    empty = want_lse.isinf()
+    assert torch.equal(lse.cpu().isinf(), empty) and not (lse.cpu()[empty] > 0).any()
+    assert_within(lse.cpu().masked_fill(empty, 0.0), want_lse.masked_fill(empty, 0.0), e_lse, "lse")
+    assert torch.equal(cache.attend(Qd, off, causal=causal, scale=scale), out)       # the same again, to the last bit
+    return out
+
+
+FORMATS = [(F32, False), (BF16, False), (F32, True), (BF16, True)]
+
+
+@pytest.mark.parametrize("dtype,mx", FORMATS)
+@pytest.mark.parametrize("H_kv,page_rows,lengths,by_frame,together", [
+    (1, 1, [1], False, True), (2, 16, [0, 1, 15, 16, 17, 33], True, True), (3, 8, [40, 7], False, False), (4, 64, [130, 64], True, False), (8, 256, [300], False, True)])
+def test_append(H_kv, page_rows, lengths, by_frame, together, dtype, mx):
+    """Rows where they belong, to the last bit, and nothing else touched: prompts, then one and three more rows of each."""
+    cache = Cache(H_kv, page_rows, [n + 4 for n in lengths], dtype, mx, by_frame, together)
+    full = [n + 4 for n in lengths]
+    g = torch.Generator().manual_seed(5)
+    K, V = (torch.randn((H_kv, sum(full), 64), generator=g) * torch.exp2(torch.randint(-40, 40, (H_kv, sum(full), 1), generator=g)) for _ in range(2))
+    K, V = K.to(dtype), V.to(dtype)
+    start = [sum(full[:s]) for s in range(len(full))]
+    for lo, hi, uniform in ((0, 0, False), (0, 1, True), (1, 4, False)):
+        lens = [n + hi for n in lengths]
+        new = lens if hi == 0 else [hi - lo] * len(lens)
+        if sum(new) == 0:
+            continue
+        index = torch.tensor([start[s] + n - a + t for s, (n, a) in enumerate(zip(lens, new)) for t in range(a)], dtype=torch.long)
+        cache.lengths = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        cache.append(K[:, index].cuda(), V[:, index].cuda(), None if uniform else _offsets(new))
+    raw = [x.contiguous().view(torch.uint8).cpu() for x in (cache.K, cache.V)]
+    for x, source, scales in zip(raw, (K, V), cache.scales):
+        left = torch.ones(x.shape[:3], dtype=torch.bool)
+        for s, n in enumerate(full):
+            j = torch.arange(n)
+            page, slot = cache.table_host[s].long()[j // page_rows], j % page_rows
+            rows = source[:, start[s]:start[s] + n].transpose(0, 1)
+            got = x[page, :, slot]
+            if mx:
+                codes, e = O.mx_encode(rows)
+                assert torch.equal(got.view(torch.float8_e4m3fn).double(), codes)
+                assert torch.equal(scales.contiguous().cpu()[page, :, slot].long(), e + 127)
+            else:
+                assert torch.equal(got, rows.contiguous().view(torch.uint8))
+            left[page, :, slot] = False
+        assert (x[left] == (0x7F if mx else 0xFF)).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_8_bit_elements(dtype):
+    """Every code, ties, the least and largest numbers, zeros, infinities and NaN."""
+    codes = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float()
+    codes = codes[codes.isfinite()]
+    between = torch.cat([codes, (codes[:-1] + codes[1:]) / 2])
+    between = between[between.abs() <= 448]
+    rows = [between.repeat(64)[i:i + 64 * 8].reshape(8, 64) for i in (0, 7, 100)]
+    x = torch.cat([*rows, torch.ldexp(rows[0], torch.arange(-140, -132)[:, None]), torch.ldexp(rows[1], torch.arange(110, 118)[:, None]),
+                   torch.zeros(1, 64), torch.full((1, 64), 3.3e38), torch.full((1, 64), 1e-45), torch.full((1, 64), 1.75), torch.full((1, 64), 1.7578125)])
+    odd = torch.randn(4, 64)
+    odd[0, 3], odd[1, 40], odd[2, 5:40], odd[3, :] = math.nan, math.inf, -math.inf, math.nan
+    x = torch.cat([x, odd]).to(dtype)
+    n = x.shape[0]
+    cache = Cache(1, 16, [n], dtype, mx=True)
+    cache.append(x[None].cuda(), x[None].cuda())
+    j = torch.arange(n)
+    page, slot = cache.table_host[0].long()[j // 16], j % 16
+    want, e = O.mx_encode(x)
+    for t, scales in zip((cache.K, cache.V), cache.scales):
+        got = t.contiguous().view(torch.uint8).cpu()[page, 0, slot].view(torch.float8_e4m3fn).double()
+        assert torch.equal(scales.contiguous().cpu()[page, 0, slot].long(), e + 127)
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(), want.nan_to_num())
+
+
+def test_8_bit_codes_are_read_exactly():
+    """A query that sees one key returns its value: every code times powers over the whole range."""
+    e = torch.tensor([10, 11, 60, 126, 127, 128, 200, 245, 246])
+    codes = torch.arange(256, dtype=torch.uint8)
+    codes = codes[(codes & 0x7F) != 0x7F]
+    rows = codes.repeat(3)[:64 * 8].reshape(8, 64)
+    n = rows.shape[0] * e.numel()
+    for dtype in (F32, BF16):
+        cache = Cache(1, 1, [1] * n, dtype, mx=True, together=False, spare=0, width=1)
+        page = cache.table_host[:, 0].long()
+        V = torch.empty(n, 64, dtype=torch.uint8)
+        s = torch.empty(n, 2, dtype=torch.uint8)
+        V[page] = rows.repeat(e.numel(), 1)
+        s[page] = e.repeat_interleave(8)[:, None].expand(-1, 2).to(torch.uint8)
+        cache.V.view(torch.uint8).copy_(V.cuda()[:, None, None])
+        cache.K.view(torch.uint8).zero_()
+        cache.scales[1].copy_(s.cuda()[:, None, None])
+        out = cache.attend(torch.randn(1, n, 64).to(dtype).cuda())
+        want = O.mx_decode(V.view(torch.float8_e4m3fn), s)[page].to(dtype)
+        assert torch.equal(out[0].cpu(), want), dtype
+
+
+@pytest.mark.parametrize("dtype,mx", FORMATS)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("H,H_kv,page_rows,lengths,by_frame", [
+    (1, 1, 16, [1], False), (8, 2, 64, [1, 40, 129, 600, 0], True), (4, 4, 16, [2100], False), (8, 1, 1, [70, 3], False), (4, 2, 2, [33, 100], True),
+    (6, 3, 4, [31, 32, 65], False), (8, 8, 8, [500, 8], True), (8, 4, 256, [700, 256, 1], False), (2, 2, 32, [31, 32, 33, 64, 1200], True)])
+def test_single_tokens(H, H_kv, page_rows, lengths, by_frame, causal, dtype, mx):
+    cache = Cache(H_kv, page_rows, lengths, dtype, mx, by_frame)
+    cache.fill()
+    _check(cache, H, [min(n, 1) for n in lengths], causal, by_frame)
+    if min(lengths) > 0:
+        _check(cache, H, [1] * len(lengths), causal, by_frame, uniform=True)
+
+
+@pytest.mark.parametrize("dtype,mx", FORMATS)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("H,H_kv,page_rows,lengths,new", [
+    (4, 2, 16, [100, 33, 200], [33, 33, 5]), (8, 8, 32, [300, 64], [64, 64]), (2, 1, 64, [400], [400]), (4, 1, 8, [150, 20], [130, 20]),
+    (2, 2, 128, [1000, 10], [127, 0]), (3, 3, 2, [140], [129]), (2, 2, 1, [90], [70]), (16, 16, 16, [333, 700, 12], [333, 260, 12]), (4, 4, 16, [0, 20], [5, 40])])
+def test_chunks(H, H_kv, page_rows, lengths, new, causal, dtype, mx):
+    """Chunks of new rows, prompts, more new rows than the cache has (the first see nothing under the mask)."""
+    cache = Cache(H_kv, page_rows, lengths, dtype, mx, by_frame=causal)
+    cache.fill()
+    _check(cache, H, new, causal, by_frame=not causal)
+
+
+@pytest.mark.parametrize("dtype,mx", FORMATS)
+def test_many_rows_and_splits(dtype, mx):
+    """Work-groups of 128 rows whose weights are rounded, and keys in splits."""
+    cache = Cache(8, 64, [3000, 1500], dtype, mx)
+    cache.fill()
+    _check(cache, 16, [1000, 1200], True)
+    cache = Cache(2, 16, [9000], dtype, mx)
+    cache.fill()
+    _check(cache, 4, [200], False)
+
+
+@pytest.mark.parametrize("dtype,mx", FORMATS)
+@pytest.mark.parametrize("causal", [False, True])
+def test_missing_pages(causal, dtype, mx):
+    """Pages that have been freed, entries out of range, sequences with no page at all: as if masked."""
+    holes = [(0, 0, -1), (0, 1, -1), (0, 5, 1 << 30), (1, 2, -(1 << 31)), (2, 0, -1), (2, 1, -1), (2, 2, -7), (3, 1, 10 ** 6)]
+    for page_rows, lengths in ((16, [200, 60, 40, 30]), (64, [500, 200, 150, 128]), (4, [64, 20, 12, 8])):
+        cache = Cache(2, page_rows, lengths, dtype, mx, holes=holes)
+        cache.fill()                  # (rows without a page are left out)
+        _check(cache, 4, [1] * 4, causal, uniform=True)
+        _check(cache, 4, [3, 20, 40, 5], causal)
+
+
+@pytest.mark.parametrize("dtype,mx", FORMATS)
+@pytest.mark.parametrize("B,longest", [(257, 40), (700, 9), (1500, 130)])
+def test_many_sequences(B, longest, dtype, mx):
+    g = torch.Generator().manual_seed(B)
+    lengths = torch.randint(0, longest + 1, (B,), generator=g).tolist()
+    lengths[B // 3] = 1500
+    cache = Cache(1, 16, lengths, dtype, mx)
+    cache.fill()
+    _check(cache, 2, [min(n, 1) for n in lengths], True)
+    _check(cache, 2, [min(n, 3 + 60 * (s == B // 3)) for s, n in enumerate(lengths)], True)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("new", [[1, 1], [40, 40]])
+def test_rows_of_no_sequence(new, dtype):
+    cache = Cache(2, 16, [50, 70], dtype)
+    cache.fill()
+    Q, Qd = _queries(4, 100, dtype)
+    out = torch.full_like(Qd, math.nan)
+    _, lse = cache.attend(Qd, _offsets(new, front=7), out=out, lse=True)
+    inside = torch.zeros(100, dtype=torch.bool)
+    inside[7:7 + sum(new)] = True
+    assert (out.cpu()[:, ~inside] == 0).all() and (lse.cpu()[:, ~inside] == -math.inf).all()
+    want, e, _, _ = O.attention(Q[:, inside], cache.rows, cache.table_host, cache.lengths_host, new, 16, False, 0.125, dtype, cache.n_pages)
+    assert_within(out[:, inside.cuda()], want, e)
+
+
+@pytest.mark.parametrize("dtype,mx", FORMATS)
+@pytest.mark.parametrize("new", [1, 40])
+def test_nonfinite_rows(new, dtype, mx):
+    """Infinities and NaN reach the rows that see them and no others."""
+    lengths = [300, 300]
+    cache = Cache(1, 16, lengths, dtype, mx)
+    K, V = cache.fill()
+    Q, Qd = _queries(2, 2 * new, dtype, wide=False)
+    clean = cache.attend(Qd, causal=True).cpu()
+    bad = 295 if new > 1 else 299                       # of the first sequence: queries from it on see it
+    V[0, bad, 5] = math.nan
+    if not mx:
+        V[0, bad, 9] = math.inf
+    cache.append(K.cuda(), V.cuda(), _offsets(lengths))
+    out = cache.attend(Qd, causal=True).cpu()
+    sees = torch.zeros(2 * new, dtype=torch.bool)
+    sees[(new - (300 - bad)):new] = True
+    assert torch.equal(out[:, ~sees], clean[:, ~sees])
+    assert out[:, sees, 5].isnan().all()
+    if not mx:
+        assert (out[:, sees, 9] == math.inf).all()
+    rest = [e for e in range(64) if e not in (5, 9)]
+    if not mx:
+        assert torch.equal(out[:, sees][..., rest], clean[:, sees][..., rest])
+    else:
+        assert out[:, sees][..., rest].isfinite().all()
+    # NaN in a key makes its score and with it the rows that see it NaN
+    K[0, bad, 0] = math.nan
+    cache.append(K.cuda(), V.cuda(), _offsets(lengths))
+    out = cache.attend(Qd, causal=True).cpu()
+    assert torch.equal(out[:, ~sees], clean[:, ~sees]) and out[:, sees].isnan().all()
+
+
+def test_packed_attention_says_the_same():
+    """Over the same rows, packed."""
+    for dtype in (F32, BF16):
+        lengths, new = [300, 65, 20], [40, 40, 20]
+        cache = Cache(2, 16, lengths, dtype)
+        K, V = cache.fill()
+        Q, Qd = _queries(4, 100, dtype)
+        packed = psa.dense_attn_packed_fwd(Qd, K.cuda(), V.cuda(), _offsets(new), _offsets(lengths), causal=True)
+        paged = cache.attend(Qd, _offsets(new), causal=True)
+        assert (packed.double() - paged.double()).norm() <= (2.0 ** -8 if dtype == BF16 else 2.0 ** -18) * packed.double().norm()
+
+
+# ----------------------------------------------------------------------------------------------------------- the holders
+def _holders(B, width, page_rows, n_pages, g, share=True):
+    """A consistent table: sequences with pages of their own and full ones in common."""
+    order = torch.randperm(n_pages, generator=g).tolist()
+    table, lengths = [], []
+    for s in range(B):
+        n = int(torch.randint(0, width * page_rows + 1, (1,), generator=g))
+        row = []
+        if share and s and float(torch.rand(1, generator=g)) < 0.6:
+            other = int(torch.randint(0, s, (1,), generator=g))
+            full = min(n, lengths[other]) // page_rows
+            row = table[other][:int(torch.randint(0, full + 1, (1,), generator=g))]
+        need = -(-n // page_rows) - len(row)
+        if need > len(order):
+            need, n = len(order), (len(order) + len(row)) * page_rows
+        row, order = row + order[:need], order[need:]
+        table.append(row)
+        lengths.append(n)
+    refs = [0] * n_pages
+    for row in table:
+        for x in row:
+            refs[x] += 1
+    return [row + [-1] * (width - len(row)) for row in table], lengths, refs
+
+
+def _ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _check_update(table, lengths, refs, page_rows, parents, grow):
+    got = psa.probsparse_cache_update(_ints(table), _ints(lengths), _ints(refs), page_rows, None if parents is None else _ints(parents), None if grow is None else _ints(grow))
+    rows, grown, counts, pairs, missing = O.update(table, lengths, refs, page_rows, parents, grow)
+    B_out = len(rows)
+    assert got[0].tolist() == rows
+    assert got[1].tolist() == grown
+    assert got[2].tolist() == counts
+    assert got[3].tolist() == [list(p) for p in pairs] + [[-1, -1]] * (B_out - len(pairs))
+    assert got[4].tolist() == [len(pairs), missing]
+    return rows, grown, counts
+
+
+@pytest.mark.parametrize("B,width,page_rows,n_pages", [(1, 1, 1, 1), (3, 4, 16, 20), (8, 5, 4, 60), (64, 9, 8, 700), (130, 3, 1, 300), (40, 30, 16, 5000), (1500, 4, 2, 4200)])
+def test_update(B, width, page_rows, n_pages):
+    """Several steps each: forks, ends, starts, growth over page borders, pages that run out, tables that are full."""
+    g = torch.Generator().manual_seed(B + n_pages)
+    state = _holders(B, width, page_rows, n_pages, g)
+    _check_update(*state, page_rows, None, None)
+    for step in range(4):
+        n = len(state[0])
+        B_out = max(1, n + [0, 5, -2, 0][step])
+        parents = torch.randint(-1, n + 1, (B_out,), generator=g).tolist()
+        grow = torch.randint(-1, [2, 3, 2 * page_rows, page_rows * width][step] + 1, (B_out,), generator=g).tolist()
+        state = _check_update(*state, page_rows, parents, grow)
+        state = _check_update(*state, page_rows, None, [1] * B_out)
+
+
+def test_update_with_pages_held_elsewhere():
+    """A last page that somebody else counts is never written to: all who grow get copies."""
+    table, lengths, refs = [[0, 1], [2, -1]], [6, 2], [1, 2, 1, 0, 0, 0]
+    rows, grown, counts = _check_update(table, lengths, refs, 4, [0, 0, 1], [1, 1, 1])
+    assert counts[1] == 1 and rows[0][1] != 1 and rows[1][1] != 1 and rows[2][0] == 2
+
+
+def test_update_of_many_sequences():
+    """Beyond what each sequence looks through for those that continue it."""
+    g = torch.Generator().manual_seed(1)
+    state = _holders(3000, 2, 4, 7000, g)
+    _check_update(*state, 4, torch.randint(-1, 3000, (5000,), generator=g).tolist(), torch.randint(0, 3, (5000,), generator=g).tolist())
+    _check_update(*_holders(4500, 2, 4, 9500, g), 4, None, [1] * 4500)
+
+
+@pytest.mark.parametrize("n_pages", [1, 2, 7, 64, 1000, 4096, 4097, 20000])
+def test_compact(n_pages):
+    g = torch.Generator().manual_seed(n_pages)
+    for used in (0, 1, n_pages // 3, n_pages // 2, n_pages - 1, n_pages):
+        pages = torch.randperm(n_pages, generator=g)[:used]
+        refs = torch.zeros(n_pages, dtype=torch.int32)
+        refs[pages] = torch.randint(1, 5, (used,), generator=g).int()
+        table = torch.full((5, max(used, 1)), -1, dtype=torch.int32)
+        table[0, :used], table[3, :used // 2] = pages.int(), pages[:used // 2].int()
+        table[1, 0] = 1 << 30
+        want = O.compact(table.tolist(), refs.tolist())
+        for alias in (False, True):
+            t = table.cuda()
+            got = psa.probsparse_cache_compact(t, refs.cuda(), table_out=t if alias else None)
+            assert got[0].tolist() == want[0] and got[1].tolist() == want[1]
+            assert got[2].tolist() == [list(p) for p in want[2]] + [[-1, -1]] * (n_pages // 2 - len(want[2]))
+            assert got[3].tolist() == [len(want[2]), used]
+
+
+@pytest.mark.parametrize("page", [(3,), (2, 5), (4, 16, 64), (1,), (70000,)])
+def test_copy(page):
+    """Pools of several types and alignments; pairs out of range, behind the count, or of a page to itself are left out."""
+    g = torch.Generator().manual_seed(0)
+    pools = [torch.randint(0, 100, (12, *page), generator=g).to(t) for t in (torch.uint8, torch.int32, torch.bfloat16)]
+    wide = torch.randint(0, 100, (12, 2, *page), generator=g).to(torch.float32)
+    device = [x.cuda() for x in pools] + [wide.cuda()[:, 1]]
+    pairs = [[0, 5], [3, 7], [-1, 2], [1, 12], [12, 1], [4, 4], [0, 6], [9, 8]]
+    psa.probsparse_cache_copy(device, _ints(pairs), _ints([7, 3]))
+    for got, x in zip(device, pools + [wide[:, 1]]):
+        want = x.clone()
+        want[5], want[7], want[6] = x[0], x[3], x[0]
+        assert torch.equal(got.cpu(), want)
+    psa.probsparse_cache_copy(device * 20, _ints([[9, 8]]))
+    assert all(torch.equal(x[8], x[9]) for x in device)
+
+
+# ------------------------------------------------------------------------------------------------------- all of them
+@pytest.mark.parametrize("dtype,mx", FORMATS)
+def test_streams_step_by_step(dtype, mx):
+    """Beams that fork, end and grow over many steps, compacted now and then: every step's attention is that over each beam's own
+    history of rows, kept apart here."""
+    H, H_kv, P, n_pages, width, beams = 4, 2, 8, 80, 10, 6
+    g = torch.Generator().manual_seed(11)
+    kind = torch.float8_e4m3fn if mx else dtype
+    size = torch.empty(0, dtype=kind).element_size()
+    pool = torch.full((n_pages, 2, H_kv, P, 64 * size), 0x7F, dtype=torch.uint8, device="cuda").view(kind)
+    scales = torch.full((n_pages, 2, H_kv, P, 2), 127, dtype=torch.uint8, device="cuda")
+    kw = dict(K_scales=scales[:, 0], V_scales=scales[:, 1]) if mx else {}
+    pools = [pool, scales] if mx else [pool]
+    table, lengths = torch.full((1, width), -1, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    refs = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+    history = [[torch.zeros(H_kv, 0, 64, dtype=dtype)] * 2]
+
+    def step(parents, new, causal):
+        nonlocal table, lengths, refs, history
+        table, lengths, refs, pairs, counts = psa.probsparse_cache_update(table, lengths, refs, P, _ints(parents), _ints(new))
+        psa.probsparse_cache_copy(pools, pairs, counts)
+        assert counts[1].item() == 0
+        T = sum(new)
+        K, V = (torch.randn((H_kv, T, 64), generator=g).to(dtype) for _ in range(2))
+        Q = torch.randn((H, T, 64), generator=g).to(dtype)
+        off = _offsets(new)
+        psa.probsparse_cache_append(K.cuda(), V.cuda(), pool[:, 0], pool[:, 1], table, lengths, off, **kw)
+        out = psa.dense_attn_paged_fwd(Q.cuda(), pool[:, 0], pool[:, 1], table, lengths, off, causal=causal, **kw)
+        parts_k, parts_v = K.split(new, 1), V.split(new, 1)
+        history = [[torch.cat(x, 1) for x in zip(history[p] if p >= 0 else [torch.zeros(H_kv, 0, 64, dtype=dtype)] * 2, (parts_k[i], parts_v[i]))] for i, p in enumerate(parents)]
+        assert lengths.tolist() == [k.shape[1] for k, _ in history]
+        at = 0
+        for (k, v), a in zip(history, new):
+            if mx:
+                k, v = (O.mx_decode(c, e + 127) for c, e in map(O.mx_encode, (k, v)))
+            n = k.shape[1]
+            seen = torch.arange(n)[None, :] <= torch.arange(a)[:, None] + (n - a) if causal else torch.ones(a, n, dtype=torch.bool)
+            for h in range(H):
+                want, e, _, _ = O.attend(Q[h, at:at + a], k[h // 2], v[h // 2], seen, 0.125, dtype, 0.0 if dtype == F32 else 2.0 ** -8)
+                assert_within(out[h, at:at + a], want, e)
+            at += a
+    step([-1], [13], True)                              # a prompt
+    step([0] * beams, [1] * beams, True)
+    for i in range(20):
+        parents = torch.randint(0, beams, (beams,), generator=g).tolist()
+        if i % 7 == 5:
+            parents[2] = -1                             # one starts anew
+        step(parents, [1 if i % 4 else 3] * beams, i % 3 != 0)
+        if i % 5 == 4:
+            table, refs, pairs, counts = psa.probsparse_cache_compact(table, refs)
+            psa.probsparse_cache_copy(pools, pairs, counts)
+            assert (refs[:counts[1].item()] > 0).all() and (refs[counts[1].item():] == 0).all()
+    assert refs.sum().item() == sum(-(-k.shape[1] // P) for k, _ in history)
