@@ -6,6 +6,8 @@
 // for all its tiles.  `chunk` is found on the device from all lengths (find_part), so that the work-groups of a call are
 // about `target` whatever the lengths are, and equal: a call that was captured serves as its sequences grow.  Sequences
 // cut in several splits leave partial sums in the workspace, joined by a second kernel.
+#include <type_traits>
+
 #include "psa_paged.h"
 
 namespace psa {
@@ -35,18 +37,25 @@ __device__ __forceinline__ int tiles_of(int nq, int G, int rows) { return (nq * 
 __device__ __forceinline__ int splits_of(int nk, int chunk) { return max(1, (units_of(nk) + chunk - 1) / chunk); }
 
 // Units of keys to a split: the work of all tiles (units times tiles) in about p.per_head shares, kLeastUnits at the least.  Every
-// work-group of a call and of its join finds the same.  Summed in float64: offsets that decrease may claim 2^67.
-__device__ __forceinline__ double wave_sum64(double x)
+// work-group of a call and of its join finds the same.  Summed in float32, in which the sum is off by 2^-18 at the most: the parts of
+// divided sequences stay at most twice p.per_head, a number below 2^17.
+__device__ __forceinline__ float wave_sum(float x)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d, 64);
-    return x;
+    auto add = [&](auto ctrl, auto rows) { x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl.value, rows.value, 0xF, false)); };
+    using std::integral_constant;
+    add(integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});
+    add(integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});
+    add(integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});
+    add(integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});
+    add(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});
+    add(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
-__device__ __forceinline__ int chunk_for(const PagedSeqs& p, double work) { return (int)fmin(fmax(ceil(work / p.per_head), (double)kLeastUnits), (double)(1 << 23)); }
-__device__ __forceinline__ double work_of(const PagedSeqs& p, int s)
+__device__ __forceinline__ int chunk_for(const PagedSeqs& p, float work) { return (int)fminf(fmaxf(ceilf(work / (float)p.per_head), (float)kLeastUnits), (float)(1 << 23)); }
+__device__ __forceinline__ float work_of(const PagedSeqs& p, int s)
 {
     const PagedSeq r = paged_seq(p, s);
-    return (double)units_of(r.nk) * tiles_of(r.nq, p.G, p.rows);
+    return (float)units_of(r.nk) * (float)tiles_of(r.nq, p.G, p.rows);
 }
 
 // What a work-group takes: tile `tile` of sequence `seq`, split `split` of `splits`; `slot`: where the partial sums of its sequence
@@ -78,9 +87,9 @@ __device__ __forceinline__ Part find_part(const PagedSeqs& p, int x)
         s0 = lo * 64;
         end = min(end, s0 + 64);
     } else {
-        double work = 0.0;
+        float work = 0.f;
         for (int s = lane; s < p.B; s += 64) work += work_of(p, s);
-        f.chunk = chunk_for(p, wave_sum64(work));
+        f.chunk = chunk_for(p, wave_sum(work));
     }
     for (; s0 < end; s0 += 64) {
         const PagedSeq r = paged_seq(p, s0 + lane);
@@ -117,15 +126,15 @@ constexpr int kMostParts = 1 << 29;
 __global__ __launch_bounds__(1024)
 void paged_before_kernel(PagedSeqs p, int* __restrict__ before)
 {
-    __shared__ double s_work[16];
+    __shared__ float s_work[16];
     __shared__ int s[2][3][16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, groups = (p.B + 63) / 64;
-    double work = 0.0;
+    float work = 0.f;
     for (int i = threadIdx.x; i < p.B; i += 1024) work += work_of(p, i);
-    work = wave_sum64(work);
+    work = wave_sum(work);
     if (lane == 0) s_work[wave] = work;
     __syncthreads();
-    work = 0.0;
+    work = 0.f;
     for (int w = 0; w < 16; ++w) work += s_work[w];
     const int chunk = chunk_for(p, work);
     if (threadIdx.x == 0) before[0] = chunk;
@@ -137,8 +146,9 @@ void paged_before_kernel(PagedSeqs p, int* __restrict__ before)
         const int64_t parts = (int64_t)tiles_of(r.nq, p.G, p.rows) * splits;
         const int64_t n[3] = {parts, splits > 1 ? parts : 0, splits > 1 ? tiles_of(r.nq, p.G, 32) : 0};
         for (int k = 0; k < 3; ++k) {
-            const double all = wave_sum64((double)n[k]);
-            if (lane == 0) s[buf][k][wave] = (int)fmin(all, (double)kMostParts);
+            const float rough = wave_sum((float)n[k]);
+            const int all = rough < (float)kMostParts ? last_lane(wave_scan((int)n[k])) : kMostParts;
+            if (lane == 0) s[buf][k][wave] = min(all, kMostParts);
         }
         __syncthreads();
         for (int k = 0; k < 3; ++k) {
@@ -154,14 +164,33 @@ void paged_before_kernel(PagedSeqs p, int* __restrict__ before)
 }
 
 // ---- rows of the cache on their way
-// Row j of a sequence: where it lies, in rows of its head's pages; < 0: on no page or behind the last.
-struct PageTable {
-    const int* row; int shift, n_pages, nk;
-    __device__ __forceinline__ int page(int j) const {
-        const int p = j < nk ? row[j >> shift] : -1;
-        return (unsigned)p < (unsigned)n_pages ? p : -1;
+// 64 entries of a sequence's table, one to a lane: a tile's pages are read from a register and no load waits for another.  Entries that name no
+// page are -1.  A new window is waited for where it is asked for, so that the loads of rows in flight are waited for by nobody else.
+struct PageWindow {
+    const int* row; int entries, n_pages, shift, first, entry;
+    bool whole;                            // no entry of the window's is -1
+    __device__ __forceinline__ void open(int from) {
+        const int lane = threadIdx.x & 63, i = from + lane;
+        int e = i < entries ? row[i] : -1;
+        if ((unsigned)e >= (unsigned)n_pages) e = -1;
+        first = from;
+        entry = e;
+        whole = __builtin_amdgcn_ballot_w64(e < 0 && i < entries) == 0;
     }
+    // rows j0 .. j0 + n - 1 are about to be asked for: at most 64 pages
+    __device__ __forceinline__ void reach(int j0, int n) { if (((j0 + n - 1) >> shift) - first >= 64) open(j0 >> shift); }
+    __device__ __forceinline__ int uniform(int j) const { return __builtin_amdgcn_readlane(entry, (j >> shift) - first); }
+    __device__ __forceinline__ int lane(int j) const { return __shfl(entry, (j >> shift) - first, 64); }
+    __device__ __forceinline__ int slot(int j) const { return j & ((1 << shift) - 1); }
 };
+// Which of the 32 rows from j on exist: on a page, before row nk
+__device__ __forceinline__ uint32_t rows_held(const PageWindow& w, int j, int nk, int c)
+{
+    if (w.whole && j + 32 <= nk) return ~0u;
+    const int page = w.lane(j + c);
+    return (uint32_t)__builtin_amdgcn_ballot_w64(page >= 0 && j + c < nk);
+}
+
 template <typename C>
 __device__ __forceinline__ const C* row_at(const PageHeads<const C>& t, int hk, int page, int slot) { return t.data + hk * t.head + page * t.page + slot * t.row; }
 
@@ -186,46 +215,59 @@ __device__ __forceinline__ uint4 mx_codes(uint32_t a, uint32_t b, float power)
 template <typename C> struct TileOf { typedef C type; };
 template <> struct TileOf<mx8_t> { typedef bf16_t type; };
 
-// Half a key's row, elements 32 h .., as the first operand of the product with the queries
-template <typename C> struct KeyRow : HeadRow<C> {
-    __device__ __forceinline__ void load(const C* row, const uint8_t*, bool valid, int h) {
-#pragma unroll
-        for (int i = 0; i < HeadRow<C>::N; ++i) this->x[i] = load_or_zero<uint4>(row + 32 * h + i * (16 / (int)sizeof(C)), valid);
-    }
-};
-template <> struct KeyRow<mx8_t> {
-    uint4 x[2];
-    uint32_t power;
-    __device__ __forceinline__ void load(const mx8_t* row, const uint8_t* scales, bool valid, int h) {
-        x[0] = load_or_zero<uint4>(row + 32 * h, valid);
-        x[1] = load_or_zero<uint4>(row + 32 * h + 16, valid);
-        power = load_or_zero<uint8_t>(scales + h, valid);
-    }
-    __device__ __forceinline__ Operand<bf16_t> step(int k) const {
-        const uint4& y = x[k >> 1];
-        return operand(k & 1 ? mx_codes(y.z, y.w, mx_power(power)) : mx_codes(y.x, y.y, mx_power(power)), bf16_t{});
-    }
-};
-// 16 bytes of a row, chunk ch of it, on their way into a tile
+// 16 bytes of a row, on their way into a tile as N chunks of the tile's type
 template <typename C> struct RowChunk {
-    static constexpr int N = 1;                        // chunks of the tile's type
+    static constexpr int N = 1;
     uint4 x;
-    __device__ __forceinline__ void load(const C* row, const uint8_t*, bool valid, int ch) { x = load_or_zero<uint4>(row + ch * (16 / (int)sizeof(C)), valid); }
     __device__ __forceinline__ void unpack(uint4* to) const { to[0] = x; }
 };
 template <> struct RowChunk<mx8_t> {
     static constexpr int N = 2;
     uint4 x;
     uint32_t power;
-    __device__ __forceinline__ void load(const mx8_t* row, const uint8_t* scales, bool valid, int ch) {
-        x = load_or_zero<uint4>(row + ch * 16, valid);
-        power = load_or_zero<uint8_t>(scales + (ch >> 1), valid);
-    }
     __device__ __forceinline__ void unpack(uint4* to) const {
         to[0] = mx_codes(x.x, x.y, mx_power(power));
         to[1] = mx_codes(x.z, x.w, mx_power(power));
     }
 };
+
+// Where rows j .. of a sequence lie that are on one page: a scalar, as their addresses are
+struct PageRef { int page, slot, n; };     // n: rows that exist, 0 on no page
+__device__ __forceinline__ PageRef page_ref(const PageWindow& w, int j, int most, int nk)
+{
+    const int page = w.uniform(j);
+    return PageRef{max(page, 0), w.slot(j), page < 0 ? 0 : max(0, min(most, nk - j))};
+}
+// K or V of a key head.  Pages of PG = 16 or 32 rows and more: rows that are asked for together lie on one page, and are a buffer that ends
+// with the sequence, so that rows behind it give zeros.  PG = 0: smaller pages, each lane finds its row's.
+template <typename C>
+struct PageRows {
+    __amdgpu_buffer_rsrc_t rows, powers;
+    int stride, power_stride;              // bytes
+    __device__ __forceinline__ PageRows(const PageHeads<const C>& t, const PageScales& s, int hk, const PageRef& r)
+        : rows(tile_rows(row_at(t, hk, r.page, r.slot), t.row, r.n)), stride((int)(t.row * (int64_t)sizeof(C))), power_stride((int)s.row)
+    {
+        if constexpr (sizeof(C) == 1) powers = __builtin_amdgcn_make_buffer_rsrc(s.at(hk, r.page, r.slot), 0, r.n > 0 ? (r.n - 1) * power_stride + 2 : 0, 0x00020000);
+    }
+    __device__ __forceinline__ uint4 bytes(int row, int at) const { return buffer_load16<uint4>(rows, row * stride + at); }
+    __device__ __forceinline__ uint32_t power(int row, int half) const { return (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(powers, row * power_stride + half, 0, 0); }
+};
+// 16 bytes of row j0 + r, chunk ch of it: the rows of a wave, 64 / CH of them and aligned so, are r0 and those behind it
+template <typename C, int PG>
+__device__ __forceinline__ void load_chunk(RowChunk<C>& to, const PageHeads<const C>& t, const PageScales& s, int hk, const PageWindow& w, int j0, int r0, int r, int ch, int nk)
+{
+    if constexpr (PG > 0) {
+        const int from = r0 & ~(PG - 1);
+        const PageRows<C> p(t, s, hk, page_ref(w, j0 + from, PG, nk));
+        to.x = p.bytes(r - from, ch * 16);
+        if constexpr (sizeof(C) == 1) to.power = p.power(r - from, ch >> 1);
+    } else {
+        const int j = j0 + r, page = w.lane(j), slot = w.slot(j);
+        const bool valid = page >= 0 && j < nk;
+        to.x = load_or_zero<uint4>(row_at(t, hk, page, slot) + ch * (16 / (int)sizeof(C)), valid);
+        if constexpr (sizeof(C) == 1) to.power = load_or_zero<uint8_t>(s.at(hk, page, slot) + (ch >> 1), valid);
+    }
+}
 
 __device__ __forceinline__ floatx16 mfma(const Operand<bf16_t>& a, const Operand<float>& b, floatx16 d)
 {
@@ -242,12 +284,11 @@ template <> __device__ __forceinline__ float value_at<mx8_t>(const mx8_t* row, c
 }
 // The infinities and NaN of values j0 .. j0 + n - 1 that were left out of the tile: to the rows that see them
 template <typename C>
-__device__ __forceinline__ void add_nonfinite(Rows32& acc, const PageHeads<const C>& V, const PageScales& vs, const PageTable& pt, int hk, int j0, int n, int n_vis, int h)
+__device__ __forceinline__ void add_nonfinite(Rows32& acc, const PageHeads<const C>& V, const PageScales& vs, const PageWindow& w, int hk, int j0, int n, int n_vis, int h)
 {
     for (int j = j0; j < j0 + n; ++j) {
-        const int page = pt.page(j);
-        if (page < 0) continue;
-        const int slot = j & ((1 << pt.shift) - 1);
+        const int page = w.row[j >> w.shift], slot = w.slot(j);
+        if ((unsigned)page >= (unsigned)w.n_pages) continue;
         const C* row = row_at(V, hk, page, slot);
 #pragma unroll
         for (int dt = 0; dt < 2; ++dt)
@@ -294,7 +335,7 @@ __device__ __forceinline__ void outside_rows(const PagedSeqs& p, const Heads<T>&
 }
 
 // ---- many rows: 4 waves of 32 rows each; tiles of KT keys and values go through LDS, the next tile's rows are on their way meanwhile.
-template <typename T, typename C, int KT, bool FINE>
+template <typename T, typename C, int PG, int KT, bool FINE>
 __global__ __launch_bounds__(256, sizeof(T) == 4 || FINE ? 2 : 3)
 void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C> V, PageScales ks, PageScales vs, PagedSeqs p, Heads<T> out,
                        float* __restrict__ lse, int H_kv, int causal, float scale, int n_part, float* __restrict__ part_o, float2* __restrict__ part_ml)
@@ -309,7 +350,7 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
     __shared__ int s_bad[2][4];
     unsigned char *const sK = lds, *const sV = lds + 2 * kBytes;
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
     const Part f = find_part<false>(p, x);
     if (f.seq < 0) { outside_rows(p, out, lse, hk, x, n_part); return; }
 
@@ -329,23 +370,23 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
 
     HeadOperand<T> q;
     q.load(Q.at(head, f.q0 + t), h);
-    const PageTable pt{p.table + (int64_t)f.seq * p.max_pages, p.shift, p.n_pages, f.nk};
-    const int slot_mask = (1 << p.shift) - 1;
+    PageWindow w{p.table + (int64_t)f.seq * p.max_pages, (f.nk + (1 << p.shift) - 1) >> p.shift, p.n_pages, p.shift, 0, 0, false};
     RowChunk<C> kr[NL], vr[NL];
     uint32_t held[NS], held_next[NS];
     auto fetch = [&](int j0) {
+        w.reach(j0, KT);
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            const int id = i * 256 + tid, j = j0 + id / CH, page = pt.page(j), slot = j & slot_mask;
-            kr[i].load(row_at(K, hk, page, slot), ks.at(hk, page, slot), page >= 0, id % CH);
-            vr[i].load(row_at(V, hk, page, slot), vs.at(hk, page, slot), page >= 0, id % CH);
+            const int id = i * 256 + tid, r0 = (i * 256 + wave * 64) / CH;
+            load_chunk<C, PG>(kr[i], K, ks, hk, w, j0, r0, id / CH, id % CH, f.nk);
+            load_chunk<C, PG>(vr[i], V, vs, hk, w, j0, r0, id / CH, id % CH, f.nk);
         }
 #pragma unroll
-        for (int n = 0; n < NS; ++n) held_next[n] = (uint32_t)__builtin_amdgcn_ballot_w64(pt.page(j0 + 32 * n + c) >= 0);
+        for (int n = 0; n < NS; ++n) held_next[n] = rows_held(w, j0 + 32 * n, f.nk, c);
     };
     Rows32 acc;
     acc.init();
-    if (begin < n_all) fetch(begin);
+    if (begin < n_all) { w.open(begin >> p.shift); fetch(begin); }
     int buf = 0;
     for (int j0 = begin; j0 < n_all; j0 += KT, buf ^= 1) {
         // a weight of 0 does not keep an infinity or NaN of a value that a row does not see out of its sum: in tiles that
@@ -400,7 +441,7 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
             int any = 0;
 #pragma unroll
             for (int w = 0; w < 4; ++w) any |= s_bad[buf][w];
-            if (any) add_nonfinite(acc, V, vs, pt, hk, j0, min(KT, f.nk - j0), n_vis, h);
+            if (any) add_nonfinite(acc, V, vs, w, hk, j0, min(KT, f.nk - j0), n_vis, h);
         }
     }
     outside_rows(p, out, lse, hk, x, n_part);          // (last: its loads would delay the others)
@@ -418,23 +459,27 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
 }
 
 // ---- few rows: 32 to a work-group, whose 4 waves divide the keys (of its split) among themselves, 32 at a time, and join their
-// sums at the end.  Keys come straight from memory as the first product's operand, values through LDS of the wave's own;
-// there is no barrier before the join.
-template <typename T, typename C>
+// sums at the end.  A wave's tiles go through LDS of its own, DEPTH of them on their way in registers; there is no barrier before
+// the join.  (float32 keys, whose three parts would take too much LDS, come straight from memory as the first product's operand.)
+template <typename C> constexpr int kDepth = sizeof(C) == 4 ? 1 : 2;
+template <typename T, typename C, int PG>
 __global__ __launch_bounds__(256, 2)
 void paged_few_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C> V, PageScales ks, PageScales vs, PagedSeqs p, Heads<T> out,
                       float* __restrict__ lse, int H_kv, int causal, float scale, int n_part, float* __restrict__ part_o, float2* __restrict__ part_ml)
 {
     typedef typename TileOf<C>::type TC;
+    constexpr bool DIRECT = sizeof(C) == 4;            // keys
     constexpr int CH = 64 * sizeof(C) / 16;
     constexpr int NL = 32 * CH / 64;                   // chunks of a tile of 32 rows, to a lane
     constexpr int NU = RowChunk<C>::N;
+    constexpr int DEPTH = kDepth<C>;
     constexpr int kBytes = kTileBytes<TC, 32>;
+    constexpr int kWave = DIRECT ? kBytes : 2 * kBytes;
     constexpr int kJoinBytes = 4 * 32 * kJoinRow * 4;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kBytes > kJoinBytes ? 4 * kBytes : kJoinBytes];
+    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kWave > kJoinBytes ? 4 * kWave : kJoinBytes];
     __shared__ float s_m[4][32], s_l[4][32];
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
     const Part f = find_part<false>(p, x);
     if (f.seq < 0) { outside_rows(p, out, lse, hk, x, n_part); return; }
     const int n_rows = f.nq * p.G;
@@ -450,32 +495,36 @@ void paged_few_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C>
 
     HeadOperand<T> q;
     q.load(Q.at(head, f.q0 + t), h);
-    const PageTable pt{p.table + (int64_t)f.seq * p.max_pages, p.shift, p.n_pages, f.nk};
-    const int slot_mask = (1 << p.shift) - 1;
-    unsigned char* sV = lds + wave * kBytes;
-    KeyRow<C> kn;
-    RowChunk<C> vn[NL];
-    uint32_t held_next = 0;
-    auto fetch = [&](int j0) {
-        const int j = j0 + c, page = pt.page(j), slot = j & slot_mask;
-        kn.load(row_at(K, hk, page, slot), ks.at(hk, page, slot), page >= 0, h);
-        held_next = (uint32_t)__builtin_amdgcn_ballot_w64(page >= 0);
+    PageWindow w{p.table + (int64_t)f.seq * p.max_pages, (f.nk + (1 << p.shift) - 1) >> p.shift, p.n_pages, p.shift, 0, 0, false};
+    unsigned char *const sV = lds + wave * kWave, *const sK = sV + kBytes;
+    struct Tile {
+        RowChunk<C> k[DIRECT ? 1 : NL], v[NL];
+        HeadRow<float> direct;
+        uint32_t held;
+    } next[DEPTH];
+    auto fetch = [&](Tile& n, int j0) {
+        w.reach(j0, 32);
+        if constexpr (DIRECT) {
+            const int page = w.lane(j0 + c);
+            const C* key = row_at(K, hk, page, w.slot(j0 + c)) + 32 * h;
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            const int id = i * 64 + lane, jv = j0 + id / CH, pv = pt.page(jv), sv = jv & slot_mask;
-            vn[i].load(row_at(V, hk, pv, sv), vs.at(hk, pv, sv), pv >= 0, id % CH);
+            for (int i = 0; i < HeadRow<float>::N; ++i) n.direct.x[i] = load_or_zero<uint4>(key + 4 * i, page >= 0 && j0 + c < f.nk);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NL; ++i) load_chunk<C, PG>(n.k[i], K, ks, hk, w, j0, i * 64 / CH, (i * 64 + lane) / CH, lane % CH, f.nk);
         }
+#pragma unroll
+        for (int i = 0; i < NL; ++i) load_chunk<C, PG>(n.v[i], V, vs, hk, w, j0, i * 64 / CH, (i * 64 + lane) / CH, lane % CH, f.nk);
+        n.held = rows_held(w, j0, f.nk, c);
     };
     Rows32 acc;
     acc.init();
-    int j0 = begin + wave * 32;
-    if (j0 < end) fetch(j0);
-    for (; j0 < end; j0 += 128) {
+    auto take = [&](Tile& n, int j0) {
         // infinities and NaN of V are left out of the product and added afterwards, in whole tiles too: the weights have parts of either
         // sign and of 0
         uint4 v[NL * NU];
 #pragma unroll
-        for (int i = 0; i < NL; ++i) vn[i].unpack(v + i * NU);
+        for (int i = 0; i < NL; ++i) n.v[i].unpack(v + i * NU);
         const bool any = __builtin_amdgcn_ballot_w64(nonfinite(v, TC{})) != 0;
         if (any)
 #pragma unroll
@@ -486,14 +535,19 @@ void paged_few_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C>
             const int id = i * 64 + lane;
 #pragma unroll
             for (int u = 0; u < NU; ++u) put<32>(sV, id / CH, id % CH * NU + u, v[i * NU + u], TC{});
-        }
-        floatx16 s[1];
-        clear(s[0]);
+            if constexpr (!DIRECT) {
+                uint4 k[NU];
+                n.k[i].unpack(k);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s[0] = mfma(kn.step(k), q.v[k], s[0]);
+                for (int u = 0; u < NU; ++u) put<32>(sK, id / CH, id % CH * NU + u, k[u], TC{});
+            }
+        }
         wave_lds_sync();
-        const uint32_t held = held_next;
-        if (j0 + 128 < end) fetch(j0 + 128);
+        floatx16 s[1];
+        if constexpr (DIRECT) s[0] = product(n.direct, q);
+        const uint32_t held = n.held;
+        if (j0 + 128 * DEPTH < end) fetch(n, j0 + 128 * DEPTH);
+        if constexpr (!DIRECT) s[0] = product_rows<T, TC, 32>(sK, 0, q, c, h);
         if (j0 + 32 > n_every || held != ~0u) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[0][r] = j0 + acc_row(r, h) < n_vis && (held >> acc_row(r, h) & 1) ? s[0][r] : -INFINITY;
@@ -501,7 +555,17 @@ void paged_few_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C>
         acc.follow(s, scale);
         acc.weights(s[0], scale);
         accumulate_rows<T, TC, 32, true>(acc.o, sV, 0, s[0], c, h);
-        if (any) add_nonfinite(acc, V, vs, pt, hk, j0, min(32, f.nk - j0), n_vis, h);
+        if (any) add_nonfinite(acc, V, vs, w, hk, j0, min(32, f.nk - j0), n_vis, h);
+    };
+    int j0 = begin + wave * 32;
+    if (j0 < end) {
+        w.open(j0 >> p.shift);
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) if (j0 + 128 * d < end) fetch(next[d], j0 + 128 * d);
+    }
+    while (j0 < end) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d, j0 += 128) if (j0 < end) take(next[d], j0);
     }
     outside_rows(p, out, lse, hk, x, n_part);
     // join: wave w's sums of row r at join[w][r]; a wave that saw no key has m = kMaxInit and sums of 0
@@ -539,6 +603,318 @@ void paged_few_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C>
     } else {
         store_joined(out.at(rh, f.q0 + rt) + e, o, sum);
         if (lse && e == 0) lse[(int64_t)rh * p.T + f.q0 + rt] = sum == 0.f ? -INFINITY : m * kLn2 + logf(sum);
+    }
+}
+
+// ---- very few rows, single tokens as a rule: 16 to a work-group.  As above, with the 16 x 16 x 32 matrix instruction: half the scores,
+// exponentials and products of a tile of 32 columns, which for one row are 31/32 in vain, and half the registers, so that twice the waves
+// have rows on their way.
+//   lane (c, g) = (lane % 16, lane / 16);  D[i][j]: i = 4 g + r, j = c;  A[i][k]: i = c, B[k][j]: j = c, 8 elements k to a lane, in an order of our own:
+//   keys    element order of a step: those that make a wave read 64 bytes and more of a row at a time (KeyPair)
+//   values  key 16 t + 4 g + r is element 4 t + r of a lane: the order that scores have in their accumulators
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ floatx4 mfma16(const uint4& a, const uint4& b, floatx4 d) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), d, 0, 0, 0); }
+__device__ __forceinline__ floatx4 mfma16(const Operand<bf16_t>& a, const Operand<bf16_t>& b, floatx4 d) { return mfma16(a.v[0], b.v[0], d); }
+__device__ __forceinline__ floatx4 mfma16(const Operand<bf16_t>& a, const Operand<float>& b, floatx4 d)
+{
+    d = mfma16(a.v[0], b.v[2], d);
+    d = mfma16(a.v[0], b.v[1], d);
+    return mfma16(a.v[0], b.v[0], d);
+}
+__device__ __forceinline__ floatx4 mfma16(const Operand<float>& a, const Operand<float>& b, floatx4 d)
+{
+    d = mfma16(a.v[2], b.v[0], d);         // small ones first
+    d = mfma16(a.v[0], b.v[2], d);
+    d = mfma16(a.v[1], b.v[1], d);
+    d = mfma16(a.v[1], b.v[0], d);
+    d = mfma16(a.v[0], b.v[1], d);
+    return mfma16(a.v[0], b.v[0], d);
+}
+// First of the 4 elements that are floats 4 u .. of the 8 that lane g has in step k of a product over a head's 64 elements, keys of type C
+template <typename C> __device__ __forceinline__ constexpr int head_element(int k, int u, int g) { return sizeof(C) == 4 ? 16 * (2 * k + u) + 4 * g : sizeof(C) == 2 ? 32 * k + 8 * g + 4 * u : 16 * g + 8 * k + 4 * u; }
+template <typename T, typename C>
+__device__ __forceinline__ void load_query(Operand<T> (&q)[2], const T* row, int g)
+{
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if constexpr (sizeof(T) == 4) {
+            float x[8];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) load_vec(reinterpret_cast<float (&)[4]>(x[4 * u]), row + head_element<C>(k, u, g), 4);
+            q[k] = operand(x);
+        } else {
+            const uint2 a = *reinterpret_cast<const uint2*>(row + head_element<C>(k, 0, g)), b = *reinterpret_cast<const uint2*>(row + head_element<C>(k, 1, g));
+            q[k].v[0] = make_uint4(a.x, a.y, b.x, b.y);
+        }
+    }
+}
+// A lane's part of row c of 16 keys on their way: N times 16 bytes, of chunk at(i) of the row's
+template <typename C> struct KeyPart {
+    static constexpr int N = sizeof(C);                // (16 elements)
+    uint4 x[N];
+    uint32_t power;
+    static __device__ __forceinline__ int at(int i, int g) { return sizeof(C) == 1 ? 16 * g : 64 * i + 16 * g; }     // bytes
+    __device__ __forceinline__ auto step(int k) const {
+        if constexpr (sizeof(C) == 4) {
+            const uint4 &a = x[2 * k], &b = x[2 * k + 1];
+            const float f[8] = {__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
+                                __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
+            return operand(f);
+        } else if constexpr (sizeof(C) == 2) {
+            return operand(x[k], bf16_t{});
+        } else {
+            return operand(k == 0 ? mx_codes(x[0].x, x[0].y, mx_power(power)) : mx_codes(x[0].z, x[0].w, mx_power(power)), bf16_t{});
+        }
+    }
+};
+// A tile of 32 values in LDS, its 16-byte chunks permuted inside a row: here a transposing read takes 32 bytes of rows 4 g .. 4 g + 3 in each group of
+// 16 lanes, so that rows 2, 4 and 8 apart have to differ in the chunk's bits 2, 1 and 0 (256 bytes of banks are two rows)
+__device__ __forceinline__ int chunk16_at(int row, int chunk) { return row * kTileRowBytes + ((chunk ^ ((row & 2) << 1) ^ ((row & 4) >> 1) ^ ((row & 8) >> 3)) & 7) * 16; }
+__device__ __forceinline__ void put16(unsigned char* s, int row, int ch, const uint4& x, bf16_t) { *reinterpret_cast<uint4*>(s + chunk16_at(row, ch)) = x; }
+__device__ __forceinline__ void put16(unsigned char* s, int row, int ch, const uint4& x, float)
+{
+    uint32_t p[2][3];
+    split_pair(__uint_as_float(x.x), __uint_as_float(x.y), p[0]);
+    split_pair(__uint_as_float(x.z), __uint_as_float(x.w), p[1]);
+    unsigned char* dst = s + chunk16_at(row, ch >> 1) + (ch & 1) * 8;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(dst + k * 32 * kTileRowBytes) = make_uint2(p[0][k], p[1][k]);
+}
+template <typename TC>
+__device__ __forceinline__ Operand<TC> transposed16(const unsigned char* s, int m, int c, int g)
+{
+    const int row = 4 * g + (c >> 2), byte = 32 * m + 8 * (c & 3);
+    Operand<TC> a;
+#pragma unroll
+    for (int i = 0; i < kParts<TC>; ++i) {
+        uint2 part[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const unsigned char* p = s + i * 32 * kTileRowBytes + chunk16_at(row + 16 * t, byte >> 4) + (byte & 15);
+            part[t] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((shortx4 __attribute__((address_space(3)))*)(p)));
+        }
+        a.v[i] = make_uint4(part[0].x, part[0].y, part[1].x, part[1].y);
+    }
+    return a;
+}
+// Weights as the second operand: bfloat16 in two parts, the small one first
+__device__ __forceinline__ void weight_operand16(Operand<float> (&b)[1], const float (&w)[8]) { b[0] = operand(w); }
+__device__ __forceinline__ void weight_operand16(Operand<bf16_t> (&b)[2], const float (&w)[8])
+{
+    uint32_t part[4][3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split_pair(w[2 * i], w[2 * i + 1], part[i]);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) b[n].v[0] = make_uint4(part[0][1 - n], part[1][1 - n], part[2][1 - n], part[3][1 - n]);
+}
+
+template <typename C> constexpr int kDepth16 = 1;
+template <typename T, typename C, int PG>
+__global__ __launch_bounds__(256, sizeof(T) == 4 || sizeof(C) == 4 ? 2 : 4)
+void paged_single_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C> V, PageScales ks, PageScales vs, PagedSeqs p, Heads<T> out,
+                         float* __restrict__ lse, int H_kv, int causal, float scale, int n_part, float* __restrict__ part_o, float2* __restrict__ part_ml)
+{
+    typedef typename TileOf<C>::type TC;
+    constexpr int CH = 64 * sizeof(C) / 16;
+    constexpr int NL = 32 * CH / 64;                   // chunks of a tile of 32 values, to a lane
+    constexpr int NU = RowChunk<C>::N;
+    constexpr int NW = sizeof(T) == 4 ? 1 : 2;         // parts of a weight
+    constexpr int DEPTH = kDepth16<C>;
+    constexpr int kBytes = kTileBytes<TC, 32>;
+    constexpr int kJoinBytes = 4 * 16 * kJoinRow * 4;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kBytes > kJoinBytes ? 4 * kBytes : kJoinBytes];
+    __shared__ float s_m[4][16], s_l[4][16];
+    const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+    const Part f = find_part<false>(p, x);
+    if (f.seq < 0) { outside_rows(p, out, lse, hk, x, n_part); return; }
+    const int n_rows = f.nq * p.G;
+    const int shift = f.nk - f.nq + 1;
+    auto visible = [&](int r) { const int t = r / p.G; return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
+    const int row0 = f.tile * 16, rc = min(row0 + c, n_rows - 1);
+    const int t = rc / p.G, head = hk * p.G + (rc - t * p.G);
+    const int n_vis = visible(rc);
+    const int begin = f.split * f.chunk * kUnit;
+    const int cut = f.split + 1 < f.splits ? begin + f.chunk * kUnit : f.nk;
+    const int end = min(cut, __builtin_amdgcn_readfirstlane(visible(min(row0 + 15, n_rows - 1))));
+    const int n_every = __builtin_amdgcn_readfirstlane(visible(row0));
+
+    Operand<T> q[2];
+    load_query<T, C>(q, Q.at(head, f.q0 + t), g);
+    PageWindow w{p.table + (int64_t)f.seq * p.max_pages, (f.nk + (1 << p.shift) - 1) >> p.shift, p.n_pages, p.shift, 0, 0, false};
+    unsigned char* const sV = lds + wave * kBytes;
+    struct Tile {
+        KeyPart<C> k[2];
+        RowChunk<C> v[NL];
+        uint32_t held;
+    } next[DEPTH];
+    auto fetch = [&](Tile& n, int j0) {
+        w.reach(j0, 32);
+        if constexpr (PG > 0) {
+#pragma unroll
+            for (int from = 0; from < 32; from += PG) {
+                const PageRef r = page_ref(w, j0 + from, PG, f.nk);
+                const PageRows<C> pk(K, ks, hk, r), pv(V, vs, hk, r);
+#pragma unroll
+                for (int t16 = from / 16; t16 < (from + PG) / 16; ++t16) {
+#pragma unroll
+                    for (int i = 0; i < KeyPart<C>::N; ++i) n.k[t16].x[i] = pk.bytes(16 * t16 - from + c, KeyPart<C>::at(i, g));
+                    if constexpr (sizeof(C) == 1) n.k[t16].power = pk.power(16 * t16 - from + c, g >> 1);
+                }
+#pragma unroll
+                for (int i = from * CH / 64; i < (from + PG) * CH / 64; ++i) {
+                    const int r_in = (i * 64 + lane) / CH - from;
+                    n.v[i].x = pv.bytes(r_in, lane % CH * 16);
+                    if constexpr (sizeof(C) == 1) n.v[i].power = pv.power(r_in, lane % CH >> 1);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int t16 = 0; t16 < 2; ++t16) {
+                const int j = j0 + 16 * t16 + c, page = w.lane(j), slot = w.slot(j);
+                const bool valid = page >= 0 && j < f.nk;
+                const unsigned char* key = reinterpret_cast<const unsigned char*>(row_at(K, hk, page, slot));
+#pragma unroll
+                for (int i = 0; i < KeyPart<C>::N; ++i) n.k[t16].x[i] = load_or_zero<uint4>(key + KeyPart<C>::at(i, g), valid);
+                if constexpr (sizeof(C) == 1) n.k[t16].power = load_or_zero<uint8_t>(ks.at(hk, page, slot) + (g >> 1), valid);
+            }
+#pragma unroll
+            for (int i = 0; i < NL; ++i) load_chunk<C, 0>(n.v[i], V, vs, hk, w, j0, 0, (i * 64 + lane) / CH, lane % CH, f.nk);
+        }
+        n.held = rows_held(w, j0, f.nk, lane & 31);
+    };
+    float m, l;
+    floatx4 o[4];
+    // Infinities and NaN of V: a weight of 0 does not keep them out of a sum, and one times a part of the other sign is NaN.  They always
+    // leave an infinity or NaN in the sums, so a wave looks at those at its end and only then takes its keys once more, with such
+    // values left out of the product and added afterwards to the rows that see them.
+    for (int careful = 0; careful < 2; ++careful) {
+        m = kMaxInit; l = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        auto take = [&](Tile& n, int j0) {
+            uint4 v[NL * NU];
+#pragma unroll
+            for (int i = 0; i < NL; ++i) n.v[i].unpack(v + i * NU);
+            bool any = false;
+            if (careful) {
+                any = __builtin_amdgcn_ballot_w64(nonfinite(v, TC{})) != 0;
+#pragma unroll
+                for (int i = 0; i < NL * NU; ++i) v[i] = finite_only(v[i], TC{});
+            }
+            wave_lds_sync();
+#pragma unroll
+            for (int i = 0; i < NL; ++i)
+#pragma unroll
+                for (int u = 0; u < NU; ++u) put16(sV, (i * 64 + lane) / CH, lane % CH * NU + u, v[i * NU + u], TC{});
+            floatx4 s[2];
+#pragma unroll
+            for (int t16 = 0; t16 < 2; ++t16) {
+                s[t16] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < 2; ++k) s[t16] = mfma16(n.k[t16].step(k), q[k], s[t16]);
+            }
+            wave_lds_sync();
+            const uint32_t held = n.held;
+            if (j0 + 128 * DEPTH < end) fetch(n, j0 + 128 * DEPTH);
+            if (j0 + 32 > n_every || held != ~0u) {
+#pragma unroll
+                for (int t16 = 0; t16 < 2; ++t16)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int j = 16 * t16 + 4 * g + r;
+                        s[t16][r] = j0 + j < n_vis && (held >> j & 1) ? s[t16][r] : -INFINITY;
+                    }
+            }
+            // the running maximum, as Rows32 follows it
+            float top = s[0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i >> 2][i & 3]);
+            top = max_xor16(max_xor32(top)) * scale;
+            const float m_new = top > m + kLagLog2 ? top : m;
+            if (__builtin_amdgcn_ballot_w64(m_new > m) != 0) {
+                const float alpha = fast_exp2(m - m_new);
+                l *= alpha;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] *= alpha;
+            }
+            m = m_new;
+            float weight[8], sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { weight[i] = fast_exp2(fmaf(s[i >> 2][i & 3], scale, -m)); sum += weight[i]; }
+            l += sum;
+            Operand<T> b[NW];
+            weight_operand16(b, weight);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const Operand<TC> a = transposed16<TC>(sV, i, c, g);
+#pragma unroll
+                for (int k = 0; k < NW; ++k) o[i] = mfma16(a, b[k], o[i]);
+            }
+            if (any) {
+                for (int j = j0; j < min(j0 + 32, f.nk); ++j) {
+                    const int page = w.row[j >> w.shift], slot = w.slot(j);
+                    if ((unsigned)page >= (unsigned)p.n_pages) continue;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float value = value_at(row_at(V, hk, page, slot), vs.at(hk, page, slot), 16 * i + 4 * g + r);
+                            if (j < n_vis && !isfinite(value)) o[i][r] += value;
+                        }
+                }
+            }
+        };
+        int j0 = begin + wave * 32;
+        if (j0 < end) {
+            w.open(j0 >> p.shift);
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d) if (j0 + 128 * d < end) fetch(next[d], j0 + 128 * d);
+        }
+        while (j0 < end) {
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d, j0 += 128) if (j0 < end) take(next[d], j0);
+        }
+        float size = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) size = fmaxf(size, isfinite(o[i >> 2][i & 3]) ? 0.f : 1.f);
+        if (__builtin_amdgcn_ballot_w64(size != 0.f) == 0) break;
+    }
+    outside_rows(p, out, lse, hk, x, n_part);
+    // join: wave w's sums of row r at join[w][r]; a wave that saw no key has m = kMaxInit and sums of 0
+    __syncthreads();
+    float* join = reinterpret_cast<float*>(lds);
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (g == 0) { s_m[wave][c] = m; s_l[wave][c] = l; }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(join + (wave * 16 + c) * kJoinRow + 16 * i + 4 * g) = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+    __syncthreads();
+    // 16 threads of 4 elements to a row
+    const int r = tid >> 4, e = (tid & 15) * 4;
+    if (row0 + r >= n_rows) return;
+    float top = s_m[0][r];
+#pragma unroll
+    for (int k = 1; k < 4; ++k) top = fmaxf(top, s_m[k][r]);
+    float sum = 0.f;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (s_m[k][r] == kMaxInit && s_l[k][r] == 0.f) continue;       // (saw no key: its accumulators may hold 0 * NaN)
+        const float f1 = fast_exp2(s_m[k][r] - top);
+        const float4 v = *reinterpret_cast<const float4*>(join + (k * 16 + r) * kJoinRow + e);
+        sum = fmaf(s_l[k][r], f1, sum);
+        a.x = fmaf(v.x, f1, a.x); a.y = fmaf(v.y, f1, a.y); a.z = fmaf(v.z, f1, a.z); a.w = fmaf(v.w, f1, a.w);
+    }
+    const int rt = (row0 + r) / p.G, rh = hk * p.G + (row0 + r - rt * p.G);
+    if (f.splits > 1) {
+        const int64_t rec = ((int64_t)(f.slot + f.split * f.tiles + f.tile) * H_kv + hk) * 16 + r;
+        *reinterpret_cast<float4*>(part_o + rec * 64 + e) = a;
+        if (e == 0) part_ml[rec] = make_float2(top, sum);
+    } else {
+        const float f1 = sum != 0.f ? 1.f / sum : 0.f;
+        store4(out.at(rh, f.q0 + rt) + e, sum != 0.f ? make_float4(a.x * f1, a.y * f1, a.z * f1, a.w * f1) : make_float4(0.f, 0.f, 0.f, 0.f));
+        if (lse && e == 0) lse[(int64_t)rh * p.T + f.q0 + rt] = sum == 0.f ? -INFINITY : top * kLn2 + logf(sum);
     }
 }
 
@@ -603,7 +979,7 @@ PagedPlan make_paged_plan(const psa_cache_t& cache, const psa_paged_shape_t& s)
     const int64_t wide = (rows / 128 + s.B) * s.H_kv;
     p.few = rows <= (int64_t)32 * s.B;
     p.fine = p.few || wide < (s.causal ? 224 : 152);
-    p.rows = p.few ? 32 : 128;
+    p.rows = rows <= (int64_t)16 * s.B ? 16 : p.few ? 32 : 128;
     const int target = p.few ? 1024 : 768;
     p.per_head = (target + s.H_kv - 1) / s.H_kv;
     const int64_t tiles = rows / p.rows + s.B;         // at most
@@ -612,7 +988,7 @@ PagedPlan make_paged_plan(const psa_cache_t& cache, const psa_paged_shape_t& s)
     p.join = (int64_t)cache.max_pages * cache.page_rows > kLeastUnits * kUnit;
     // of sequences with several splits the parts are at most twice their work over the chunk, and a row is joined in parts of 32
     const int64_t slots = p.join ? 2 * (int64_t)p.per_head : 0;
-    p.n_join = slots * (p.rows / 32) / 2 + 1;
+    p.n_join = slots * (p.rows > 32 ? p.rows / 32 : 1) / 2 + 1;
     size_t at = 0;
     if (s.B > kPagedMany) at += ((size_t)(3 * ((s.B + 63) / 64) + 1) * sizeof(int) + 255) & ~(size_t)255;
     p.off_ml = at;
@@ -639,7 +1015,11 @@ static void paged_go(const PagedPlan& p, const psa_paged_shape_t& s, const psa_h
     constexpr int KT = sizeof(C) == 4 ? 32 : 64;
     constexpr bool FINE = sizeof(T) == 2;
     const unsigned grid = (unsigned)(p.n_part * s.H_kv);
-    (p.few ? paged_few_kernel<T, C> : p.fine ? paged_rows_kernel<T, C, KT, FINE> : paged_rows_kernel<T, C, KT, false>)<<<grid, 256, 0, stream>>>(
+    const bool wide = cache.page_rows >= 32, mid = cache.page_rows == 16;
+    (p.rows == 16 ? (wide ? paged_single_kernel<T, C, 32> : mid ? paged_single_kernel<T, C, 16> : paged_single_kernel<T, C, 0>)
+     : p.few ? (wide ? paged_few_kernel<T, C, 32> : mid ? paged_few_kernel<T, C, 16> : paged_few_kernel<T, C, 0>)
+     : p.fine ? (wide ? paged_rows_kernel<T, C, 32, KT, FINE> : mid ? paged_rows_kernel<T, C, 16, KT, FINE> : paged_rows_kernel<T, C, 0, KT, FINE>)
+              : (wide ? paged_rows_kernel<T, C, 32, KT, false> : mid ? paged_rows_kernel<T, C, 16, KT, false> : paged_rows_kernel<T, C, 0, KT, false>))<<<grid, 256, 0, stream>>>(
         heads_of<const T>(Q), page_heads_of<const C>(cache.K), page_heads_of<const C>(cache.V), page_scales_of(cache.K_scales), page_scales_of(cache.V_scales), seqs,
         heads_of<T>(out), lse, s.H_kv, s.causal, scale, (int)p.n_part, part_o, part_ml);
     if (p.join) paged_join_kernel<T><<<(unsigned)(p.n_join * s.H_kv), 256, 0, stream>>>(part_o, part_ml, seqs, s.H_kv, heads_of<T>(out), lse);
