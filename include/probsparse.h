@@ -464,8 +464,9 @@ int probsparse_cache_append(const psa_heads_t* K, const psa_heads_t* V, const in
  * the cache (new query t sees all of them or, `causal`, rows j <= t + lengths[s] - n), those on a page.
  * A query that sees no key, and a row of Q in no sequence, get zeros in out and -infinity in lse [H, T] float32 DEVICE
  * (may be NULL).  What a query does not see, rows behind a sequence's last among it, has no part in its output, whatever lies there.
- * Arithmetic as there: 8-bit elements are taken exactly; bfloat16 weights are kept to 16 bits where sequences have few new
- * rows (T * (H / H_kv) / B <= 32) or where W < 152 (causal: 224) with W = (T * (H / H_kv) / 128 + B) * H_kv, else rounded.
+ * Arithmetic as there: 8-bit elements are taken exactly; with R = T * (H / H_kv) bfloat16 weights are kept to 16 bits where
+ * R <= 32 B (few new rows to a sequence), where (R / 16 + B) * H_kv <= 192 or where (R / 128 + B) * H_kv < 152 (causal: 224), divisions of
+ * integers, else rounded.
  * The keys of long sequences are divided among work-groups by the lengths that the device finds, so a captured call serves while sequences grow.
  * The order of all sums is fixed by the shape and the lengths. */
 size_t dense_attn_paged_workspace_bytes(const psa_cache_t* cache, const psa_paged_shape_t* shape);

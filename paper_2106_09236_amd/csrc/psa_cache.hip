@@ -122,8 +122,9 @@ hipError_t launch_cache_append(const psa_heads_t& K, const psa_heads_t& V, const
 }
 
 // ---- the sequences of the next step
-// Three launches: refs and the workspace; the tables' rows, with the changes of refs that they make; one work-group for what
-// depends on all of them, which is little: the pages that are given away, in ascending order.
+// Small calls (update_is_small) are one work-group's, with refs in LDS: what they cost is launches and chains of loads.  Else three
+// launches: refs and the workspace; the tables' rows, with the changes of refs that they make; one work-group for what depends on all
+// of them, which is little: the pages that are given away, in ascending order.
 constexpr int kScanParents = 4096;         // new sequences up to which each old one looks through all of them for those that continue it
 struct UpdateRoom {
     int *growers, *first, *given;          // [n_pages]: sequences that write to a page next, the first of them; free pages in order of need
@@ -318,8 +319,112 @@ void update_end_kernel(CacheUpdate u, UpdateRoom w)
         u.counts[1] = (int)min((unsigned long long)max(need - found, 0) + s_over, (unsigned long long)INT_MAX);
     }
 }
+// The same by one work-group.  A sequence to a thread; entries of the tables to any.
+constexpr int kSmallPages = 12288, kSmallSequences = 1024, kSmallEntries = 32768;
+static bool update_is_small(const CacheUpdate& u)
+{
+    return u.n_pages <= kSmallPages && u.B <= kSmallSequences && u.B_out <= kSmallSequences && (int64_t)u.B * u.max_pages <= kSmallEntries &&
+           (int64_t)u.B_out * u.max_pages <= kSmallEntries;
+}
+__global__ __launch_bounds__(1024)
+void update_small_kernel(CacheUpdate u)
+{
+    extern __shared__ int lds[];
+    int *const refs = lds, *const mark = lds + u.n_pages, *const given = lds + 2 * u.n_pages;
+    __shared__ int s_had_in[kSmallSequences], s_had[kSmallSequences], s_parent[kSmallSequences];
+    __shared__ int s[2][16];
+    __shared__ unsigned long long s_over;
+    const int tid = threadIdx.x, shift = __builtin_ctz((unsigned)u.page_rows);
+    Child c{};
+    int last = -1;                                     // the page that this thread's sequence writes to next, where it has rows of others
+    if (tid == 0) s_over = 0;
+    if (tid < u.B_out) {
+        c = child_of(u, tid);
+        last = partial_page(u, c);
+        s_had[tid] = c.had;
+        s_parent[tid] = c.parent;
+        u.lengths_out[tid] = c.n_out;
+    }
+    if (tid < u.B) s_had_in[tid] = (min(max(u.lengths[tid], 0), u.max_pages * u.page_rows) + u.page_rows - 1) >> shift;
+    for (int p = tid; p < u.n_pages; p += 1024) { refs[p] = u.refs[p]; mark[p] = INT_MAX; }
+    __syncthreads();
+    if (c.over > 0) atomicAdd(&s_over, (unsigned long long)c.over);
+    // who holds what: the old sequences' entries go, the new ones' come (without parents they are the same)
+    const int entries = u.B * u.max_pages, entries_out = u.B_out * u.max_pages;
+    if (u.parents) {
+        for (int e = tid; e < entries; e += 1024) {
+            const int b = e / u.max_pages;
+            if (e - b * u.max_pages >= s_had_in[b]) continue;
+            const int page = u.table[e];
+            if ((unsigned)page < (unsigned)u.n_pages) atomicAdd(refs + page, -1);
+        }
+    }
+    for (int e = tid; e < entries_out; e += 1024) {
+        const int i = e / u.max_pages, j = e - i * u.max_pages;
+        int page = -1;
+        if (j < s_had[i]) {
+            page = u.table[s_parent[i] * u.max_pages + j];
+            if ((unsigned)page >= (unsigned)u.n_pages) page = -1;
+            else if (u.parents) atomicAdd(refs + page, 1);
+        }
+        u.table_out[e] = page;
+    }
+    // of those that write to one page the first, then how many they are
+    if (last >= 0) atomicMin(mark + last, tid);
+    __syncthreads();
+    const bool is_first = last >= 0 && mark[last] == tid;
+    __syncthreads();
+    if (last >= 0) mark[last] = 0;
+    __syncthreads();
+    if (last >= 0) atomicAdd(mark + last, 1);
+    __syncthreads();
+    const int copied = last >= 0 && !(is_first && refs[last] == mark[last]);
+    int need, all, found = 0, buf = 0;
+    int at = group_scan(tid < u.B_out ? c.want - c.had + copied : 0, s[1], need);
+    for (int p0 = 0; p0 < u.n_pages && found < need; p0 += 4096, buf ^= 1) {
+        const int p = p0 + 4 * tid;
+        bool is_free[4];
+        int n = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            is_free[k] = p + k < u.n_pages && refs[min(p + k, u.n_pages - 1)] == 0;
+            n += is_free[k];
+        }
+        int to = found + group_scan(n, s[buf], all);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (is_free[k]) given[to++] = p + k;
+        found += all;
+    }
+    __syncthreads();                                   // (all of `given` is written, refs have been read, and the tables' stores are done)
+    int pairs;
+    const bool with_page = copied && at < found;
+    const int pair = group_scan(with_page, s[0], pairs);
+    if (copied) atomicAdd(refs + last, -1);
+    if (with_page) { u.pairs[2 * pair] = last; u.pairs[2 * pair + 1] = given[at]; }
+    if (tid < u.B_out) {
+        for (int j = c.had - copied; j < c.want; ++j, ++at) {
+            const int page = at < found ? given[at] : -1;
+            u.table_out[tid * u.max_pages + j] = page;
+            if (page >= 0) refs[page] = 1;             // (it was 0: nobody else's)
+        }
+    }
+    if (tid >= pairs && tid < u.B_out) u.pairs[2 * tid] = u.pairs[2 * tid + 1] = -1;
+    if (tid == 0) {
+        u.counts[0] = pairs;
+        u.counts[1] = (int)min((unsigned long long)max(need - found, 0) + s_over, (unsigned long long)INT_MAX);
+    }
+    __syncthreads();
+    for (int p = tid; p < u.n_pages; p += 1024) u.refs_out[p] = refs[p];
+}
+
 hipError_t launch_cache_update(const CacheUpdate& u, void* workspace, hipStream_t stream)
 {
+    if (update_is_small(u)) {
+        if (const hipError_t e = init_cache(); e != hipSuccess) return e;
+        update_small_kernel<<<1, 1024, 3 * u.n_pages * sizeof(int), stream>>>(u);
+        return hipGetLastError();
+    }
     const UpdateRoom w = update_room(u, workspace);
     const int n = w.children && u.B > u.n_pages ? u.B : u.n_pages;
     update_begin_kernel<<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(u, w);
@@ -330,7 +435,8 @@ hipError_t launch_cache_update(const CacheUpdate& u, void* workspace, hipStream_
 }
 
 // ---- compaction
-// One work-group counts the pages in use and ranks those that move and the holes they move to; then all pages and entries follow.
+// One work-group counts the pages in use and ranks those that move and the holes they move to; then all pages and entries follow, in
+// small calls in the same work-group.
 // workspace: [n_pages], where a page at n or behind goes
 size_t cache_compact_bytes(int n_pages) { return ((size_t)n_pages * sizeof(int) + 255) & ~(size_t)255; }
 __global__ __launch_bounds__(1024)
@@ -384,20 +490,92 @@ void compact_table_kernel(const int* table, int64_t entries, int n_pages, const 
         table_out[i] = moves ? to[page] : page;
     }
 }
+constexpr int kSmallCompactPages = 16384, kSmallCompactEntries = 65536;
+__global__ __launch_bounds__(1024)
+void compact_small_kernel(const int* table, const int* __restrict__ refs, int entries, int n_pages, int* table_out, int* __restrict__ refs_out, int* __restrict__ pairs,
+                          int* __restrict__ counts)
+{
+    extern __shared__ int lds[];
+    int *const r = lds, *const from = lds + n_pages, *const hole = from + n_pages / 2;
+    __shared__ int s[2][2][16];
+    const int tid = threadIdx.x;
+    int all, used = 0;
+    for (int p = tid; p < n_pages; p += 1024) {
+        const int x = refs[p];
+        r[p] = x;
+        used += x != 0;
+    }
+    group_scan(used, s[0][0], used);
+    int holes = 0, moved = 0, buf = 1;
+    for (int p0 = 0; p0 < n_pages; p0 += 4096, buf ^= 1) {
+        const int p = p0 + 4 * tid;
+        bool is_hole[4], is_moved[4];
+        int h = 0, m = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const bool in = p + k < n_pages, taken = in && r[min(p + k, n_pages - 1)] != 0;
+            h += is_hole[k] = p + k < used && !taken;
+            m += is_moved[k] = p + k >= used && taken;
+        }
+        h = holes + group_scan(h, s[buf][0], all);
+        holes += all;
+        m = moved + group_scan(m, s[buf][1], all);
+        moved += all;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (is_hole[k]) hole[h++] = p + k;
+            if (is_moved[k]) from[m++] = p + k;
+        }
+    }
+    __syncthreads();
+    for (int p = tid; p < n_pages; p += 1024)
+        if (p >= used || r[p] != 0) refs_out[p] = p < used ? r[p] : 0;
+    __syncthreads();
+    for (int i = tid; i < n_pages / 2; i += 1024) {
+        int2 pair = make_int2(-1, -1);
+        if (i < moved) {
+            pair = make_int2(from[i], hole[i]);
+            refs_out[pair.y] = r[pair.x];
+            r[pair.x] = pair.y;                        // from here on, of pages at `used` and behind: where they go
+        }
+        pairs[2 * i] = pair.x;
+        pairs[2 * i + 1] = pair.y;
+    }
+    if (tid == 0) { counts[0] = moved; counts[1] = used; }
+    __syncthreads();
+    for (int e = tid; e < entries; e += 1024) {
+        int page = table[e];
+        // (a free page has 0 there, a page that moves its new place, which may be 0 as well)
+        if (page >= used && page < n_pages && refs[page] != 0) page = r[page];
+        table_out[e] = page;
+    }
+}
+static std::atomic<uint64_t> g_update_small{0}, g_compact_small{0};
+hipError_t init_cache()
+{
+    hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&update_small_kernel), 3 * kSmallPages * sizeof(int), g_update_small);
+    if (e == hipSuccess) e = ensure_lds_limit(reinterpret_cast<const void*>(&compact_small_kernel), 2 * kSmallCompactPages * sizeof(int), g_compact_small);
+    return e;
+}
 hipError_t launch_cache_compact(const int* table, const int* refs, int B, int n_pages, int max_pages, int* table_out, int* refs_out, int* pairs, int* counts, void* workspace, hipStream_t stream)
 {
+    const int64_t entries = (int64_t)B * max_pages, groups = (entries + 255) / 256;
+    if (n_pages <= kSmallCompactPages && entries <= kSmallCompactEntries) {
+        if (const hipError_t e = init_cache(); e != hipSuccess) return e;
+        compact_small_kernel<<<1, 1024, 2 * n_pages * sizeof(int), stream>>>(table, refs, (int)entries, n_pages, table_out, refs_out, pairs, counts);
+        return hipGetLastError();
+    }
     int* to = static_cast<int*>(workspace);
     compact_rank_kernel<<<1, 1024, 0, stream>>>(refs, n_pages, pairs, counts);
     compact_map_kernel<<<(unsigned)((n_pages + 255) / 256), 256, 0, stream>>>(refs, n_pages, pairs, counts, refs_out, to);
-    const int64_t entries = (int64_t)B * max_pages, groups = (entries + 255) / 256;
     compact_table_kernel<<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, stream>>>(table, entries, n_pages, refs, counts, to, table_out);
     return hipGetLastError();
 }
 
 // ---- copies of pages
-constexpr int kPools = 64;                 // of a launch
+constexpr int kPools = 64, kFewPools = 4;  // of a launch; those of a launch whose arguments are short
 constexpr int kCopyBytes = 16384;          // of a page that a work-group takes at a time
-struct Pools { unsigned char* data[kPools]; int64_t stride[kPools], bytes[kPools]; int unit[kPools]; };
+template <int N> struct Pools { unsigned char* data[N]; int64_t stride[N], bytes[N]; int unit[N]; };
 template <typename W>
 __device__ __forceinline__ void copy_bytes(unsigned char* to, const unsigned char* from, int bytes)
 {
@@ -413,8 +591,9 @@ __device__ __forceinline__ void copy_bytes(unsigned char* to, const unsigned cha
         if (i + 768 < n) dst[i + 768] = d;
     }
 }
+template <int N>
 __global__ __launch_bounds__(256)
-void cache_copy_kernel(Pools pools, int n_pools, int parts, int n_pages, const int* __restrict__ pairs, const int* __restrict__ counts, int n_pairs)
+void cache_copy_kernel(Pools<N> pools, int n_pools, int parts, int n_pages, const int* __restrict__ pairs, const int* __restrict__ counts, int n_pairs)
 {
     const int n = counts ? min(max(counts[0], 0), n_pairs) : n_pairs;
     const int64_t items = (int64_t)n * n_pools * parts;
@@ -433,23 +612,27 @@ void cache_copy_kernel(Pools pools, int n_pools, int parts, int n_pages, const i
         else copy_bytes<uint8_t>(dst, src, bytes);
     }
 }
+template <int N>
+static void copy_go(const psa_pool_t* pools, int n, int n_pages, const int* pairs, const int* counts, int n_pairs, hipStream_t stream)
+{
+    Pools<N> p{};
+    int64_t most = 0;
+    for (int i = 0; i < n; ++i) {
+        p.data[i] = static_cast<unsigned char*>(pools[i].data);
+        p.stride[i] = pools[i].page_stride;
+        p.bytes[i] = pools[i].page_bytes;
+        const uintptr_t bits = reinterpret_cast<uintptr_t>(pools[i].data) | (uintptr_t)pools[i].page_stride | (uintptr_t)pools[i].page_bytes;
+        p.unit[i] = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 1;
+        if (pools[i].page_bytes > most) most = pools[i].page_bytes;
+    }
+    const int64_t parts = (most + kCopyBytes - 1) / kCopyBytes, items = n_pairs * parts * n;
+    cache_copy_kernel<N><<<(unsigned)(items < 2048 ? items : 2048), 256, 0, stream>>>(p, n, (int)parts, n_pages, pairs, counts, n_pairs);
+}
 hipError_t launch_cache_copy(const psa_pool_t* pools, int n_pools, int n_pages, const int* pairs, const int* counts, int n_pairs, hipStream_t stream)
 {
     for (int first = 0; first < n_pools; first += kPools) {
         const int n = n_pools - first < kPools ? n_pools - first : kPools;
-        Pools p{};
-        int64_t most = 0;
-        for (int i = 0; i < n; ++i) {
-            const psa_pool_t& t = pools[first + i];
-            p.data[i] = static_cast<unsigned char*>(t.data);
-            p.stride[i] = t.page_stride;
-            p.bytes[i] = t.page_bytes;
-            const uintptr_t bits = reinterpret_cast<uintptr_t>(t.data) | (uintptr_t)t.page_stride | (uintptr_t)t.page_bytes;
-            p.unit[i] = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 1;
-            if (t.page_bytes > most) most = t.page_bytes;
-        }
-        const int64_t parts = (most + kCopyBytes - 1) / kCopyBytes, items = n_pairs * parts * n;
-        cache_copy_kernel<<<(unsigned)(items < 2048 ? items : 2048), 256, 0, stream>>>(p, n, (int)parts, n_pages, pairs, counts, n_pairs);
+        (n <= kFewPools ? copy_go<kFewPools> : copy_go<kPools>)(pools + first, n, n_pages, pairs, counts, n_pairs, stream);
     }
     return hipGetLastError();
 }

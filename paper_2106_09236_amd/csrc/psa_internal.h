@@ -127,6 +127,7 @@ hipError_t init_measure();
 hipError_t init_attend();
 hipError_t init_backward();
 hipError_t init_project();
+hipError_t init_cache();
 
 hipError_t launch_measure(const Plan& p, const Args& a, const Scratch& w);
 hipError_t launch_select(const Plan& p, const Args& a, const Scratch& w);
@@ -201,7 +202,7 @@ hipError_t launch_packed_bwd(const PackedBwdPlan& p, const psa_packed_shape_t& s
                              const psa_heads_t& dQ, const psa_heads_t& dK, const psa_heads_t& dV, void* workspace, hipStream_t stream);
 
 // Dense attention over a cache in pages (psa_paged.hip).
-//   few       1: 32 rows to a work-group, whose waves divide its keys; 0: 128 rows, 32 to a wave
+//   few       1: 16 rows to a work-group, whose waves divide its keys; 0: `rows` of them, 32 to a wave
 //   fine      1: bfloat16 weights in two parts
 //   per_head  work-groups of a key head that the work is divided into, beside one for each tile of rows; n_part: the most there are
 //   join      1: sequences may be divided; n_join: parts of 32 rows to join, at most

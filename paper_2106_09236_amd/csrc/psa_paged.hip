@@ -6,6 +6,7 @@
 // for all its tiles.  `chunk` is found on the device from all lengths (find_part), so that the work-groups of a call are
 // about `target` whatever the lengths are, and equal: a call that was captured serves as its sequences grow.  Sequences
 // cut in several splits leave partial sums in the workspace, joined by a second kernel.
+#include <algorithm>
 #include <type_traits>
 
 #include "psa_paged.h"
@@ -300,9 +301,17 @@ __device__ __forceinline__ void add_nonfinite(Rows32& acc, const PageHeads<const
     }
 }
 
-// D^T[e][col] += sum over 32 values of V[value][e] w[value] as accumulate() of the packed kernels, the values' tile of another type
-template <typename T, typename TC, int ROWS, bool FINE>
-__device__ __forceinline__ void accumulate_rows(floatx16 (&d)[2], const unsigned char* s, int row0, const floatx16& w, int c, int h)
+// -infinity in the scores of a tile of 32 keys that are not held, or not among the first n
+__device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? ~0u : (1u << max(n, 0)) - 1; }
+__device__ __forceinline__ void hide(floatx16& s, uint32_t held, int n, int h)
+{
+    const uint32_t seen = (held & first_bits(n)) >> (4 * h);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = seen >> acc_row(r, 0) & 1 ? s[r] : -INFINITY;
+}
+// accumulate() of the packed kernels with the values' tile of another type
+template <typename T, typename TC, bool FINE>
+__device__ __forceinline__ void accumulate_rows(floatx16 (&d)[2], const Transposed<TC>& a, const floatx16& w)
 {
     constexpr int N = kWeightParts<T, FINE>;
 #pragma unroll
@@ -310,11 +319,9 @@ __device__ __forceinline__ void accumulate_rows(floatx16 (&d)[2], const unsigned
         Operand<T> b[N];
         weight_operand(b, w, st);
 #pragma unroll
-        for (int dt = 0; dt < 2; ++dt) {
-            const Operand<TC> a = tile_transposed<TC, ROWS>(s, row0, st, dt, c, h);
+        for (int dt = 0; dt < 2; ++dt)
 #pragma unroll
-            for (int n = 0; n < N; ++n) d[dt] = mfma(a, b[n], d[dt]);
-        }
+            for (int n = 0; n < N; ++n) d[dt] = mfma(a.v[st][dt], b[n], d[dt]);
     }
 }
 template <typename T, typename TC, int ROWS>
@@ -334,20 +341,27 @@ __device__ __forceinline__ void outside_rows(const PagedSeqs& p, const Heads<T>&
     zero_outside(out, p.offsets, p.B, p.T, hk * p.G, p.G, x, n_part, [&](int head, int row) { if (lse) lse[(int64_t)head * p.T + row] = -INFINITY; });
 }
 
-// ---- many rows: 4 waves of 32 rows each; tiles of KT keys and values go through LDS, the next tile's rows are on their way meanwhile.
-template <typename T, typename C, int PG, int KT, bool FINE>
-__global__ __launch_bounds__(256, sizeof(T) == 4 || FINE ? 2 : 3)
+// ---- many rows: RW x KW waves, KW of them to the same 32 rows, which take alternate KT keys and join their sums in LDS; tiles of
+// KT x KW keys and values go through LDS, the next tile's rows are on their way meanwhile.
+//
+// Infinities and NaN of V: a weight of 0 does not keep them out of a sum (and, in two parts, one times a part of the other sign is NaN).
+// They always leave an infinity or NaN in the sums, so a work-group looks at those at its end, and only then takes its keys once
+// more, with such values left out of the product and added afterwards to the rows that see them.
+template <typename T, typename C, int PG, int KT, int RW, int KW, bool FINE>
+__global__ __launch_bounds__(64 * RW * KW, sizeof(T) == 4 || FINE ? 2 : 3)
 void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C> V, PageScales ks, PageScales vs, PagedSeqs p, Heads<T> out,
                        float* __restrict__ lse, int H_kv, int causal, float scale, int n_part, float* __restrict__ part_o, float2* __restrict__ part_ml)
 {
     typedef typename TileOf<C>::type TC;
+    constexpr int ROWS = 32 * RW, NT = 64 * RW * KW, NWAVE = RW * KW, TILE = KT * KW;
     constexpr int CH = 64 * sizeof(C) / 16;            // 16-byte chunks of a row in the cache
-    constexpr int NL = KT * CH / 256;                  // chunks of a tile, to a thread
+    constexpr int NL = TILE * CH / NT;                 // chunks of a tile, to a thread
     constexpr int NS = KT / 32;
     constexpr int NU = RowChunk<C>::N;
-    constexpr int kBytes = kTileBytes<TC, KT>;
+    constexpr int kBytes = kTileBytes<TC, TILE>;
+    static_assert(KW == 1 || 4 * kBytes >= ROWS * (kJoinRow + 2) * 4, "the join does not fit the tiles");
     __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kBytes];
-    __shared__ int s_bad[2][4];
+    __shared__ int s_bad[2][NWAVE];
     unsigned char *const sK = lds, *const sV = lds + 2 * kBytes;
     const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
@@ -357,98 +371,121 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
     const int n_rows = f.nq * p.G;
     const int shift = f.nk - f.nq + 1;                 // causal: query t sees the first t + shift keys
     auto visible = [&](int r) { const int t = r / p.G; return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
-    const int row0 = f.tile * 128 + wave * 32;
+    const int rw = wave % RW, kg = wave / RW;          // which rows, which keys
+    const int row0 = f.tile * ROWS + rw * 32;
     const int row = row0 + c, rc = min(row, n_rows - 1);
     const int t = rc / p.G, head = hk * p.G + (rc - t * p.G);
     const int n_vis = visible(rc);
     const int begin = f.split * f.chunk * kUnit;
     const int cut = f.split + 1 < f.splits ? begin + f.chunk * kUnit : f.nk;
-    const int n_all = min(cut, __builtin_amdgcn_readfirstlane(visible(min(f.tile * 128 + 127, n_rows - 1))));
-    const int n_every = __builtin_amdgcn_readfirstlane(visible(f.tile * 128));
+    const int n_all = min(cut, __builtin_amdgcn_readfirstlane(visible(min(f.tile * ROWS + ROWS - 1, n_rows - 1))));       // keys any row of the work-group sees
     const int n_wave = min(cut, __builtin_amdgcn_readfirstlane(row0 < n_rows ? visible(min(row0 + 31, n_rows - 1)) : 0));
-    const int n_wave_every = __builtin_amdgcn_readfirstlane(visible(min(row0, n_rows - 1)));
+    const int n_wave_every = __builtin_amdgcn_readfirstlane(visible(min(row0, n_rows - 1)));                              // ... and those that all of a wave's see
 
     HeadOperand<T> q;
     q.load(Q.at(head, f.q0 + t), h);
     PageWindow w{p.table + (int64_t)f.seq * p.max_pages, (f.nk + (1 << p.shift) - 1) >> p.shift, p.n_pages, p.shift, 0, 0, false};
     RowChunk<C> kr[NL], vr[NL];
-    uint32_t held[NS], held_next[NS];
+    uint32_t held_next[NS];
     auto fetch = [&](int j0) {
-        w.reach(j0, KT);
+        w.reach(j0, TILE);
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            const int id = i * 256 + tid, r0 = (i * 256 + wave * 64) / CH;
+            const int id = i * NT + tid, r0 = (i * NT + wave * 64) / CH;
             load_chunk<C, PG>(kr[i], K, ks, hk, w, j0, r0, id / CH, id % CH, f.nk);
             load_chunk<C, PG>(vr[i], V, vs, hk, w, j0, r0, id / CH, id % CH, f.nk);
         }
 #pragma unroll
-        for (int n = 0; n < NS; ++n) held_next[n] = rows_held(w, j0 + 32 * n, f.nk, c);
+        for (int n = 0; n < NS; ++n) held_next[n] = rows_held(w, j0 + kg * KT + 32 * n, f.nk, c);
     };
     Rows32 acc;
-    acc.init();
-    if (begin < n_all) { w.open(begin >> p.shift); fetch(begin); }
-    int buf = 0;
-    for (int j0 = begin; j0 < n_all; j0 += KT, buf ^= 1) {
-        // a weight of 0 does not keep an infinity or NaN of a value that a row does not see out of its sum: in tiles that
-        // some row sees in part they are left out and added afterwards (float32: in all, since an infinity has no parts)
-        const bool look = sizeof(T) == 4 || FINE || j0 + KT > n_every;
-        uint4 v[NL * NU];
+    auto pass = [&](auto again) {
+        constexpr bool careful = decltype(again)::value;
+        acc.init();
+        if (begin < n_all) { w.open(begin >> p.shift); fetch(begin); }
+        int buf = 0;
+        for (int j0 = begin; j0 < n_all; j0 += TILE, buf ^= 1) {
+            uint4 v[NL * NU];
 #pragma unroll
-        for (int i = 0; i < NL; ++i) vr[i].unpack(v + i * NU);
-        if (look) {
-            const bool any = __builtin_amdgcn_ballot_w64(nonfinite(v, TC{})) != 0;
-            if (lane == 0) s_bad[buf][wave] = any;
-            if (any)
+            for (int i = 0; i < NL; ++i) vr[i].unpack(v + i * NU);
+            if constexpr (careful) {
+                const bool any = __builtin_amdgcn_ballot_w64(nonfinite(v, TC{})) != 0;
+                if (lane == 0) s_bad[buf][wave] = any;
 #pragma unroll
                 for (int i = 0; i < NL * NU; ++i) v[i] = finite_only(v[i], TC{});
-        }
+            }
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            const int id = i * 256 + tid;
-            uint4 k[NU];
-            kr[i].unpack(k);
+            for (int i = 0; i < NL; ++i) {
+                const int id = i * NT + tid;
+                uint4 k[NU];
+                kr[i].unpack(k);
 #pragma unroll
-            for (int u = 0; u < NU; ++u) {
-                put<KT>(sK + buf * kBytes, id / CH, id % CH * NU + u, k[u], TC{});
-                put<KT>(sV + buf * kBytes, id / CH, id % CH * NU + u, v[i * NU + u], TC{});
+                for (int u = 0; u < NU; ++u) {
+                    put<TILE>(sK + buf * kBytes, id / CH, id % CH * NU + u, k[u], TC{});
+                    put<TILE>(sV + buf * kBytes, id / CH, id % CH * NU + u, v[i * NU + u], TC{});
+                }
+            }
+            uint32_t held[NS], all = ~0u;
+#pragma unroll
+            for (int n = 0; n < NS; ++n) { held[n] = held_next[n]; all &= held[n]; }
+            if (j0 + TILE < n_all) fetch(j0 + TILE);
+            lds_barrier();
+            const int j = j0 + kg * KT;
+            if (j >= n_wave) continue;
+            floatx16 s[NS];
+#pragma unroll
+            for (int n = 0; n < NS; ++n) s[n] = product_rows<T, TC, TILE>(sK + buf * kBytes, kg * KT + 32 * n, q, c, h);
+            reads_first<4 * NS * kParts<TC>, 4 * NS * (sizeof(T) == 2 ? 1 : sizeof(C) == 4 ? 6 : 3)>();
+            if (j + KT > n_wave_every || all != ~0u) {
+#pragma unroll
+                for (int n = 0; n < NS; ++n) hide(s[n], held[n], n_vis - (j + 32 * n), h);
+            }
+            acc.follow(s, scale);
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+                const Transposed<TC> vt = transposed<TC, TILE>(sV + buf * kBytes, kg * KT + 32 * n, c, h);
+                reads_first<8 * kParts<TC>, 0>();
+                acc.weights(s[n], scale);
+                accumulate_rows<T, TC, FINE>(acc.o, vt, s[n]);
+            }
+            if constexpr (careful) {
+                int any = 0;
+#pragma unroll
+                for (int k = 0; k < NWAVE; ++k) any |= s_bad[buf][k];
+                if (any) add_nonfinite(acc, V, vs, w, hk, j, min(KT, f.nk - j), n_vis, h);
             }
         }
+        bool bad = false;
 #pragma unroll
-        for (int n = 0; n < NS; ++n) held[n] = held_next[n];
-        if (j0 + KT < n_all) fetch(j0 + KT);
-        lds_barrier();
-        if (j0 >= n_wave) continue;
-        floatx16 s[NS];
-        uint32_t all = ~0u;
+        for (int dt = 0; dt < 2; ++dt)
 #pragma unroll
-        for (int n = 0; n < NS; ++n) {
-            s[n] = product_rows<T, TC, KT>(sK + buf * kBytes, 32 * n, q, c, h);
-            all &= held[n];
-        }
-        if (j0 + KT > n_wave_every || all != ~0u) {
-#pragma unroll
-            for (int n = 0; n < NS; ++n)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[n][r] = j0 + 32 * n + acc_row(r, h) < n_vis && (held[n] >> acc_row(r, h) & 1) ? s[n][r] : -INFINITY;
-        }
-        acc.follow(s, scale);
-#pragma unroll
-        for (int n = 0; n < NS; ++n) {
-            acc.weights(s[n], scale);
-            accumulate_rows<T, TC, KT, FINE>(acc.o, sV + buf * kBytes, 32 * n, s[n], c, h);
-        }
-        if (look) {
-            int any = 0;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) any |= s_bad[buf][w];
-            if (any) add_nonfinite(acc, V, vs, w, hk, j0, min(KT, f.nk - j0), n_vis, h);
-        }
-    }
+            for (int r = 0; r < 16; ++r) bad |= !isfinite(acc.o[dt][r]);
+        return __syncthreads_or(bad) != 0;
+    };
+    if (pass(std::false_type{})) pass(std::true_type{});
     outside_rows(p, out, lse, hk, x, n_part);          // (last: its loads would delay the others)
+    float l = acc.l + swap_half(acc.l);
+    if constexpr (KW == 2) {
+        float* join = reinterpret_cast<float*>(lds) + (rw * 32 + c) * kJoinRow;
+        float* join_ml = reinterpret_cast<float*>(lds) + ROWS * kJoinRow + (rw * 32 + c) * 2;
+        if (kg == 1) {                                 // (a barrier lies behind the last reads of the tiles)
+            store_row(join, acc.o, 1.f, h);
+            if (h == 0) { join_ml[0] = acc.m; join_ml[1] = l; }
+        }
+        __syncthreads();
+        if (kg == 1) return;
+        const float m1 = join_ml[0], l1 = join_ml[1], m = fmaxf(acc.m, m1);
+        const float a0 = fast_exp2(acc.m - m), a1 = fast_exp2(m1 - m);
+        l = l * a0 + l1 * a1;
+        acc.m = m;
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc.o[dt][r] = acc.o[dt][r] * a0 + join[32 * dt + acc_row(r, h)] * a1;
+    }
     if (row >= n_rows) return;
-    const float l = acc.l + swap_half(acc.l);
     if (f.splits > 1) {
-        const int64_t rec = ((int64_t)(f.slot + f.split * f.tiles + f.tile) * H_kv + hk) * 128 + wave * 32 + c;
+        const int64_t rec = ((int64_t)(f.slot + f.split * f.tiles + f.tile) * H_kv + hk) * ROWS + rw * 32 + c;
         store_row(part_o + rec * 64, acc.o, 1.f, h);
         if (h == 0) part_ml[rec] = make_float2(acc.m, l);
         return;
@@ -458,159 +495,17 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
     if (lse && h == 0) lse[(int64_t)head * p.T + f.q0 + t] = l != 0.f ? acc.m * kLn2 + logf(l) : -INFINITY;
 }
 
-// ---- few rows: 32 to a work-group, whose 4 waves divide the keys (of its split) among themselves, 32 at a time, and join their
-// sums at the end.  A wave's tiles go through LDS of its own, DEPTH of them on their way in registers; there is no barrier before
-// the join.  (float32 keys, whose three parts would take too much LDS, come straight from memory as the first product's operand.)
-template <typename C> constexpr int kDepth = sizeof(C) == 4 ? 1 : 2;
-template <typename T, typename C, int PG>
-__global__ __launch_bounds__(256, 2)
-void paged_few_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C> V, PageScales ks, PageScales vs, PagedSeqs p, Heads<T> out,
-                      float* __restrict__ lse, int H_kv, int causal, float scale, int n_part, float* __restrict__ part_o, float2* __restrict__ part_ml)
-{
-    typedef typename TileOf<C>::type TC;
-    constexpr bool DIRECT = sizeof(C) == 4;            // keys
-    constexpr int CH = 64 * sizeof(C) / 16;
-    constexpr int NL = 32 * CH / 64;                   // chunks of a tile of 32 rows, to a lane
-    constexpr int NU = RowChunk<C>::N;
-    constexpr int DEPTH = kDepth<C>;
-    constexpr int kBytes = kTileBytes<TC, 32>;
-    constexpr int kWave = DIRECT ? kBytes : 2 * kBytes;
-    constexpr int kJoinBytes = 4 * 32 * kJoinRow * 4;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kWave > kJoinBytes ? 4 * kWave : kJoinBytes];
-    __shared__ float s_m[4][32], s_l[4][32];
-    const int hk = blockIdx.x % H_kv, x = blockIdx.x / H_kv;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
-    const Part f = find_part<false>(p, x);
-    if (f.seq < 0) { outside_rows(p, out, lse, hk, x, n_part); return; }
-    const int n_rows = f.nq * p.G;
-    const int shift = f.nk - f.nq + 1;
-    auto visible = [&](int r) { const int t = r / p.G; return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
-    const int row0 = f.tile * 32, row = row0 + c, rc = min(row, n_rows - 1);
-    const int t = rc / p.G, head = hk * p.G + (rc - t * p.G);
-    const int n_vis = visible(rc);
-    const int begin = f.split * f.chunk * kUnit;
-    const int cut = f.split + 1 < f.splits ? begin + f.chunk * kUnit : f.nk;
-    const int end = min(cut, __builtin_amdgcn_readfirstlane(visible(min(row0 + 31, n_rows - 1))));
-    const int n_every = __builtin_amdgcn_readfirstlane(visible(row0));
-
-    HeadOperand<T> q;
-    q.load(Q.at(head, f.q0 + t), h);
-    PageWindow w{p.table + (int64_t)f.seq * p.max_pages, (f.nk + (1 << p.shift) - 1) >> p.shift, p.n_pages, p.shift, 0, 0, false};
-    unsigned char *const sV = lds + wave * kWave, *const sK = sV + kBytes;
-    struct Tile {
-        RowChunk<C> k[DIRECT ? 1 : NL], v[NL];
-        HeadRow<float> direct;
-        uint32_t held;
-    } next[DEPTH];
-    auto fetch = [&](Tile& n, int j0) {
-        w.reach(j0, 32);
-        if constexpr (DIRECT) {
-            const int page = w.lane(j0 + c);
-            const C* key = row_at(K, hk, page, w.slot(j0 + c)) + 32 * h;
-#pragma unroll
-            for (int i = 0; i < HeadRow<float>::N; ++i) n.direct.x[i] = load_or_zero<uint4>(key + 4 * i, page >= 0 && j0 + c < f.nk);
-        } else {
-#pragma unroll
-            for (int i = 0; i < NL; ++i) load_chunk<C, PG>(n.k[i], K, ks, hk, w, j0, i * 64 / CH, (i * 64 + lane) / CH, lane % CH, f.nk);
-        }
-#pragma unroll
-        for (int i = 0; i < NL; ++i) load_chunk<C, PG>(n.v[i], V, vs, hk, w, j0, i * 64 / CH, (i * 64 + lane) / CH, lane % CH, f.nk);
-        n.held = rows_held(w, j0, f.nk, c);
-    };
-    Rows32 acc;
-    acc.init();
-    auto take = [&](Tile& n, int j0) {
-        // infinities and NaN of V are left out of the product and added afterwards, in whole tiles too: the weights have parts of either
-        // sign and of 0
-        uint4 v[NL * NU];
-#pragma unroll
-        for (int i = 0; i < NL; ++i) n.v[i].unpack(v + i * NU);
-        const bool any = __builtin_amdgcn_ballot_w64(nonfinite(v, TC{})) != 0;
-        if (any)
-#pragma unroll
-            for (int i = 0; i < NL * NU; ++i) v[i] = finite_only(v[i], TC{});
-        wave_lds_sync();
-#pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            const int id = i * 64 + lane;
-#pragma unroll
-            for (int u = 0; u < NU; ++u) put<32>(sV, id / CH, id % CH * NU + u, v[i * NU + u], TC{});
-            if constexpr (!DIRECT) {
-                uint4 k[NU];
-                n.k[i].unpack(k);
-#pragma unroll
-                for (int u = 0; u < NU; ++u) put<32>(sK, id / CH, id % CH * NU + u, k[u], TC{});
-            }
-        }
-        wave_lds_sync();
-        floatx16 s[1];
-        if constexpr (DIRECT) s[0] = product(n.direct, q);
-        const uint32_t held = n.held;
-        if (j0 + 128 * DEPTH < end) fetch(n, j0 + 128 * DEPTH);
-        if constexpr (!DIRECT) s[0] = product_rows<T, TC, 32>(sK, 0, q, c, h);
-        if (j0 + 32 > n_every || held != ~0u) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[0][r] = j0 + acc_row(r, h) < n_vis && (held >> acc_row(r, h) & 1) ? s[0][r] : -INFINITY;
-        }
-        acc.follow(s, scale);
-        acc.weights(s[0], scale);
-        accumulate_rows<T, TC, 32, true>(acc.o, sV, 0, s[0], c, h);
-        if (any) add_nonfinite(acc, V, vs, w, hk, j0, min(32, f.nk - j0), n_vis, h);
-    };
-    int j0 = begin + wave * 32;
-    if (j0 < end) {
-        w.open(j0 >> p.shift);
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d) if (j0 + 128 * d < end) fetch(next[d], j0 + 128 * d);
-    }
-    while (j0 < end) {
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d, j0 += 128) if (j0 < end) take(next[d], j0);
-    }
-    outside_rows(p, out, lse, hk, x, n_part);
-    // join: wave w's sums of row r at join[w][r]; a wave that saw no key has m = kMaxInit and sums of 0
-    __syncthreads();
-    float* join = reinterpret_cast<float*>(lds);
-    const float l = acc.l + swap_half(acc.l);
-    if (h == 0) { s_m[wave][c] = acc.m; s_l[wave][c] = l; }
-    store_row(join + (wave * 32 + c) * kJoinRow, acc.o, 1.f, h);
-    __syncthreads();
-    // 8 threads of 8 elements to a row
-    const int r = tid >> 3, e = (tid & 7) * 8;
-    if (row0 + r >= n_rows) return;
-    float m = s_m[0][r];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) m = fmaxf(m, s_m[w][r]);
-    float sum = 0.f, o[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        if (s_m[w][r] == kMaxInit && s_l[w][r] == 0.f) continue;       // (saw no key: its accumulators may hold 0 * NaN)
-        const float a = fast_exp2(s_m[w][r] - m);
-        sum = fmaf(s_l[w][r], a, sum);
-        const float* src = join + (w * 32 + r) * kJoinRow + e;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = fmaf(src[i], a, o[i]);
-    }
-    const int rt = (row0 + r) / p.G, rh = hk * p.G + (row0 + r - rt * p.G);
-    if (f.splits > 1) {
-        const int64_t rec = ((int64_t)(f.slot + f.split * f.tiles + f.tile) * H_kv + hk) * 32 + r;
-        float4* dst = reinterpret_cast<float4*>(part_o + rec * 64 + e);
-        dst[0] = make_float4(o[0], o[1], o[2], o[3]);
-        dst[1] = make_float4(o[4], o[5], o[6], o[7]);
-        if (e == 0) part_ml[rec] = make_float2(m, sum);
-    } else {
-        store_joined(out.at(rh, f.q0 + rt) + e, o, sum);
-        if (lse && e == 0) lse[(int64_t)rh * p.T + f.q0 + rt] = sum == 0.f ? -INFINITY : m * kLn2 + logf(sum);
-    }
-}
-
-// ---- very few rows, single tokens as a rule: 16 to a work-group.  As above, with the 16 x 16 x 32 matrix instruction: half the scores,
-// exponentials and products of a tile of 32 columns, which for one row are 31/32 in vain, and half the registers, so that twice the waves
-// have rows on their way.
+// ---- few rows, single tokens as a rule: 16 to a work-group, whose 4 waves divide the keys (of its split) among themselves, 32 at a time, and
+// join their sums at the end.  Keys come straight from memory as the first product's operand, values through LDS of the wave's own; there
+// is no barrier before the join.
+//
+// Bound by memory, and with few keys by the chain of loads before the first of them.  16 x 16 x 32 matrix instructions: for one row a tile of 32
+// columns computes 31/32 of its scores, exponentials and products in vain and takes twice the registers, so that half the waves have rows on their
+// way: 64 streams of 1 to 4096 keys, 8 heads to 2, bfloat16, 22.6 | 17.0 us, 16 of 4096 to 32768, 8 heads, 8-bit, 118 | 78; with up to 128 rows
+// to a sequence it was never more than a tenth better.  A second tile on its way in registers (3 waves to a SIMD instead of 4): 20.3 -> 21.8 and 73.9 -> 78.3
+// (whole calls).  8 waves to a work-group: 60 streams of 8000 keys 178 -> 162, but 8 of 1000 to 2000 11.8 -> 12.7, 64 of 300 to 2000 in float32 37.4 -> 42.3.
 //   lane (c, g) = (lane % 16, lane / 16);  D[i][j]: i = 4 g + r, j = c;  A[i][k]: i = c, B[k][j]: j = c, 8 elements k to a lane, in an order of our own:
-//   keys    element order of a step: those that make a wave read 64 bytes and more of a row at a time (KeyPair)
+//   keys    element order of a step: those that make a wave read 64 bytes and more of a row at a time (head_element)
 //   values  key 16 t + 4 g + r is element 4 t + r of a lane: the order that scores have in their accumulators
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ floatx4 mfma16(const uint4& a, const uint4& b, floatx4 d) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), d, 0, 0, 0); }
@@ -708,7 +603,6 @@ __device__ __forceinline__ void weight_operand16(Operand<bf16_t> (&b)[2], const 
     for (int n = 0; n < 2; ++n) b[n].v[0] = make_uint4(part[0][1 - n], part[1][1 - n], part[2][1 - n], part[3][1 - n]);
 }
 
-template <typename C> constexpr int kDepth16 = 1;
 template <typename T, typename C, int PG>
 __global__ __launch_bounds__(256, sizeof(T) == 4 || sizeof(C) == 4 ? 2 : 4)
 void paged_single_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C> V, PageScales ks, PageScales vs, PagedSeqs p, Heads<T> out,
@@ -719,7 +613,6 @@ void paged_single_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const
     constexpr int NL = 32 * CH / 64;                   // chunks of a tile of 32 values, to a lane
     constexpr int NU = RowChunk<C>::N;
     constexpr int NW = sizeof(T) == 4 ? 1 : 2;         // parts of a weight
-    constexpr int DEPTH = kDepth16<C>;
     constexpr int kBytes = kTileBytes<TC, 32>;
     constexpr int kJoinBytes = 4 * 16 * kJoinRow * 4;
     __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kBytes > kJoinBytes ? 4 * kBytes : kJoinBytes];
@@ -747,7 +640,7 @@ void paged_single_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const
         KeyPart<C> k[2];
         RowChunk<C> v[NL];
         uint32_t held;
-    } next[DEPTH];
+    } next;
     auto fetch = [&](Tile& n, int j0) {
         w.reach(j0, 32);
         if constexpr (PG > 0) {
@@ -816,15 +709,11 @@ void paged_single_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const
             }
             wave_lds_sync();
             const uint32_t held = n.held;
-            if (j0 + 128 * DEPTH < end) fetch(n, j0 + 128 * DEPTH);
+            if (j0 + 128 < end) fetch(n, j0 + 128);
             if (j0 + 32 > n_every || held != ~0u) {
+                const uint32_t seen = (held & first_bits(n_vis - j0)) >> (4 * g);
 #pragma unroll
-                for (int t16 = 0; t16 < 2; ++t16)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int j = 16 * t16 + 4 * g + r;
-                        s[t16][r] = j0 + j < n_vis && (held >> j & 1) ? s[t16][r] : -INFINITY;
-                    }
+                for (int i = 0; i < 8; ++i) s[i >> 2][i & 3] = seen >> (16 * (i >> 2) + (i & 3)) & 1 ? s[i >> 2][i & 3] : -INFINITY;
             }
             // the running maximum, as Rows32 follows it
             float top = s[0][0];
@@ -868,13 +757,9 @@ void paged_single_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const
         int j0 = begin + wave * 32;
         if (j0 < end) {
             w.open(j0 >> p.shift);
-#pragma unroll
-            for (int d = 0; d < DEPTH; ++d) if (j0 + 128 * d < end) fetch(next[d], j0 + 128 * d);
+            fetch(next, j0);
         }
-        while (j0 < end) {
-#pragma unroll
-            for (int d = 0; d < DEPTH; ++d, j0 += 128) if (j0 < end) take(next[d], j0);
-        }
+        for (; j0 < end; j0 += 128) take(next, j0);
         float size = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) size = fmaxf(size, isfinite(o[i >> 2][i & 3]) ? 0.f : 1.f);
@@ -918,7 +803,8 @@ void paged_single_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const
     }
 }
 
-// Joins the splits of 32 rows of a sequence that has several: a wave to a row, 16 lanes of 4 elements for every fourth split.
+// Joins the splits of 32 rows of a sequence that has several: 16 lanes of 4 elements to a row, with four splits on their way; where there are few
+// rows, four such groups to a row, for every fourth split each.
 template <typename T>
 __global__ __launch_bounds__(256, 2)
 void paged_join_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, PagedSeqs p, int H_kv, Heads<T> out, float* __restrict__ lse)
@@ -926,23 +812,27 @@ void paged_join_kernel(const float* __restrict__ part_o, const float2* __restric
     const int hk = blockIdx.x % H_kv;
     const Part f = find_part<true>(p, blockIdx.x / H_kv);
     if (f.seq < 0) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = (lane & 15) * 4, s0 = lane >> 4;
-    for (int r = f.tile * 32 + wave; r < min(f.tile * 32 + 32, f.nq * p.G); r += 4) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = (lane & 15) * 4, group = lane >> 4;
+    const int r0 = f.tile * 32, r1 = min(r0 + 32, f.nq * p.G);
+    const bool shared = r1 - r0 <= 8;                  // four groups to a row
+    const int every = shared ? 4 : 1, s0 = shared ? group : 0;
+    for (int r = r0 + (shared ? wave : wave * 4 + group); r < r1; r += shared ? 4 : 16) {
         const int t = r / p.G, head = hk * p.G + (r - t * p.G), tile = r / p.rows;
         const int64_t first = ((int64_t)(f.slot + tile) * H_kv + hk) * p.rows + r % p.rows, step = (int64_t)f.tiles * H_kv * p.rows;
         float m = kMaxInit, sum = 0.f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int base = s0; base < f.splits; base += 16) {
+        for (int base = s0; base < f.splits; base += 4 * every) {
             float2 ml[4];
             float4 v[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int64_t rec = first + min(base + 4 * k, f.splits - 1) * step;
+                const int64_t rec = first + min(base + every * k, f.splits - 1) * step;
                 ml[k] = part_ml[rec];
                 v[k] = *reinterpret_cast<const float4*>(part_o + rec * 64 + e);
-                // (a split that saw no key may hold 0 * NaN)
-                if (base + 4 * k >= f.splits || ml[k].y == 0.f) { ml[k] = make_float2(kMaxInit, 0.f); v[k] = make_float4(0.f, 0.f, 0.f, 0.f); }
             }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)                // (a split that saw no key may hold 0 * NaN)
+                if (base + every * k >= f.splits || ml[k].y == 0.f) { ml[k] = make_float2(kMaxInit, 0.f); v[k] = make_float4(0.f, 0.f, 0.f, 0.f); }
             const float top = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m);
             const float a0 = fast_exp2(m - top);
             sum *= a0; o.x *= a0; o.y *= a0; o.z *= a0; o.w *= a0;
@@ -954,41 +844,50 @@ void paged_join_kernel(const float* __restrict__ part_o, const float2* __restric
                 o.x = fmaf(v[k].x, a, o.x); o.y = fmaf(v[k].y, a, o.y); o.z = fmaf(v[k].z, a, o.z); o.w = fmaf(v[k].w, a, o.w);
             }
         }
+        if (shared) {
 #pragma unroll
-        for (int k = 16; k < 64; k *= 2) {
-            const float m2 = __shfl_xor(m, k, 64), top = fmaxf(m, m2);
-            const float a = fast_exp2(m - top), b = fast_exp2(m2 - top);
-            sum = sum * a + __shfl_xor(sum, k, 64) * b;
-            o.x = o.x * a + __shfl_xor(o.x, k, 64) * b;
-            o.y = o.y * a + __shfl_xor(o.y, k, 64) * b;
-            o.z = o.z * a + __shfl_xor(o.z, k, 64) * b;
-            o.w = o.w * a + __shfl_xor(o.w, k, 64) * b;
-            m = top;
+            for (int k = 16; k < 64; k *= 2) {
+                const float m2 = __shfl_xor(m, k, 64), top = fmaxf(m, m2);
+                const float a = fast_exp2(m - top), b = fast_exp2(m2 - top);
+                sum = sum * a + __shfl_xor(sum, k, 64) * b;
+                o.x = o.x * a + __shfl_xor(o.x, k, 64) * b;
+                o.y = o.y * a + __shfl_xor(o.y, k, 64) * b;
+                o.z = o.z * a + __shfl_xor(o.z, k, 64) * b;
+                o.w = o.w * a + __shfl_xor(o.w, k, 64) * b;
+                m = top;
+            }
+            if (group != 0) continue;
         }
-        if (s0 != 0) continue;
         const float f1 = sum != 0.f ? 1.f / sum : 0.f;
         store4(out.at(head, f.q0 + t) + e, sum != 0.f ? make_float4(o.x * f1, o.y * f1, o.z * f1, o.w * f1) : make_float4(0.f, 0.f, 0.f, 0.f));
         if (lse && e == 0) lse[(int64_t)head * p.T + f.q0 + t] = sum == 0.f ? -INFINITY : m * kLn2 + logf(sum);
     }
 }
 
+// 16, 64 or 128 rows to a work-group?  16 for at most 32 rows to a sequence, and for calls with few work-groups.  16 | 64 or 128 rows, bfloat16: 8 sequences
+// of 500 to 1500 keys and 64 rows, 4 heads, 14.8 | 16.0 us, 64 of them with 200 to 900 keys 21.6 | 19.3; 32 of 300 to 1500 keys and 32 rows, 8
+// heads, 23.1 | 20.3 (float32 46.6 | 54.3); 4 of 1000 to 2000 keys and 128 rows, 8 heads, 18.5 | 17.3 (float32 40 | 28); 32 of 300 to 1000 and 100 rows 33 | 28
+// (float32 75 | 48).  64 | 128 rows: 16 of 600 to 2048 keys and 64 rows 21.0 | 23.3; 64 of 200 to 900, 4 heads, 19.3 | 21.6.
+//
+// Shares of the work: as many as compute units hold work-groups, but where tiles are about as many shares are larger, since their sizes even out
+// and sums that are joined cost 528 bytes of traffic a row and split.
 PagedPlan make_paged_plan(const psa_cache_t& cache, const psa_paged_shape_t& s)
 {
     PagedPlan p{};
     const int64_t rows = (int64_t)s.T * (s.H / s.H_kv);
     const int64_t wide = (rows / 128 + s.B) * s.H_kv;
-    p.few = rows <= (int64_t)32 * s.B;
+    p.few = rows <= (int64_t)32 * s.B || (rows / 16 + s.B) * s.H_kv <= 192;
     p.fine = p.few || wide < (s.causal ? 224 : 152);
-    p.rows = rows <= (int64_t)16 * s.B ? 16 : p.few ? 32 : 128;
-    const int target = p.few ? 1024 : 768;
-    p.per_head = (target + s.H_kv - 1) / s.H_kv;
+    p.rows = p.few ? 16 : rows <= (int64_t)64 * s.B && s.dtype == PSA_BF16 ? 64 : 128;
     const int64_t tiles = rows / p.rows + s.B;         // at most
+    const int64_t shares = ((p.few ? 1024 : 768) + s.H_kv - 1) / s.H_kv;
+    p.per_head = std::max((int64_t)1, shares * shares / (shares + std::min(shares, tiles)));
     // splits: sum of ceil(tiles units / chunk) is at most per_head more than the tiles
     p.n_part = tiles + p.per_head;
     p.join = (int64_t)cache.max_pages * cache.page_rows > kLeastUnits * kUnit;
     // of sequences with several splits the parts are at most twice their work over the chunk, and a row is joined in parts of 32
     const int64_t slots = p.join ? 2 * (int64_t)p.per_head : 0;
-    p.n_join = slots * (p.rows > 32 ? p.rows / 32 : 1) / 2 + 1;
+    p.n_join = std::min(slots * std::max(p.rows / 32, 1) / 2 + 1, rows / 32 + s.B);
     size_t at = 0;
     if (s.B > kPagedMany) at += ((size_t)(3 * ((s.B + 63) / 64) + 1) * sizeof(int) + 255) & ~(size_t)255;
     p.off_ml = at;
@@ -1015,11 +914,15 @@ static void paged_go(const PagedPlan& p, const psa_paged_shape_t& s, const psa_h
     constexpr int KT = sizeof(C) == 4 ? 32 : 64;
     constexpr bool FINE = sizeof(T) == 2;
     const unsigned grid = (unsigned)(p.n_part * s.H_kv);
-    const bool wide = cache.page_rows >= 32, mid = cache.page_rows == 16;
-    (p.rows == 16 ? (wide ? paged_single_kernel<T, C, 32> : mid ? paged_single_kernel<T, C, 16> : paged_single_kernel<T, C, 0>)
-     : p.few ? (wide ? paged_few_kernel<T, C, 32> : mid ? paged_few_kernel<T, C, 16> : paged_few_kernel<T, C, 0>)
-     : p.fine ? (wide ? paged_rows_kernel<T, C, 32, KT, FINE> : mid ? paged_rows_kernel<T, C, 16, KT, FINE> : paged_rows_kernel<T, C, 0, KT, FINE>)
-              : (wide ? paged_rows_kernel<T, C, 32, KT, false> : mid ? paged_rows_kernel<T, C, 16, KT, false> : paged_rows_kernel<T, C, 0, KT, false>))<<<grid, 256, 0, stream>>>(
+    auto pick = [&](auto pg) {
+        constexpr int PG = decltype(pg)::value;
+        if (p.few) return paged_single_kernel<T, C, PG>;
+        if constexpr (sizeof(T) == 2)
+            if (p.rows == 64) return p.fine ? paged_rows_kernel<T, C, PG, 32, 2, 2, true> : paged_rows_kernel<T, C, PG, 32, 2, 2, false>;
+        return p.fine ? paged_rows_kernel<T, C, PG, KT, 4, 1, FINE> : paged_rows_kernel<T, C, PG, KT, 4, 1, false>;
+    };
+    using std::integral_constant;
+    (cache.page_rows >= 32 ? pick(integral_constant<int, 32>{}) : cache.page_rows == 16 ? pick(integral_constant<int, 16>{}) : pick(integral_constant<int, 0>{}))<<<grid, 256, 0, stream>>>(
         heads_of<const T>(Q), page_heads_of<const C>(cache.K), page_heads_of<const C>(cache.V), page_scales_of(cache.K_scales), page_scales_of(cache.V_scales), seqs,
         heads_of<T>(out), lse, s.H_kv, s.causal, scale, (int)p.n_part, part_o, part_ml);
     if (p.join) paged_join_kernel<T><<<(unsigned)(p.n_join * s.H_kv), 256, 0, stream>>>(part_o, part_ml, seqs, s.H_kv, heads_of<T>(out), lse);

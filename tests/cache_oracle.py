@@ -34,7 +34,7 @@ def mx_decode(codes, bytes_):
 def fine(T, H, H_kv, B, causal):
     """Whether bfloat16 weights are kept to 16 bits."""
     rows = T * (H // H_kv)
-    return rows <= 32 * B or (rows // 128 + B) * H_kv < (224 if causal else 152)
+    return rows <= 32 * B or (rows // 16 + B) * H_kv <= 192 or (rows // 128 + B) * H_kv < (224 if causal else 152)
 
 
 def attend(Q, K, V, seen, scale, dtype, round_p):
