@@ -59,21 +59,21 @@ __device__ __forceinline__ float work_of(const PagedSeqs& p, int s)
     return (float)units_of(r.nk) * (float)tiles_of(r.nq, p.G, p.rows);
 }
 
-// What a work-group takes: tile `tile` of sequence `seq`, split `split` of `splits`; `slot`: where the partial sums of its sequence
+// What a work-group takes: tile `tile` of sequence `seq`, split `split` of `splits`, `per` units of keys each; `slot`: where the partial sums of its sequence
 // begin (tile t, split i at slot + i * tiles + t); seq < 0: nothing.  JOIN: the pieces are the 32-row parts of the sequences with
 // more than one split, and `tile` counts those.
-struct Part { int seq, q0, nq, nk, tiles, tile, split, splits, chunk, slot; };
+struct Part { int seq, q0, nq, nk, tiles, tile, split, splits, per, slot; };
 template <bool JOIN>
 __device__ __forceinline__ Part find_part(const PagedSeqs& p, int x)
 {
     Part f{};
     f.seq = -1;
     const int lane = threadIdx.x & 63;
-    int s0 = 0, end = p.B, slot = 0;
+    int s0 = 0, end = p.B, slot = 0, chunk;
     if (p.before) {
         // many sequences: the chunk and the parts, slots and joined pieces before each 64 of them have been summed up; the last 64
         // with at most x before them
-        f.chunk = p.before[0];
+        chunk = p.before[0];
         const int groups = (p.B + 63) / 64;
         const int* before = p.before + 1 + (JOIN ? 2 * groups : 0);
         int lo = 0, n = groups;
@@ -90,11 +90,11 @@ __device__ __forceinline__ Part find_part(const PagedSeqs& p, int x)
     } else {
         float work = 0.f;
         for (int s = lane; s < p.B; s += 64) work += work_of(p, s);
-        f.chunk = chunk_for(p, wave_sum(work));
+        chunk = chunk_for(p, wave_sum(work));
     }
     for (; s0 < end; s0 += 64) {
         const PagedSeq r = paged_seq(p, s0 + lane);
-        const int tiles = tiles_of(r.nq, p.G, p.rows), splits = splits_of(r.nk, f.chunk);
+        const int tiles = tiles_of(r.nq, p.G, p.rows), splits = splits_of(r.nk, chunk);
         // (a call has fewer than 2^24 parts, but where offsets decrease each sequence may claim all of its rows; there are never more
         // slots than twice p.per_head, since a sequence's parts are at most twice its work over the chunk)
         const int parts = tiles * splits, slots = splits > 1 ? parts : 0;
@@ -106,6 +106,7 @@ __device__ __forceinline__ Part find_part(const PagedSeqs& p, int x)
             f.seq = s0 + l;
             f.q0 = __builtin_amdgcn_readlane(r.q0, l); f.nq = __builtin_amdgcn_readlane(r.nq, l); f.nk = __builtin_amdgcn_readlane(r.nk, l);
             f.tiles = __builtin_amdgcn_readlane(tiles, l); f.splits = __builtin_amdgcn_readlane(splits, l);
+            f.per = (units_of(f.nk) + f.splits - 1) / f.splits;
             f.slot = slot + __builtin_amdgcn_readlane(slot_sum - slots, l);
             const int y = x - __builtin_amdgcn_readlane(sum - n, l);
             if (JOIN) {
@@ -376,8 +377,7 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
     const int row = row0 + c, rc = min(row, n_rows - 1);
     const int t = rc / p.G, head = hk * p.G + (rc - t * p.G);
     const int n_vis = visible(rc);
-    const int begin = f.split * f.chunk * kUnit;
-    const int cut = f.split + 1 < f.splits ? begin + f.chunk * kUnit : f.nk;
+    const int begin = f.split * f.per * kUnit, cut = min(begin + f.per * kUnit, f.nk);
     const int n_all = min(cut, __builtin_amdgcn_readfirstlane(visible(min(f.tile * ROWS + ROWS - 1, n_rows - 1))));       // keys any row of the work-group sees
     const int n_wave = min(cut, __builtin_amdgcn_readfirstlane(row0 < n_rows ? visible(min(row0 + 31, n_rows - 1)) : 0));
     const int n_wave_every = __builtin_amdgcn_readfirstlane(visible(min(row0, n_rows - 1)));                              // ... and those that all of a wave's see
@@ -627,8 +627,7 @@ void paged_single_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const
     const int row0 = f.tile * 16, rc = min(row0 + c, n_rows - 1);
     const int t = rc / p.G, head = hk * p.G + (rc - t * p.G);
     const int n_vis = visible(rc);
-    const int begin = f.split * f.chunk * kUnit;
-    const int cut = f.split + 1 < f.splits ? begin + f.chunk * kUnit : f.nk;
+    const int begin = f.split * f.per * kUnit, cut = min(begin + f.per * kUnit, f.nk);
     const int end = min(cut, __builtin_amdgcn_readfirstlane(visible(min(row0 + 15, n_rows - 1))));
     const int n_every = __builtin_amdgcn_readfirstlane(visible(row0));
 
@@ -869,8 +868,9 @@ void paged_join_kernel(const float* __restrict__ part_o, const float2* __restric
 // heads, 23.1 | 20.3 (float32 46.6 | 54.3); 4 of 1000 to 2000 keys and 128 rows, 8 heads, 18.5 | 17.3 (float32 40 | 28); 32 of 300 to 1000 and 100 rows 33 | 28
 // (float32 75 | 48).  64 | 128 rows: 16 of 600 to 2048 keys and 64 rows 21.0 | 23.3; 64 of 200 to 900, 4 heads, 19.3 | 21.6.
 //
-// Shares of the work: as many as compute units hold work-groups, but where tiles are about as many shares are larger, since their sizes even out
-// and sums that are joined cost 528 bytes of traffic a row and split.
+// Shares of the work: as many as compute units hold work-groups while tiles are less than a quarter (128 rows: a third) of those, down to a quarter as
+// many where they are half (two thirds) of them: their own number evens out what is left, and sums to be joined are 528 bytes of traffic a row and split.  Then, with sequences that
+// can only be so long, nothing is divided, and no join launched (64 sequences of 1300 keys, 8 heads, one new row: 40 | 34 us; 64 new rows 49 | 36).
 PagedPlan make_paged_plan(const psa_cache_t& cache, const psa_paged_shape_t& s)
 {
     PagedPlan p{};
@@ -879,12 +879,14 @@ PagedPlan make_paged_plan(const psa_cache_t& cache, const psa_paged_shape_t& s)
     p.few = rows <= (int64_t)32 * s.B || (rows / 16 + s.B) * s.H_kv <= 192;
     p.fine = p.few || wide < (s.causal ? 224 : 152);
     p.rows = p.few ? 16 : rows <= (int64_t)64 * s.B && s.dtype == PSA_BF16 ? 64 : 128;
-    const int64_t tiles = rows / p.rows + s.B;         // at most
-    const int64_t shares = ((p.few ? 1024 : 768) + s.H_kv - 1) / s.H_kv;
-    p.per_head = std::max((int64_t)1, shares * shares / (shares + std::min(shares, tiles)));
-    // splits: sum of ceil(tiles units / chunk) is at most per_head more than the tiles
-    p.n_part = tiles + p.per_head;
-    p.join = (int64_t)cache.max_pages * cache.page_rows > kLeastUnits * kUnit;
+    const int64_t keys = (int64_t)cache.max_pages * cache.page_rows;
+    const int64_t shares = ((p.few ? 1024 : 768) + s.H_kv - 1) / s.H_kv, each = (rows + s.B - 1) / s.B, tiles = s.B * ((each + p.rows - 1) / p.rows);
+    const double full = std::min(std::max((p.few ? 4.0 : 3.0) * tiles / shares - 1.0, 0.0), 1.0);
+    p.join = keys > kLeastUnits * kUnit && !(full == 1.0 && keys <= (p.few ? 4096 : 2048));
+    // (each tile's last share is half a one on average)
+    p.per_head = p.join ? std::max((int64_t)1, (int64_t)((shares - 0.5 * std::min(tiles, shares)) * (1.0 - 0.75 * full))) : 1;
+    // sum of ceil(tiles units / chunk) is at most per_head more than the tiles (without a join the chunk is all units of the call)
+    p.n_part = rows / p.rows + s.B + p.per_head;
     // of sequences with several splits the parts are at most twice their work over the chunk, and a row is joined in parts of 32
     const int64_t slots = p.join ? 2 * (int64_t)p.per_head : 0;
     p.n_join = std::min(slots * std::max(p.rows / 32, 1) / 2 + 1, rows / 32 + s.B);
