@@ -152,23 +152,25 @@ hipError_t launch_cache_append(const psa_heads_t& K, const psa_heads_t& V, const
 // of them, which is little: the pages that are given away, in ascending order.
 constexpr int kScanParents = 4096;         // new sequences up to which each old one looks through all of them for those that continue it
 struct UpdateRoom {
+    unsigned long long* over;              // pages beyond the tables' rows
     int *growers, *first, *given;          // [n_pages]: sequences that write to a page next, the first of them; free pages in order of need
+    int *last, *had, *want;                // [B_out]: the page that it writes to next (-1: a new one); pages that it has and will have
     int *at, *copied;                      // [B_out]: pages needed before it; whether its last page is copied
     int *children;                         // [B], beyond kScanParents: sequences that continue it
 };
 static UpdateRoom update_room(const CacheUpdate& u, void* room)
 {
-    int* p = static_cast<int*>(room);
     UpdateRoom w{};
+    w.over = static_cast<unsigned long long*>(room);
+    int* p = static_cast<int*>(room) + 2;
     w.growers = p; p += u.n_pages;
     w.first = p; p += u.n_pages;
     w.given = p; p += u.n_pages;
-    w.at = p; p += u.B_out;
-    w.copied = p; p += u.B_out;
+    for (int** a : {&w.last, &w.had, &w.want, &w.at, &w.copied}) { *a = p; p += u.B_out; }
     if (u.B_out > kScanParents) w.children = p;
     return w;
 }
-size_t cache_update_bytes(int B, int B_out, int n_pages) { return ((3 * (size_t)n_pages + 2 * (size_t)B_out + (B_out > kScanParents ? B : 0)) * sizeof(int) + 255) & ~(size_t)255; }
+size_t cache_update_bytes(int B, int B_out, int n_pages) { return ((2 + 3 * (size_t)n_pages + 5 * (size_t)B_out + (B_out > kScanParents ? B : 0)) * sizeof(int) + 255) & ~(size_t)255; }
 
 // Sequence i of the new ones: whom it continues (-1: nobody), the rows and pages it has from there, the rows and pages it will have, and the
 // pages that a row of the table cannot hold
@@ -205,6 +207,7 @@ void update_begin_kernel(CacheUpdate u, UpdateRoom w)
         w.first[i] = INT_MAX;
     }
     if (w.children && i < u.B) w.children[i] = 0;
+    if (i == 0) *w.over = 0;
 }
 __global__ __launch_bounds__(256)
 void update_children_kernel(CacheUpdate u, UpdateRoom w)
@@ -250,10 +253,14 @@ void update_rows_kernel(CacheUpdate u, UpdateRoom w)
     if (tid == 0) {
         u.lengths_out[i] = c.n_out;
         const int page = partial_page(u, c);
+        w.last[i] = page;
+        w.had[i] = c.had;
+        w.want[i] = c.want;
         if (page >= 0) {
             atomicAdd(w.growers + page, 1);
             atomicMin(w.first + page, i);
         }
+        if (c.over > 0) atomicAdd(w.over, (unsigned long long)c.over);
     }
 }
 
@@ -273,31 +280,33 @@ __device__ __forceinline__ int group_scan(int x, int* s, int& all)
     }
     return before + sum - x;
 }
+constexpr int kGivenLds = 4096;
 __global__ __launch_bounds__(1024)
 void update_end_kernel(CacheUpdate u, UpdateRoom w)
 {
     __shared__ int s[2][16];
-    __shared__ unsigned long long s_over;
+    __shared__ int s_given[kGivenLds];
     const int tid = threadIdx.x;
     int buf = 0, all;
-    if (tid == 0) s_over = 0;
-    __syncthreads();
+    // (the first pages are looked at while what is needed is counted)
+    int refs[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) refs[k] = u.refs_out[min(4 * tid + k, u.n_pages - 1)];
     // pages that are needed: as many free ones are looked for
-    int need = 0;
+    int need = 0, last = -1, had = 0, want = 0, copied = 0, at = 0;
     for (int i0 = 0; i0 < u.B_out; i0 += 1024, buf ^= 1) {
         const int i = i0 + tid;
-        int n = 0, copied = 0;
+        int n = 0;
         if (i < u.B_out) {
-            const Child c = child_of(u, i);
-            const int page = partial_page(u, c);
-            copied = page >= 0 && !(u.refs_out[page] == w.growers[page] && w.first[page] == i);
-            n = c.want - c.had + copied;
-            if (c.over > 0) atomicAdd(&s_over, (unsigned long long)c.over);
+            last = w.last[i]; had = w.had[i]; want = w.want[i];
+            copied = last >= 0 && !(u.refs_out[last] == w.growers[last] && w.first[last] == i);
+            n = want - had + copied;
         }
-        const int at = need + group_scan(n, s[buf], all);
-        if (i < u.B_out) { w.at[i] = at; w.copied[i] = copied; }
+        at = need + group_scan(n, s[buf], all);
+        if (i < u.B_out && u.B_out > 1024) { w.at[i] = at; w.copied[i] = copied; }
         need += all;                                   // (at most B_out * max_pages <= 2^30)
     }
+    int* const given = need <= kGivenLds ? s_given : w.given;
     int found = 0;
     for (int p0 = 0; p0 < u.n_pages && found < need; p0 += 4096, buf ^= 1) {
         const int p = p0 + 4 * tid;
@@ -305,34 +314,32 @@ void update_end_kernel(CacheUpdate u, UpdateRoom w)
         int n = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            is_free[k] = p + k < u.n_pages && u.refs_out[min(p + k, u.n_pages - 1)] == 0;
+            is_free[k] = p + k < u.n_pages && refs[k] == 0;
             n += is_free[k];
+            refs[k] = u.refs_out[min(p + 4096 + k, u.n_pages - 1)];
         }
-        int at = found + group_scan(n, s[buf], all);
+        int to = found + group_scan(n, s[buf], all);
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-            if (is_free[k]) w.given[at++] = p + k;     // (each page once: at most n_pages)
+            if (is_free[k]) { if (to < need) given[to] = p + k; ++to; }
         found += all;
     }
     __syncthreads();                                   // (all of `given` is written, and refs have been read)
     int pairs = 0;
     for (int i0 = 0; i0 < u.B_out; i0 += 1024, buf ^= 1) {
         const int i = i0 + tid;
-        int copied = 0, at = 0;
-        if (i < u.B_out) { copied = w.copied[i]; at = w.at[i]; }
-        const bool with_page = copied && at < found;
+        if (i < u.B_out && u.B_out > 1024) { last = w.last[i]; had = w.had[i]; want = w.want[i]; copied = w.copied[i]; at = w.at[i]; }
+        const bool with_page = i < u.B_out && copied && at < found;
         const int pair = pairs + group_scan(with_page, s[buf], all);
         pairs += all;
         if (i < u.B_out) {
-            const Child c = child_of(u, i);
             int* row = u.table_out + (int64_t)i * u.max_pages;
             if (copied) {
-                const int old = partial_page(u, c);
-                atomicAdd(u.refs_out + old, -1);
-                if (with_page) { u.pairs[2 * pair] = old; u.pairs[2 * pair + 1] = w.given[at]; }
+                atomicAdd(u.refs_out + last, -1);
+                if (with_page) { u.pairs[2 * pair] = last; u.pairs[2 * pair + 1] = given[at]; }
             }
-            for (int j = c.had - copied; j < c.want; ++j, ++at) {
-                const int page = at < found ? w.given[at] : -1;
+            for (int j = had - copied; j < want; ++j, ++at) {
+                const int page = at < found ? given[at] : -1;
                 row[j] = page;
                 if (page >= 0) u.refs_out[page] = 1;   // (it was 0: nobody else's)
             }
@@ -341,7 +348,7 @@ void update_end_kernel(CacheUpdate u, UpdateRoom w)
     for (int i = pairs + tid; i < u.B_out; i += 1024) u.pairs[2 * i] = u.pairs[2 * i + 1] = -1;
     if (tid == 0) {
         u.counts[0] = pairs;
-        u.counts[1] = (int)min((unsigned long long)max(need - found, 0) + s_over, (unsigned long long)INT_MAX);
+        u.counts[1] = (int)min((unsigned long long)max(need - found, 0) + *w.over, (unsigned long long)INT_MAX);
     }
 }
 // The same by one work-group.  A sequence to a thread; entries of the tables to any.
@@ -362,6 +369,11 @@ void update_small_kernel(CacheUpdate u)
     const int tid = threadIdx.x, shift = __builtin_ctz((unsigned)u.page_rows);
     Child c{};
     int last = -1;                                     // the page that this thread's sequence writes to next, where it has rows of others
+    // (asked for before the chain of loads that each sequence is)
+    constexpr int AHEAD = kSmallPages / 1024;
+    int held[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) held[k] = u.refs[min(tid + 1024 * k, u.n_pages - 1)];
     if (tid == 0) s_over = 0;
     if (tid < u.B_out) {
         c = child_of(u, tid);
@@ -371,12 +383,15 @@ void update_small_kernel(CacheUpdate u)
         u.lengths_out[tid] = c.n_out;
     }
     if (tid < u.B) s_had_in[tid] = (min(max(u.lengths[tid], 0), u.max_pages * u.page_rows) + u.page_rows - 1) >> shift;
-    for (int p = tid; p < u.n_pages; p += 1024) { refs[p] = u.refs[p]; mark[p] = INT_MAX; }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+        if (tid + 1024 * k < u.n_pages) { refs[tid + 1024 * k] = held[k]; mark[tid + 1024 * k] = INT_MAX; }
     __syncthreads();
     if (c.over > 0) atomicAdd(&s_over, (unsigned long long)c.over);
     // who holds what: the old sequences' entries go, the new ones' come (without parents they are the same)
     const int entries = u.B * u.max_pages, entries_out = u.B_out * u.max_pages;
     if (u.parents) {
+#pragma unroll 4
         for (int e = tid; e < entries; e += 1024) {
             const int b = e / u.max_pages;
             if (e - b * u.max_pages >= s_had_in[b]) continue;
@@ -384,6 +399,7 @@ void update_small_kernel(CacheUpdate u)
             if ((unsigned)page < (unsigned)u.n_pages) atomicAdd(refs + page, -1);
         }
     }
+#pragma unroll 4
     for (int e = tid; e < entries_out; e += 1024) {
         const int i = e / u.max_pages, j = e - i * u.max_pages;
         int page = -1;
