@@ -454,7 +454,7 @@ typedef struct psa_paged_shape {
  * decreasing, clamped to [0, T]; NULL: T / B rows each), n of them, and its rows lengths[s] - n .. lengths[s] - 1 in the
  * cache: lengths count them already.
  *
- * probsparse_cache_append writes K and V [H_kv, T, 64] there.  Rows whose position would be negative, and rows without a page, are
+ * probsparse_cache_append writes K and V [H_kv, T, 64] there (T / 32 * H_kv / 4, or T / 16 * H_kv / 4 of float32, fewer than 2^24).  Rows whose position would be negative, and rows without a page, are
  * left out.  H, causal and scale are ignored.  No two sequences may hold the page that one of them writes to
  * (probsparse_cache_update sees to that); where they do the order is unspecified. */
 int probsparse_cache_append(const psa_heads_t* K, const psa_heads_t* V, const int32_t* offsets, const psa_cache_t* cache,

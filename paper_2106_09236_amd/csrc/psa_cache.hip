@@ -71,7 +71,6 @@ __device__ __forceinline__ void put_chunk(const uint4& x, const PageHeads<mx8_t>
     if (ch % LANES == 0) *(scales.at(hk, (int)page, slot) + ch / LANES) = (uint8_t)(e + 127);
 }
 
-constexpr int kAppendHeads = 4;
 template <typename T, typename C>
 __global__ __launch_bounds__(256)
 void cache_append_kernel(Heads<const T> K, Heads<const T> V, PagedSeqs p, PageHeads<C> Kc, PageHeads<C> Vc, PageScales ks, PageScales vs, int H_kv)
@@ -126,7 +125,7 @@ void cache_append_kernel(Heads<const T> K, Heads<const T> V, PagedSeqs p, PageHe
 template <typename T, typename C>
 static void append_go(const psa_heads_t& K, const psa_heads_t& V, const PagedSeqs& seqs, const psa_cache_t& cache, int H_kv, hipStream_t stream)
 {
-    constexpr int ROWS = 4 * 64 * 16 / (64 * (int)sizeof(T));                  // of a work-group
+    constexpr int ROWS = 4 * 64 / (64 * (int)sizeof(T) / 16);                  // of a work-group
     const dim3 grid((unsigned)((seqs.T + ROWS - 1) / ROWS), (unsigned)((H_kv + kAppendHeads - 1) / kAppendHeads));
     cache_append_kernel<T, C><<<grid, 256, 0, stream>>>(heads_of<const T>(K), heads_of<const T>(V), seqs, page_heads_of<C>(cache.K), page_heads_of<C>(cache.V),
                                                         page_scales_of(cache.K_scales), page_scales_of(cache.V_scales), H_kv);

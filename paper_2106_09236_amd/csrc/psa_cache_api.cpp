@@ -17,7 +17,7 @@ static int check_shape(const psa_paged_shape_t& s, bool attention)
 {
     if (s.dtype != PSA_F32 && s.dtype != PSA_BF16) return PSA_ERR_DTYPE;
     if (s.B < 1 || s.B > kMostSequences || s.H_kv < 1 || s.H_kv > 65535 || s.T < 1 || s.T > (1 << 28) || s.D != kD) return PSA_ERR_SHAPE;
-    if (!attention) return PSA_OK;
+    if (!attention) return append_groups(s) > kMostGroups ? PSA_ERR_SHAPE : PSA_OK;
     if (s.H < 1 || s.H > 65535 || s.H % s.H_kv != 0 || (int64_t)s.T * (s.H / s.H_kv) > INT32_MAX - 65536) return PSA_ERR_SHAPE;
     // (the kernels hold scale * log2(e) in float32: 0 there would make NaN of a masked score)
     if ((s.causal != 0 && s.causal != 1) || !(s.scale >= 1e-30) || !(s.scale <= 1e30)) return PSA_ERR_ARG;

@@ -212,6 +212,9 @@ hipError_t launch_paged(const PagedPlan& p, const psa_paged_shape_t& s, const ps
                         float* lse, void* workspace, hipStream_t stream);
 
 // Rows into a cache, its pages' holders, compaction and copies (psa_cache.hip).
+constexpr int kAppendHeads = 4;            // of a work-group
+inline int64_t append_rows(int dtype) { return 4 * (dtype == PSA_F32 ? 4 : 8); }
+inline int64_t append_groups(const psa_paged_shape_t& s) { return (s.T + append_rows(s.dtype) - 1) / append_rows(s.dtype) * ((s.H_kv + kAppendHeads - 1) / kAppendHeads); }
 hipError_t launch_cache_append(const psa_heads_t& K, const psa_heads_t& V, const int* offsets, const psa_cache_t& cache, const psa_paged_shape_t& s, hipStream_t stream);
 struct CacheUpdate {
     const int *table, *lengths, *refs, *parents, *grow;

@@ -10,6 +10,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/core/LegacyTypeDispatch.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
@@ -556,11 +557,22 @@ PyObject* paged_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
 }
 
 int32_t* ints(const Arg& a) { return static_cast<int32_t*>(a.ptr); }
-void make_ints(Arg& a, at::Tensor& made, const at::Tensor& like, at::IntArrayRef sizes)
+// The integer outputs that the caller did not bring, as parts of one allocation: each of its own takes 0.7 us of a call whose kernel takes 7
+struct Ints { Arg& a; at::Tensor& made; int64_t rows, cols; };     // cols 0: one dimension
+void make_ints(std::initializer_list<Ints> all, const at::Tensor& like)
 {
-    if (a.t) return;
-    made = at::empty(sizes, like.options());
-    a.ptr = made.data_ptr();
+    auto size = [](const Ints& x) { return (x.rows * (x.cols ? x.cols : 1) + 3) & ~(int64_t)3; };
+    int64_t total = 0, at = 0;
+    for (const Ints& x : all) if (!x.a.t) total += size(x);
+    if (total == 0) return;
+    const at::AutoDispatchBelowADInplaceOrView quick;
+    const at::Tensor room = at::empty({total}, like.options());
+    for (const Ints& x : all) {
+        if (x.a.t) continue;
+        x.made = x.cols ? room.as_strided({x.rows, x.cols}, {x.cols, 1}, at) : room.as_strided({x.rows}, {1}, at);
+        x.a.ptr = room.data_ptr<int32_t>() + at;
+        at += size(x);
+    }
 }
 bool int_arg(PyObject* o, int32_t* x)
 {
@@ -591,11 +603,7 @@ PyObject* cache_update(PyObject*, PyObject* const* a, Py_ssize_t n)
     {
         const Unlocked unlocked;
         if (!ws.t) { room = at::empty({(int64_t)bytes}, table.t->options().dtype(at::kByte)); ws.ptr = room.data_ptr(); }
-        make_ints(out[0], made[0], *table.t, {B_out, max_pages});
-        make_ints(out[1], made[1], *table.t, {B_out});
-        make_ints(out[2], made[2], *table.t, {n_pages});
-        make_ints(out[3], made[3], *table.t, {B_out, 2});
-        make_ints(out[4], made[4], *table.t, {2});
+        make_ints({{out[0], made[0], B_out, max_pages}, {out[1], made[1], B_out, 0}, {out[2], made[2], n_pages, 0}, {out[3], made[3], B_out, 2}, {out[4], made[4], 2, 0}}, *table.t);
         rc = probsparse_cache_update(ints(table), ints(lengths), ints(refs), (int32_t)B, ints(parents), ints(grow), (int32_t)B_out, (int32_t)n_pages, page_rows, (int32_t)max_pages,
                                      ints(out[0]), ints(out[1]), ints(out[2]), ints(out[3]), ints(out[4]), ws.ptr, bytes, stream());
     }
@@ -621,10 +629,7 @@ PyObject* cache_compact(PyObject*, PyObject* const* a, Py_ssize_t n)
     {
         const Unlocked unlocked;
         if (!ws.t) { room = at::empty({(int64_t)bytes}, table.t->options().dtype(at::kByte)); ws.ptr = room.data_ptr(); }
-        make_ints(out[0], made[0], *table.t, {B, max_pages});
-        make_ints(out[1], made[1], *table.t, {n_pages});
-        make_ints(out[2], made[2], *table.t, {n_pages / 2, 2});
-        make_ints(out[3], made[3], *table.t, {2});
+        make_ints({{out[0], made[0], B, max_pages}, {out[1], made[1], n_pages, 0}, {out[2], made[2], n_pages / 2, 2}, {out[3], made[3], 2, 0}}, *table.t);
         rc = probsparse_cache_compact(ints(table), ints(refs), (int32_t)B, (int32_t)n_pages, (int32_t)max_pages, ints(out[0]), ints(out[1]), ints(out[2]), ints(out[3]), ws.ptr,
                                       bytes, stream());
     }

@@ -63,6 +63,7 @@ def test_cache_refusals(call):
 
 
 def test_append_refusals():
+    assert _append(shape=_shape(T=1 << 28)) == _append(shape=_shape(T=1 << 25, H_kv=64, dtype=BF16)) == SHAPE        # too many work-groups
     assert _append(K=None) == _append(V=None) == _append(K=_heads(data=None)) == NULL
     assert _append(K=_heads(data=0x1004)) == _append(V=_heads(head=1026)) == ALIGN
     # rows of the cache must not overlap: they are written
@@ -87,10 +88,10 @@ def test_attention_refusals():
 
 
 def test_workspace_does_not_grow_with_the_cache():
-    """A call that was sized once serves while its sequences grow."""
+    """What long sequences need does not depend on how long they may be."""
     size = psa.load().dense_attn_paged_workspace_bytes
     shape = _shape(B=64, H=8, H_kv=8, T=64, dtype=BF16)
-    sizes = {size(_ref(_cache(n_pages=1 << 16, page_rows=64, max_pages=m)), _ref(shape)) for m in (64, 512, 4096, 1 << 16)}
+    sizes = {size(_ref(_cache(n_pages=1 << 16, page_rows=64, max_pages=m)), _ref(shape)) for m in (65, 512, 4096, 1 << 16)}
     assert len(sizes) == 1 and sizes.pop() < 1 << 28
 
 
