@@ -53,9 +53,8 @@ __device__ __forceinline__ float wave_sum(float x)
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 __device__ __forceinline__ int chunk_for(const PagedSeqs& p, float work) { return (int)fminf(fmaxf(ceilf(work / (float)p.per_head), (float)kLeastUnits), (float)(1 << 23)); }
-__device__ __forceinline__ float work_of(const PagedSeqs& p, int s)
+__device__ __forceinline__ float work_of(const PagedSeqs& p, const PagedSeq& r)
 {
-    const PagedSeq r = paged_seq(p, s);
     return (float)units_of(r.nk) * (float)tiles_of(r.nq, p.G, p.rows);
 }
 
@@ -70,6 +69,7 @@ __device__ __forceinline__ Part find_part(const PagedSeqs& p, int x)
     f.seq = -1;
     const int lane = threadIdx.x & 63;
     int s0 = 0, end = p.B, slot = 0, chunk;
+    PagedSeq r = paged_seq(p, lane);
     if (p.before) {
         // many sequences: the chunk and the parts, slots and joined pieces before each 64 of them have been summed up; the last 64
         // with at most x before them
@@ -88,12 +88,12 @@ __device__ __forceinline__ Part find_part(const PagedSeqs& p, int x)
         s0 = lo * 64;
         end = min(end, s0 + 64);
     } else {
-        float work = 0.f;
-        for (int s = lane; s < p.B; s += 64) work += work_of(p, s);
+        float work = work_of(p, r);
+        for (int s = lane + 64; s < p.B; s += 64) work += work_of(p, paged_seq(p, s));
         chunk = chunk_for(p, wave_sum(work));
     }
     for (; s0 < end; s0 += 64) {
-        const PagedSeq r = paged_seq(p, s0 + lane);
+        if (s0 > 0) r = paged_seq(p, s0 + lane);
         const int tiles = tiles_of(r.nq, p.G, p.rows), splits = splits_of(r.nk, chunk);
         // (a call has fewer than 2^24 parts, but where offsets decrease each sequence may claim all of its rows; there are never more
         // slots than twice p.per_head, since a sequence's parts are at most twice its work over the chunk)
@@ -132,7 +132,7 @@ void paged_before_kernel(PagedSeqs p, int* __restrict__ before)
     __shared__ int s[2][3][16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, groups = (p.B + 63) / 64;
     float work = 0.f;
-    for (int i = threadIdx.x; i < p.B; i += 1024) work += work_of(p, i);
+    for (int i = threadIdx.x; i < p.B; i += 1024) work += work_of(p, paged_seq(p, i));
     work = wave_sum(work);
     if (lane == 0) s_work[wave] = work;
     __syncthreads();
@@ -253,22 +253,19 @@ struct PageRows {
     }
     __device__ __forceinline__ uint4 bytes(int row, int at) const { return buffer_load16<uint4>(rows, row * stride + at); }
     __device__ __forceinline__ uint32_t power(int row, int half) const { return (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(powers, row * power_stride + half, 0, 0); }
-};
-// 16 bytes of row j0 + r, chunk ch of it: the rows of a wave, 64 / CH of them and aligned so, are r0 and those behind it
-template <typename C, int PG>
-__device__ __forceinline__ void load_chunk(RowChunk<C>& to, const PageHeads<const C>& t, const PageScales& s, int hk, const PageWindow& w, int j0, int r0, int r, int ch, int nk)
-{
-    if constexpr (PG > 0) {
-        const int from = r0 & ~(PG - 1);
-        const PageRows<C> p(t, s, hk, page_ref(w, j0 + from, PG, nk));
-        to.x = p.bytes(r - from, ch * 16);
-        if constexpr (sizeof(C) == 1) to.power = p.power(r - from, ch >> 1);
-    } else {
-        const int j = j0 + r, page = w.lane(j), slot = w.slot(j);
-        const bool valid = page >= 0 && j < nk;
-        to.x = load_or_zero<uint4>(row_at(t, hk, page, slot) + ch * (16 / (int)sizeof(C)), valid);
-        if constexpr (sizeof(C) == 1) to.power = load_or_zero<uint8_t>(s.at(hk, page, slot) + (ch >> 1), valid);
+    __device__ __forceinline__ void load(RowChunk<C>& to, int row, int ch) const {
+        to.x = bytes(row, ch * 16);
+        if constexpr (sizeof(C) == 1) to.power = power(row, ch >> 1);
     }
+};
+// 16 bytes of row j, chunk ch of it, where each lane finds its row's page
+template <typename C>
+__device__ __forceinline__ void load_chunk(RowChunk<C>& to, const PageHeads<const C>& t, const PageScales& s, int hk, const PageWindow& w, int j, int ch, int nk)
+{
+    const int page = w.lane(j), slot = w.slot(j);
+    const bool valid = page >= 0 && j < nk;
+    to.x = load_or_zero<uint4>(row_at(t, hk, page, slot) + ch * (16 / (int)sizeof(C)), valid);
+    if constexpr (sizeof(C) == 1) to.power = load_or_zero<uint8_t>(s.at(hk, page, slot) + (ch >> 1), valid);
 }
 
 __device__ __forceinline__ floatx16 mfma(const Operand<bf16_t>& a, const Operand<float>& b, floatx16 d)
@@ -391,9 +388,17 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
         w.reach(j0, TILE);
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            const int id = i * NT + tid, r0 = (i * NT + wave * 64) / CH;
-            load_chunk<C, PG>(kr[i], K, ks, hk, w, j0, r0, id / CH, id % CH, f.nk);
-            load_chunk<C, PG>(vr[i], V, vs, hk, w, j0, r0, id / CH, id % CH, f.nk);
+            const int id = i * NT + tid, r = id / CH, ch = id % CH;
+            if constexpr (PG > 0) {
+                const int from = (i * NT + wave * 64) / CH & ~(PG - 1);        // (the rows of a wave are on one page)
+                const PageRef page = page_ref(w, j0 + from, PG, f.nk);
+                const PageRows<C> pk(K, ks, hk, page), pv(V, vs, hk, page);
+                pk.load(kr[i], r - from, ch);
+                pv.load(vr[i], r - from, ch);
+            } else {
+                load_chunk(kr[i], K, ks, hk, w, j0 + r, ch, f.nk);
+                load_chunk(vr[i], V, vs, hk, w, j0 + r, ch, f.nk);
+            }
         }
 #pragma unroll
         for (int n = 0; n < NS; ++n) held_next[n] = rows_held(w, j0 + kg * KT + 32 * n, f.nk, c);
@@ -403,8 +408,8 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
         constexpr bool careful = decltype(again)::value;
         acc.init();
         if (begin < n_all) { w.open(begin >> p.shift); fetch(begin); }
-        int buf = 0;
-        for (int j0 = begin; j0 < n_all; j0 += TILE, buf ^= 1) {
+        auto tile = [&](int j0, auto which) {            // (the buffer known, its addresses are constants)
+            constexpr int buf = decltype(which)::value;
             uint4 v[NL * NU];
 #pragma unroll
             for (int i = 0; i < NL; ++i) vr[i].unpack(v + i * NU);
@@ -431,7 +436,7 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
             if (j0 + TILE < n_all) fetch(j0 + TILE);
             lds_barrier();
             const int j = j0 + kg * KT;
-            if (j >= n_wave) continue;
+            if (j >= n_wave) return;
             floatx16 s[NS];
 #pragma unroll
             for (int n = 0; n < NS; ++n) s[n] = product_rows<T, TC, TILE>(sK + buf * kBytes, kg * KT + 32 * n, q, c, h);
@@ -454,6 +459,10 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
                 for (int k = 0; k < NWAVE; ++k) any |= s_bad[buf][k];
                 if (any) add_nonfinite(acc, V, vs, w, hk, j, min(KT, f.nk - j), n_vis, h);
             }
+        };
+        for (int j0 = begin; j0 < n_all; j0 += 2 * TILE) {
+            tile(j0, std::integral_constant<int, 0>{});
+            if (j0 + TILE < n_all) tile(j0 + TILE, std::integral_constant<int, 1>{});
         }
         bool bad = false;
 #pragma unroll
@@ -654,11 +663,8 @@ void paged_single_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const
                     if constexpr (sizeof(C) == 1) n.k[t16].power = pk.power(16 * t16 - from + c, g >> 1);
                 }
 #pragma unroll
-                for (int i = from * CH / 64; i < (from + PG) * CH / 64; ++i) {
-                    const int r_in = (i * 64 + lane) / CH - from;
-                    n.v[i].x = pv.bytes(r_in, lane % CH * 16);
-                    if constexpr (sizeof(C) == 1) n.v[i].power = pv.power(r_in, lane % CH >> 1);
-                }
+                for (int i = from * CH / 64; i < (from + PG) * CH / 64; ++i)
+                    pv.load(n.v[i], (i * 64 + lane) / CH - from, lane % CH);
             }
         } else {
 #pragma unroll
@@ -671,7 +677,7 @@ void paged_single_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const
                 if constexpr (sizeof(C) == 1) n.k[t16].power = load_or_zero<uint8_t>(ks.at(hk, page, slot) + (g >> 1), valid);
             }
 #pragma unroll
-            for (int i = 0; i < NL; ++i) load_chunk<C, 0>(n.v[i], V, vs, hk, w, j0, 0, (i * 64 + lane) / CH, lane % CH, f.nk);
+            for (int i = 0; i < NL; ++i) load_chunk(n.v[i], V, vs, hk, w, j0 + (i * 64 + lane) / CH, lane % CH, f.nk);
         }
         n.held = rows_held(w, j0, f.nk, lane & 31);
     };
