@@ -346,7 +346,7 @@ def _check_update(table, lengths, refs, page_rows, parents, grow):
 
 
 @pytest.mark.parametrize("B,width,page_rows,n_pages", [(1, 1, 1, 1), (3, 4, 16, 20), (8, 5, 4, 60), (64, 9, 8, 700), (130, 3, 1, 300), (40, 30, 16, 5000), (1500, 4, 2, 4200),
-                                                       (30, 9, 8, 12288), (30, 9, 8, 12289), (1024, 3, 4, 4000), (300, 120, 1, 40000)])
+                                                       (30, 9, 8, 8192), (30, 9, 8, 8193), (1024, 3, 4, 4000), (1024, 8, 4, 4000), (1024, 9, 4, 8000), (300, 120, 1, 40000)])
 def test_update(B, width, page_rows, n_pages):
     """Several steps each: forks, ends, starts, growth over page borders, pages that run out, tables that are full."""
     g = torch.Generator().manual_seed(B + n_pages)
@@ -376,10 +376,10 @@ def test_update_of_many_sequences():
     _check_update(*_holders(4500, 2, 4, 9500, g), 4, None, [1] * 4500)
 
 
-@pytest.mark.parametrize("n_pages", [1, 2, 7, 64, 1000, 4096, 4097, 16383, 20000])
+@pytest.mark.parametrize("n_pages", [1, 2, 7, 64, 1000, 4096, 4097, 8192, 8193, 12288, 20000, 300001])
 def test_compact(n_pages):
     g = torch.Generator().manual_seed(n_pages)
-    for used in (0, 1, n_pages // 3, n_pages // 2, n_pages - 1, n_pages):
+    for used in (0, 1, n_pages // 3, n_pages // 2, n_pages - 1, n_pages, min(4096, n_pages), min(4095, n_pages)):
         pages = torch.randperm(n_pages, generator=g)[:used]
         refs = torch.zeros(n_pages, dtype=torch.int32)
         refs[pages] = torch.randint(1, 5, (used,), generator=g).int()
