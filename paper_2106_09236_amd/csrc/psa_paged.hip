@@ -2,10 +2,10 @@
 // lie in pages named by a table.  The arithmetic is that of the packed kernels (psa_packed.h): rows are (query, head of the
 // group) pairs, 32 to a wave, on the columns of the matrix instruction; keys in one pass with online softmax.
 //
-// Work.  The rows of a sequence are tiles of ROWS, and its keys are cut into splits of `chunk` keys, the same number
-// for all its tiles.  `chunk` is found on the device from all lengths (find_part), so that the work-groups of a call are
-// about `target` whatever the lengths are, and equal: a call that was captured serves as its sequences grow.  Sequences
-// cut in several splits leave partial sums in the workspace, joined by a second kernel.
+// Work.  The rows of a sequence are tiles, and its keys are cut into equal splits, the same for all its tiles.  How many is found
+// on the device from all lengths (find_part), so that a call has about as many work-groups as the card holds, of about one size, whatever
+// the lengths are: a call that was captured serves as its sequences grow.  Sequences cut in several splits leave partial sums in
+// the workspace, joined by a second kernel.
 #include <algorithm>
 #include <type_traits>
 
