@@ -133,7 +133,7 @@ static void append_go(const psa_heads_t& K, const psa_heads_t& V, const PagedSeq
 hipError_t launch_cache_append(const psa_heads_t& K, const psa_heads_t& V, const int* offsets, const psa_cache_t& cache, const psa_paged_shape_t& s, hipStream_t stream)
 {
     const PagedSeqs seqs{offsets, cache.lengths, cache.table, s.B, s.T, s.T / s.B, 1, cache.max_pages * cache.page_rows, page_shift(cache.page_rows), cache.n_pages,
-                         cache.max_pages, 0, 1, nullptr};
+                         cache.max_pages, 0, 1, 1, nullptr};
     const bool mx = cache.format == PSA_CACHE_MX;
     if (s.dtype == PSA_F32) {
         if (mx) append_go<float, mx8_t>(K, V, seqs, cache, s.H_kv, stream);

@@ -8,7 +8,6 @@ namespace psa {
 struct mx8_t { uint8_t x; };               // an 8-bit float (e4m3); a byte for each 32 of a row holds the power of two they are multiplied by
 
 constexpr int kUnit = 128;                 // keys: a round of the 4 waves of a work-group
-constexpr int kLeastUnits = 2;             // ... of a split at the least
 constexpr int kPagedMany = 256;            // sequences beyond which the parts of a call are counted by a kernel of its own
 
 // K or V of a pool, and the powers of two of 8-bit ones (strides in elements)
@@ -27,7 +26,7 @@ inline int page_shift(int page_rows) { return __builtin_ctz((unsigned)page_rows)
 // The sequences of a call: their new rows (offsets, or `uniform` each) and their rows in the cache
 struct PagedSeqs {
     const int* offsets; const int* lengths; const int* table;
-    int B, T, uniform, G, capacity, shift, n_pages, max_pages, rows, per_head;
+    int B, T, uniform, G, capacity, shift, n_pages, max_pages, rows, per_head, least;
     const int* before;
 };
 

@@ -35,9 +35,15 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedSeqs& p, int s)
 __device__ __forceinline__ int units_of(int nk) { return (nk + kUnit - 1) / kUnit; }
 // tiles of a sequence of nq rows, and the splits of its keys, `chunk` units each
 __device__ __forceinline__ int tiles_of(int nq, int G, int rows) { return (nq * G + rows - 1) / rows; }
-__device__ __forceinline__ int splits_of(int nk, int chunk) { return max(1, (units_of(nk) + chunk - 1) / chunk); }
+// (at most 4 sqrt(units): a join takes 16 of them at a time, in about the time of a round of keys, so that more would take longer to join than they save: one sequence
+// of 120000 keys, 8 heads to 2, one new row, 469 splits 36 us, 122 21)
+__device__ __forceinline__ int splits_of(int nk, int chunk)
+{
+    const int units = units_of(nk);
+    return max(1, min((units + chunk - 1) / chunk, (int)(4.f * __builtin_sqrtf((float)units))));
+}
 
-// Units of keys to a split: the work of all tiles (units times tiles) in about p.per_head shares, kLeastUnits at the least.  Every
+// Units of keys to a split: the work of all tiles (units times tiles) in about p.per_head shares, p.least at the least.  Every
 // work-group of a call and of its join finds the same.  Summed in float32, in which the sum is off by 2^-18 at the most: the parts of
 // divided sequences stay at most twice p.per_head, a number below 2^17.
 __device__ __forceinline__ float wave_sum(float x)
@@ -52,7 +58,7 @@ __device__ __forceinline__ float wave_sum(float x)
     add(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
-__device__ __forceinline__ int chunk_for(const PagedSeqs& p, float work) { return (int)fminf(fmaxf(ceilf(work / (float)p.per_head), (float)kLeastUnits), (float)(1 << 23)); }
+__device__ __forceinline__ int chunk_for(const PagedSeqs& p, float work) { return (int)fminf(fmaxf(ceilf(work / (float)p.per_head), (float)p.least), (float)(1 << 23)); }
 __device__ __forceinline__ float work_of(const PagedSeqs& p, const PagedSeq& r)
 {
     return (float)units_of(r.nk) * (float)tiles_of(r.nq, p.G, p.rows);
@@ -102,14 +108,38 @@ __device__ __forceinline__ Part find_part(const PagedSeqs& p, int x)
         const int sum = wave_scan(n), all = last_lane(sum);
         const int slot_sum = wave_scan(slots);
         if (x < all) {
-            const int l = __builtin_popcountll(__builtin_amdgcn_ballot_w64(sum <= x));
+            int l, y;
+            // Undivided sequences with several tiles: of 16 sequences those with the highest index first, which have the most work under a causal mask;
+            // what starts last should be short (8 x 2048 causal, 8 heads, 84 -> 60 us, 64 of 100 to 900 67 -> 58).
+            const bool by_index = !JOIN && __builtin_amdgcn_ballot_w64(splits > 1) == 0 && __builtin_amdgcn_ballot_w64(tiles > 1) != 0;
+            if (by_index) {
+                int group = 0;
+#pragma unroll
+                for (int k = 0; k < 3; ++k) group += x >= __builtin_amdgcn_readlane(sum, 16 * k + 15);
+                y = x - (group > 0 ? __builtin_amdgcn_readlane(sum, 16 * group - 1) : 0);
+                const int mine = (lane >> 4) == group ? n : 0;
+                // tiles of index >= t: sum of max(mine - t, 0).  The t with more than y of them, of t + 1 at most y
+                int lo = 0, hi = 1;
+                while (wave_sum(max(mine - hi, 0)) > y) { lo = hi; hi *= 2; }
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) / 2;
+                    if (wave_sum(max(mine - mid, 0)) > y) lo = mid; else hi = mid;
+                }
+                const int k = y - wave_sum(max(mine - hi, 0));         // of the sequences with more than lo tiles, which
+                const uint64_t with = __builtin_amdgcn_ballot_w64(mine > lo);
+                const int rank = __builtin_popcountll(with & (((uint64_t)1 << lane) - 1));
+                l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(mine > lo && rank == k));
+                y = lo;
+            } else {
+                l = __builtin_popcountll(__builtin_amdgcn_ballot_w64(sum <= x));
+                y = x - __builtin_amdgcn_readlane(sum - n, l);
+            }
             f.seq = s0 + l;
             f.q0 = __builtin_amdgcn_readlane(r.q0, l); f.nq = __builtin_amdgcn_readlane(r.nq, l); f.nk = __builtin_amdgcn_readlane(r.nk, l);
             f.tiles = __builtin_amdgcn_readlane(tiles, l); f.splits = __builtin_amdgcn_readlane(splits, l);
             f.per = (units_of(f.nk) + f.splits - 1) / f.splits;
             f.slot = slot + __builtin_amdgcn_readlane(slot_sum - slots, l);
-            const int y = x - __builtin_amdgcn_readlane(sum - n, l);
-            if (JOIN) {
+            if (JOIN || by_index) {
                 f.tile = y;
             } else {
                 f.split = y / f.tiles;                 // (the tiles of one split after each other: they read the same keys)
@@ -877,6 +907,9 @@ void paged_join_kernel(const float* __restrict__ part_o, const float2* __restric
 // Shares of the work: as many as compute units hold work-groups while tiles are less than a quarter (128 rows: a third) of those, down to a quarter as
 // many where they are half (two thirds) of them: their own number evens out what is left, and sums to be joined are 528 bytes of traffic a row and split.  Then, with sequences that
 // can only be so long, nothing is divided, and no join launched (64 sequences of 1300 keys, 8 heads, one new row: 40 | 34 us; 64 new rows 49 | 36).
+// A share is at least 2 units of keys; 4 where bfloat16 calls have 64 tiles of 128 rows and more, since what a row leaves for the join is as many bytes as 2 units of its
+// keys and values: 32 clips of 40 to 500, 4 heads, 22.7 | 19.5 us, 16 of 2000 keys and 128 rows, 8 heads, 30.1 | 27.7, but 4 of 1000 to 2000 and 128 rows (32 tiles) 17.6 | 21.7,
+// and in float32 28.5 | 41.
 PagedPlan make_paged_plan(const psa_cache_t& cache, const psa_paged_shape_t& s)
 {
     PagedPlan p{};
@@ -888,7 +921,8 @@ PagedPlan make_paged_plan(const psa_cache_t& cache, const psa_paged_shape_t& s)
     const int64_t keys = (int64_t)cache.max_pages * cache.page_rows;
     const int64_t shares = ((p.few ? 1024 : 768) + s.H_kv - 1) / s.H_kv, each = (rows + s.B - 1) / s.B, tiles = s.B * ((each + p.rows - 1) / p.rows);
     const double full = std::min(std::max((p.few ? 4.0 : 3.0) * tiles / shares - 1.0, 0.0), 1.0);
-    p.join = keys > kLeastUnits * kUnit && !(full == 1.0 && keys <= (p.few ? 4096 : 2048));
+    p.least = p.rows == 128 && s.dtype == PSA_BF16 && tiles * s.H_kv >= 64 ? 4 : 2;
+    p.join = keys > p.least * kUnit && !(full == 1.0 && keys <= (p.few ? 4096 : 2048));
     // (each tile's last share is half a one on average)
     p.per_head = p.join ? std::max((int64_t)1, (int64_t)((shares - 0.5 * std::min(tiles, shares)) * (1.0 - 0.75 * full))) : 1;
     // sum of ceil(tiles units / chunk) is at most per_head more than the tiles (without a join the chunk is all units of the call)
@@ -939,7 +973,7 @@ hipError_t launch_paged(const PagedPlan& p, const psa_paged_shape_t& s, const ps
                         float* lse, void* workspace, hipStream_t stream)
 {
     const PagedSeqs seqs{offsets, cache.lengths, cache.table, s.B, s.T, s.T / s.B, s.H / s.H_kv, cache.max_pages * cache.page_rows, page_shift(cache.page_rows), cache.n_pages,
-                         cache.max_pages, p.rows, (int)p.per_head, nullptr};
+                         cache.max_pages, p.rows, (int)p.per_head, p.least, nullptr};
     const bool mx = cache.format == PSA_CACHE_MX;
     if (s.dtype == PSA_F32) {
         if (mx) paged_go<float, mx8_t>(p, s, Q, cache, seqs, out, lse, workspace, stream);

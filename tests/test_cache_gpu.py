@@ -188,7 +188,7 @@ def test_8_bit_codes_are_read_exactly():
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("H,H_kv,page_rows,lengths,by_frame", [
     (1, 1, 16, [1], False), (8, 2, 64, [1, 40, 129, 600, 0], True), (4, 4, 16, [2100], False), (8, 1, 1, [70, 3], False), (4, 2, 2, [33, 100], True),
-    (6, 3, 4, [31, 32, 65], False), (8, 8, 8, [500, 8], True), (8, 4, 256, [700, 256, 1], False), (2, 2, 32, [31, 32, 33, 64, 1200], True)])
+    (6, 3, 4, [31, 32, 65], False), (96, 1, 32, [70, 300], False), (34, 2, 16, [200], True), (8, 8, 8, [500, 8], True), (8, 4, 256, [700, 256, 1], False), (2, 2, 32, [31, 32, 33, 64, 1200], True)])
 def test_single_tokens(H, H_kv, page_rows, lengths, by_frame, causal, dtype, mx):
     cache = Cache(H_kv, page_rows, lengths, dtype, mx, by_frame)
     cache.fill()
@@ -211,7 +211,16 @@ def test_chunks(H, H_kv, page_rows, lengths, new, causal, dtype, mx):
 
 @pytest.mark.parametrize("dtype,mx", FORMATS)
 def test_many_rows_and_splits(dtype, mx):
-    """Work-groups of 128 rows whose weights are rounded, and keys in splits."""
+    """Work-groups of 128 rows whose weights are rounded, and keys in splits; undivided prompts of several tiles, more than 16 of them; a table
+    for far more rows than there are."""
+    cache = Cache(8, 16, [300, 1, 0, 500, 129, 128, 260] * 3, dtype, mx)
+    cache.fill()
+    for causal in (False, True):
+        _check(cache, 8, cache.lengths_host, causal)
+    cache = Cache(2, 16, [300, 20], dtype, mx, width=5000)
+    cache.fill()
+    _check(cache, 4, [1, 1], True, uniform=True)
+    _check(cache, 4, [200, 20], True)
     cache = Cache(8, 64, [3000, 1500], dtype, mx)
     cache.fill()
     _check(cache, 16, [1000, 1200], True)
