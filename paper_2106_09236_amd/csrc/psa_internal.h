@@ -204,9 +204,10 @@ hipError_t launch_packed_bwd(const PackedBwdPlan& p, const psa_packed_shape_t& s
 // Dense attention over a cache in pages (psa_paged.hip).
 //   few       1: 16 rows to a work-group, whose waves divide its keys; 0: `rows` of them, 32 to a wave
 //   fine      1: bfloat16 weights in two parts
+//   pairs     1: two waves to 32 rows of the 128 take alternate keys
 //   per_head  work-groups of a key head that the work is divided into, beside one for each tile of rows; n_part: the most there are
 //   join      1: sequences may be divided, in splits of `least` units of keys or more; n_join: parts of 32 rows to join, at most
-struct PagedPlan { int few, fine, rows, join, least; int64_t per_head, n_part, n_join; size_t off_ml, off_part, total; };
+struct PagedPlan { int few, fine, pairs, rows, join, least; int64_t per_head, n_part, n_join; size_t off_ml, off_part, total; };
 PagedPlan make_paged_plan(const psa_cache_t& cache, const psa_paged_shape_t& s);
 hipError_t launch_paged(const PagedPlan& p, const psa_paged_shape_t& s, const psa_heads_t& Q, const int* offsets, const psa_cache_t& cache, const psa_heads_t& out,
                         float* lse, void* workspace, hipStream_t stream);

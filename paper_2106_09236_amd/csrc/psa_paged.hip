@@ -910,6 +910,11 @@ void paged_join_kernel(const float* __restrict__ part_o, const float2* __restric
 // A share is at least 2 units of keys; 4 where bfloat16 calls have 64 tiles of 128 rows and more, since what a row leaves for the join is as many bytes as 2 units of its
 // keys and values: 32 clips of 40 to 500, 4 heads, 22.7 | 19.5 us, 16 of 2000 keys and 128 rows, 8 heads, 30.1 | 27.7, but 4 of 1000 to 2000 and 128 rows (32 tiles) 17.6 | 21.7,
 // and in float32 28.5 | 41.
+//
+// One | two waves to the same 32 rows, float32: two where tiles are about as many as the 256 compute units, which then have two waves to a
+// SIMD without a division: 24 prompts of 120 to 750, 2 heads of 2, 51.9 | 40.6 us; 16 of 512, 4 heads, 40.7 | 34.1; 32 of 500 to 1500 keys and
+// 120 rows, 8 heads, 85.8 | 74.8; of 6000 to 8000 keys 430 | 400.  With fewer tiles or more four waves fill the compute units more
+// evenly: 192 tiles, 8000 keys, 235 | 343; 384, 700 keys, 60.8 | 65.9; 1024 of 8 x 2048 216 | 226.
 PagedPlan make_paged_plan(const psa_cache_t& cache, const psa_paged_shape_t& s)
 {
     PagedPlan p{};
@@ -919,7 +924,9 @@ PagedPlan make_paged_plan(const psa_cache_t& cache, const psa_paged_shape_t& s)
     p.fine = p.few || wide < (s.causal ? 224 : 152);
     p.rows = p.few ? 16 : rows <= (int64_t)64 * s.B && s.dtype == PSA_BF16 ? 64 : 128;
     const int64_t keys = (int64_t)cache.max_pages * cache.page_rows;
-    const int64_t shares = ((p.few ? 1024 : 768) + s.H_kv - 1) / s.H_kv, each = (rows + s.B - 1) / s.B, tiles = s.B * ((each + p.rows - 1) / p.rows);
+    const int64_t each = (rows + s.B - 1) / s.B, tiles = s.B * ((each + p.rows - 1) / p.rows);
+    p.pairs = !p.few && s.dtype == PSA_F32 && cache.format == PSA_CACHE_PLAIN && tiles * s.H_kv >= 224 && tiles * s.H_kv <= 352;
+    const int64_t shares = ((p.few ? 1024 : p.pairs ? 256 : 768) + s.H_kv - 1) / s.H_kv;
     const double full = std::min(std::max((p.few ? 4.0 : 3.0) * tiles / shares - 1.0, 0.0), 1.0);
     p.least = p.rows == 128 && s.dtype == PSA_BF16 && tiles * s.H_kv >= 64 ? 4 : 2;
     p.join = keys > p.least * kUnit && !(full == 1.0 && keys <= (p.few ? 4096 : 2048));
@@ -961,10 +968,12 @@ static void paged_go(const PagedPlan& p, const psa_paged_shape_t& s, const psa_h
         if (p.few) return paged_single_kernel<T, C, PG>;
         if constexpr (sizeof(T) == 2)
             if (p.rows == 64) return p.fine ? paged_rows_kernel<T, C, PG, 32, 2, 2, true> : paged_rows_kernel<T, C, PG, 32, 2, 2, false>;
+        if constexpr (sizeof(C) == 4)
+            if (p.pairs) return paged_rows_kernel<T, C, PG, KT, 4, 2, FINE>;
         return p.fine ? paged_rows_kernel<T, C, PG, KT, 4, 1, FINE> : paged_rows_kernel<T, C, PG, KT, 4, 1, false>;
     };
     using std::integral_constant;
-    (cache.page_rows >= 32 ? pick(integral_constant<int, 32>{}) : cache.page_rows == 16 ? pick(integral_constant<int, 16>{}) : pick(integral_constant<int, 0>{}))<<<grid, 256, 0, stream>>>(
+    (cache.page_rows >= 32 ? pick(integral_constant<int, 32>{}) : cache.page_rows == 16 ? pick(integral_constant<int, 16>{}) : pick(integral_constant<int, 0>{}))<<<grid, p.pairs ? 512 : 256, 0, stream>>>(
         heads_of<const T>(Q), page_heads_of<const C>(cache.K), page_heads_of<const C>(cache.V), page_scales_of(cache.K_scales), page_scales_of(cache.V_scales), seqs,
         heads_of<T>(out), lse, s.H_kv, s.causal, scale, (int)p.n_part, part_o, part_ml);
     if (p.join) paged_join_kernel<T><<<(unsigned)(p.n_join * s.H_kv), 256, 0, stream>>>(part_o, part_ml, seqs, s.H_kv, heads_of<T>(out), lse);

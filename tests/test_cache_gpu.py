@@ -230,6 +230,17 @@ def test_many_rows_and_splits(dtype, mx):
 
 
 @pytest.mark.parametrize("dtype,mx", FORMATS)
+@pytest.mark.parametrize("page_rows", [4, 16, 64])
+def test_as_many_tiles_as_compute_units(page_rows, dtype, mx):
+    """32 sequences of one tile of 128 rows and 8 heads, undivided and, beside a long one, divided."""
+    for lengths in ([40 + 9 * i for i in range(32)], [130 + i for i in range(31)] + [3500]):
+        cache = Cache(8, page_rows, lengths, dtype, mx)
+        cache.fill()
+        for causal in (False, True):
+            _check(cache, 8, [100 - i for i in range(32)], causal)
+
+
+@pytest.mark.parametrize("dtype,mx", FORMATS)
 @pytest.mark.parametrize("causal", [False, True])
 def test_missing_pages(causal, dtype, mx):
     """Pages that have been freed, entries out of range, sequences with no page at all: as if masked."""
@@ -299,6 +310,31 @@ def test_nonfinite_rows(new, dtype, mx):
     cache.append(K.cuda(), V.cuda(), _offsets(lengths))
     out = cache.attend(Qd, causal=True).cpu()
     assert torch.equal(out[:, ~sees], clean[:, ~sees]) and out[:, sees].isnan().all()
+
+
+@pytest.mark.parametrize("dtype,mx", FORMATS)
+@pytest.mark.parametrize("B,new", [(32, 40), (32, 100), (64, 130)])
+def test_nonfinite_values_of_many_rows(B, new, dtype, mx):
+    """The same in the work-groups of many rows: in one head of one sequence, for its last rows."""
+    lengths = [new + 70 + i for i in range(B)]
+    cache = Cache(8, 16, lengths, dtype, mx)
+    K, V = cache.fill()
+    Q, Qd = _queries(8, B * new, dtype, wide=False)
+    clean = cache.attend(Qd, causal=True).cpu()
+    bad, first = lengths[3] - 5, sum(lengths[:3])
+    V[2, first + bad, 5] = math.nan
+    V[2, first + bad, 9] = math.nan if mx else -math.inf
+    cache.append(K.cuda(), V.cuda(), _offsets(lengths))
+    out = cache.attend(Qd, causal=True).cpu()
+    sees = torch.zeros(8, B * new, dtype=torch.bool)
+    sees[2, 4 * new - 5:4 * new] = True
+    assert torch.equal(out[~sees], clean[~sees])
+    assert out[sees][:, 5].isnan().all() and (out[sees][:, 9].isnan() if mx else out[sees][:, 9] == -math.inf).all()
+    rest = [e for e in range(64) if e not in (5, 9)]
+    if mx:
+        assert out[sees][:, rest].isfinite().all()          # (the scale of the values beside it changed)
+    else:
+        assert torch.equal(out[sees][:, rest], clean[sees][:, rest])
 
 
 def test_packed_attention_says_the_same():
