@@ -26,7 +26,7 @@ inline int page_shift(int page_rows) { return __builtin_ctz((unsigned)page_rows)
 // The sequences of a call: their new rows (offsets, or `uniform` each) and their rows in the cache
 struct PagedSeqs {
     const int* offsets; const int* lengths; const int* table;
-    int B, T, uniform, G, capacity, shift, n_pages, max_pages, rows, per_head, least;
+    int B, T, uniform, G, capacity, shift, n_pages, max_pages, row_shift, per_head, least;
     const int* before;
 };
 

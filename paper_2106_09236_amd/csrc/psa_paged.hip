@@ -17,6 +17,8 @@ __device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readla
 
 // Sequence s as the call has it: rows q0 .. q0 + nq - 1, nk keys
 struct PagedSeq { int q0, nq, nk; };
+// The query of row r of a key head (rows are G to a query)
+__device__ __forceinline__ int query_of(int r, int G) { return G == 1 ? r : r / G; }
 __device__ __forceinline__ PagedSeq paged_seq(const PagedSeqs& p, int s)
 {
     PagedSeq r{0, 0, 0};
@@ -34,11 +36,13 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedSeqs& p, int s)
 }
 __device__ __forceinline__ int units_of(int nk) { return (nk + kUnit - 1) / kUnit; }
 // tiles of a sequence of nq rows, and the splits of its keys, `chunk` units each
-__device__ __forceinline__ int tiles_of(int nq, int G, int rows) { return (nq * G + rows - 1) / rows; }
+__device__ __forceinline__ int tiles_of(int nq, int G, int row_shift) { return (nq * G + (1 << row_shift) - 1) >> row_shift; }
 // (at most 4 sqrt(units): a join takes 16 of them at a time, in about the time of a round of keys, so that more would take longer to join than they save: one sequence
 // of 120000 keys, 8 heads to 2, one new row, 469 splits 36 us, 122 21)
-__device__ __forceinline__ int splits_of(int nk, int chunk)
+// (p.per_head 0: nothing is divided)
+__device__ __forceinline__ int splits_of(const PagedSeqs& p, int nk, int chunk)
 {
+    if (p.per_head == 0) return 1;
     const int units = units_of(nk);
     return max(1, min((units + chunk - 1) / chunk, (int)(4.f * __builtin_sqrtf((float)units))));
 }
@@ -58,10 +62,10 @@ __device__ __forceinline__ float wave_sum(float x)
     add(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
-__device__ __forceinline__ int chunk_for(const PagedSeqs& p, float work) { return (int)fminf(fmaxf(ceilf(work / (float)p.per_head), (float)p.least), (float)(1 << 23)); }
+__device__ __forceinline__ int chunk_for(const PagedSeqs& p, float work) { return (int)fminf(fmaxf(ceilf(work / (float)max(p.per_head, 1)), (float)p.least), (float)(1 << 23)); }
 __device__ __forceinline__ float work_of(const PagedSeqs& p, const PagedSeq& r)
 {
-    return (float)units_of(r.nk) * (float)tiles_of(r.nq, p.G, p.rows);
+    return (float)units_of(r.nk) * (float)tiles_of(r.nq, p.G, p.row_shift);
 }
 
 // What a work-group takes: tile `tile` of sequence `seq`, split `split` of `splits`, `per` units of keys each; `slot`: where the partial sums of its sequence
@@ -93,6 +97,8 @@ __device__ __forceinline__ Part find_part(const PagedSeqs& p, int x)
         slot = p.before[1 + groups + lo];
         s0 = lo * 64;
         end = min(end, s0 + 64);
+    } else if (p.per_head == 0) {
+        chunk = 1 << 23;
     } else {
         float work = work_of(p, r);
         for (int s = lane + 64; s < p.B; s += 64) work += work_of(p, paged_seq(p, s));
@@ -100,11 +106,11 @@ __device__ __forceinline__ Part find_part(const PagedSeqs& p, int x)
     }
     for (; s0 < end; s0 += 64) {
         if (s0 > 0) r = paged_seq(p, s0 + lane);
-        const int tiles = tiles_of(r.nq, p.G, p.rows), splits = splits_of(r.nk, chunk);
+        const int tiles = tiles_of(r.nq, p.G, p.row_shift), splits = splits_of(p, r.nk, chunk);
         // (a call has fewer than 2^24 parts, but where offsets decrease each sequence may claim all of its rows; there are never more
         // slots than twice p.per_head, since a sequence's parts are at most twice its work over the chunk)
         const int parts = tiles * splits, slots = splits > 1 ? parts : 0;
-        const int n = min(JOIN ? (splits > 1 ? tiles_of(r.nq, p.G, 32) : 0) : parts, 1 << 24);
+        const int n = min(JOIN ? (splits > 1 ? tiles_of(r.nq, p.G, 5) : 0) : parts, 1 << 24);
         const int sum = wave_scan(n), all = last_lane(sum);
         const int slot_sum = wave_scan(slots);
         if (x < all) {
@@ -137,7 +143,7 @@ __device__ __forceinline__ Part find_part(const PagedSeqs& p, int x)
             f.seq = s0 + l;
             f.q0 = __builtin_amdgcn_readlane(r.q0, l); f.nq = __builtin_amdgcn_readlane(r.nq, l); f.nk = __builtin_amdgcn_readlane(r.nk, l);
             f.tiles = __builtin_amdgcn_readlane(tiles, l); f.splits = __builtin_amdgcn_readlane(splits, l);
-            f.per = (units_of(f.nk) + f.splits - 1) / f.splits;
+            f.per = f.splits > 1 ? (units_of(f.nk) + f.splits - 1) / f.splits : units_of(f.nk);
             f.slot = slot + __builtin_amdgcn_readlane(slot_sum - slots, l);
             if (JOIN || by_index) {
                 f.tile = y;
@@ -174,9 +180,9 @@ void paged_before_kernel(PagedSeqs p, int* __restrict__ before)
     for (int g0 = 0, buf = 0; g0 < groups; g0 += 16, buf ^= 1) {
         const int g = g0 + wave;
         const PagedSeq r = paged_seq(p, g < groups ? g * 64 + lane : p.B);
-        const int splits = splits_of(r.nk, chunk);
-        const int64_t parts = (int64_t)tiles_of(r.nq, p.G, p.rows) * splits;
-        const int64_t n[3] = {parts, splits > 1 ? parts : 0, splits > 1 ? tiles_of(r.nq, p.G, 32) : 0};
+        const int splits = splits_of(p, r.nk, chunk);
+        const int64_t parts = (int64_t)tiles_of(r.nq, p.G, p.row_shift) * splits;
+        const int64_t n[3] = {parts, splits > 1 ? parts : 0, splits > 1 ? tiles_of(r.nq, p.G, 5) : 0};
         for (int k = 0; k < 3; ++k) {
             const float rough = wave_sum((float)n[k]);
             const int all = rough < (float)kMostParts ? last_lane(wave_scan((int)n[k])) : kMostParts;
@@ -197,10 +203,18 @@ void paged_before_kernel(PagedSeqs p, int* __restrict__ before)
 
 // ---- rows of the cache on their way
 // 64 entries of a sequence's table, one to a lane: a tile's pages are read from a register and no load waits for another.  Entries that name no
-// page are -1.  A new window is waited for where it is asked for, so that the loads of rows in flight are waited for by nobody else.
+// page are -1.  Pages of PG = 16 rows and more: rows that are asked for together lie on one page, whose addresses, of K and of V, the lanes hold as well.  A
+// new window is waited for where it is asked for, so that the loads of rows in flight are waited for by nobody else.
+template <typename C, int PG>
 struct PageWindow {
-    const int* row; int entries, n_pages, shift, first, entry;
-    bool whole;                            // no entry of the window's is -1
+    const int* row; int entries, n_pages, shift;
+    const C *k, *v; int64_t k_page, v_page;            // of the key head
+    int first, entry;
+    bool whole;                                        // no entry of the window's is -1
+    uint32_t lo[2], hi[2];                             // addresses; bit 31 of hi: no page
+    __device__ __forceinline__ PageWindow(const PagedSeqs& p, int seq, int nk, const PageHeads<const C>& K, const PageHeads<const C>& V, int hk)
+        : row(p.table + (int64_t)seq * p.max_pages), entries((nk + (1 << p.shift) - 1) >> p.shift), n_pages(p.n_pages), shift(p.shift),
+          k(K.data + hk * K.head), v(V.data + hk * V.head), k_page(K.page), v_page(V.page), first(0), entry(-1), whole(false), lo{0, 0}, hi{0, 0} {}
     __device__ __forceinline__ void open(int from) {
         const int lane = threadIdx.x & 63, i = from + lane;
         int e = i < entries ? row[i] : -1;
@@ -208,19 +222,25 @@ struct PageWindow {
         first = from;
         entry = e;
         whole = __builtin_amdgcn_ballot_w64(e < 0 && i < entries) == 0;
+        if constexpr (PG > 0) {
+            const uint64_t a[2] = {reinterpret_cast<uint64_t>(k + max(e, 0) * k_page), reinterpret_cast<uint64_t>(v + max(e, 0) * v_page)};
+#pragma unroll
+            for (int x = 0; x < 2; ++x) { lo[x] = (uint32_t)a[x]; hi[x] = (uint32_t)(a[x] >> 32) | (e < 0 ? 0x80000000u : 0u); }
+        }
     }
     // rows j0 .. j0 + n - 1 are about to be asked for: at most 64 pages
     __device__ __forceinline__ void reach(int j0, int n) { if (((j0 + n - 1) >> shift) - first >= 64) open(j0 >> shift); }
-    __device__ __forceinline__ int uniform(int j) const { return __builtin_amdgcn_readlane(entry, (j >> shift) - first); }
     __device__ __forceinline__ int lane(int j) const { return __shfl(entry, (j >> shift) - first, 64); }
+    __device__ __forceinline__ bool held(int j) const { return __shfl(PG > 0 ? (int)hi[0] : entry, (j >> shift) - first, 64) >= 0; }
     __device__ __forceinline__ int slot(int j) const { return j & ((1 << shift) - 1); }
 };
 // Which of the 32 rows from j on exist: on a page, before row nk
-__device__ __forceinline__ uint32_t rows_held(const PageWindow& w, int j, int nk, int c)
+template <typename W>
+__device__ __forceinline__ uint32_t rows_held(const W& w, int j, int nk, int c)
 {
     if (w.whole && j + 32 <= nk) return ~0u;
-    const int page = w.lane(j + c);
-    return (uint32_t)__builtin_amdgcn_ballot_w64(page >= 0 && j + c < nk);
+    const bool held = w.held(j + c);
+    return (uint32_t)__builtin_amdgcn_ballot_w64(held && j + c < nk);
 }
 
 template <typename C>
@@ -263,23 +283,25 @@ template <> struct RowChunk<mx8_t> {
     }
 };
 
-// Where rows j .. of a sequence lie that are on one page: a scalar, as their addresses are
-struct PageRef { int page, slot, n; };     // n: rows that exist, 0 on no page
-__device__ __forceinline__ PageRef page_ref(const PageWindow& w, int j, int most, int nk)
-{
-    const int page = w.uniform(j);
-    return PageRef{max(page, 0), w.slot(j), page < 0 ? 0 : max(0, min(most, nk - j))};
-}
-// K or V of a key head.  Pages of PG = 16 or 32 rows and more: rows that are asked for together lie on one page, and are a buffer that ends
-// with the sequence, so that rows behind it give zeros.  PG = 0: smaller pages, each lane finds its row's.
+// Rows j .. of a sequence in K (0) or V (1) that are on one page: a buffer that ends with the sequence, so that rows behind it give zeros, as rows
+// on no page do.  Scalars; what the host sees to (rows_regular): a row's stride is its width or more, and a page's span less than 2^31 bytes.
 template <typename C>
 struct PageRows {
     __amdgpu_buffer_rsrc_t rows, powers;
     int stride, power_stride;              // bytes
-    __device__ __forceinline__ PageRows(const PageHeads<const C>& t, const PageScales& s, int hk, const PageRef& r)
-        : rows(tile_rows(row_at(t, hk, r.page, r.slot), t.row, r.n)), stride((int)(t.row * (int64_t)sizeof(C))), power_stride((int)s.row)
+    template <int PG>
+    __device__ __forceinline__ void open(const PageWindow<C, PG>& w, int which, const PageHeads<const C>& t, const PageScales& s, int hk, int j, int nk)
     {
-        if constexpr (sizeof(C) == 1) powers = __builtin_amdgcn_make_buffer_rsrc(s.at(hk, r.page, r.slot), 0, r.n > 0 ? (r.n - 1) * power_stride + 2 : 0, 0x00020000);
+        const int i = (j >> w.shift) - w.first, slot = w.slot(j);
+        const uint32_t lo = __builtin_amdgcn_readlane(w.lo[which], i), hi = __builtin_amdgcn_readlane(w.hi[which], i);
+        const int n = (int)hi < 0 ? 0 : min(PG, nk - j);
+        stride = (int)(t.row * (int64_t)sizeof(C));
+        const uint64_t base = ((uint64_t)(hi & 0x7FFFFFFFu) << 32 | lo) + (uint32_t)slot * (uint32_t)stride;
+        rows = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(base), 0, max(n * stride + (64 * (int)sizeof(C) - stride), 0), 0x00020000);
+        if constexpr (sizeof(C) == 1) {
+            power_stride = (int)s.row;
+            powers = __builtin_amdgcn_make_buffer_rsrc(s.at(hk, max(__builtin_amdgcn_readlane(w.entry, i), 0), slot), 0, max(n * power_stride + (2 - power_stride), 0), 0x00020000);
+        }
     }
     __device__ __forceinline__ uint4 bytes(int row, int at) const { return buffer_load16<uint4>(rows, row * stride + at); }
     __device__ __forceinline__ uint32_t power(int row, int half) const { return (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(powers, row * power_stride + half, 0, 0); }
@@ -289,8 +311,8 @@ struct PageRows {
     }
 };
 // 16 bytes of row j, chunk ch of it, where each lane finds its row's page
-template <typename C>
-__device__ __forceinline__ void load_chunk(RowChunk<C>& to, const PageHeads<const C>& t, const PageScales& s, int hk, const PageWindow& w, int j, int ch, int nk)
+template <typename C, typename W>
+__device__ __forceinline__ void load_chunk(RowChunk<C>& to, const PageHeads<const C>& t, const PageScales& s, int hk, const W& w, int j, int ch, int nk)
 {
     const int page = w.lane(j), slot = w.slot(j);
     const bool valid = page >= 0 && j < nk;
@@ -312,8 +334,8 @@ template <> __device__ __forceinline__ float value_at<mx8_t>(const mx8_t* row, c
     return (row[e].x & 0x7F) == 0x7F ? __uint_as_float(0x7FC00000u) : 0.f;       // (no infinities, and nothing else is asked for)
 }
 // The infinities and NaN of values j0 .. j0 + n - 1 that were left out of the tile: to the rows that see them
-template <typename C>
-__device__ __forceinline__ void add_nonfinite(Rows32& acc, const PageHeads<const C>& V, const PageScales& vs, const PageWindow& w, int hk, int j0, int n, int n_vis, int h)
+template <typename C, typename W>
+__device__ __forceinline__ void add_nonfinite(Rows32& acc, const PageHeads<const C>& V, const PageScales& vs, const W& w, int hk, int j0, int n, int n_vis, int h)
 {
     for (int j = j0; j < j0 + n; ++j) {
         const int page = w.row[j >> w.shift], slot = w.slot(j);
@@ -398,11 +420,11 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
 
     const int n_rows = f.nq * p.G;
     const int shift = f.nk - f.nq + 1;                 // causal: query t sees the first t + shift keys
-    auto visible = [&](int r) { const int t = r / p.G; return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
+    auto visible = [&](int r) { const int t = query_of(r, p.G); return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
     const int rw = wave % RW, kg = wave / RW;          // which rows, which keys
     const int row0 = f.tile * ROWS + rw * 32;
     const int row = row0 + c, rc = min(row, n_rows - 1);
-    const int t = rc / p.G, head = hk * p.G + (rc - t * p.G);
+    const int t = query_of(rc, p.G), head = hk * p.G + (rc - t * p.G);
     const int n_vis = visible(rc);
     const int begin = f.split * f.per * kUnit, cut = min(begin + f.per * kUnit, f.nk);
     const int n_all = min(cut, __builtin_amdgcn_readfirstlane(visible(min(f.tile * ROWS + ROWS - 1, n_rows - 1))));       // keys any row of the work-group sees
@@ -411,18 +433,22 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
 
     HeadOperand<T> q;
     q.load(Q.at(head, f.q0 + t), h);
-    PageWindow w{p.table + (int64_t)f.seq * p.max_pages, (f.nk + (1 << p.shift) - 1) >> p.shift, p.n_pages, p.shift, 0, 0, false};
+    PageWindow<C, PG> w(p, f.seq, f.nk, K, V, hk);
     RowChunk<C> kr[NL], vr[NL];
     uint32_t held_next[NS];
     auto fetch = [&](int j0) {
         w.reach(j0, TILE);
+        PageRows<C> pk, pv;
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int id = i * NT + tid, r = id / CH, ch = id % CH;
             if constexpr (PG > 0) {
-                const int from = (i * NT + wave * 64) / CH & ~(PG - 1);        // (the rows of a wave are on one page)
-                const PageRef page = page_ref(w, j0 + from, PG, f.nk);
-                const PageRows<C> pk(K, ks, hk, page), pv(V, vs, hk, page);
+                // (the rows of a wave are on one page; those of all waves where it has NT / CH rows)
+                const int from = NT / CH <= PG ? i * (NT / CH) & ~(PG - 1) : i * (NT / CH) + (wave * 64 / CH & ~(PG - 1));
+                if (NT / CH >= PG || i * (NT / CH) % PG == 0) {
+                    pk.open(w, 0, K, ks, hk, j0 + from, f.nk);
+                    pv.open(w, 1, V, vs, hk, j0 + from, f.nk);
+                }
                 pk.load(kr[i], r - from, ch);
                 pv.load(vr[i], r - from, ch);
             } else {
@@ -662,9 +688,9 @@ void paged_single_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const
     if (f.seq < 0) { outside_rows(p, out, lse, hk, x, n_part); return; }
     const int n_rows = f.nq * p.G;
     const int shift = f.nk - f.nq + 1;
-    auto visible = [&](int r) { const int t = r / p.G; return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
+    auto visible = [&](int r) { const int t = query_of(r, p.G); return causal ? min(max(t + shift, 0), f.nk) : f.nk; };
     const int row0 = f.tile * 16, rc = min(row0 + c, n_rows - 1);
-    const int t = rc / p.G, head = hk * p.G + (rc - t * p.G);
+    const int t = query_of(rc, p.G), head = hk * p.G + (rc - t * p.G);
     const int n_vis = visible(rc);
     const int begin = f.split * f.per * kUnit, cut = min(begin + f.per * kUnit, f.nk);
     const int end = min(cut, __builtin_amdgcn_readfirstlane(visible(min(row0 + 15, n_rows - 1))));
@@ -672,7 +698,7 @@ void paged_single_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const
 
     Operand<T> q[2];
     load_query<T, C>(q, Q.at(head, f.q0 + t), g);
-    PageWindow w{p.table + (int64_t)f.seq * p.max_pages, (f.nk + (1 << p.shift) - 1) >> p.shift, p.n_pages, p.shift, 0, 0, false};
+    PageWindow<C, PG> w(p, f.seq, f.nk, K, V, hk);
     unsigned char* const sV = lds + wave * kBytes;
     struct Tile {
         KeyPart<C> k[2];
@@ -684,8 +710,9 @@ void paged_single_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const
         if constexpr (PG > 0) {
 #pragma unroll
             for (int from = 0; from < 32; from += PG) {
-                const PageRef r = page_ref(w, j0 + from, PG, f.nk);
-                const PageRows<C> pk(K, ks, hk, r), pv(V, vs, hk, r);
+                PageRows<C> pk, pv;
+                pk.open(w, 0, K, ks, hk, j0 + from, f.nk);
+                pv.open(w, 1, V, vs, hk, j0 + from, f.nk);
 #pragma unroll
                 for (int t16 = from / 16; t16 < (from + PG) / 16; ++t16) {
 #pragma unroll
@@ -852,8 +879,8 @@ void paged_join_kernel(const float* __restrict__ part_o, const float2* __restric
     const bool shared = r1 - r0 <= 8;                  // four groups to a row
     const int every = shared ? 4 : 1, s0 = shared ? group : 0;
     for (int r = r0 + (shared ? wave : wave * 4 + group); r < r1; r += shared ? 4 : 16) {
-        const int t = r / p.G, head = hk * p.G + (r - t * p.G), tile = r / p.rows;
-        const int64_t first = ((int64_t)(f.slot + tile) * H_kv + hk) * p.rows + r % p.rows, step = (int64_t)f.tiles * H_kv * p.rows;
+        const int t = query_of(r, p.G), head = hk * p.G + (r - t * p.G), tile = r >> p.row_shift, rows = 1 << p.row_shift;
+        const int64_t first = ((int64_t)(f.slot + tile) * H_kv + hk) * rows + (r & (rows - 1)), step = (int64_t)f.tiles * H_kv * rows;
         float m = kMaxInit, sum = 0.f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int base = s0; base < f.splits; base += 4 * every) {
@@ -931,8 +958,8 @@ PagedPlan make_paged_plan(const psa_cache_t& cache, const psa_paged_shape_t& s)
     p.least = p.rows == 128 && s.dtype == PSA_BF16 && tiles * s.H_kv >= 64 ? 4 : 2;
     p.join = keys > p.least * kUnit && !(full == 1.0 && keys <= (p.few ? 4096 : 2048));
     // (each tile's last share is half a one on average)
-    p.per_head = p.join ? std::max((int64_t)1, (int64_t)((shares - 0.5 * std::min(tiles, shares)) * (1.0 - 0.75 * full))) : 1;
-    // sum of ceil(tiles units / chunk) is at most per_head more than the tiles (without a join the chunk is all units of the call)
+    p.per_head = p.join ? std::max((int64_t)1, (int64_t)((shares - 0.5 * std::min(tiles, shares)) * (1.0 - 0.75 * full))) : 0;
+    // sum of ceil(tiles units / chunk) is at most per_head more than the tiles
     p.n_part = rows / p.rows + s.B + p.per_head;
     // of sequences with several splits the parts are at most twice their work over the chunk, and a row is joined in parts of 32
     const int64_t slots = p.join ? 2 * (int64_t)p.per_head : 0;
@@ -947,6 +974,14 @@ PagedPlan make_paged_plan(const psa_cache_t& cache, const psa_paged_shape_t& s)
     return p;
 }
 
+// May a page's rows be a buffer with 32-bit offsets?
+static bool rows_regular(const psa_cache_t& c, int size)
+{
+    auto good = [&](const psa_heads_t& t, int64_t width, int64_t bytes) {
+        return t.row_stride >= width && t.row_stride * bytes <= 1 << 20 && t.row_stride * bytes * c.page_rows < INT32_MAX;
+    };
+    return good(c.K, 64, size) && good(c.V, 64, size) && (c.format != PSA_CACHE_MX || (good(c.K_scales, 2, 1) && good(c.V_scales, 2, 1)));
+}
 template <typename T, typename C>
 static void paged_go(const PagedPlan& p, const psa_paged_shape_t& s, const psa_heads_t& Q, const psa_cache_t& cache, PagedSeqs seqs, const psa_heads_t& out,
                      float* lse, void* workspace, hipStream_t stream)
@@ -964,8 +999,8 @@ static void paged_go(const PagedPlan& p, const psa_paged_shape_t& s, const psa_h
     constexpr bool FINE = sizeof(T) == 2;
     const unsigned grid = (unsigned)(p.n_part * s.H_kv);
     auto pick = [&](auto pg) {
-        constexpr int PG = decltype(pg)::value;
-        if (p.few) return paged_single_kernel<T, C, PG>;
+        constexpr int MOST = decltype(pg)::value, PG = MOST < KT ? MOST : KT;
+        if (p.few) return paged_single_kernel<T, C, (MOST < 32 ? MOST : 32)>;
         if constexpr (sizeof(T) == 2)
             if (p.rows == 64) return p.fine ? paged_rows_kernel<T, C, PG, 32, 2, 2, true> : paged_rows_kernel<T, C, PG, 32, 2, 2, false>;
         if constexpr (sizeof(C) == 4)
@@ -973,7 +1008,8 @@ static void paged_go(const PagedPlan& p, const psa_paged_shape_t& s, const psa_h
         return p.fine ? paged_rows_kernel<T, C, PG, KT, 4, 1, FINE> : paged_rows_kernel<T, C, PG, KT, 4, 1, false>;
     };
     using std::integral_constant;
-    (cache.page_rows >= 32 ? pick(integral_constant<int, 32>{}) : cache.page_rows == 16 ? pick(integral_constant<int, 16>{}) : pick(integral_constant<int, 0>{}))<<<grid, p.pairs ? 512 : 256, 0, stream>>>(
+    const int pg = rows_regular(cache, sizeof(C)) ? std::min(cache.page_rows, 64) : 0;
+    (pg == 64 ? pick(integral_constant<int, 64>{}) : pg == 32 ? pick(integral_constant<int, 32>{}) : pg == 16 ? pick(integral_constant<int, 16>{}) : pick(integral_constant<int, 0>{}))<<<grid, p.pairs ? 512 : 256, 0, stream>>>(
         heads_of<const T>(Q), page_heads_of<const C>(cache.K), page_heads_of<const C>(cache.V), page_scales_of(cache.K_scales), page_scales_of(cache.V_scales), seqs,
         heads_of<T>(out), lse, s.H_kv, s.causal, scale, (int)p.n_part, part_o, part_ml);
     if (p.join) paged_join_kernel<T><<<(unsigned)(p.n_join * s.H_kv), 256, 0, stream>>>(part_o, part_ml, seqs, s.H_kv, heads_of<T>(out), lse);
@@ -982,7 +1018,7 @@ hipError_t launch_paged(const PagedPlan& p, const psa_paged_shape_t& s, const ps
                         float* lse, void* workspace, hipStream_t stream)
 {
     const PagedSeqs seqs{offsets, cache.lengths, cache.table, s.B, s.T, s.T / s.B, s.H / s.H_kv, cache.max_pages * cache.page_rows, page_shift(cache.page_rows), cache.n_pages,
-                         cache.max_pages, p.rows, (int)p.per_head, p.least, nullptr};
+                         cache.max_pages, page_shift(p.rows), (int)p.per_head, p.least, nullptr};
     const bool mx = cache.format == PSA_CACHE_MX;
     if (s.dtype == PSA_F32) {
         if (mx) paged_go<float, mx8_t>(p, s, Q, cache, seqs, out, lse, workspace, stream);

@@ -337,6 +337,33 @@ def test_nonfinite_values_of_many_rows(B, new, dtype, mx):
         assert torch.equal(out[sees][:, rest], clean[sees][:, rest])
 
 
+@pytest.mark.parametrize("dtype,mx", FORMATS)
+def test_rows_far_apart_and_on_top_of_each_other(dtype, mx):
+    """Rows that are megabytes apart, and one row for all of a page: as their copies."""
+    H_kv, P, lengths = 2, 32, [33, 64]
+    cache = Cache(H_kv, P, lengths, dtype, mx)
+    cache.fill()
+    n = cache.K.shape[0]
+    far = 1 + (1 << 20) // cache.K.element_size()
+    far += -far % 16
+    room = torch.empty(n * P * far, dtype=cache.K.dtype, device="cuda")
+    pages = lambda at: room.as_strided((n, H_kv, P, 64), (P * far, 128, far, 1), at)
+    K, V = pages(0), pages(64)
+    K.copy_(cache.K)
+    V.copy_(cache.V)
+    for new in ([1, 1], [33, 60]):
+        Q, Qd = _queries(2 * H_kv, sum(new), dtype)
+        args = (cache.table, cache.lengths, _offsets(new), True)
+        want = psa.dense_attn_paged_fwd(Qd, cache.K, cache.V, *args, **cache.kw)
+        assert torch.equal(psa.dense_attn_paged_fwd(Qd, K, V, *args, **cache.kw), want)
+        same = cache.V[:, :, :1].expand_as(cache.V)
+        kw = dict(cache.kw)
+        if mx:
+            kw["V_scales"] = kw["V_scales"][:, :, :1].expand_as(kw["V_scales"])
+        copied = {k: v.contiguous() for k, v in kw.items()}
+        assert torch.equal(psa.dense_attn_paged_fwd(Qd, cache.K, same, *args, **kw), psa.dense_attn_paged_fwd(Qd, cache.K, same.contiguous(), *args, **copied))
+
+
 def test_packed_attention_says_the_same():
     """Over the same rows, packed."""
     for dtype in (F32, BF16):
