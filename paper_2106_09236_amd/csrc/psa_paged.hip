@@ -406,9 +406,11 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
     constexpr int ROWS = 32 * RW, NT = 64 * RW * KW, NWAVE = RW * KW, TILE = KT * KW;
     constexpr int CH = 64 * sizeof(C) / 16;            // 16-byte chunks of a row in the cache
     constexpr int NL = TILE * CH / NT;                 // chunks of a tile, to a thread
+    constexpr int WR = TILE / NWAVE;                   // rows of a tile that a wave brings, 16 at most: on one page
     constexpr int NS = KT / 32;
     constexpr int NU = RowChunk<C>::N;
     constexpr int kBytes = kTileBytes<TC, TILE>;
+    static_assert(WR <= 16 && (PG == 0 || PG == 16), "a wave's rows have to be on one page");
     static_assert(KW == 1 || 4 * kBytes >= ROWS * (kJoinRow + 2) * 4, "the join does not fit the tiles");
     __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kBytes];
     __shared__ int s_bad[2][NWAVE];
@@ -436,21 +438,20 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
     PageWindow<C, PG> w(p, f.seq, f.nk, K, V, hk);
     RowChunk<C> kr[NL], vr[NL];
     uint32_t held_next[NS];
+    auto row_of = [&](int i) { return wave * WR + i * (64 / CH) + lane / CH; };
     auto fetch = [&](int j0) {
         w.reach(j0, TILE);
         PageRows<C> pk, pv;
+        if constexpr (PG > 0) {
+            pk.open(w, 0, K, ks, hk, j0 + wave * WR, f.nk);
+            pv.open(w, 1, V, vs, hk, j0 + wave * WR, f.nk);
+        }
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            const int id = i * NT + tid, r = id / CH, ch = id % CH;
+            const int r = row_of(i), ch = lane % CH;
             if constexpr (PG > 0) {
-                // (the rows of a wave are on one page; those of all waves where it has NT / CH rows)
-                const int from = NT / CH <= PG ? i * (NT / CH) & ~(PG - 1) : i * (NT / CH) + (wave * 64 / CH & ~(PG - 1));
-                if (NT / CH >= PG || i * (NT / CH) % PG == 0) {
-                    pk.open(w, 0, K, ks, hk, j0 + from, f.nk);
-                    pv.open(w, 1, V, vs, hk, j0 + from, f.nk);
-                }
-                pk.load(kr[i], r - from, ch);
-                pv.load(vr[i], r - from, ch);
+                pk.load(kr[i], r - wave * WR, ch);
+                pv.load(vr[i], r - wave * WR, ch);
             } else {
                 load_chunk(kr[i], K, ks, hk, w, j0 + r, ch, f.nk);
                 load_chunk(vr[i], V, vs, hk, w, j0 + r, ch, f.nk);
@@ -477,13 +478,12 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
             }
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
-                const int id = i * NT + tid;
                 uint4 k[NU];
                 kr[i].unpack(k);
 #pragma unroll
                 for (int u = 0; u < NU; ++u) {
-                    put<TILE>(sK + buf * kBytes, id / CH, id % CH * NU + u, k[u], TC{});
-                    put<TILE>(sV + buf * kBytes, id / CH, id % CH * NU + u, v[i * NU + u], TC{});
+                    put<TILE>(sK + buf * kBytes, row_of(i), lane % CH * NU + u, k[u], TC{});
+                    put<TILE>(sV + buf * kBytes, row_of(i), lane % CH * NU + u, v[i * NU + u], TC{});
                 }
             }
             uint32_t held[NS], all = ~0u;
@@ -999,8 +999,8 @@ static void paged_go(const PagedPlan& p, const psa_paged_shape_t& s, const psa_h
     constexpr bool FINE = sizeof(T) == 2;
     const unsigned grid = (unsigned)(p.n_part * s.H_kv);
     auto pick = [&](auto pg) {
-        constexpr int MOST = decltype(pg)::value, PG = MOST < KT ? MOST : KT;
-        if (p.few) return paged_single_kernel<T, C, (MOST < 32 ? MOST : 32)>;
+        constexpr int SINGLE = decltype(pg)::value, PG = SINGLE < 16 ? SINGLE : 16;
+        if (p.few) return paged_single_kernel<T, C, SINGLE>;
         if constexpr (sizeof(T) == 2)
             if (p.rows == 64) return p.fine ? paged_rows_kernel<T, C, PG, 32, 2, 2, true> : paged_rows_kernel<T, C, PG, 32, 2, 2, false>;
         if constexpr (sizeof(C) == 4)
@@ -1008,8 +1008,8 @@ static void paged_go(const PagedPlan& p, const psa_paged_shape_t& s, const psa_h
         return p.fine ? paged_rows_kernel<T, C, PG, KT, 4, 1, FINE> : paged_rows_kernel<T, C, PG, KT, 4, 1, false>;
     };
     using std::integral_constant;
-    const int pg = rows_regular(cache, sizeof(C)) ? std::min(cache.page_rows, 64) : 0;
-    (pg == 64 ? pick(integral_constant<int, 64>{}) : pg == 32 ? pick(integral_constant<int, 32>{}) : pg == 16 ? pick(integral_constant<int, 16>{}) : pick(integral_constant<int, 0>{}))<<<grid, p.pairs ? 512 : 256, 0, stream>>>(
+    const int pg = rows_regular(cache, sizeof(C)) ? std::min(cache.page_rows, 32) : 0;
+    (pg == 32 ? pick(integral_constant<int, 32>{}) : pg == 16 ? pick(integral_constant<int, 16>{}) : pick(integral_constant<int, 0>{}))<<<grid, p.pairs ? 512 : 256, 0, stream>>>(
         heads_of<const T>(Q), page_heads_of<const C>(cache.K), page_heads_of<const C>(cache.V), page_scales_of(cache.K_scales), page_scales_of(cache.V_scales), seqs,
         heads_of<T>(out), lse, s.H_kv, s.causal, scale, (int)p.n_part, part_o, part_ml);
     if (p.join) paged_join_kernel<T><<<(unsigned)(p.n_join * s.H_kv), 256, 0, stream>>>(part_o, part_ml, seqs, s.H_kv, heads_of<T>(out), lse);
