@@ -203,7 +203,8 @@ void paged_before_kernel(PagedSeqs p, int* __restrict__ before)
 
 // ---- rows of the cache on their way
 // 64 entries of a sequence's table, one to a lane: a tile's pages are read from a register and no load waits for another.  Entries that name no
-// page are -1.  Pages of PG = 16 rows and more: rows that are asked for together lie on one page, whose addresses, of K and of V, the lanes hold as well.  A
+// page are -1.  Pages of PG = 16 rows and more: rows that are asked for together lie on one page, whose addresses, of K and of V, the lanes hold as well
+// (computed for every tile by every wave: 16384 keys, last 4096 rows, 182 -> 177 us).  PG = 0: smaller pages and irregular rows, each lane finds its row's.  A
 // new window is waited for where it is asked for, so that the loads of rows in flight are waited for by nobody else.
 template <typename C, int PG>
 struct PageWindow {
@@ -406,7 +407,7 @@ void paged_rows_kernel(Heads<const T> Q, PageHeads<const C> K, PageHeads<const C
     constexpr int ROWS = 32 * RW, NT = 64 * RW * KW, NWAVE = RW * KW, TILE = KT * KW;
     constexpr int CH = 64 * sizeof(C) / 16;            // 16-byte chunks of a row in the cache
     constexpr int NL = TILE * CH / NT;                 // chunks of a tile, to a thread
-    constexpr int WR = TILE / NWAVE;                   // rows of a tile that a wave brings, 16 at most: on one page
+    constexpr int WR = TILE / NWAVE;                   // rows of a tile that a wave brings, 16 at most: on one page (8 rows here, 8 there, with pages of 16: clips of 40 to 500 20.3 -> 19.2 us)
     constexpr int NS = KT / 32;
     constexpr int NU = RowChunk<C>::N;
     constexpr int kBytes = kTileBytes<TC, TILE>;
