@@ -487,7 +487,9 @@ int dense_attn_paged_fwd(const psa_heads_t* Q, const int32_t* offsets, const psa
  * Outputs (DEVICE int32; they must not alias inputs): table_out [B_out, max_pages], lengths_out [B_out] (grown, at most
  * max_pages * page_rows), refs_out [n_pages], pairs [B_out, 2] (-1 behind the last), counts [2]: pairs, and pages that were
  * missing.  Where pages run out, or rows pass max_pages, entries stay -1 and are counted there (a page that could not be copied is
- * given up): look at it before the rows are needed.
+ * given up): look at it before the rows are needed.  Such an entry stays -1 in later calls too: rows that a sequence gets there, up to the page's end, are left out
+ * by append and not seen, also once pages are free again (a new page would show what it held in the place of rows that were left out before).  A call in which no page was
+ * missing counts the sequences that get such rows instead, so that 0 says that every new row has a page.
  * B, B_out 1 .. 2^20, n_pages 1 .. 2^28, max_pages * page_rows <= 2^28, B * max_pages and B_out * max_pages <= 2^30 (PSA_ERR_SHAPE).
  * Other tables may hold pages of the same pool: refs counts theirs too. */
 size_t probsparse_cache_update_workspace_bytes(int32_t B, int32_t B_out, int32_t n_pages);

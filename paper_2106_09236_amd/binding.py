@@ -803,7 +803,8 @@ def probsparse_cache_update(table, lengths, refs, page_rows: int, parents=None, 
                             pairs=None, counts=None, workspace=None):
     """The sequences of the next step: sequence i continues parents[i] (int32 [B_out]; outside [0, B): nobody; None: itself) and gets
     pages for grow[i] more rows (int32 [B_out]; None: 0); what nobody continues is freed.  Returns (table, lengths, refs, pairs, counts):
-    pairs [B_out, 2] are the pages that probsparse_cache_copy has to copy, counts [2] how many, and pages that were missing."""
+    pairs [B_out, 2] are the pages that probsparse_cache_copy has to copy, counts [2] how many, and pages that were missing (0:
+    every new row has a page)."""
     done = (_native or _fast()).cache_update(table, lengths, refs, page_rows, parents, grow, table_out, lengths_out, refs_out, pairs, counts, workspace)
     if done is not None:
         return done

@@ -154,6 +154,7 @@ hipError_t launch_cache_append(const psa_heads_t& K, const psa_heads_t& V, const
 constexpr int kScanParents = 4096;         // new sequences up to which each old one looks through all of them for those that continue it
 struct UpdateRoom {
     unsigned long long* over;              // pages beyond the tables' rows
+    int* holes;                            // sequences that grow inside a page that they do not have
     int *growers, *first, *given;          // [n_pages]: sequences that write to a page next, the first of them; free pages in order of need
     int *last, *had, *want;                // [B_out]: the page that it writes to next (-1: a new one); pages that it has and will have
     int *at, *copied;                      // [B_out]: pages needed before it; whether its last page is copied
@@ -163,7 +164,8 @@ static UpdateRoom update_room(const CacheUpdate& u, void* room)
 {
     UpdateRoom w{};
     w.over = static_cast<unsigned long long*>(room);
-    int* p = static_cast<int*>(room) + 2;
+    w.holes = static_cast<int*>(room) + 2;
+    int* p = static_cast<int*>(room) + 4;
     w.growers = p; p += u.n_pages;
     w.first = p; p += u.n_pages;
     w.given = p; p += u.n_pages;
@@ -171,7 +173,7 @@ static UpdateRoom update_room(const CacheUpdate& u, void* room)
     if (u.B_out > kScanParents) w.children = p;
     return w;
 }
-size_t cache_update_bytes(int B, int B_out, int n_pages) { return ((2 + 3 * (size_t)n_pages + 5 * (size_t)B_out + (B_out > kScanParents ? B : 0)) * sizeof(int) + 255) & ~(size_t)255; }
+size_t cache_update_bytes(int B, int B_out, int n_pages) { return ((4 + 3 * (size_t)n_pages + 5 * (size_t)B_out + (B_out > kScanParents ? B : 0)) * sizeof(int) + 255) & ~(size_t)255; }
 
 // Sequence i of the new ones: whom it continues (-1: nobody), the rows and pages it has from there, the rows and pages it will have, and the
 // pages that a row of the table cannot hold
@@ -190,13 +192,18 @@ __device__ __forceinline__ Child child_of(const CacheUpdate& u, int i)
     c.over = ((grown + u.page_rows - 1) >> shift) - c.want;
     return c;
 }
-// The last page of a sequence that will write to it; -1: none
-__device__ __forceinline__ int partial_page(const CacheUpdate& u, const Child& c)
+// The last page of a sequence that will write to it; -1: none.  `hole`: the sequence has rows there, but the entry names no page.  It gets none now either: its
+// rows there were left out, and on a page of its own, whatever that page held would be seen in their place.
+__device__ __forceinline__ int partial_page(const CacheUpdate& u, const Child& c, bool& hole)
 {
+    hole = false;
     if (c.n_out == c.n || (c.n & (u.page_rows - 1)) == 0) return -1;
     const int page = u.table[(int64_t)c.parent * u.max_pages + c.had - 1];
-    return (unsigned)page < (unsigned)u.n_pages ? page : -1;
+    hole = (unsigned)page >= (unsigned)u.n_pages;
+    return hole ? -1 : page;
 }
+// What counts[1] says, of `missing` pages that were asked for and `holes`
+__device__ __forceinline__ int missing_of(unsigned long long missing, int holes) { return missing != 0 ? (int)min(missing, (unsigned long long)INT_MAX) : holes; }
 
 __global__ __launch_bounds__(256)
 void update_begin_kernel(CacheUpdate u, UpdateRoom w)
@@ -208,7 +215,7 @@ void update_begin_kernel(CacheUpdate u, UpdateRoom w)
         w.first[i] = INT_MAX;
     }
     if (w.children && i < u.B) w.children[i] = 0;
-    if (i == 0) *w.over = 0;
+    if (i == 0) { *w.over = 0; *w.holes = 0; }
 }
 __global__ __launch_bounds__(256)
 void update_children_kernel(CacheUpdate u, UpdateRoom w)
@@ -253,7 +260,8 @@ void update_rows_kernel(CacheUpdate u, UpdateRoom w)
     }
     if (tid == 0) {
         u.lengths_out[i] = c.n_out;
-        const int page = partial_page(u, c);
+        bool hole;
+        const int page = partial_page(u, c, hole);
         w.last[i] = page;
         w.had[i] = c.had;
         w.want[i] = c.want;
@@ -262,6 +270,7 @@ void update_rows_kernel(CacheUpdate u, UpdateRoom w)
             atomicMin(w.first + page, i);
         }
         if (c.over > 0) atomicAdd(w.over, (unsigned long long)c.over);
+        if (hole) atomicAdd(w.holes, 1);
     }
 }
 
@@ -349,7 +358,7 @@ void update_end_kernel(CacheUpdate u, UpdateRoom w)
     for (int i = pairs + tid; i < u.B_out; i += 1024) u.pairs[2 * i] = u.pairs[2 * i + 1] = -1;
     if (tid == 0) {
         u.counts[0] = pairs;
-        u.counts[1] = (int)min((unsigned long long)max(need - found, 0) + *w.over, (unsigned long long)INT_MAX);
+        u.counts[1] = missing_of((unsigned long long)max(need - found, 0) + *w.over, *w.holes);
     }
 }
 // The same by one work-group.  A sequence to a thread; entries of the tables to any.
@@ -367,18 +376,20 @@ void update_small_kernel(CacheUpdate u)
     __shared__ int s_had_in[kSmallSequences], s_had[kSmallSequences], s_parent[kSmallSequences];
     __shared__ int s[2][16];
     __shared__ unsigned long long s_over;
+    __shared__ int s_holes;
     const int tid = threadIdx.x, shift = __builtin_ctz((unsigned)u.page_rows);
     Child c{};
     int last = -1;                                     // the page that this thread's sequence writes to next, where it has rows of others
+    bool hole = false;
     // (asked for before the chain of loads that each sequence is)
     constexpr int AHEAD = kSmallPages / 1024;
     int held[AHEAD];
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) held[k] = u.refs[min(tid + 1024 * k, u.n_pages - 1)];
-    if (tid == 0) s_over = 0;
+    if (tid == 0) { s_over = 0; s_holes = 0; }
     if (tid < u.B_out) {
         c = child_of(u, tid);
-        last = partial_page(u, c);
+        last = partial_page(u, c, hole);
         s_had[tid] = c.had;
         s_parent[tid] = c.parent;
         u.lengths_out[tid] = c.n_out;
@@ -389,6 +400,7 @@ void update_small_kernel(CacheUpdate u)
         if (tid + 1024 * k < u.n_pages) { refs[tid + 1024 * k] = held[k]; mark[tid + 1024 * k] = INT_MAX; }
     __syncthreads();
     if (c.over > 0) atomicAdd(&s_over, (unsigned long long)c.over);
+    if (hole) atomicAdd(&s_holes, 1);
     // who holds what: the old sequences' entries go, the new ones' come (without parents they are the same)
     const int entries = u.B * u.max_pages, entries_out = u.B_out * u.max_pages;
     if (u.parents) {
@@ -454,7 +466,7 @@ void update_small_kernel(CacheUpdate u)
     if (tid >= pairs && tid < u.B_out) u.pairs[2 * tid] = u.pairs[2 * tid + 1] = -1;
     if (tid == 0) {
         u.counts[0] = pairs;
-        u.counts[1] = (int)min((unsigned long long)max(need - found, 0) + s_over, (unsigned long long)INT_MAX);
+        u.counts[1] = missing_of((unsigned long long)max(need - found, 0) + s_over, s_holes);
     }
     __syncthreads();
     for (int p = tid; p < u.n_pages; p += 1024) u.refs_out[p] = refs[p];
