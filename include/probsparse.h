@@ -420,7 +420,8 @@ int dense_attn_packed_bwd(const psa_heads_t* Q, const psa_heads_t* K, const psa_
  * A pool holds n_pages pages of `page_rows` rows (a power of two) of H_kv heads.  Row j of sequence s, its position from
  * the sequence's start, is row j % page_rows of page table[s * max_pages + j / page_rows]; lengths[s] rows exist.  An
  * entry outside [0, n_pages) names no page (-1 as a rule): its rows cannot be written and are not seen, as if a mask left
- * them out, so that pages of rows too old to matter may be freed.  Sequences may share pages.
+ * them out, so that pages of rows too old to matter may be freed (memory is given back; attention still
+ * goes over such rows).  Sequences may share pages.
  *   K, V      psa_heads_t with pages in the place of batch items: element e of row r of head h of page p is
  *             data[p * batch_stride + h * head_stride + r * row_stride + e].  By head, by frame, K and V side by side in a
  *             page or apart, several layers in a page: whatever the strides say

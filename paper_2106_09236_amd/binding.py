@@ -804,7 +804,7 @@ def probsparse_cache_update(table, lengths, refs, page_rows: int, parents=None, 
     """The sequences of the next step: sequence i continues parents[i] (int32 [B_out]; outside [0, B): nobody; None: itself) and gets
     pages for grow[i] more rows (int32 [B_out]; None: 0); what nobody continues is freed.  Returns (table, lengths, refs, pairs, counts):
     pairs [B_out, 2] are the pages that probsparse_cache_copy has to copy, counts [2] how many, and pages that were missing (0:
-    every new row has a page)."""
+    every new row has a page).  Outputs that are not brought may be parts of one allocation, which lives as long as any of them."""
     done = (_native or _fast()).cache_update(table, lengths, refs, page_rows, parents, grow, table_out, lengths_out, refs_out, pairs, counts, workspace)
     if done is not None:
         return done
@@ -830,7 +830,8 @@ def probsparse_cache_update(table, lengths, refs, page_rows: int, parents=None, 
 
 def probsparse_cache_compact(table, refs, table_out=None, refs_out=None, pairs=None, counts=None, workspace=None):
     """The pages in use to the front of the pools.  Returns (table, refs, pairs, counts): pairs [n_pages / 2, 2] are the pages that
-    probsparse_cache_copy has to move, counts [2] how many, and pages in use.  table_out may be table."""
+    probsparse_cache_copy has to move, counts [2] how many, and pages in use.  table_out may be table.  Outputs that are not
+    brought may be parts of one allocation."""
     done = (_native or _fast()).cache_compact(table, refs, table_out, refs_out, pairs, counts, workspace)
     if done is not None:
         return done

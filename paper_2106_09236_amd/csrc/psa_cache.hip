@@ -150,7 +150,10 @@ hipError_t launch_cache_append(const psa_heads_t& K, const psa_heads_t& V, const
 // launches: refs and the workspace; the tables' rows, with the changes of refs that they make; one work-group for what depends on all
 // of them, which is little: the pages that are given away, in ascending order.  (In the last work-group that is done with its rows, by a ticket, instead of
 // a launch of its own: 13.3 -> 15.7 us, everything it reads comes from memory then.)  One | three launches: 16 x 8 beams, 1161 pages, with the copies 12.5 |
-// 19.9 us; 12288 pages and 256 sequences of 128 entries, updates alone, 23.8 | 10.6.  1024 sequences of 256 entries and 200000 pages: 20.
+// 19.9 us; 12288 pages and 256 sequences of 128 entries, updates alone, 23.8 | 10.6.  1024 sequences of 256 entries and 200000 pages, free ones among the first: 20.
+// Two things take longer.  Free pages are looked for from page 0 on, 4096 at a time: 500000 pages of which 399872 are used, 512 sequences that grow by a page each, 12.6 us where the free ones
+// are scattered, 94.8 where they lie behind the used ones, as after a compaction.  And the pages that one sequence grows into are given by one thread, one after the other: 24 prompts of 120 to 750 rows in
+// pages of 16 8.5 | 14.5 us (small | large call), one of 32768 rows 143 | 245, 16 of them 320.
 constexpr int kScanParents = 4096;         // new sequences up to which each old one looks through all of them for those that continue it
 struct UpdateRoom {
     unsigned long long* over;              // pages beyond the tables' rows

@@ -48,8 +48,10 @@ __device__ __forceinline__ int splits_of(const PagedSeqs& p, int nk, int chunk)
 }
 
 // Units of keys to a split: the work of all tiles (units times tiles) in about p.per_head shares, p.least at the least.  Every
-// work-group of a call and of its join finds the same.  Summed in float32, in which the sum is off by 2^-18 at the most: the parts of
-// divided sequences stay at most twice p.per_head, a number below 2^17.
+// work-group of a call and of its join finds the same.  Summed in float32: a thread adds up to 1024 numbers (2^20 sequences in paged_before_kernel), and 22 more
+// additions join them, so that the sum is off by less than 2^-13 of it.  p.per_head is at most 1024.  A divided sequence has u >= chunk + 1 units, hence at most 2 (u - 1) / chunk
+// splits: the parts of all of them are fewer than 2 p.per_head (1 + 2^-13) <= 2 p.per_head + 1/4, a whole number, so at most twice p.per_head; in the same way all parts are
+// at most p.per_head more than the tiles.  More than 4096 shares would need a more exact sum.
 __device__ __forceinline__ float wave_sum(float x)
 {
     auto add = [&](auto ctrl, auto rows) { x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl.value, rows.value, 0xF, false)); };
@@ -934,7 +936,9 @@ void paged_join_kernel(const float* __restrict__ part_o, const float2* __restric
 //
 // Shares of the work: as many as compute units hold work-groups while tiles are less than a quarter (128 rows: a third) of those, down to a quarter as
 // many where they are half (two thirds) of them: their own number evens out what is left, and sums to be joined are 528 bytes of traffic a row and split.  Then, with sequences that
-// can only be so long, nothing is divided, and no join launched (64 sequences of 1300 keys, 8 heads, one new row: 40 | 34 us; 64 new rows 49 | 36).
+// can only be so long, nothing is divided, and no join launched (64 sequences of 1300 keys, 8 heads, one new row: 40 | 34 us; 64 new rows 49 | 36).  The host knows how
+// long they can be, by the tables' width, not how long they are: with tables for 32768 rows the same sequences are searched for shares and joined, though nothing is divided.  Tables as
+// wide as the sequences | for 32768 rows: 31.5 | 33.9 us, 64 new rows 33.5 | 36.0, 96 of 128 rows, all new, 14.7 | 18.5; where shares are searched for anyway the same (16 x 64 of 600 to 2048 20.1 | 20.1).
 // A share is at least 2 units of keys; 4 where bfloat16 calls have 64 tiles of 128 rows and more, since what a row leaves for the join is as many bytes as 2 units of its
 // keys and values: 32 clips of 40 to 500, 4 heads, 22.7 | 19.5 us, 16 of 2000 keys and 128 rows, 8 heads, 30.1 | 27.7, but 4 of 1000 to 2000 and 128 rows (32 tiles) 17.6 | 21.7,
 // and in float32 28.5 | 41.
